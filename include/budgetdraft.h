@@ -20,6 +20,9 @@
  *   bd_write_block_rows  writes the block's new K/V rows into the caches;
  *   bd_advance        slides the observation window over the settled block rows and
  *                     appends their positions to the sparse view (Algorithm 2, Update).
+ * and a 4-bit form of the caches in four more:
+ *   bd_quant_write / bd_quant_read  quantise rows into a 4-bit cache and read them back;
+ *   bd_quant_draft_attn / bd_quant_verify_attn  the two attentions over it.
  * Around them: bd_workspace_size / bd_workspace_status (scratch and device-side
  * errors), bd_draft_attn_static / bd_draft_static_status (bd_draft_attn without a
  * workspace, and its error word),
@@ -93,18 +96,20 @@ typedef struct bd_shape {
   const int32_t* seq_lens;  /* per-sequence lengths [batch] or NULL  */
 } bd_shape;
 
-/* Element types of bd_argmax logits. */
+/* Element types of bd_argmax logits and of the rows bd_quant_write takes and bd_quant_read gives. */
 enum { BD_DTYPE_BF16 = 1, BD_DTYPE_F32 = 2 };
 
 /* Operation codes for bd_workspace_size. */
-enum { BD_OP_SELECT = 1, BD_OP_DRAFT = 2, BD_OP_VERIFY = 3 };
+enum { BD_OP_SELECT = 1, BD_OP_DRAFT = 2, BD_OP_VERIFY = 3, BD_OP_QUANT_DRAFT = 4, BD_OP_QUANT_VERIFY = 5 };
 
 /*
  * Workspace bytes needed by one operation on `shape` (0 on invalid input).
  *   BD_OP_SELECT: budget = B, n_q = window W (window queries per head);
  *   BD_OP_DRAFT:  budget = B, n_q = the largest step_j + 1 that will be passed;
  *   BD_OP_VERIFY: budget ignored, n_q = queries per head in the block, or the most that
- *                 will be passed (with or without an output).
+ *                 will be passed (with or without an output);
+ *   BD_OP_QUANT_DRAFT, BD_OP_QUANT_VERIFY: like BD_OP_DRAFT and BD_OP_VERIFY, for
+ *                 bd_quant_draft_attn and bd_quant_verify_attn (t_ctx may be 0).
  * The size depends on the current device's SM count.  Sizes for different ops may
  * be satisfied by one buffer of the largest of them.
  */
@@ -330,6 +335,78 @@ int bd_advance(const bd_shape* shape, int window, int n_q, const int32_t* n_acce
  */
 int bd_write_block_rows(const bd_shape* shape, int n_rows, const void* k_rows, const void* v_rows, void* k_cache,
                         void* v_cache, void* stream);
+
+/*
+ * A 4-bit KV cache (no counterpart in the paper): 3.6 times as many positions in the same
+ * memory as bf16, and as much less to read for the attention over it.  A row of head_dim
+ * elements x is held as codes, two to a byte (element 2 j in the low half of byte j), and
+ * one scale for each group of 32 elements:
+ *     scale = bf16(max |x| / 7)
+ *     code  = clamp(round(x / scale), -7, 7) + 8    (fp32 quotient, rounded half to even)
+ *     value = (code - 8) * scale
+ * A scale of 0 (a group of zeros, or too small for bf16) gives codes of 8; a group that holds a
+ * NaN or an infinity has the scale NaN, and all its values are NaN.
+ * Any code 0 .. 15 and any scale >= 0 may be in a cache that something else wrote.
+ *   k_codes, v_codes    uint8 [batch, h_kv, t_cap, head_dim / 2]
+ *   k_scales, v_scales  bf16  [batch, h_kv, t_cap, head_dim / 32]
+ * All four 16-byte aligned, dense.  The struct is read during a call only.  Rows hold what the
+ * rows of a bf16 cache of the same bd_shape hold, and bd_shape means the same; t_ctx, and a
+ * sequence's own length, may also be 0 (an empty cache).
+ */
+typedef struct bd_quant_cache {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} bd_quant_cache;
+
+/*
+ * Quantises K and V rows into a 4-bit cache: rows t_ctx .. t_ctx + n_rows - 1 (T_b .. with
+ * per-sequence lengths) of every (sequence, KV head).  A block's rows, or with t_ctx = 0 a
+ * prefill's.
+ *   dtype           BD_DTYPE_BF16 or BD_DTYPE_F32, of both tensors;
+ *   k_rows, v_rows  [batch, h_kv, n_rows, head_dim]; either may be NULL (that tensor of the
+ *                   cache is left alone), not both.  16-byte aligned;
+ *   k_strides, v_strides  elements from one sequence, KV head and row to the next (HOST int64
+ *                   [3]), or NULL for dense rows; multiples of 16 bytes, not negative; the
+ *                   elements of a row are adjacent.  E.g. a projection's [batch, row, head, d].
+ * A T_b outside [0, t_ctx] is clamped.  Constraints: n_rows >= 0 (0 is a no-op),
+ * t_ctx + n_rows <= t_cap.  No workspace.
+ */
+int bd_quant_write(const bd_shape* shape, int n_rows, int dtype, const void* k_rows, const int64_t* k_strides,
+                   const void* v_rows, const int64_t* v_strides, const bd_quant_cache* cache, void* stream);
+
+enum { BD_QUANT_BLOCK_ROWS = -1 };
+
+/*
+ * Reads rows of a 4-bit cache back as bf16 (the value rounded once) or fp32 (the value): rows first_row ..
+ * first_row + n_rows - 1 of every (sequence, KV head), or with first_row = BD_QUANT_BLOCK_ROWS
+ * the rows behind the context, t_ctx (T_b) ...  Arguments as of bd_quant_write, the rows being
+ * written; strides between different rows are at least head_dim.  No workspace.
+ */
+int bd_quant_read(const bd_shape* shape, int first_row, int n_rows, int dtype, const bd_quant_cache* cache, void* k_rows,
+                  const int64_t* k_strides, void* v_rows, const int64_t* v_strides, void* stream);
+
+/*
+ * bd_draft_attn over a 4-bit cache: the same arguments, results and constraints (view size
+ * apart: budget + step_j < 2^30), and ws of at least bd_workspace_size(BD_OP_QUANT_DRAFT) bytes.
+ * An index outside the sequence's context is recorded in the status word and skipped.
+ */
+int bd_quant_draft_attn(const bd_shape* shape, const void* q, const bd_quant_cache* cache, const int32_t* idx,
+                        const int32_t* count, int budget, int step_j, unsigned flags, void* o_out, float* lse_out, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/*
+ * bd_verify_attn over a 4-bit cache (n_q = 1: decoding one token): query i of head h attends to keys
+ * [0, t_ctx + i], all of them as the cache holds them, its own block's rows among them.
+ *   q        bf16 [batch, h_q, n_q, d];  o_out bf16 [batch, h_q, n_q, d];
+ *   lse_out  fp32 [batch, h_q, n_q] (may be NULL).
+ * Constraints: 1 <= n_q, t_ctx + n_q <= t_cap, (h_q/h_kv)*n_q <= 768; ws of at least
+ * bd_workspace_size(BD_OP_QUANT_VERIFY) bytes.  Cache rows past a sequence's own block are never
+ * used: they may hold anything.
+ */
+int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_quant_cache* cache, void* o_out,
+                         float* lse_out, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Diagnostic of the device-side error path (the paper has no counterpart): launches one

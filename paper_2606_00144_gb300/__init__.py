@@ -13,10 +13,13 @@ from .binding import (  # noqa: F401
     BD_DTYPE_BF16,
     BD_DTYPE_F32,
     BD_OP_DRAFT,
+    BD_OP_QUANT_DRAFT,
+    BD_OP_QUANT_VERIFY,
     BD_OP_SELECT,
     BD_OP_VERIFY,
     BdShape,
     BudgetDraftError,
+    QuantCache,
     Workspace,
     bd_accept,
     bd_advance,
@@ -26,6 +29,10 @@ from .binding import (  # noqa: F401
     bd_draft_attn,
     bd_draft_attn_static,
     bd_draft_static_status,
+    bd_quant_draft_attn,
+    bd_quant_read,
+    bd_quant_verify_attn,
+    bd_quant_write,
     bd_select_budget,
     bd_strerror,
     bd_verify_attn,

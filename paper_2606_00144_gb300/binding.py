@@ -16,7 +16,9 @@ from .build import LIB_PATH
 
 BD_OK = 0
 BD_ERR_CUDA = -5
-BD_OP_SELECT, BD_OP_DRAFT, BD_OP_VERIFY = 1, 2, 3
+BD_OP_SELECT, BD_OP_DRAFT, BD_OP_VERIFY, BD_OP_QUANT_DRAFT, BD_OP_QUANT_VERIFY = 1, 2, 3, 4, 5
+BD_QUANT_BLOCK_ROWS = -1
+BD_QUANT_GROUP = 32
 BD_DRAFT_VIEW_READY = 1
 BD_SELECT_WINDOW_READY = 1
 BD_DTYPE_BF16, BD_DTYPE_F32 = 1, 2
@@ -32,6 +34,11 @@ class BdShape(ctypes.Structure):
                 f"t_ctx={self.t_ctx}, t_cap={self.t_cap})")
 
 
+class BdQuantCache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p)]
+
+
 class BudgetDraftError(RuntimeError):
     def __init__(self, func, status):
         self.status = status
@@ -41,6 +48,8 @@ class BudgetDraftError(RuntimeError):
 _lib = None
 _P = ctypes.c_void_p
 _SHAPE = ctypes.POINTER(BdShape)
+_QCACHE = ctypes.POINTER(BdQuantCache)
+_STRIDES = ctypes.POINTER(ctypes.c_int64)
 _SIGNATURES = {
     "bd_workspace_size": (ctypes.c_size_t, [_SHAPE, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
     "bd_select_budget": (ctypes.c_int, [_SHAPE, _P, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -58,6 +67,12 @@ _SIGNATURES = {
     "bd_advance": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, ctypes.c_int, _P,
                                   _P]),
     "bd_write_block_rows": (ctypes.c_int, [_SHAPE, ctypes.c_int, _P, _P, _P, _P, _P]),
+    "bd_quant_write": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, _P, _STRIDES, _P, _STRIDES, _QCACHE, _P]),
+    "bd_quant_read": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, ctypes.c_int, _QCACHE, _P, _STRIDES, _P,
+                                     _STRIDES, _P]),
+    "bd_quant_draft_attn": (ctypes.c_int, [_SHAPE, _P, _QCACHE, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_uint, _P,
+                                           _P, _P, ctypes.c_size_t, _P]),
+    "bd_quant_verify_attn": (ctypes.c_int, [_SHAPE, _P, ctypes.c_int, _QCACHE, _P, _P, _P, ctypes.c_size_t, _P]),
     "bd_check_wait_timeout": (ctypes.c_int, [_P, ctypes.c_size_t, ctypes.c_int, _P]),
     "bd_workspace_status": (ctypes.c_int, [_P, _P]),
     "bd_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -241,6 +256,127 @@ def bd_write_block_rows(shape, n_rows, k_rows, v_rows, k_cache, v_cache, stream=
     st = library().bd_write_block_rows(ctypes.byref(shape), int(n_rows), _ptr(k_rows), _ptr(v_rows), _ptr(k_cache),
                                        _ptr(v_cache), _stream(stream))
     _check("bd_write_block_rows", st)
+
+
+class QuantCache:
+    """A 4-bit KV cache (the format is in the header): uint8 codes [batch, h_kv, t_cap, head_dim / 2]
+    and bf16 scales [batch, h_kv, t_cap, head_dim / 32] of K and of V.  The tensors stay the caller's:
+    they may be views that other code reads, as long as each is dense."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        if k_codes.dim() != 4 or k_codes.shape[3] not in (32, 64):
+            raise ValueError("QuantCache: codes must be [batch, h_kv, t_cap, head_dim / 2] with head_dim 64 or 128")
+        self.batch, self.h_kv, self.t_cap = (int(x) for x in k_codes.shape[:3])
+        self.head_dim = 2 * int(k_codes.shape[3])
+        for codes, scales in ((k_codes, k_scales), (v_codes, v_scales)):
+            if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+                raise TypeError("QuantCache: codes are uint8, scales bf16")
+            if codes.shape != k_codes.shape or tuple(scales.shape) != (*k_codes.shape[:3], self.head_dim // BD_QUANT_GROUP):
+                raise ValueError("QuantCache: codes and scales must cover the same rows")
+            if not (codes.is_contiguous() and scales.is_contiguous()):
+                raise ValueError("QuantCache: codes and scales must be contiguous")
+            if codes.device != k_codes.device or scales.device != k_codes.device:
+                raise ValueError("QuantCache: codes and scales must be on one device")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self._struct = BdQuantCache(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
+
+    @classmethod
+    def empty(cls, batch, h_kv, t_cap, head_dim, device="cuda"):
+        """A cache whose rows are not written yet."""
+        def one():
+            return (torch.empty(batch, h_kv, t_cap, head_dim // 2, dtype=torch.uint8, device=device),
+                    torch.empty(batch, h_kv, t_cap, head_dim // BD_QUANT_GROUP, dtype=torch.bfloat16, device=device))
+        return cls(*one(), *one())
+
+    def shape(self, h_q: int, t_ctx: int, seq_lens=None) -> BdShape:
+        return make_shape(self.batch, h_q, self.h_kv, self.head_dim, t_ctx, self.t_cap, seq_lens)
+
+    @property
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in (self.k_codes, self.k_scales, self.v_codes, self.v_scales))
+
+
+def _quant_cache(name, shape, cache: QuantCache):
+    if (shape.batch, shape.h_kv, shape.head_dim, shape.t_cap) != (cache.batch, cache.h_kv, cache.head_dim, cache.t_cap):
+        raise ValueError(f"{name}: the cache is not one of this shape: {shape}")
+    return ctypes.byref(cache._struct)
+
+
+def _quant_rows(name, shape, k_rows, v_rows):
+    """dtype code, row count and strides of a write's or read's tensors [batch, h_kv, n, head_dim]."""
+    given = [t for t in (k_rows, v_rows) if t is not None]
+    if not given:
+        raise ValueError(f"{name}: K rows, V rows or both")
+    n = int(given[0].shape[2]) if given[0].dim() == 4 else -1
+    strides = []
+    for t in (k_rows, v_rows):
+        if t is None:
+            strides.append(None)
+            continue
+        if tuple(t.shape) != (shape.batch, shape.h_kv, n, shape.head_dim):
+            raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim], got {tuple(t.shape)}")
+        if t.dtype != given[0].dtype or t.dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
+        if t.stride(3) != 1:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
+        strides.append((ctypes.c_int64 * 3)(*t.stride()[:3]))
+    return n, BD_DTYPE_BF16 if given[0].dtype == torch.bfloat16 else BD_DTYPE_F32, strides
+
+
+def _dense(name, what, t, dtype, shape):
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: {what} must be a contiguous {tuple(shape)} tensor, got {tuple(t.shape)}")
+
+
+def bd_quant_write(shape, k_rows, v_rows, cache: QuantCache, stream=None):
+    """Quantises rows [batch, h_kv, n, head_dim] (bf16 or fp32; any strides of whole 16 bytes; either may
+    be None) into the cache, behind the context (each sequence's length, if the shape has lengths)."""
+    n, dtype, (ks, vs) = _quant_rows("bd_quant_write", shape, k_rows, v_rows)
+    st = library().bd_quant_write(ctypes.byref(shape), n, dtype, _ptr(k_rows), ks, _ptr(v_rows), vs,
+                                  _quant_cache("bd_quant_write", shape, cache), _stream(stream))
+    _check("bd_quant_write", st)
+
+
+def bd_quant_read(shape, cache: QuantCache, k_out, v_out=None, first_row=None, stream=None):
+    """Reads the cache's rows first_row .. first_row + n - 1 (None: those behind the context) into
+    [batch, h_kv, n, head_dim] tensors, bf16 or fp32; either may be None."""
+    n, dtype, (ks, vs) = _quant_rows("bd_quant_read", shape, k_out, v_out)
+    if first_row is not None and first_row < 0:
+        raise ValueError("bd_quant_read: first_row must not be negative")
+    st = library().bd_quant_read(ctypes.byref(shape), BD_QUANT_BLOCK_ROWS if first_row is None else int(first_row), n,
+                                 dtype, _quant_cache("bd_quant_read", shape, cache), _ptr(k_out), ks, _ptr(v_out), vs,
+                                 _stream(stream))
+    _check("bd_quant_read", st)
+
+
+def bd_quant_draft_attn(shape, q, cache: QuantCache, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
+                        stream=None, flags=0):
+    """bd_draft_attn over a 4-bit cache."""
+    name = "bd_quant_draft_attn"
+    _dense(name, "q", q, torch.bfloat16, (shape.batch, shape.h_q, shape.head_dim))
+    _dense(name, "o_out", o_out, torch.bfloat16, q.shape)
+    _dense(name, "idx", idx, torch.int32, (shape.batch, shape.h_kv, int(budget)))
+    _dense(name, "count", count, torch.int32, (shape.batch, shape.h_kv))
+    if lse_out is not None:
+        _dense(name, "lse_out", lse_out, torch.float32, q.shape[:2])
+    st = library().bd_quant_draft_attn(ctypes.byref(shape), _ptr(q), _quant_cache(name, shape, cache), _ptr(idx),
+                                       _ptr(count), int(budget), int(step_j), int(flags), _ptr(o_out), _ptr(lse_out),
+                                       ws.ptr, ws.nbytes, _stream(stream))
+    _check(name, st)
+
+
+def bd_quant_verify_attn(shape, q, n_q, cache: QuantCache, o_out, lse_out, ws: Workspace, stream=None):
+    """bd_verify_attn over a 4-bit cache; n_q = 1 decodes one token."""
+    name = "bd_quant_verify_attn"
+    _dense(name, "q", q, torch.bfloat16, (shape.batch, shape.h_q, int(n_q), shape.head_dim))
+    _dense(name, "o_out", o_out, torch.bfloat16, q.shape)
+    if lse_out is not None:
+        _dense(name, "lse_out", lse_out, torch.float32, q.shape[:3])
+    st = library().bd_quant_verify_attn(ctypes.byref(shape), _ptr(q), int(n_q), _quant_cache(name, shape, cache),
+                                        _ptr(o_out), _ptr(lse_out), ws.ptr, ws.nbytes, _stream(stream))
+    _check(name, st)
 
 
 def bd_check_wait_timeout(ws: Workspace, limit_us: int, stream=None):

@@ -97,13 +97,20 @@ cudaError_t make_rows_map(CUtensorMap* map, const void* base, long long n_rows, 
 
 using namespace bd;
 
+#define BD_TRY(x)                  \
+  do {                             \
+    const int _st = (x);           \
+    if (_st != BD_OK) return _st;  \
+  } while (0)
+
 namespace {
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-int check_shape(const bd_shape* s) {
+// least_t: 1, or 0 for the calls that take an empty context
+int check_shape(const bd_shape* s, int least_t = 1) {
   if (!s) return BD_ERR_INVALID_ARG;
-  if (s->batch < 1 || s->h_q < 1 || s->h_kv < 1 || s->h_q % s->h_kv != 0 || s->t_ctx < 1 || s->t_cap < s->t_ctx)
+  if (s->batch < 1 || s->h_q < 1 || s->h_kv < 1 || s->h_q % s->h_kv != 0 || s->t_ctx < least_t || s->t_cap < s->t_ctx)
     return BD_ERR_INVALID_ARG;
   if (s->head_dim != 64 && s->head_dim != 128) return BD_ERR_UNSUPPORTED;
   // every per-unit row offset must stay addressable by the TMA (rows < 2^31)
@@ -127,18 +134,47 @@ void* region(void* ws, int units) { return static_cast<uint8_t*>(ws) + ws_region
 
 bool group_supported_by_draft(int g) { return g >= 1 && g <= 16; }
 
-}  // namespace
+constexpr int kQuantMaxRows = 768;   // query rows of a KV head in one block over a 4-bit cache
 
-#define BD_TRY(x)                  \
-  do {                             \
-    const int _st = (x);           \
-    if (_st != BD_OK) return _st;  \
-  } while (0)
+// A 4-bit cache's tensors, of K and / or V.
+int check_quant_cache(const bd_quant_cache* c, bool k, bool v) {
+  if (!c) return BD_ERR_INVALID_ARG;
+  if (k) {
+    BD_TRY(check_tensor(c->k_codes, 16));
+    BD_TRY(check_tensor(c->k_scales, 16));
+  }
+  if (v) {
+    BD_TRY(check_tensor(c->v_codes, 16));
+    BD_TRY(check_tensor(c->v_scales, 16));
+  }
+  return BD_OK;
+}
+
+// The rows of one tensor of a write or a read: [batch, h_kv, n_rows, d], dense where strides is null.
+// The destination of a read must not overlap itself: no stride of 0 between rows that differ.
+int quant_rows(const bd_shape& s, const void* rows, const int64_t* strides, int n_rows, int dtype, bool write, QuantTensor* t) {
+  t->rows = const_cast<void*>(rows);
+  if (!rows) return BD_OK;
+  const int64_t d = s.head_dim, n = std::max(n_rows, 1), dense[3] = {s.h_kv * n * d, n * d, d};
+  const int64_t* st = strides ? strides : dense;
+  const int64_t vec = dtype == BD_DTYPE_F32 ? 4 : 8, size[3] = {s.batch, s.h_kv, n_rows};
+  for (int i = 0; i < 3; ++i) {
+    if (st[i] < 0 || st[i] >= (int64_t)1 << 48) return BD_ERR_INVALID_ARG;
+    if (size[i] > 1 && st[i] % vec != 0) return BD_ERR_MISALIGNED;
+    if (!write && size[i] > 1 && st[i] < d) return BD_ERR_INVALID_ARG;
+  }
+  t->sb = st[0];
+  t->sh = st[1];
+  t->sn = st[2];
+  return check_tensor(rows, 16);
+}
+
+}  // namespace
 
 extern "C" {
 
 size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
-  if (check_shape(shape) != BD_OK) return 0;
+  if (check_shape(shape, op == BD_OP_QUANT_VERIFY || op == BD_OP_QUANT_DRAFT ? 0 : 1) != BD_OK) return 0;
   const bd_shape& s = *shape;
   const int units = s.batch * s.h_kv;
   switch (op) {
@@ -164,6 +200,23 @@ size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
                            ? base + lse_region_bytes(s, n_q)
                            : 0;
       return std::max(a, b);
+    }
+    case BD_OP_QUANT_DRAFT: {
+      const int g = s.h_q / s.h_kv;
+      QuantAttnPlan qp;
+      if (n_q < 1 || budget < 1 || !group_supported_by_draft(g) || !quant_attn_plan(s, g, (long)budget + n_q, &qp)) return 0;
+      return ws_region_offset(units) + quant_attn_bytes(s, g, qp);
+    }
+    case BD_OP_QUANT_VERIFY: {
+      const long long g = s.h_q / s.h_kv;
+      if (n_q < 1 || g * n_q > kQuantMaxRows) return 0;
+      size_t bytes = 0;
+      for (int n = 1; n <= n_q; ++n) {       // (a shorter block's rows may be split over more CTAs)
+        QuantAttnPlan qp;
+        if (!quant_attn_plan(s, (int)g * n, (long)s.t_ctx + n, &qp)) return 0;
+        bytes = std::max(bytes, quant_attn_bytes(s, (int)g * n, qp));
+      }
+      return ws_region_offset(units) + bytes;
     }
     default:
       return 0;
@@ -371,6 +424,82 @@ int bd_write_block_rows(const bd_shape* shape, int n_rows, const void* k_rows, c
       return BD_ERR_CUDA;
   }
   return BD_OK;
+}
+
+int bd_quant_write(const bd_shape* shape, int n_rows, int dtype, const void* k_rows, const int64_t* k_strides,
+                   const void* v_rows, const int64_t* v_strides, const bd_quant_cache* cache, void* stream) {
+  BD_TRY(check_shape(shape, 0));
+  const bd_shape& s = *shape;
+  if (n_rows < 0 || (long long)s.t_ctx + n_rows > s.t_cap || (!k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
+  BD_TRY(check_quant_cache(cache, k_rows != nullptr, v_rows != nullptr));
+  QuantTensor k, v;
+  BD_TRY(quant_rows(s, k_rows, k_strides, n_rows, dtype, true, &k));
+  BD_TRY(quant_rows(s, v_rows, v_strides, n_rows, dtype, true, &v));
+  if (n_rows == 0) return BD_OK;
+  return map_cuda(launch_quant_write(s, n_rows, dtype, *cache, k, v, static_cast<cudaStream_t>(stream)));
+}
+
+int bd_quant_read(const bd_shape* shape, int first_row, int n_rows, int dtype, const bd_quant_cache* cache, void* k_rows,
+                  const int64_t* k_strides, void* v_rows, const int64_t* v_strides, void* stream) {
+  BD_TRY(check_shape(shape, 0));
+  const bd_shape& s = *shape;
+  const long long first = first_row == BD_QUANT_BLOCK_ROWS ? s.t_ctx : first_row;
+  if (first < 0 || n_rows < 0 || first + n_rows > s.t_cap || (!k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
+  BD_TRY(check_quant_cache(cache, k_rows != nullptr, v_rows != nullptr));
+  QuantTensor k, v;
+  BD_TRY(quant_rows(s, k_rows, k_strides, n_rows, dtype, false, &k));
+  BD_TRY(quant_rows(s, v_rows, v_strides, n_rows, dtype, false, &v));
+  if (n_rows == 0) return BD_OK;
+  return map_cuda(launch_quant_read(s, first_row, n_rows, dtype, *cache, k, v, static_cast<cudaStream_t>(stream)));
+}
+
+int bd_quant_draft_attn(const bd_shape* shape, const void* q, const bd_quant_cache* cache, const int32_t* idx,
+                        const int32_t* count, int budget, int step_j, unsigned flags, void* o_out, float* lse_out, void* ws,
+                        size_t ws_bytes, void* stream) {
+  BD_TRY(check_shape(shape, 0));
+  const bd_shape& s = *shape;
+  BD_TRY(check_tensor(q, 16));
+  BD_TRY(check_quant_cache(cache, true, true));
+  BD_TRY(check_tensor(idx, 4));
+  BD_TRY(check_tensor(count, 4));
+  BD_TRY(check_tensor(o_out, 16));
+  if (lse_out) BD_TRY(check_tensor(lse_out, 4));
+  if (budget < 1 || step_j < 0 || (long long)s.t_ctx + step_j >= s.t_cap) return BD_ERR_INVALID_ARG;
+  if (flags & ~BD_DRAFT_VIEW_READY) return BD_ERR_INVALID_ARG;
+  const int g = s.h_q / s.h_kv, units = s.batch * s.h_kv;
+  QuantAttnPlan qp;
+  if (!group_supported_by_draft(g) || (long long)budget + step_j >= (1LL << 30) ||
+      !quant_attn_plan(s, g, (long)budget + step_j + 1, &qp))
+    return BD_ERR_UNSUPPORTED;
+  if (!ws) return BD_ERR_WORKSPACE;
+  if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
+  if (ws_bytes < ws_region_offset(units) + quant_attn_bytes(s, g, qp)) return BD_ERR_WORKSPACE;
+  const QuantAttnCall call = {q, o_out, lse_out, g, 1, idx, count, budget, step_j};
+  return map_cuda(launch_quant_attn(s, qp, call, *cache, region(ws, units), counters(ws), status_word(ws),
+                                    static_cast<cudaStream_t>(stream)));
+}
+
+int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_quant_cache* cache, void* o_out,
+                         float* lse_out, void* ws, size_t ws_bytes, void* stream) {
+  BD_TRY(check_shape(shape, 0));
+  const bd_shape& s = *shape;
+  BD_TRY(check_tensor(q, 16));
+  BD_TRY(check_quant_cache(cache, true, true));
+  BD_TRY(check_tensor(o_out, 16));
+  if (lse_out) BD_TRY(check_tensor(lse_out, 4));
+  if (n_q < 1 || (long long)s.t_ctx + n_q > s.t_cap) return BD_ERR_INVALID_ARG;
+  const long long rows = (long long)(s.h_q / s.h_kv) * n_q;
+  const int units = s.batch * s.h_kv;
+  QuantAttnPlan qp;
+  if (rows > kQuantMaxRows || !quant_attn_plan(s, (int)rows, (long)s.t_ctx + n_q, &qp)) return BD_ERR_UNSUPPORTED;
+  if (!ws) return BD_ERR_WORKSPACE;
+  if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
+  if (ws_bytes < ws_region_offset(units) + quant_attn_bytes(s, (int)rows, qp)) return BD_ERR_WORKSPACE;
+  const QuantAttnCall call = {q, o_out, lse_out, (int)rows, n_q, nullptr, nullptr, 0, 0};
+  return map_cuda(launch_quant_attn(s, qp, call, *cache, region(ws, units), counters(ws), status_word(ws),
+                                    static_cast<cudaStream_t>(stream)));
 }
 
 int bd_check_wait_timeout(void* ws, size_t ws_bytes, int limit_us, void* stream) {

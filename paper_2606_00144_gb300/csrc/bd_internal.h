@@ -153,6 +153,39 @@ cudaError_t launch_advance(const bd_shape& s, int window, int n_q, const int32_t
                            const float* verify_lse, void* q_window, float* window_lse, int32_t* idx, int32_t* count,
                            int capacity, int32_t* advance_out, cudaStream_t stream);
 
+// ---------------------------------------------------------------------------- 4-bit caches
+struct QuantTensor {    // one tensor's rows of a write or a read: strides in elements; rows null: not this tensor
+  void* rows;
+  long long sb, sh, sn;
+};
+cudaError_t launch_quant_write(const bd_shape& s, int n_rows, int dtype, const bd_quant_cache& c, const QuantTensor& k,
+                               const QuantTensor& v, cudaStream_t stream);
+// first_row < 0: the rows behind each sequence's length.
+cudaError_t launch_quant_read(const bd_shape& s, int first_row, int n_rows, int dtype, const bd_quant_cache& c,
+                              const QuantTensor& k, const QuantTensor& v, cudaStream_t stream);
+
+struct QuantAttnCall {
+  const void* q;        // [units][rows][head_dim]
+  void* o_out;
+  float* lse_out;
+  int rows;             // query rows of a KV head: group * n_q
+  int n_q;              // queries per head (a drafter pass: 1)
+  const int32_t* idx;   // a drafter pass's view (null: a verify block)
+  const int32_t* count;
+  int budget, step_j;
+};
+struct QuantAttnPlan {
+  int nt, chunks;       // n8 tiles of a CTA's query rows; chunks of a KV head's rows
+  int n_split;          // CTAs of a unit's entries
+  int most_split;       // the most that any length of this shape takes
+};
+// entries: the most that a unit attends to
+bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* plan);
+// Op region for any number of entries with this many query rows.
+size_t quant_attn_bytes(const bd_shape& s, int rows, const QuantAttnPlan& plan);
+cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
+                              void* ws_region, int* counters, int* status, cudaStream_t stream);
+
 // ---------------------------------------------------------------------------- TMA maps
 // 3-D map over a [units, rows_total (stride t_cap), head_dim] bf16 cache: only rows
 // [0, n_rows) of each unit are addressable (the rest reads as zero).  Box = 64 columns x

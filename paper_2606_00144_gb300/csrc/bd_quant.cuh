@@ -1,0 +1,71 @@
+// What the kernels over a 4-bit cache (include/budgetdraft.h, bd_quant_cache) share.
+//
+// A row of D elements is D/2 bytes of 4-bit codes (element 2 j in the low half of byte j) and one bf16
+// scale for every group of 32 elements; code c of group g stands for (c - 8) * scale[g].
+//
+// Codes reach the tensor cores without a conversion: a code in the low bits of an fp16's mantissa
+// is the subnormal c * 2^-24, exactly, and the next one, left where it lies four bits higher, 16 c *
+// 2^-24.  One AND of a 32-bit word that holds two 16-bit units so makes two operands, and four
+// ANDs and a shift unpack eight codes.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "bd_common.cuh"
+
+namespace bd {
+
+constexpr int kQGroup = 32;                  // elements of a scale's group
+constexpr uint32_t kNibble0 = 0x000f000fu;   // codes 0 of a word's two 16-bit units, as c * 2^-24
+constexpr uint32_t kNibble1 = 0x00f000f0u;   // codes 1, as 16 c * 2^-24
+
+__device__ __forceinline__ float bf16_bits_to_float(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 2^e for -126 <= e <= 127.
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
+
+__device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Codes 0, codes 1 of a word's two 16-bit units as (c - 8) * 2^-10, exactly.
+__device__ __forceinline__ uint32_t fma_half2(uint32_t a, uint32_t b, uint32_t c) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b),
+                            *reinterpret_cast<const __half2*>(&c));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t centred0(uint32_t w) {   // c 2^-24 * 2^14 - 2^-7
+  return fma_half2(w & kNibble0, 0x74007400u, 0xa000a000u);
+}
+__device__ __forceinline__ uint32_t centred1(uint32_t w) {   // 16 c 2^-24 * 2^10 - 2^-7
+  return fma_half2(w & kNibble1, 0x64006400u, 0xa000a000u);
+}
+
+// 4- and 8-byte cp.async (through L1), zero bytes where !valid.
+template <int BYTES>
+__device__ __forceinline__ void cp_async_small(void* dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES),
+               "r"(valid ? BYTES : 0)
+               : "memory");
+}
+
+// The exponent that normalises a cache row's V scales: floor(log2) of the largest, within [-100, 126].
+// Scales are taken to fp16 as scale * 2^-e (the largest in [1, 2)) and 2^e joins the row's softmax
+// weight, so that V of any size keeps its precision in fp16.  A row of zeros (or smaller than
+// 2^-100) has -100; a row with a NaN scale 0 (its products are NaN whatever e is).
+__device__ __forceinline__ int scale_exponent(uint32_t largest_bits) {
+  const int e = (int)((largest_bits >> 7) & 0xffu);
+  return e == 255 ? 0 : min(max(e - 127, -100), 126);
+}
+
+}  // namespace bd

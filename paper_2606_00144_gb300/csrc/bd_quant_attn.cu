@@ -1,0 +1,544 @@
+// Attention over a 4-bit cache on mma.sync: the drafter's pass over a sparse view
+// (bd_quant_draft_attn), and verify blocks (bd_quant_verify_attn).
+//
+// A warp takes tiles of 32 entries of its CTA's slice; K is the A operand (16 entries x 16 elements), the
+// query rows the n8 side, as in the bf16 kernels, and the codes become fp16 operands by masking (bd_quant.cuh):
+//   D_g   = sum over group g of c q - 8 sum q      the -8 sum is the accumulator's first value, so the
+//                                                  group's products leave the MMA centred;
+//   S     = sum_g scale_g D_g                      fp32, exact products of a 4-bit and an 8-bit number;
+//   P_g   = 2^(S - M + e) ns_g                     fp16, ns_g the row's V scale of group g over 2^e
+//                                                  (scale_exponent): 11 bits, where bf16 would keep 8; a
+//                                                  weight below 2^-30 of the largest is lost;
+//   O^T_g += (V_codes - 8)^T P_g                   centred before the MMA (one FMA for two codes): with the
+//                                                  offset in, an element whose heavy rows hold zeros is
+//                                                  what is left of a cancellation, to 2^-17 of the weights
+//                                                  (the MMA aligns a subnormal as if its leading zeros counted).
+// ldmatrix lays a row's 16-byte group out as the A operand of S (a 32-bit word a lane), its transposed form as the
+// A operand of O^T (16-bit units of two rows in a word), so neither side needs a shuffle.
+// M is a running maximum of S + e that may trail by 2^8; each warp keeps its own, and the warps, then the CTAs
+// of a unit, are merged at the end (the last CTA to arrive merges, in the CTAs' order).
+#include <algorithm>
+
+#include "bd_internal.h"
+#include "bd_quant.cuh"
+
+namespace bd {
+
+constexpr int kQaWarps = 4;
+constexpr int kQaThreads = 32 * kQaWarps;
+constexpr int kQaTile = 32;          // entries of a warp's tile
+constexpr int kQaStages = 3;
+constexpr int kQaMaxSplit = 32;      // CTAs of a unit
+constexpr float kQaSlack = 8.f;      // log2 of how far the running maximum may trail
+constexpr float kQaLift = 6.f;       // weights are kept 2^6 higher: fp16's range is wider above 1 than P needs
+
+struct QuantAttnParams {
+  const uint8_t* kc;           // [units][t_cap][D / 2]
+  const uint16_t* ks;          // [units][t_cap][D / 32]
+  const uint8_t* vc;
+  const uint16_t* vs;
+  const __nv_bfloat16* q;      // [units][rows][D]: rows = query heads of a KV head x n_q
+  __nv_bfloat16* o;
+  float* lse;                  // or null
+  float* o_part;               // [units][n_split][rows][D], normalised
+  float* lse_part;             // [units][n_split][rows]
+  int* counters;               // [units]
+  int* status;
+  const int32_t* seq_lens;
+  const int32_t* idx;          // drafter pass: [units][budget]
+  const int32_t* count;
+  int h_kv, t_ctx, t_cap, n_q, rows, budget, step_j, n_split;
+  float scale_log2;            // log2(e) / sqrt(D)
+};
+
+template <int D>
+struct QaStage {
+  static constexpr int CODES = kQaTile * D / 2;                  // bytes of a tile's codes
+  static constexpr int SCALES = kQaTile * D / kQGroup * 2;
+  static constexpr int BYTES = 2 * (CODES + SCALES);
+};
+// Byte offset of 16-byte group g of row r in a tile of codes: groups rotate so that eight rows' reads of one
+// group fall into different banks.
+template <int D>
+__device__ __forceinline__ uint32_t code_offset(int r, int g) {
+  return D == 128 ? r * 64 + ((g ^ (r >> 1 & 3)) << 4) : r * 32 + ((g ^ (r >> 2 & 1)) << 4);
+}
+
+template <int D, int NT>
+struct QaSmem {
+  static constexpr size_t kRing = (size_t)kQaWarps * kQaStages * QaStage<D>::BYTES;
+  static constexpr size_t kMerge = (size_t)kQaWarps * 8 * NT * (D + 4 + 2) * 4;
+  static constexpr size_t kTotal = (kRing > kMerge ? kRing : kMerge);
+};
+
+__device__ __forceinline__ int quant_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
+  if (seq_lens == nullptr) return t_ctx;
+  int t = seq_lens[b];
+  if (t < 0 || t > t_ctx) {
+    if (status) record_error(status, BD_ERR_INVALID_ARG);
+    t = min(max(t, 0), t_ctx);
+  }
+  return t;
+}
+
+// NT: n8 tiles of query rows; GATHER: entries come from idx (and the drafted rows), else entry = cache row.
+template <int D, int NT, bool GATHER>
+__global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_constant__ QuantAttnParams p) {
+  using ST = QaStage<D>;
+  constexpr int G = D / 32, NQC = 8 * NT;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const int split = blockIdx.x, unit = blockIdx.y, row0 = blockIdx.z * NQC;
+  const int rows = min(p.rows - row0, NQC);
+  const int b = unit / p.h_kv;
+  grid_dependency_wait();
+  allow_dependent_launch();
+
+  int* status = tid == 0 ? p.status : nullptr;
+  const int t_unit = quant_context(p.seq_lens, b, p.t_ctx, status);
+  int cnt = 0;
+  if (GATHER) {
+    cnt = __ldg(p.count + unit);
+    if (cnt < 0 || cnt > p.budget) {
+      if (status) record_error(status, BD_ERR_INVALID_ARG);
+      cnt = min(max(cnt, 0), p.budget);
+    }
+  }
+  const int n_entries = GATHER ? cnt + p.step_j + 1 : t_unit + p.n_q;
+  // equal slices of whole 16-entry sub-tiles; n_seg of them hold entries
+  const int per = ((n_entries + 16 * p.n_split - 1) / (16 * p.n_split)) * 16;
+  const int n_seg = (n_entries + per - 1) / per;
+  if (split >= n_seg) return;
+  const int e_begin = split * per, e_end = min(n_entries, e_begin + per);
+  const int n_tiles = (e_end - e_begin + kQaTile - 1) / kQaTile;
+
+  const size_t base = (size_t)unit * p.t_cap;
+  uint8_t* ring = smem + (size_t)warp * kQaStages * ST::BYTES;
+
+  // entry `lane` of a tile: its cache row, or -1
+  auto entry_row = [&](int tile) {
+    const int e = e_begin + tile * kQaTile + lane;
+    if (e >= e_end) return -1;
+    if (!GATHER) return e;
+    if (e >= cnt) return t_unit + (e - cnt);
+    const int r = __ldg(p.idx + (size_t)unit * p.budget + e);
+    if (r < 0 || r >= t_unit) {
+      record_error(p.status, BD_ERR_INVALID_ARG);
+      return -1;
+    }
+    return r;
+  };
+  // row: this lane's entry_row; returns which of the tile's entries are there (the rest are zero-filled)
+  auto fetch = [&](int row, int slot) {
+    uint8_t* st = ring + slot * ST::BYTES;
+    constexpr int PER = 32 / G;                // rows a pass of the warp covers, G 16-byte groups each
+#pragma unroll
+    for (int it = 0; it < G; ++it) {
+      const int r = it * PER + lane / G, g = lane % G;
+      const int src_row = __shfl_sync(0xffffffffu, row, r);
+      const size_t src = (base + max(src_row, 0)) * (D / 2) + 16 * g;
+      const uint32_t off = code_offset<D>(r, g);
+      cp_async16_zfill(st + off, p.kc + src, src_row >= 0);
+      cp_async16_zfill(st + ST::CODES + off, p.vc + src, src_row >= 0);
+    }
+    const size_t src = (base + max(row, 0)) * G;
+    cp_async_small<2 * G>(st + 2 * ST::CODES + lane * 2 * G, p.ks + src, row >= 0);
+    cp_async_small<2 * G>(st + 2 * ST::CODES + ST::SCALES + lane * 2 * G, p.vs + src, row >= 0);
+    return __ballot_sync(0xffffffffu, row >= 0);
+  };
+
+  // this warp's tiles: warp, warp + kQaWarps, ...
+  const int mine = n_tiles > warp ? (n_tiles - warp + kQaWarps - 1) / kQaWarps : 0;
+  uint32_t live[kQaStages] = {};                    // of this iteration's tile and the next ones
+#pragma unroll
+  for (int i = 0; i < kQaStages - 1; ++i) {
+    if (i < mine) live[i] = fetch(entry_row(warp + i * kQaWarps), i);
+    cp_async_commit();
+  }
+  int next_row = kQaStages - 1 < mine ? entry_row(warp + (kQaStages - 1) * kQaWarps) : -1;
+
+  // ---- the query rows as B operands: fp16 over a power of two of their own, odd elements over 16 more
+  uint32_t bq[NT][G][4];
+  float bias[NT][G][2], mult[NT][2];
+  int lim[NT][2];                              // last visible entry of this lane's columns
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 8 * nt + gid;                // B column gid
+    uint4 w[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      w[g] = r < rows ? *reinterpret_cast<const uint4*>(p.q + ((size_t)unit * p.rows + row0 + r) * D + 32 * g + 8 * tig)
+                      : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t top = 0;                          // largest exponent of the row's finite elements
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
+        top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+      }
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int qe = min(max((int)top - 127, -100), 100);        // the row's elements are below 2^(qe + 1)
+    const float down = pow2i(13 - qe);                         // to fp16: below 2^14
+    float sums[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(x[e] << 16) * down;
+        f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
+      }
+      // element pairs (0, 4), (1, 5), (2, 6), (3, 7): the codes that one mask of a word leaves
+      bq[nt][g][0] = pack_half2(f[0], f[4]);
+      bq[nt][g][1] = pack_half2(f[1] * 0.0625f, f[5] * 0.0625f);
+      bq[nt][g][2] = pack_half2(f[2], f[6]);
+      bq[nt][g][3] = pack_half2(f[3] * 0.0625f, f[7] * 0.0625f);
+      float s = 0.f;                           // of what the MMA will multiply
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&bq[nt][g][e]));
+        s += (h.x + h.y) * (e & 1 ? 16.f : 1.f);
+      }
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);
+      sums[g] = s;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {              // this lane's accumulator columns
+      const int src = 4 * (2 * tig + e), col = 8 * nt + 2 * tig + e;
+#pragma unroll
+      for (int g = 0; g < G; ++g) bias[nt][g][e] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], src);
+      // S over the products' 2^-24 and the row's own power of two, in log2 units
+      mult[nt][e] = p.scale_log2 * 0x1p11f * pow2i(__shfl_sync(0xffffffffu, qe, src));
+      lim[nt][e] = GATHER || col >= rows ? 0x7fffffff : t_unit + (row0 + col) % p.n_q;
+    }
+  }
+
+  float o[2 * G][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < 2 * G; ++mt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[mt][nt][c] = 0.f;
+  }
+
+  for (int i = 0; i < mine; ++i) {
+    const int tile = warp + i * kQaWarps;
+    // the tile two further on, its rows looked up an iteration ago
+    if (i + kQaStages - 1 < mine) live[kQaStages - 1] = fetch(next_row, (i + kQaStages - 1) % kQaStages);
+    cp_async_commit();
+    if (i + kQaStages < mine) next_row = entry_row(tile + kQaStages * kQaWarps);
+    cp_async_wait<kQaStages - 1>();
+    __syncwarp();
+    const uint8_t* st = ring + (i % kQaStages) * ST::BYTES;
+    const uint32_t kbase = smem_u32(st), vbase = kbase + ST::CODES;
+    const uint16_t* ksm = reinterpret_cast<const uint16_t*>(st + 2 * ST::CODES);
+    const uint16_t* vsm = reinterpret_cast<const uint16_t*>(st + 2 * ST::CODES + ST::SCALES);
+    const int e0 = e_begin + tile * kQaTile;
+
+    // ---------------------------------------------------------------- S of two 16-entry sub-tiles
+    float s[2][NT][4], vn[2][2][G], ve[2][2];   // scores; V scales over 2^ve of rows gid, gid + 8
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      uint32_t kw[2 * G];                       // [group][row half]
+#pragma unroll
+      for (int gp = 0; gp < G; gp += 2) {
+        uint32_t r4[4];
+        const int r = 16 * sub + (lane & 15), g = gp + (lane >> 4);
+        ldmatrix_x4(r4, kbase + code_offset<D>(r, g));
+        kw[2 * gp] = r4[0], kw[2 * gp + 1] = r4[1], kw[2 * gp + 2] = r4[2], kw[2 * gp + 3] = r4[3];
+      }
+      float kscale[2][G];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = 16 * sub + 8 * h + gid;
+        uint32_t top = 0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          kscale[h][g] = bf16_bits_to_float(ksm[r * G + g]);
+          const uint32_t v = vsm[r * G + g];
+          vn[sub][h][g] = bf16_bits_to_float(v);
+          top = max(top, v & 0x7fffu);
+        }
+        const int e = scale_exponent(top);
+        ve[sub][h] = (float)e;
+        const float down = pow2i(-e);
+#pragma unroll
+        for (int g = 0; g < G; ++g) vn[sub][h][g] *= down;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[sub][nt][c] = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const uint32_t w0 = kw[2 * g], w1 = kw[2 * g + 1], x0 = w0 >> 8, x1 = w1 >> 8;
+          float d[4] = {bias[nt][g][0], bias[nt][g][1], bias[nt][g][0], bias[nt][g][1]};
+          mma_16816_f16(d, w0 & kNibble0, w1 & kNibble0, w0 & kNibble1, w1 & kNibble1, bq[nt][g][0], bq[nt][g][1]);
+          mma_16816_f16(d, x0 & kNibble0, x1 & kNibble0, x0 & kNibble1, x1 & kNibble1, bq[nt][g][2], bq[nt][g][3]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[sub][nt][c] = fmaf(d[c], kscale[c >> 1][g], s[sub][nt][c]);
+        }
+      }
+    }
+
+    // ---------------------------------------------------------------- weights
+    const bool masked = live[0] != 0xffffffffu || (!GATHER && e0 + kQaTile - 1 > t_unit);
+    bool grow = false;
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float y = s[sub][nt][c] * mult[nt][c & 1] + ve[sub][c >> 1];
+          if (masked) {
+            const int r = 16 * sub + 8 * (c >> 1) + gid;
+            if ((live[0] >> r & 1) == 0 || (!GATHER && e0 + r > lim[nt][c & 1])) y = -INFINITY;
+          }
+          s[sub][nt][c] = y;
+          grow |= y > m[nt][c & 1] + kQaSlack;
+        }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(fmaxf(s[0][nt][e], s[0][nt][e + 2]), fmaxf(s[1][nt][e], s[1][nt][e + 2]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          mx = fmaxf(mx, m[nt][e]);
+          const float alpha = mx == -INFINITY ? 1.f : fast_exp2(m[nt][e] - mx);
+          m[nt][e] = mx;
+          l[nt][e] *= alpha;
+#pragma unroll
+          for (int mt = 0; mt < 2 * G; ++mt) {
+            o[mt][nt][e] *= alpha;
+            o[mt][nt][e + 2] *= alpha;
+          }
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float nm = kQaLift - (m[nt][e] == -INFINITY ? 0.f : m[nt][e]);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float w = fast_exp2(s[sub][nt][2 * h + e] + nm);
+            s[sub][nt][2 * h + e] = w;
+            l[nt][e] = fmaf(w, pow2i(-(int)ve[sub][h]), l[nt][e]);
+          }
+      }
+
+    // ---------------------------------------------------------------- O^T += V^T P^T
+    uint32_t vw[2][2 * G];                      // [sub][group][entry half]
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int gp = 0; gp < G; gp += 2) {
+        uint32_t r4[4];
+        const int r = 16 * sub + (lane & 15), g = gp + (lane >> 4);
+        ldmatrix_x4_trans(r4, vbase + code_offset<D>(r, g));
+        vw[sub][2 * gp] = r4[0], vw[sub][2 * gp + 1] = r4[1], vw[sub][2 * gp + 2] = r4[2], vw[sub][2 * gp + 3] = r4[3];
+      }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+          const float* w = s[sub][nt];
+          const uint32_t b0 = movmatrix_trans(pack_half2(w[0] * vn[sub][0][g], w[1] * vn[sub][0][g]));
+          const uint32_t b1 = movmatrix_trans(pack_half2(w[2] * vn[sub][1][g], w[3] * vn[sub][1][g]));
+          const uint32_t w0 = vw[sub][2 * g], w1 = vw[sub][2 * g + 1], x0 = w0 >> 8, x1 = w1 >> 8;
+          mma_16816_f16(o[2 * g][nt], centred0(w0), centred1(w0), centred0(w1), centred1(w1), b0, b1);
+          mma_16816_f16(o[2 * g + 1][nt], centred0(x0), centred1(x0), centred0(x1), centred1(x1), b0, b1);
+        }
+      }
+    __syncwarp();                               // the slot is free
+#pragma unroll
+    for (int k = 0; k + 1 < kQaStages; ++k) live[k] = live[k + 1];
+  }
+  cp_async_wait<0>();
+  __syncthreads();                              // every warp's ring is free: the merge area
+
+  // ---------------------------------------------------------------- the warps' states
+  constexpr int OP = D + 4;
+  float* o_s = reinterpret_cast<float*>(smem);                 // [warp][NQC][OP]
+  float* m_s = o_s + kQaWarps * NQC * OP;                      // [warp][NQC]
+  float* l_s = m_s + kQaWarps * NQC;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float sum = l[nt][e];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+      const int at = warp * NQC + 8 * nt + 2 * tig + e;
+      if (gid == 0) {
+        m_s[at] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] - kQaLift;
+        l_s[at] = sum;
+      }
+      // four adjacent elements 32 g + 4 gid ..
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        *reinterpret_cast<float4*>(o_s + (size_t)at * OP + 32 * g + 4 * gid) =
+            make_float4(o[2 * g][nt][e] * 0x1p10f, o[2 * g][nt][e + 2] * 0x1p10f, o[2 * g + 1][nt][e] * 0x1p10f,
+                        o[2 * g + 1][nt][e + 2] * 0x1p10f);
+    }
+  __syncthreads();
+  const size_t out0 = (size_t)unit * p.rows + row0;
+  const size_t part0 = ((size_t)unit * p.n_split + split) * p.rows + row0;
+  const bool whole = n_seg == 1;
+  for (int i = tid; i < rows * (D / 4); i += kQaThreads) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4;
+    float mx = -INFINITY, tot = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kQaWarps; ++w) mx = fmaxf(mx, m_s[w * NQC + r]);
+#pragma unroll
+    for (int w = 0; w < kQaWarps; ++w) {
+      const float mw = m_s[w * NQC + r], lw = l_s[w * NQC + r];
+      if (mw == -INFINITY && lw == 0.f) continue;              // a warp without entries for this row
+      const float f = fast_exp2(mw - mx);
+      const float4 v = *reinterpret_cast<const float4*>(o_s + (size_t)(w * NQC + r) * OP + d);
+      tot = fmaf(f, lw, tot);
+      a.x = fmaf(f, v.x, a.x);
+      a.y = fmaf(f, v.y, a.y);
+      a.z = fmaf(f, v.z, a.z);
+      a.w = fmaf(f, v.w, a.w);
+    }
+    const float inv = tot == 0.f ? 0.f : 1.f / tot;            // (a NaN stays one)
+    a.x *= inv, a.y *= inv, a.z *= inv, a.w *= inv;
+    const float lse = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * kLn2;
+    if (whole) {
+      *reinterpret_cast<uint2*>(p.o + (out0 + r) * D + d) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+      if (d == 0 && p.lse) p.lse[out0 + r] = lse;
+    } else {
+      *reinterpret_cast<float4*>(p.o_part + (part0 + r) * D + d) = a;
+      if (d == 0) p.lse_part[part0 + r] = lse;
+    }
+  }
+  if (whole) return;
+
+  // ---------------------------------------------------------------- the unit's last CTA merges
+  __shared__ int last;
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) last = atomicAdd(&p.counters[unit], 1) == n_seg * (int)gridDim.z - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  const float* part = p.o_part + (size_t)unit * p.n_split * p.rows * D;
+  const float* lses = p.lse_part + (size_t)unit * p.n_split * p.rows;
+  for (int i = tid; i < p.rows * (D / 4); i += kQaThreads) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4;
+    float mx = -INFINITY, tot = 0.f;
+    for (int sp = 0; sp < n_seg; ++sp) mx = fmaxf(mx, __ldcg(lses + (size_t)sp * p.rows + r));
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int sp = 0; sp < n_seg; ++sp) {
+      const float ls = __ldcg(lses + (size_t)sp * p.rows + r);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)sp * p.rows + r) * D + d));
+      if (ls == -INFINITY) continue;
+      const float f = fast_exp2((ls - mx) * kLog2e);
+      tot += f;
+      a.x = fmaf(f, v.x, a.x);
+      a.y = fmaf(f, v.y, a.y);
+      a.z = fmaf(f, v.z, a.z);
+      a.w = fmaf(f, v.w, a.w);
+    }
+    const float inv = tot == 0.f ? 0.f : 1.f / tot;
+    *reinterpret_cast<uint2*>(p.o + ((size_t)unit * p.rows + r) * D + d) =
+        make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+    if (d == 0 && p.lse) p.lse[(size_t)unit * p.rows + r] = tot == 0.f ? -INFINITY : mx + logf(tot);
+  }
+  if (tid == 0) p.counters[unit] = 0;
+}
+
+// ============================================================================ host side
+
+namespace {
+
+struct QaInfo {
+  const void* fn;
+  size_t smem;
+};
+template <int D, int NT>
+QaInfo qa_info(bool gather) {
+  return {gather ? reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, true>)
+                 : reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, false>),
+          QaSmem<D, NT>::kTotal};
+}
+QaInfo qa_kernel(int d, int nt, bool gather) {
+  if (d == 64) return nt == 1 ? qa_info<64, 1>(gather) : qa_info<64, 2>(gather);
+  return nt == 1 ? qa_info<128, 1>(gather) : qa_info<128, 2>(gather);
+}
+
+}  // namespace
+
+bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* plan) {
+  const long units = (long)s.batch * s.h_kv;
+  plan->nt = rows <= 8 ? 1 : 2;
+  plan->chunks = (rows + 8 * plan->nt - 1) / (8 * plan->nt);
+  if (units > 65535 || plan->chunks > 65535) return false;
+  // two CTAs an SM in one wave, none with fewer than 64 entries
+  const long slots = 2L * current_sm_count();
+  plan->most_split = (int)std::min<long>(kQaMaxSplit, std::max(1L, slots / (units * plan->chunks)));
+  plan->n_split = (int)std::max(1L, std::min<long>(plan->most_split, (entries + 63) / 64));
+  return true;
+}
+
+size_t quant_attn_bytes(const bd_shape& s, int rows, const QuantAttnPlan& plan) {
+  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.most_split * rows;
+  return plan.most_split > 1 ? align_up(part_rows * s.head_dim * 4, 256) + align_up(part_rows * 4, 256) : 0;
+}
+
+cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
+                              void* ws_region, int* counters, int* status, cudaStream_t stream) {
+  QuantAttnParams p;
+  p.kc = static_cast<const uint8_t*>(cache.k_codes);
+  p.ks = static_cast<const uint16_t*>(cache.k_scales);
+  p.vc = static_cast<const uint8_t*>(cache.v_codes);
+  p.vs = static_cast<const uint16_t*>(cache.v_scales);
+  p.q = static_cast<const __nv_bfloat16*>(c.q);
+  p.o = static_cast<__nv_bfloat16*>(c.o_out);
+  p.lse = c.lse_out;
+  p.rows = c.rows;
+  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.n_split * c.rows;
+  p.o_part = static_cast<float*>(ws_region);
+  p.lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws_region) + align_up(part_rows * s.head_dim * 4, 256));
+  p.counters = counters;
+  p.status = status;
+  p.seq_lens = s.seq_lens;
+  p.idx = c.idx;
+  p.count = c.count;
+  p.h_kv = s.h_kv;
+  p.t_ctx = s.t_ctx;
+  p.t_cap = s.t_cap;
+  p.n_q = c.n_q;
+  p.budget = c.budget;
+  p.step_j = c.step_j;
+  p.n_split = plan.n_split;
+  p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
+  const QaInfo k = qa_kernel(s.head_dim, plan.nt, c.idx != nullptr);
+  cudaError_t err = allow_shared_memory(k.fn, 128);
+  if (err != cudaSuccess) return err;
+  void* args[] = {&p};
+  return launch_kernel(k.fn, dim3(plan.n_split, s.batch * s.h_kv, plan.chunks), dim3(kQaThreads), k.smem, stream, args, 0);
+}
+
+}  // namespace bd
