@@ -80,6 +80,20 @@ cudaError_t make_cache_map(CUtensorMap* map, const void* base, int units, int t_
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_codes_map(CUtensorMap* map, const void* base, int units, int t_cap, int n_rows, int head_dim, int box_rows) {
+  auto fn = encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t row = (cuuint64_t)head_dim / 2;
+  const cuuint64_t dims[3] = {row, (cuuint64_t)n_rows, (cuuint64_t)units};
+  const cuuint64_t strides[2] = {row, (cuuint64_t)t_cap * row};
+  const cuuint32_t box[3] = {(cuuint32_t)row, (cuuint32_t)box_rows, 1};
+  const cuuint32_t estride[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estride,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 cudaError_t make_rows_map(CUtensorMap* map, const void* base, long long n_rows, int head_dim, int box_rows) {
   auto fn = encode_fn();
   if (!fn) return cudaErrorNotSupported;
@@ -211,10 +225,10 @@ size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
       const long long g = s.h_q / s.h_kv;
       if (n_q < 1 || g * n_q > kQuantMaxRows) return 0;
       size_t bytes = 0;
-      for (int n = 1; n <= n_q; ++n) {       // (a shorter block's rows may be split over more CTAs)
-        QuantAttnPlan qp;
-        if (!quant_attn_plan(s, (int)g * n, (long)s.t_ctx + n, &qp)) return 0;
-        bytes = std::max(bytes, quant_attn_bytes(s, (int)g * n, qp));
+      for (int n = 1; n <= n_q; ++n) {       // (a shorter block may need more partials than a longer one)
+        QuantVerifyPlan qp;
+        if (!quant_verify_plan(s, (int)g * n, n, &qp)) return 0;
+        bytes = std::max(bytes, qp.bytes);
       }
       return ws_region_offset(units) + bytes;
     }
@@ -492,14 +506,15 @@ int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd
   if (n_q < 1 || (long long)s.t_ctx + n_q > s.t_cap) return BD_ERR_INVALID_ARG;
   const long long rows = (long long)(s.h_q / s.h_kv) * n_q;
   const int units = s.batch * s.h_kv;
-  QuantAttnPlan qp;
-  if (rows > kQuantMaxRows || !quant_attn_plan(s, (int)rows, (long)s.t_ctx + n_q, &qp)) return BD_ERR_UNSUPPORTED;
+  QuantVerifyPlan qp;
+  if (rows > kQuantMaxRows || !quant_verify_plan(s, (int)rows, n_q, &qp)) return BD_ERR_UNSUPPORTED;
   if (!ws) return BD_ERR_WORKSPACE;
   if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
-  if (ws_bytes < ws_region_offset(units) + quant_attn_bytes(s, (int)rows, qp)) return BD_ERR_WORKSPACE;
+  if (ws_bytes < ws_region_offset(units) + qp.bytes) return BD_ERR_WORKSPACE;
   const QuantAttnCall call = {q, o_out, lse_out, (int)rows, n_q, nullptr, nullptr, 0, 0};
-  return map_cuda(launch_quant_attn(s, qp, call, *cache, region(ws, units), counters(ws), status_word(ws),
-                                    static_cast<cudaStream_t>(stream)));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (qp.on_tc) return map_cuda(launch_quant_tc(s, qp.tc, call, *cache, region(ws, units), status_word(ws), st));
+  return map_cuda(launch_quant_attn(s, qp.warps, call, *cache, region(ws, units), counters(ws), status_word(ws), st));
 }
 
 int bd_check_wait_timeout(void* ws, size_t ws_bytes, int limit_us, void* stream) {

@@ -186,12 +186,35 @@ size_t quant_attn_bytes(const bd_shape& s, int rows, const QuantAttnPlan& plan);
 cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
                               void* ws_region, int* counters, int* status, cudaStream_t stream);
 
+// Verify blocks on the tcgen05 kernel.
+struct QuantTcPlan {
+  int chunks, nq_rows;  // chunks of a KV head's query rows, rows of one: units = batch * h_kv * chunks
+  int tiles_per_unit, tiles_per_cta, seg_cost, grid, max_seg;   // as in VerifyPlan, of 128 keys
+  size_t smem;
+};
+bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan);
+size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan);
+cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
+                            void* ws_region, int* status, cudaStream_t stream);
+
+// Which kernel takes a verify block, and its plan.
+struct QuantVerifyPlan {
+  bool on_tc;
+  QuantTcPlan tc;
+  QuantAttnPlan warps;
+  size_t bytes;         // op region
+};
+bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan);
+
 // ---------------------------------------------------------------------------- TMA maps
 // 3-D map over a [units, rows_total (stride t_cap), head_dim] bf16 cache: only rows
 // [0, n_rows) of each unit are addressable (the rest reads as zero).  Box = 64 columns x
 // box_rows rows x 1 unit, 128-byte swizzle.
 cudaError_t make_cache_map(CUtensorMap* map, const void* base, int units, int t_cap, int n_rows,
                            int head_dim, int box_rows);
+// 3-D map over a [units, n_rows (stride t_cap), head_dim / 2] array of 4-bit codes, rows past n_rows reading as zero.
+// Box = a whole row x box_rows rows x 1 unit, swizzled over the row's 64 (32) bytes.
+cudaError_t make_codes_map(CUtensorMap* map, const void* base, int units, int t_cap, int n_rows, int head_dim, int box_rows);
 // 2-D map over a dense [n_rows, head_dim] bf16 matrix; box = 64 columns x box_rows rows,
 // 128-byte swizzle; rows past n_rows read as zero.
 cudaError_t make_rows_map(CUtensorMap* map, const void* base, long long n_rows, int head_dim, int box_rows);

@@ -1,0 +1,886 @@
+// Verify blocks and single-token decoding over a 4-bit cache on the 5th-generation tensor cores.
+//
+// A 4-bit cache halves the bytes of an 8-bit one and moves the work to the codes' unpacking, so the kernel is built
+// around it: both MMAs take the unpacked cache as their A operand from TENSOR MEMORY, written there straight
+// from the registers it is unpacked in, and the few query rows are the N side.
+//   S^T = K Q^T      M = 128 keys, N = 32 (64) query rows, K = D.  A thread unpacks a key's row: lane = key.
+//   P^T = 2^(S^T - M + e), one thread per key; e the exponent of the key's V scales (scale_exponent)
+//   O^T += V^T P^T   M = D, N = query rows, K = 128 keys.  ldmatrix.trans lays a group's 32 channels of two keys
+//                    out as the 16-lane halves of a 16x128b store: lane = channel, column = key pair.
+// Unpacking is a mask and one packed FMA for two codes (bd_quant.cuh): c * 2^-k * scale + (-8 scale 2^-j), rounded
+// once, exact but where a group's scale is below 2^-7 of its row's largest.  Each row's scales are divided by a
+// power of two of its own, which joins the scores (K) or the weights (V): fp16 holds any cache.
+//
+//   warps 0-3    K: unpack a key's row into TMEM           warps 8-11 (8-15)  softmax, 32 query rows a group of four,
+//   warps 4-7    V: unpack 32 channels into TMEM                              and a segment's output
+//   then         one producer warp (TMA, 64-byte swizzle), one MMA issuer
+// K, V, S and P have two buffers each, so a tile's unpacking, its S, its softmax and its P V run side by side.
+// Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
+// per SM, partials merged by quant_merge_kernel.
+#include <algorithm>
+
+#include "bd_internal.h"
+#include "bd_quant.cuh"
+#include "bd_verify.cuh"
+
+namespace bd {
+
+constexpr int kQtKeys = 128;          // keys of a tile
+constexpr int kQtStages = 6;          // tiles of codes in flight
+constexpr int kQtRows = 32;           // query rows of a group of softmax warps
+constexpr float kQtSlack = 8.f;       // log2 of how far a running maximum may trail
+constexpr float kQtLift = 6.f;        // weights are kept 2^6 higher (fp16 reaches further above 1 than P needs)
+
+struct QuantTcParams {
+  const uint16_t* ks;          // [units][t_cap][D / 32]
+  const uint16_t* vs;
+  const __nv_bfloat16* q;      // [units][rows_total][D]
+  __nv_bfloat16* o;
+  float* lse;                  // or null
+  float* o_part;               // [units x chunks][max_seg][nq_rows][D], normalised
+  float* lse_part;             // [units x chunks][max_seg][nq_rows]
+  int* nseg;                   // [units x chunks] segments
+  int* status;
+  const int32_t* seq_lens;
+  int h_kv, n_q, nq_rows, rows_total, row_chunks, t_ctx, t_cap, units;
+  int tiles_per_unit, max_seg, seg_cost, vtiles_per_cta;
+  float scale_log2;            // log2(e) / sqrt(D)
+};
+
+// NSG groups of softmax warps, each of NC query rows (the MMAs' N side is 32 a group).
+template <int D, int NSG>
+struct QuantTcSmem {
+  static constexpr int N = kQtRows * NSG;
+  static constexpr uint32_t TILE = kQtKeys * D / 2;            // codes of one tensor
+  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = kQtKeys * N * 2;
+  static constexpr uint32_t SCALES = 2048;                     // two buffers of 4 groups x 128 keys, fp16
+  static constexpr uint32_t FIXED = 1024 + 5120;               // barriers | exchange
+  static constexpr size_t kTotal = 1024 + FIXED + SCALES + Q_BYTES + 2 * P_BYTES + kQtStages * 2 * TILE;
+};
+
+template <int N>
+__device__ __forceinline__ void tc_ld_cols(uint32_t taddr, float (&v)[N]);
+__device__ __forceinline__ void tc_ld_8(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+template <>
+__device__ __forceinline__ void tc_ld_cols<8>(uint32_t taddr, float (&v)[8]) {
+  tc_ld_8(taddr, v);
+}
+template <>
+__device__ __forceinline__ void tc_ld_cols<24>(uint32_t taddr, float (&v)[24]) {
+  tc_ld_16cols(taddr, *reinterpret_cast<float(*)[16]>(&v[0]));
+  tc_ld_8(taddr + 16, v + 16);
+}
+template <>
+__device__ __forceinline__ void tc_ld_cols<32>(uint32_t taddr, float (&v)[32]) {
+  tc_ld_32cols(taddr, v);
+}
+__device__ __forceinline__ void tc_st_8(uint32_t taddr, const float* v) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 16 lanes x 32 columns: register 2 i (2 i + 1) of lane l is TMEM lane l / 4 (+ 8), column 4 i + l % 4.
+__device__ __forceinline__ void tc_st_16x128b_8(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// MMA with A in tensor memory, B in shared memory; desc_hi: B's high descriptor word.
+__device__ __forceinline__ void tc_mma_ts_hi(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
+                                             uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 q, %0, 0;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 db, {%3, %6};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], db, %4, p;\n\t}" ::"r"(lead),
+      "r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(b_hi)
+      : "memory");
+}
+// Instruction descriptor: kind::f16 with fp16 A and B, fp32 D, K-major operands.
+__host__ __device__ constexpr uint32_t umma_idesc_f16(int m, int n) {
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+// Whether any of n threads says so; a barrier over them.
+__device__ __forceinline__ bool bar_any(int id, int n, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(id), "r"(n)
+      : "memory");
+  return r != 0;
+}
+
+// Floats as integers of the same order (NaN above all).
+__device__ __forceinline__ int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// A cache row's scales as they lie (D / 32 bf16), zero where there is no row.
+template <int D>
+struct RowScales {
+  uint32_t w[D / 64];
+  __device__ __forceinline__ void load(const uint16_t* p, bool valid) {
+    if constexpr (D == 128) {
+      const uint2 v = valid ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      w[0] = valid ? __ldg(reinterpret_cast<const uint32_t*>(p)) : 0u;
+    }
+  }
+  __device__ __forceinline__ int exponent() const {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+    return scale_exponent(top);
+  }
+  __device__ __forceinline__ float scale(int g) const { return __uint_as_float(g & 1 ? w[g >> 1] & 0xffff0000u : w[g >> 1] << 16); }
+};
+
+__device__ __forceinline__ int quant_tc_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
+  if (seq_lens == nullptr) return t_ctx;
+  int t = seq_lens[b];
+  if (t < 0 || t > t_ctx) {
+    if (status) record_error(status, BD_ERR_INVALID_ARG);
+    t = min(max(t, 0), t_ctx);
+  }
+  return t;
+}
+
+template <int D, int NC, int NSG>
+__global__ void __launch_bounds__(32 * (10 + 4 * NSG), 1) quant_tc_kernel(const __grid_constant__ QuantTcParams p,
+                                                                         const __grid_constant__ CUtensorMap kmap,
+                                                                         const __grid_constant__ CUtensorMap vmap) {
+  using L = QuantTcSmem<D, NSG>;
+  constexpr int N = L::N, G = D / 32, ST = kQtStages, THREADS = 32 * (10 + 4 * NSG), SOFT = 128 * NSG;
+  constexpr int kKWarp = 0, kVWarp = 4, kSWarp = 8, kPWarp = 8 + 4 * NSG, kMWarp = kPWarp + 1;
+  constexpr uint32_t TILE = L::TILE;
+  // B of P V: MN-major, the rows of N weights of a key in one swizzle atom of 8 keys
+  constexpr uint32_t P_PITCH = N * 2, P_ATOM = 8 * P_PITCH;
+  constexpr uint32_t kPDescHi = (P_ATOM >> 4) | (1u << 14) | ((N == 64 ? 2u : 4u) << 29);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem);      // [ST] codes of a tile
+  uint64_t* empty = full + ST;
+  uint64_t* k_full = empty + ST;                           // [2] unpacked K is in TMEM
+  uint64_t* s_full = k_full + 2;                           // [2] S is in TMEM (and K's buffer free)
+  uint64_t* v_full = s_full + 2;                           // [2] unpacked V is in TMEM
+  uint64_t* p_ready = v_full + 2;                          // [2] P is in shared memory (and S read)
+  uint64_t* pv_done = p_ready + 2;                         // [2] P V is done (V's and P's buffers free)
+  uint64_t* q_full = pv_done + 2;
+  uint64_t* o_free = q_full + 1;                           // the segment's O has been read
+  uint64_t* drain = o_free + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* red = reinterpret_cast<int*>(smem + 1024);          // [N][4] a column's maximum (or sum) in each warp
+  int* qpos = red + 4 * N;                                 // [N] a query row's place in its block
+  float* nm_s = reinterpret_cast<float*>(qpos + N);        // [N] lift - running maximum (1e30: none yet)
+  int* qtop = reinterpret_cast<int*>(nm_s + N);            // [4 NSG]
+  uint8_t* scales = smem + L::FIXED;                       // [2][4][4][16][2] fp16
+  uint8_t* qbuf = scales + L::SCALES;
+  uint8_t* pbuf = qbuf + L::Q_BYTES;
+  uint8_t* ring = pbuf + 2 * L::P_BYTES;
+  int* pref = reinterpret_cast<int*>(ring + ST * 2 * TILE);
+  static_assert((L::FIXED + L::SCALES) % 1024 == 0 && L::Q_BYTES % 1024 == 0 && L::P_BYTES % 1024 == 0, "aligned tiles");
+
+  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31, quad = warp & 3;
+  if (tid == 0) {
+    for (int s = 0; s < ST; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 8);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&k_full[b], 4);
+      mbar_init(&s_full[b], 1);
+      mbar_init(&v_full[b], 4);
+      mbar_init(&p_ready[b], 4 * NSG);
+      mbar_init(&pv_done[b], 1);
+    }
+    mbar_init(q_full, 4 * NSG);
+    mbar_init(o_free, 4 * NSG);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == kMWarp) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  // P's columns past the query rows are never written again
+  for (uint32_t i = tid; i < 2 * L::P_BYTES / 16; i += THREADS) reinterpret_cast<uint4*>(pbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t t_k = tmem, t_v = tmem + D, t_s = tmem + D + 128, t_o = t_s + 2 * N;   // K, V: two buffers of D / 2, 64
+
+  grid_dependency_wait();
+  allow_dependent_launch();
+  VerifyMap map{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
+  if (p.seq_lens) {
+    lay_out_spans<THREADS>(p.units, [&](int u) {
+      return (quant_tc_context(p.seq_lens, u / p.row_chunks / p.h_kv, p.t_ctx, nullptr) + p.n_q + kQtKeys - 1) / kQtKeys + p.seg_cost;
+    }, reinterpret_cast<int*>(smem + 512), pref);
+    map.pref = pref;
+    map.vtpc = max((pref[p.units] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
+  }
+  const int v_total = map.vbase(p.units);
+  const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
+  const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
+  bool alive = true;      // false once a wait gave up; every role then walks on without work, so that barriers still meet
+  int job = 0;            // tiles of this CTA before the segment
+
+  // Every role walks the same segments: body(unit, kv_unit, first tile, tiles, context length).
+  auto segments = [&](auto body) {
+    for (int unit = u_first; unit <= u_last; ++unit) {
+      const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
+      if (n <= 0) continue;
+      const int kv_unit = unit / p.row_chunks;
+      const int t_unit = quant_tc_context(p.seq_lens, kv_unit / p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
+      body(unit, kv_unit, tb, n, t_unit);
+      job += n;
+    }
+  };
+
+  if (warp >= kKWarp && warp < kKWarp + 4) {
+    // ---------------------------------------------------------------- K: a thread unpacks a key's row
+    const int row = quad * 32 + lane;
+    const uint32_t t_mine = t_k + ((uint32_t)(quad * 32) << 16);
+    segments([&](int, int kv_unit, int tb, int n, int t_unit) {
+      const int end = t_unit + p.n_q;
+      const uint16_t* src = p.ks + (size_t)kv_unit * p.t_cap * G;
+      RowScales<D> next;
+      next.load(src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
+      for (int t = 0; t < n; ++t) {
+        const int j = job + t, s = j % ST, b = j & 1;
+        const RowScales<D> sc = next;
+        const int key = (tb + t + 1) * kQtKeys + row;
+        next.load(src + (size_t)key * G, t + 1 < n && key < end);
+        const float down = pow2i(-sc.exponent());
+        uint32_t s0[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float ns = sc.scale(g) * down * 0x1p14f;
+          s0[g] = pack_half2(ns, ns);
+        }
+        alive = alive && mbar_wait_warp(&full[s], (j / ST) & 1, p.status, abort_flag);
+        uint4 w[G];
+        const uint8_t* tile = ring + s * 2 * TILE;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          w[g] = *reinterpret_cast<const uint4*>(tile + (D == 128 ? row * 64 + ((g ^ (row >> 1 & 3)) << 4) : row * 32 + ((g ^ (row >> 2 & 1)) << 4)));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[s]);
+        if (j >= 2) alive = alive && mbar_wait_warp(&s_full[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
+        if (alive) {
+          tc_fence_after();
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint32_t s1 = mul_half2(s0[g], 0x2c002c00u);       // 2^-4
+            const uint32_t c = mul_half2(s0[g], 0x80088008u);        // -2^-21: -8 ns 2^-10
+            const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
+            uint32_t out[16];                                        // element pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t hi = x[i] >> 8;
+              out[4 * i] = fma_half2(x[i] & kNibble0, s0[g], c);
+              out[4 * i + 1] = fma_half2(x[i] & kNibble1, s1, c);
+              out[4 * i + 2] = fma_half2(hi & kNibble0, s0[g], c);
+              out[4 * i + 3] = fma_half2(hi & kNibble1, s1, c);
+            }
+            tc_st_16cols(t_mine + b * (D / 2) + 16 * g, out);
+          }
+          tc_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&k_full[b]);
+      }
+    });
+  } else if (warp >= kVWarp && warp < kVWarp + 4) {
+    // ---------------------------------------------------------------- V: a warp unpacks a group's 32 channels
+    const int tok = quad * 32 + lane, tig = lane & 3;
+    const uint32_t t_mine = t_v + ((uint32_t)(quad * 32) << 16);
+    const bool has_rows = quad < G;
+    segments([&](int, int kv_unit, int tb, int n, int t_unit) {
+      const int end = t_unit + p.n_q;
+      const uint16_t* src = p.vs + (size_t)kv_unit * p.t_cap * G;
+      RowScales<D> next;
+      next.load(src + (size_t)(tb * kQtKeys + tok) * G, tb * kQtKeys + tok < end);
+      for (int t = 0; t < n; ++t) {
+        const int j = job + t, s = j % ST, b = j & 1;
+        const RowScales<D> sc = next;
+        const int key = (tb + t + 1) * kQtKeys + tok;
+        next.load(src + (size_t)key * G, t + 1 < n && key < end);
+        // the keys' scales, each thread one key's, laid out by (group, lane of a quad, key pair)
+        const float down = pow2i(-sc.exponent()) * 0x1p14f;
+        uint8_t* sb = scales + b * 1024;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          *reinterpret_cast<__half*>(sb + g * 256 + (tok >> 1 & 3) * 64 + (tok >> 3) * 4 + (tok & 1) * 2) = __float2half_rn(sc.scale(g) * down);
+        named_bar(3, 128);
+        alive = alive && mbar_wait_warp(&full[s], (j / ST) & 1, p.status, abort_flag);
+        uint32_t w[16], sp[16];
+        if (has_rows) {
+          const uint32_t tile = smem_u32(ring + s * 2 * TILE + TILE);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 32 * k + lane;
+            const uint32_t off = D == 128 ? r * 64 + ((quad ^ (r >> 1 & 3)) << 4) : r * 32 + ((quad ^ (r >> 2 & 1)) << 4);
+            ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), tile + off);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(sb + quad * 256 + tig * 64 + 16 * k);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[s]);
+        if (j >= 2) alive = alive && mbar_wait_warp(&pv_done[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
+        if (alive && has_rows) {
+          tc_fence_after();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t lo[16], hi[16];          // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t s0 = sp[8 * h + i], s1 = mul_half2(s0, 0x2c002c00u);   // 2^-4
+              const uint32_t c = mul_half2(s0, 0x80408040u);                        // -2^-18: -8 ns 2^-7
+              const uint32_t x = w[8 * h + i] << 3, y = w[8 * h + i] >> 5;
+              lo[2 * i] = fma_half2(x & 0x00780078u, s0, c);        // c 2^-21 * ns 2^14
+              lo[2 * i + 1] = fma_half2(x & 0x07800780u, s1, c);    // c 2^-17 * ns 2^10
+              hi[2 * i] = fma_half2(y & 0x00780078u, s0, c);
+              hi[2 * i + 1] = fma_half2(y & 0x07800780u, s1, c);
+            }
+            tc_st_16x128b_8(t_mine + b * 64 + 32 * h, lo);
+            tc_st_16x128b_8(t_mine + b * 64 + 32 * h + (16u << 16), hi);
+          }
+          tc_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&v_full[b]);
+      }
+    });
+  } else if (warp == kPWarp) {
+    // ---------------------------------------------------------------- producer
+    if (lane == 0) {
+      tma_prefetch_map(&kmap);
+      tma_prefetch_map(&vmap);
+    }
+    int issued = 0;
+    segments([&](int, int kv_unit, int tb, int n, int) {
+      if (lane == 0) {
+        for (int t = 0; t < n && alive; ++t) {
+          const int j = job + t, s = j % ST;
+          if (j >= ST) alive = mbar_wait(&empty[s], ((j / ST) & 1) ^ 1, p.status, abort_flag);
+          if (!alive) break;
+          mbar_arrive_expect_tx(&full[s], 2 * TILE);
+          tma_load_3d(ring + s * 2 * TILE, &kmap, &full[s], 0, (tb + t) * kQtKeys, kv_unit);
+          tma_load_3d(ring + s * 2 * TILE + TILE, &vmap, &full[s], 0, (tb + t) * kQtKeys, kv_unit);
+          issued = j + 1;
+        }
+      }
+    });
+    if (lane == 0 && *abort_flag) {   // no copy may land in shared memory after the CTA exits
+      for (int j = max(0, issued - ST); j < issued; ++j) mbar_wait(&full[j % ST], (j / ST) & 1, p.status, nullptr);
+    }
+    __syncwarp();
+  } else if (warp == kMWarp) {
+    // ---------------------------------------------------------------- MMA issuer (whole warp, see elect_leader)
+    const uint32_t lead = elect_leader();
+    constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
+    int seg = 0;
+    segments([&](int, int, int, int n, int) {
+      alive = alive && mbar_wait_warp(q_full, seg & 1, p.status, abort_flag);
+      for (int t = 0; t <= n && alive; ++t) {
+        if (t < n) {                                  // S of tile t
+          const int j = job + t, b = j & 1;
+          alive = mbar_wait_warp(&k_full[b], (j >> 1) & 1, p.status, abort_flag);
+          if (!alive) break;
+          tc_fence_after();
+          const uint32_t b_lo = desc_k(smem_u32(qbuf));
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+            tc_mma_ts_hi(lead, t_s + N * b, t_k + b * (D / 2) + 8 * ks, b_lo + ((ks >> 2) * (N * 128) + (ks & 3) * 32) / 16, kDescHi,
+                         idesc_s, ks > 0 ? 1u : 0u);
+          tc_commit(lead, &s_full[b]);
+        }
+        if (t > 0) {                                  // P V of tile t - 1
+          const int j = job + t - 1, b = j & 1;
+          if (t == 1 && seg > 0) alive = mbar_wait_warp(o_free, (seg - 1) & 1, p.status, abort_flag);
+          alive = alive && mbar_wait_warp(&v_full[b], (j >> 1) & 1, p.status, abort_flag);
+          alive = alive && mbar_wait_warp(&p_ready[b], (j >> 1) & 1, p.status, abort_flag);
+          if (!alive) break;
+          tc_fence_after();
+          const uint32_t b_lo = desc_mn(smem_u32(pbuf + b * L::P_BYTES), L::P_BYTES);
+#pragma unroll
+          for (int ks = 0; ks < kQtKeys / 16; ++ks)
+            tc_mma_ts_hi(lead, t_o, t_v + b * 64 + 8 * ks, b_lo + ks * (2 * P_ATOM / 16), kPDescHi, idesc_o,
+                         t > 1 || ks > 0 ? 1u : 0u);
+          tc_commit(lead, &pv_done[b]);
+        }
+      }
+      ++seg;
+    });
+    // every MMA this warp issued has completed before TMEM is released
+    tc_commit(lead, drain);
+    mbar_wait(drain, 0, p.status, nullptr);
+  } else {
+    // ---------------------------------------------------------------- softmax: a thread has a key, NC query rows
+    const int grp = (warp - kSWarp) >> 2, stid = tid - 32 * kSWarp, col0 = kQtRows * grp;
+    const int row = quad * 32 + lane, bar = 1 + grp;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    int* my_red = red + 4 * col0;
+    float* my_nm = nm_s + col0;
+    segments([&](int unit, int kv_unit, int tb, int n, int t_unit) {
+      const int row_base = (unit - kv_unit * p.row_chunks) * p.nq_rows;
+      const int rows = min(p.nq_rows, p.rows_total - row_base);
+      const size_t orow0 = (size_t)kv_unit * p.rows_total + row_base;
+      // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in
+      {
+        constexpr int CH = D / 8, PER = N * CH / SOFT;
+        uint4 w[PER];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int it = stid + i * SOFT, r = it / CH, c = it % CH;
+          w[i] = r < rows ? __ldg(reinterpret_cast<const uint4*>(p.q + (orow0 + r) * D + 8 * c)) : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
+            top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+          }
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        named_bar(4, SOFT);                    // (the segment before has read its own)
+        if (lane == 0) qtop[warp - kSWarp] = (int)top;
+        if (stid < N) {
+          qpos[stid] = stid < rows ? (row_base + stid) % p.n_q : 0x7fffffff;
+          nm_s[stid] = 1e30f;
+        }
+        named_bar(4, SOFT);
+        int t = 0;
+#pragma unroll
+        for (int i = 0; i < 4 * NSG; ++i) t = max(t, qtop[i]);
+        const float down = pow2i(13 - min(max(t - 127, -100), 100));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int it = stid + i * SOFT, r = it / CH, c = it % CH;
+          const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[2 * e] = __uint_as_float(x[e] << 16) * down;
+            f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
+          }
+          *reinterpret_cast<uint4*>(qbuf + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+              make_uint4(pack_half2(f[0], f[4]), pack_half2(f[1], f[5]), pack_half2(f[2], f[6]), pack_half2(f[3], f[7]));
+        }
+      }
+      int qt = 0;
+#pragma unroll
+      for (int i = 0; i < 4 * NSG; ++i) qt = max(qt, qtop[i]);
+      // S over the queries' power of two and the codes' 2^-10, in log2 units (the key's own power comes with it)
+      const float base = p.scale_log2 * pow2i(min(max(qt - 127, -100), 100) - 3);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+
+      float l[NC];                             // sums of this thread's keys' weights
+#pragma unroll
+      for (int c = 0; c < NC; ++c) l[c] = 0.f;
+      const int end = t_unit + p.n_q;
+      const size_t src = (size_t)kv_unit * p.t_cap * G;
+      RowScales<D> kn, vn;
+      kn.load(p.ks + src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
+      vn.load(p.vs + src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
+      for (int t = 0; t < n; ++t) {
+        const int j = job + t, b = j & 1, key = (tb + t) * kQtKeys + row;
+        const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
+        const int ev = vn.exponent();
+        const float e = (float)ev, el = pow2i(-ev);
+        kn.load(p.ks + src + (size_t)(key + kQtKeys) * G, t + 1 < n && key + kQtKeys < end);
+        vn.load(p.vs + src + (size_t)(key + kQtKeys) * G, t + 1 < n && key + kQtKeys < end);
+        const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
+        float y[NC];
+        // the tile's scores plus e, in log2 units, -inf where hidden
+        auto load_scores = [&]() {
+          tc_ld_cols<NC>(t_s + lanes + N * b + col0, y);
+          tc_wait_ld();
+#pragma unroll
+          for (int c = 0; c < NC; c += 2) {
+            const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
+            y[c] = r.x;
+            y[c + 1] = r.y;
+          }
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) y[c] = key - t_unit <= qpos[col0 + c] ? y[c] : -INFINITY;
+          }
+        };
+        auto lower = [&]() {                   // less the running maximum
+#pragma unroll
+          for (int c = 0; c < NC; c += 4) {
+            const float4 m = *reinterpret_cast<const float4*>(my_nm + c);
+            const float2 r0 = fadd2(make_float2(y[c], y[c + 1]), make_float2(m.x, m.y));
+            const float2 r1 = fadd2(make_float2(y[c + 2], y[c + 3]), make_float2(m.z, m.w));
+            y[c] = r0.x;
+            y[c + 1] = r0.y;
+            y[c + 2] = r1.x;
+            y[c + 3] = r1.y;
+          }
+        };
+        alive = alive && mbar_wait_warp(&s_full[b], (j >> 1) & 1, p.status, abort_flag);
+        float mx = -INFINITY;
+        if (alive) {
+          tc_fence_after();
+          load_scores();
+          lower();
+#pragma unroll
+          for (int c = 0; c < NC; ++c) mx = fmaxf(mx, y[c]);
+        }
+        if (bar_any(bar, 128, mx > kQtSlack + kQtLift)) {
+          // ---- some row's maximum grows by more than the slack: all rows take theirs
+          if (alive) {
+            load_scores();
+            int mine = 0;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+              const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
+              mine = lane == c ? r : mine;
+            }
+            if (lane < NC) my_red[4 * lane + quad] = mine;
+          }
+          named_bar(bar, 128);
+          // O holds the earlier tiles of the segment: scaled once the MMA that adds the last of them is done
+          if (t > 0) alive = alive && mbar_wait_warp(&pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, p.status, abort_flag);
+          if (alive) tc_fence_after();
+          // (a NaN score is passed over: its row is NaN all the same)
+          auto raised = [&](int c) {
+            const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * c);
+            const float top = unordered(max(max(r.x, r.y), max(r.z, r.w)));
+            return fminf(my_nm[c], top == -INFINITY ? 1e30f : kQtLift - top);
+          };
+#pragma unroll
+          for (int c = 0; c < NC; c += 8) {
+            float alpha[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              alpha[i] = fast_exp2(raised(c + i) - my_nm[c + i]);
+              l[c + i] *= alpha[i];
+            }
+            if (t > 0 && quad < G && alive) {
+              float o[8];
+              tc_ld_8(t_o + lanes + col0 + c, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] *= alpha[i];
+              tc_st_8(t_o + lanes + col0 + c, o);
+            }
+          }
+          const float m = lane < NC ? raised(lane) : 0.f;
+          named_bar(bar, 128);
+          if (quad == 0 && lane < NC) my_nm[lane] = m;
+          named_bar(bar, 128);
+          if (alive) {
+            tc_wait_st();
+            load_scores();
+            lower();
+          }
+        }
+        if (j >= 2) alive = alive && mbar_wait_warp(&pv_done[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
+        if (alive) {
+          uint8_t* prow = pbuf + b * L::P_BYTES + row * P_PITCH;
+#pragma unroll
+          for (int c = 0; c < NC; c += 8) {
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x0 = fast_exp2(y[c + 2 * i]), x1 = fast_exp2(y[c + 2 * i + 1]);
+              const float2 s = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(l[c + 2 * i], l[c + 2 * i + 1]));
+              l[c + 2 * i] = s.x;
+              l[c + 2 * i + 1] = s.y;
+              h[i] = pack_half2(x0, x1);
+            }
+            const int ch = (col0 + c) >> 3;
+            *reinterpret_cast<uint4*>(prow + ((N == 64 ? ch ^ (row & 7) : ch ^ (row >> 1 & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_ready[b]);
+      }
+      // ---------------------------------------------------------------- end of the segment
+      const int last = job + n - 1;
+      alive = alive && mbar_wait_warp(&pv_done[last & 1], (last >> 1) & 1, p.status, abort_flag);
+      tc_fence_after();
+      // the rows' sums: lane c ends with column c of this warp's keys
+      float sum[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) sum[c] = c < NC ? l[c < NC ? c : 0] : 0.f;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < off; ++i) {
+          const bool upper = (lane & off) != 0;
+          const float send = upper ? sum[i] : sum[i + off], keep = upper ? sum[i + off] : sum[i];
+          sum[i] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+        }
+      named_bar(bar, 128);                     // (the maxima there have been read)
+      if (lane < NC) my_red[4 * lane + quad] = __float_as_int(sum[0]);
+      named_bar(bar, 128);
+      const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * (lane < NC ? lane : 0));
+      const float tot = (__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w));
+      const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - my_nm[lane < NC ? lane : 0]) * kLn2;
+      const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;       // (V's 2^-7; a NaN stays one)
+      const int c_first = map.owner(unit, 0), c_last = map.owner(unit, map.tiles(unit) - 1);
+      const bool whole = c_first == c_last;
+      const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first);
+      if ((int)blockIdx.x == c_first && stid == 0 && p.max_seg > 1) p.nseg[unit] = c_last - c_first + 1;
+      if (alive) {
+        if (quad == 0 && lane < NC && col0 + lane < rows) {
+          if (!whole) p.lse_part[slot * p.nq_rows + col0 + lane] = lse;
+          else if (p.lse) p.lse[orow0 + col0 + lane] = lse;
+        }
+        if (quad < G) {
+          const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);       // this lane's channel
+#pragma unroll
+          for (int c = 0; c < NC; c += 8) {
+            float o[8];
+            tc_ld_8(t_o + lanes + col0 + c, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float x = o[i] * __shfl_sync(0xffffffffu, inv, c + i);
+              const int r = col0 + c + i;
+              if (r < rows) {
+                if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(x);
+                else p.o_part[(slot * p.nq_rows + r) * D + ch] = x;
+              }
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(o_free);
+    });
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMWarp) tmem_dealloc(tmem, 512);
+}
+
+// Merge of the segments' partials, one warp per query row of a unit (a unit of one segment was written by
+// quant_tc_kernel itself).  A lane takes four adjacent channels (at D 64 half of the segments); the parts' loads
+// are all in flight before their weights are known.
+template <int D>
+__global__ void __launch_bounds__(128) quant_merge_kernel(const float* o_part, const float* lse_part, const int* nseg, int max_seg,
+                                                          int nq_rows, int rows_total, int row_chunks, __nv_bfloat16* o, float* lse) {
+  constexpr int Q = D / 4, NG = 32 / Q, AT = 8;          // lanes of a row's channels; segment groups; parts at a time
+  grid_dependency_wait();
+  allow_dependent_launch();
+  const int unit = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int kv_unit = unit / row_chunks, row_base = (unit - kv_unit * row_chunks) * nq_rows;
+  const int n = min(__ldcg(nseg + unit), max_seg);
+  if (n <= 1 || r >= min(nq_rows, rows_total - row_base)) return;
+  const size_t base = (size_t)unit * max_seg;
+  const int q = lane % Q, g = lane / Q;
+  const float* lp = lse_part + base * nq_rows + r;
+  const float4* op = reinterpret_cast<const float4*>(o_part + (base * nq_rows + r) * D) + q;
+  float mx = -INFINITY;
+  const float l0 = lane < n ? __ldcg(lp + (size_t)lane * nq_rows) : -INFINITY;
+  const float l1 = lane + 32 < n ? __ldcg(lp + (size_t)(lane + 32) * nq_rows) : -INFINITY;
+  mx = fmaxf(l0, l1);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+  // (empty parts weigh nothing; a NaN stays one)
+  const float w0 = l0 == -INFINITY ? 0.f : fast_exp2((l0 - mx) * kLog2e), w1 = l1 == -INFINITY ? 0.f : fast_exp2((l1 - mx) * kLog2e);
+  float tot = w0 + w1;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, off);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < n; s0 += AT * NG) {
+    float4 v[AT];
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int s = s0 + i * NG + g;
+      v[i] = s < n ? __ldcg(op + (size_t)s * nq_rows * Q) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int s = s0 + i * NG + g;
+      const float wl = __shfl_sync(0xffffffffu, w0, s & 31), wh = __shfl_sync(0xffffffffu, w1, s & 31);
+      const float w = s < 32 ? wl : wh;
+      if (s < n && w != 0.f) {
+        a.x = fmaf(w, v[i].x, a.x);
+        a.y = fmaf(w, v[i].y, a.y);
+        a.z = fmaf(w, v[i].z, a.z);
+        a.w = fmaf(w, v[i].w, a.w);
+      }
+    }
+  }
+  if (NG == 2) {
+    a.x += __shfl_xor_sync(0xffffffffu, a.x, Q);
+    a.y += __shfl_xor_sync(0xffffffffu, a.y, Q);
+    a.z += __shfl_xor_sync(0xffffffffu, a.z, Q);
+    a.w += __shfl_xor_sync(0xffffffffu, a.w, Q);
+  }
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  const size_t orow = (size_t)kv_unit * rows_total + row_base + r;
+  if (g == 0)
+    *reinterpret_cast<uint2*>(o + orow * D + 4 * q) = make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+  if (lane == 0 && lse) lse[orow] = tot == 0.f ? -INFINITY : mx + logf(tot);
+}
+
+// ============================================================================ host side
+
+namespace {
+
+struct QtInfo {
+  const void* fn;
+  size_t smem;
+  int threads;
+};
+template <int D, int NC, int NSG>
+QtInfo qt_info() {
+  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC, NSG>), QuantTcSmem<D, NSG>::kTotal, 32 * (10 + 4 * NSG)};
+}
+template <int D>
+QtInfo qt_kernel(int rows) {
+  return rows <= 8 ? qt_info<D, 8, 1>() : rows <= 24 ? qt_info<D, 24, 1>() : qt_info<D, 32, 1>();
+}
+QtInfo qt_kernel(int d, int rows) { return d == 64 ? qt_kernel<64>(rows) : qt_kernel<128>(rows); }
+
+constexpr int kQtMaxRows = 32;        // query rows of a unit
+
+}  // namespace
+
+bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
+  plan->chunks = (rows + kQtMaxRows - 1) / kQtMaxRows;
+  plan->nq_rows = (rows + plan->chunks - 1) / plan->chunks;
+  plan->smem = qt_kernel(s.head_dim, plan->nq_rows).smem;
+  plan->tiles_per_unit = (int)(((long)s.t_ctx + n_q + kQtKeys - 1) / kQtKeys);
+  const long units = (long)s.batch * s.h_kv * plan->chunks, ctas = std::max(1, current_sm_count());
+  const int tpu = plan->tiles_per_unit, a = 6;
+  const long vtotal = units * (tpu + a);
+  if (vtotal >= (1L << 31)) return false;
+  long vtpc = (vtotal + ctas - 1) / ctas;
+  vtpc = std::max<long>(vtpc, (tpu + a + kVMaxSeg - 2) / (kVMaxSeg - 1));   // <= kVMaxSeg segments
+  plan->seg_cost = a;
+  plan->tiles_per_cta = (int)vtpc;
+  plan->grid = (int)((vtotal + vtpc - 1) / vtpc);
+  int max_seg = 1;
+  for (long u = 0; u < std::min(units, vtpc); ++u) {   // (units' offsets in the CTA ranges repeat after vtpc units)
+    const int c0 = tile_owner((int)(u * tpu), tpu, a, (int)vtpc);
+    const int c1 = tile_owner((int)(u * tpu + tpu - 1), tpu, a, (int)vtpc);
+    max_seg = std::max(max_seg, c1 - c0 + 1);
+  }
+  if (max_seg > kVMaxSeg) return false;
+  plan->max_seg = max_seg;
+  if (s.seq_lens) {
+    plan->tiles_per_cta = (int)((tpu + a + kVMaxSeg - 2) / (kVMaxSeg - 1));
+    plan->max_seg = kVMaxSeg;
+    plan->smem += align_up((size_t)(units + 1) * 4, 16);
+    if (plan->smem > kMaxSmem) return false;
+  }
+  return true;
+}
+
+size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
+  if (plan.max_seg <= 1) return 0;
+  const size_t units = (size_t)s.batch * s.h_kv * plan.chunks, rows = units * plan.max_seg * plan.nq_rows;
+  return align_up(rows * s.head_dim * 4, 256) + align_up(rows * 4, 256) + align_up(units * 4, 256);
+}
+
+bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
+  // One n8 tile of query rows at head_dim 64 stays on mma.sync: half of quant_tc_kernel's V warps have no channels
+  // there (64 units of 16K, 4 rows: 35 us, 44 on quant_tc_kernel; 24 rows: 100 / 55; d 128: 63 / 49 and 115 / 58).
+  plan->on_tc = !(s.head_dim == 64 && rows <= 8) && quant_tc_plan(s, rows, n_q, &plan->tc);
+  if (plan->on_tc) {
+    plan->bytes = quant_tc_bytes(s, plan->tc);
+    return true;
+  }
+  if (!quant_attn_plan(s, rows, (long)s.t_ctx + n_q, &plan->warps)) return false;
+  plan->bytes = quant_attn_bytes(s, rows, plan->warps);
+  return true;
+}
+
+cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
+                            void* ws_region, int* status, cudaStream_t stream) {
+  const int kv_units = s.batch * s.h_kv;
+  CUtensorMap kmap, vmap;
+  cudaError_t err = make_codes_map(&kmap, cache.k_codes, kv_units, s.t_cap, s.t_ctx + c.n_q, s.head_dim, kQtKeys);
+  if (err == cudaSuccess) err = make_codes_map(&vmap, cache.v_codes, kv_units, s.t_cap, s.t_ctx + c.n_q, s.head_dim, kQtKeys);
+  if (err != cudaSuccess) return err;
+  QuantTcParams p;
+  p.ks = static_cast<const uint16_t*>(cache.k_scales);
+  p.vs = static_cast<const uint16_t*>(cache.v_scales);
+  p.q = static_cast<const __nv_bfloat16*>(c.q);
+  p.o = static_cast<__nv_bfloat16*>(c.o_out);
+  p.lse = c.lse_out;
+  p.units = kv_units * plan.chunks;
+  const size_t rows = (size_t)p.units * plan.max_seg * plan.nq_rows;
+  p.o_part = static_cast<float*>(ws_region);
+  p.lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws_region) + align_up(rows * s.head_dim * 4, 256));
+  p.nseg = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(p.lse_part) + align_up(rows * 4, 256));
+  p.status = status;
+  p.seq_lens = s.seq_lens;
+  p.h_kv = s.h_kv;
+  p.n_q = c.n_q;
+  p.nq_rows = plan.nq_rows;
+  p.rows_total = c.rows;
+  p.row_chunks = plan.chunks;
+  p.t_ctx = s.t_ctx;
+  p.t_cap = s.t_cap;
+  p.tiles_per_unit = plan.tiles_per_unit;
+  p.max_seg = plan.max_seg;
+  p.seg_cost = plan.seg_cost;
+  p.vtiles_per_cta = plan.tiles_per_cta;
+  p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
+  const QtInfo k = qt_kernel(s.head_dim, plan.nq_rows);
+  err = allow_shared_memory(k.fn);
+  if (err != cudaSuccess) return err;
+  void* args[] = {&p, &kmap, &vmap};
+  err = launch_kernel(k.fn, dim3(plan.grid), dim3(k.threads), plan.smem, stream, args, 0);
+  if (err != cudaSuccess || plan.max_seg <= 1) return err;
+  const float* op = p.o_part;
+  const float* lp = p.lse_part;
+  const int* ns = p.nseg;
+  int max_seg = plan.max_seg, nq = plan.nq_rows, total = c.rows, chunks = plan.chunks;
+  __nv_bfloat16* o = p.o;
+  float* l = p.lse;
+  void* margs[] = {&op, &lp, &ns, &max_seg, &nq, &total, &chunks, &o, &l};
+  const void* mfn = s.head_dim == 64 ? reinterpret_cast<const void*>(&quant_merge_kernel<64>) : reinterpret_cast<const void*>(&quant_merge_kernel<128>);
+  return launch_kernel(mfn, dim3(p.units, (nq + 3) / 4), dim3(128), 0, stream, margs, 0);
+}
+
+}  // namespace bd

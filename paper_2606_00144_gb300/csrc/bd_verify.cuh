@@ -71,17 +71,13 @@ struct VerifyMap {
 };
 
 // Per-sequence lengths: every CTA lays out the units' virtual tile spans itself, pref[u] =
-// vbase(u) for u = 0 .. units, by all NTHREADS threads (wtot: one int per warp).  The lengths
-// may come from the preceding kernel, so the caller has passed the dependency wait.
-template <int NTHREADS, int KEYS>
-__device__ __forceinline__ void lay_out_units(const VerifyParams& p, int n_units, int* wtot, int* pref) {
+// vbase(u) for u = 0 .. units, by all NTHREADS threads (wtot: one int per warp); span(u) is unit u's.
+// The lengths may come from the preceding kernel, so the caller has passed the dependency wait.
+template <int NTHREADS, typename Span>
+__device__ __forceinline__ void lay_out_spans(int n_units, Span span, int* wtot, int* pref) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int per = (n_units + NTHREADS - 1) / NTHREADS;
   const int u0 = min(n_units, tid * per), u1 = min(n_units, u0 + per);
-  auto span = [&](int u) {
-    const int t_u = unit_context(p.seq_lens, u / p.row_chunks, p.h_kv, p.t_ctx, nullptr);
-    return (t_u + p.n_q + KEYS - 1) / KEYS + p.seg_cost;
-  };
   int sum = 0;
   for (int u = u0; u < u1; ++u) sum += span(u);
   int incl = sum;
@@ -100,6 +96,14 @@ __device__ __forceinline__ void lay_out_units(const VerifyParams& p, int n_units
   }
   if (tid == NTHREADS - 1) pref[n_units] = run;
   __syncthreads();
+}
+template <int NTHREADS, int KEYS>
+__device__ __forceinline__ void lay_out_units(const VerifyParams& p, int n_units, int* wtot, int* pref) {
+  auto span = [&](int u) {
+    const int t_u = unit_context(p.seq_lens, u / p.row_chunks, p.h_kv, p.t_ctx, nullptr);
+    return (t_u + p.n_q + KEYS - 1) / KEYS + p.seg_cost;
+  };
+  lay_out_spans<NTHREADS>(n_units, span, wtot, pref);
 }
 
 // The tcgen05 kernel's instance for q_tiles (1 or 2) M tiles of query rows per unit, and its
