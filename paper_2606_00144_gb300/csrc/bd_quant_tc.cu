@@ -11,10 +11,10 @@
 // once, exact but where a group's scale is below 2^-7 of its row's largest.  Each row's scales are divided by a
 // power of two of its own, which joins the scores (K) or the weights (V): fp16 holds any cache.
 //
-//   warps 0-3    K: unpack a key's row into TMEM           warps 8-11 (8-15)  softmax, 32 query rows a group of four,
-//   warps 4-7    V: unpack 32 channels into TMEM                              and a segment's output
-//   then         one producer warp (TMA, 64-byte swizzle), one MMA issuer
-// K, V, S and P have two buffers each, so a tile's unpacking, its S, its softmax and its P V run side by side.
+// Four warpgroups take the tiles in turn, each through the whole chain with buffers of its own: unpack K, start S,
+// unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
+// warps, with two buffers between them) left every warp a chain of waits: 1700 cycles a tile, of which its work
+// was 600; the issue slots of the whole chain come to about 700.
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
 #include <algorithm>
@@ -26,8 +26,10 @@
 namespace bd {
 
 constexpr int kQtKeys = 128;          // keys of a tile
-constexpr int kQtStages = 6;          // tiles of codes in flight
-constexpr int kQtRows = 32;           // query rows of a group of softmax warps
+constexpr int kQtGroups = 4;          // warpgroups
+constexpr int kQtThreads = 128 * kQtGroups;
+constexpr int kQtStages = 2;          // tiles of codes in flight for each of them
+constexpr int kQtRows = 32;           // query rows of a unit: the MMAs' N side
 constexpr float kQtSlack = 8.f;       // log2 of how far a running maximum may trail
 constexpr float kQtLift = 6.f;        // weights are kept 2^6 higher (fp16 reaches further above 1 than P needs)
 
@@ -47,15 +49,14 @@ struct QuantTcParams {
   float scale_log2;            // log2(e) / sqrt(D)
 };
 
-// NSG groups of softmax warps, each of NC query rows (the MMAs' N side is 32 a group).
-template <int D, int NSG>
+template <int D>
 struct QuantTcSmem {
-  static constexpr int N = kQtRows * NSG;
+  static constexpr int N = kQtRows;
   static constexpr uint32_t TILE = kQtKeys * D / 2;            // codes of one tensor
   static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = kQtKeys * N * 2;
-  static constexpr uint32_t SCALES = 2048;                     // two buffers of 4 groups x 128 keys, fp16
+  static constexpr uint32_t SCALES = kQtGroups * 1024;         // a tile's V scales: 4 groups x 128 keys, fp16
   static constexpr uint32_t FIXED = 1024 + 5120;               // barriers | exchange
-  static constexpr size_t kTotal = 1024 + FIXED + SCALES + Q_BYTES + 2 * P_BYTES + kQtStages * 2 * TILE;
+  static constexpr size_t kTotal = 1024 + FIXED + SCALES + Q_BYTES + kQtGroups * P_BYTES + kQtGroups * kQtStages * 2 * TILE;
 };
 
 template <int N>
@@ -170,79 +171,80 @@ __device__ __forceinline__ int quant_tc_context(const int32_t* seq_lens, int b, 
   return t;
 }
 
-template <int D, int NC, int NSG>
-__global__ void __launch_bounds__(32 * (10 + 4 * NSG), 1) quant_tc_kernel(const __grid_constant__ QuantTcParams p,
-                                                                         const __grid_constant__ CUtensorMap kmap,
-                                                                         const __grid_constant__ CUtensorMap vmap) {
-  using L = QuantTcSmem<D, NSG>;
-  constexpr int N = L::N, G = D / 32, ST = kQtStages, THREADS = 32 * (10 + 4 * NSG), SOFT = 128 * NSG;
-  constexpr int kKWarp = 0, kVWarp = 4, kSWarp = 8, kPWarp = 8 + 4 * NSG, kMWarp = kPWarp + 1;
+// Where a warpgroup's loads are: the segment of the next one (its unit, first tile and tiles, the CTA's tiles before it),
+// the loads made, and the place of each stage's tile.
+struct Ahead {
+  int unit, job, n, tb, k_issued, v_issued;
+  int v_unit[kQtStages], v_key[kQtStages];
+};
+
+// NC: columns of query rows that a softmax takes.
+template <int D, int NC>
+__global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_constant__ QuantTcParams p,
+                                                                const __grid_constant__ CUtensorMap kmap,
+                                                                const __grid_constant__ CUtensorMap vmap) {
+  using L = QuantTcSmem<D>;
+  constexpr int N = L::N, G = D / 32, ST = kQtStages, GROUPS = kQtGroups;
   constexpr uint32_t TILE = L::TILE;
-  // B of P V: MN-major, the rows of N weights of a key in one swizzle atom of 8 keys
+  // B of P V: MN-major, the N weights of a key in one row of a 64-byte swizzle atom of 8 keys
   constexpr uint32_t P_PITCH = N * 2, P_ATOM = 8 * P_PITCH;
-  constexpr uint32_t kPDescHi = (P_ATOM >> 4) | (1u << 14) | ((N == 64 ? 2u : 4u) << 29);
+  constexpr uint32_t kPDescHi = (P_ATOM >> 4) | (1u << 14) | (4u << 29);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem);      // [ST] codes of a tile
-  uint64_t* empty = full + ST;
-  uint64_t* k_full = empty + ST;                           // [2] unpacked K is in TMEM
-  uint64_t* s_full = k_full + 2;                           // [2] S is in TMEM (and K's buffer free)
-  uint64_t* v_full = s_full + 2;                           // [2] unpacked V is in TMEM
-  uint64_t* p_ready = v_full + 2;                          // [2] P is in shared memory (and S read)
-  uint64_t* pv_done = p_ready + 2;                         // [2] P V is done (V's and P's buffers free)
-  uint64_t* q_full = pv_done + 2;
-  uint64_t* o_free = q_full + 1;                           // the segment's O has been read
-  uint64_t* drain = o_free + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem);    // [GROUPS][ST] codes of K, of V have arrived
+  uint64_t* v_full = k_full + GROUPS * ST;
+  uint64_t* s_done = v_full + GROUPS * ST;                 // [GROUPS] S is in TMEM, K's columns are free
+  uint64_t* pv_done = s_done + GROUPS;                     // [GROUPS] O is up to date, V's columns and P are free
+  uint64_t* drain = pv_done + GROUPS;                      // [GROUPS]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + GROUPS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* red = reinterpret_cast<int*>(smem + 1024);          // [N][4] a column's maximum (or sum) in each warp
-  int* qpos = red + 4 * N;                                 // [N] a query row's place in its block
-  float* nm_s = reinterpret_cast<float*>(qpos + N);        // [N] lift - running maximum (1e30: none yet)
-  int* qtop = reinterpret_cast<int*>(nm_s + N);            // [4 NSG]
-  uint8_t* scales = smem + L::FIXED;                       // [2][4][4][16][2] fp16
+  int* red = reinterpret_cast<int*>(smem + 1024);          // [GROUPS][N][4] a column's maximum (or sum) in each warp
+  float* nm_s = reinterpret_cast<float*>(red + 4 * N * GROUPS);   // [GROUPS][N] lift - running maximum (1e30: none yet)
+  int* qpos = reinterpret_cast<int*>(nm_s + N * GROUPS);   // [N] a query row's place in its block
+  int* qtop = qpos + N;                                    // [4 GROUPS]
+  Ahead* ahead_s = reinterpret_cast<Ahead*>(qtop + 4 * GROUPS);   // [GROUPS]
+  uint8_t* scales = smem + L::FIXED;                       // [GROUPS][4][4][16][2] fp16
   uint8_t* qbuf = scales + L::SCALES;
-  uint8_t* pbuf = qbuf + L::Q_BYTES;
-  uint8_t* ring = pbuf + 2 * L::P_BYTES;
-  int* pref = reinterpret_cast<int*>(ring + ST * 2 * TILE);
+  uint8_t* pbuf = qbuf + L::Q_BYTES;                       // [GROUPS]
+  uint8_t* ring = pbuf + GROUPS * L::P_BYTES;              // [GROUPS][ST][K, V]
+  int* pref = reinterpret_cast<int*>(ring + GROUPS * ST * 2 * TILE);
   static_assert((L::FIXED + L::SCALES) % 1024 == 0 && L::Q_BYTES % 1024 == 0 && L::P_BYTES % 1024 == 0, "aligned tiles");
 
-  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31, quad = warp & 3;
+  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31, quad = warp & 3, grp = warp >> 2;
   if (tid == 0) {
-    for (int s = 0; s < ST; ++s) {
-      mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 8);
+    for (int i = 0; i < GROUPS * ST; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&v_full[i], 1);
     }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(&k_full[b], 4);
-      mbar_init(&s_full[b], 1);
-      mbar_init(&v_full[b], 4);
-      mbar_init(&p_ready[b], 4 * NSG);
-      mbar_init(&pv_done[b], 1);
+    for (int i = 0; i < GROUPS; ++i) {
+      mbar_init(&s_done[i], 1);
+      mbar_init(&pv_done[i], 1);
+      mbar_init(&drain[i], 1);
     }
-    mbar_init(q_full, 4 * NSG);
-    mbar_init(o_free, 4 * NSG);
-    mbar_init(drain, 1);
     *abort_flag = 0;
     mbar_fence_init();
+    tma_prefetch_map(&kmap);
+    tma_prefetch_map(&vmap);
   }
-  if (warp == kMWarp) {
+  if (warp == 0) {
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
   // P's columns past the query rows are never written again
-  for (uint32_t i = tid; i < 2 * L::P_BYTES / 16; i += THREADS) reinterpret_cast<uint4*>(pbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (uint32_t i = tid; i < GROUPS * L::P_BYTES / 16; i += kQtThreads) reinterpret_cast<uint4*>(pbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  const uint32_t t_k = tmem, t_v = tmem + D, t_s = tmem + D + 128, t_o = t_s + 2 * N;   // K, V: two buffers of D / 2, 64
+  // a warpgroup's columns: K's, then V's operand (64), S (32), O (32)
+  const uint32_t tmem = *tmem_slot, lanes = (uint32_t)(quad * 32) << 16;
+  const uint32_t t_kv = tmem + 128 * grp, t_s = t_kv + 64, t_o = t_kv + 96;
 
   grid_dependency_wait();
   allow_dependent_launch();
   VerifyMap map{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
   if (p.seq_lens) {
-    lay_out_spans<THREADS>(p.units, [&](int u) {
+    lay_out_spans<kQtThreads>(p.units, [&](int u) {
       return (quant_tc_context(p.seq_lens, u / p.row_chunks / p.h_kv, p.t_ctx, nullptr) + p.n_q + kQtKeys - 1) / kQtKeys + p.seg_cost;
     }, reinterpret_cast<int*>(smem + 512), pref);
     map.pref = pref;
@@ -251,51 +253,168 @@ __global__ void __launch_bounds__(32 * (10 + 4 * NSG), 1) quant_tc_kernel(const 
   const int v_total = map.vbase(p.units);
   const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
   const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
-  bool alive = true;      // false once a wait gave up; every role then walks on without work, so that barriers still meet
-  int job = 0;            // tiles of this CTA before the segment
+  bool alive = true;      // false once a wait gave up; a warp then walks on without work, so that barriers still meet
 
-  // Every role walks the same segments: body(unit, kv_unit, first tile, tiles, context length).
-  auto segments = [&](auto body) {
-    for (int unit = u_first; unit <= u_last; ++unit) {
-      const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
-      if (n <= 0) continue;
-      const int kv_unit = unit / p.row_chunks;
-      const int t_unit = quant_tc_context(p.seq_lens, kv_unit / p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
-      body(unit, kv_unit, tb, n, t_unit);
-      job += n;
+  // ---- the warpgroup's loads, by one of its warps (another SMSP's in each): local tile i is job grp + GROUPS i of
+  // the CTA's list of tiles; the list is walked ahead of the work, across segments.
+  const bool issuer = quad == grp;
+  const uint32_t lead = elect_leader();
+  uint64_t* my_k_full = k_full + grp * ST;
+  uint64_t* my_v_full = v_full + grp * ST;
+  uint8_t* my_ring = ring + grp * ST * 2 * TILE;
+  Ahead* ahead = ahead_s + grp;                // (in shared memory: it is the issuing warp's alone and seldom used)
+  if (issuer) {
+    if (lane == 0) *ahead = Ahead{u_first - 1, 0, 0, 0, 0, 0, {}, {}};
+    __syncwarp();
+  }
+  // K of the next tile, if there is one, into stage s; then the V of the tile there
+  auto issue_k = [&](int s) {
+    Ahead st = *ahead;
+    const int j = grp + GROUPS * st.k_issued;
+    while (j >= st.job + st.n && st.unit < u_last) {
+      st.job += st.n;
+      ++st.unit;
+      st.tb = map.first_tile(st.unit, v0);
+      st.n = max(0, map.end_tile(st.unit, v1) - st.tb);
     }
+    const bool found = j < st.job + st.n;
+    const int unit = st.unit / p.row_chunks, key = (st.tb + j - st.job) * kQtKeys;
+    if (found && lead) {
+      mbar_arrive_expect_tx(&my_k_full[s], TILE);
+      tma_load_3d(my_ring + s * 2 * TILE, &kmap, &my_k_full[s], 0, key, unit);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      ahead->unit = st.unit;
+      ahead->job = st.job;
+      ahead->n = st.n;
+      ahead->tb = st.tb;
+      ahead->k_issued = st.k_issued + found;
+      ahead->v_unit[s] = unit;
+      ahead->v_key[s] = key;
+    }
+    __syncwarp();
   };
+  auto issue_v = [&](int s) {
+    const int v_issued = ahead->v_issued;
+    if (v_issued >= ahead->k_issued) return;
+    if (lead) {
+      mbar_arrive_expect_tx(&my_v_full[s], TILE);
+      tma_load_3d(my_ring + s * 2 * TILE + TILE, &vmap, &my_v_full[s], 0, ahead->v_key[s], ahead->v_unit[s]);
+    }
+    __syncwarp();
+    if (lane == 0) ahead->v_issued = v_issued + 1;
+    __syncwarp();
+  };
+  if (issuer) {
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      issue_k(s);
+      issue_v(s);
+    }
+  }
 
-  if (warp >= kKWarp && warp < kKWarp + 4) {
-    // ---------------------------------------------------------------- K: a thread unpacks a key's row
-    const int row = quad * 32 + lane;
-    const uint32_t t_mine = t_k + ((uint32_t)(quad * 32) << 16);
-    segments([&](int, int kv_unit, int tb, int n, int t_unit) {
-      const int end = t_unit + p.n_q;
-      const uint16_t* src = p.ks + (size_t)kv_unit * p.t_cap * G;
-      RowScales<D> next;
-      next.load(src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
-      for (int t = 0; t < n; ++t) {
-        const int j = job + t, s = j % ST, b = j & 1;
-        const RowScales<D> sc = next;
-        const int key = (tb + t + 1) * kQtKeys + row;
-        next.load(src + (size_t)key * G, t + 1 < n && key < end);
-        const float down = pow2i(-sc.exponent());
+  const int row = quad * 32 + lane, tig = lane & 3;   // this thread's key of a tile
+  const bool has_rows = quad < G;                     // this warp has channels of V (and of O)
+  uint8_t* my_scales = scales + grp * 1024;
+  uint8_t* my_p = pbuf + grp * L::P_BYTES;
+  int* my_red = red + 4 * N * grp;
+  float* my_nm = nm_s + N * grp;
+  const int bar = 1 + grp;
+  constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
+
+  int job = 0, i = 0;     // tiles of the CTA before the segment; this warpgroup's tiles so far
+  for (int unit = u_first; unit <= u_last; ++unit) {
+    const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
+    if (n <= 0) continue;
+    const int kv_unit = unit / p.row_chunks;
+    const int t_unit = quant_tc_context(p.seq_lens, kv_unit / p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
+    const int row_base = (unit - kv_unit * p.row_chunks) * p.nq_rows;
+    const int rows = min(p.nq_rows, p.rows_total - row_base);
+    const int end = t_unit + p.n_q;
+    // the first tile's scales, on their way while the queries are laid out
+    const int row0 = kv_unit * p.t_cap;        // (a cache has fewer than 2^31 rows)
+    const int t_first = (grp - job) & (GROUPS - 1);   // this group's tiles of the segment: t_first, t_first + GROUPS, ...
+    RowScales<D> kn, vn;
+    {
+      const int key = (tb + t_first) * kQtKeys + row;
+      kn.load(p.ks + (size_t)(row0 + key) * G, t_first < n && key < end);
+      vn.load(p.vs + (size_t)(row0 + key) * G, t_first < n && key < end);
+    }
+    // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in
+    float base;
+    {
+      constexpr int CH = D / 8;
+      static_assert(N * CH <= kQtThreads, "a thread has eight elements at most");
+      const int r = tid / CH, c = tid % CH;
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (r < rows) w = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)kv_unit * p.rows_total + row_base + r) * D + 8 * c));
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
+        top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      __syncthreads();                         // (the segment before has read its own)
+      if (lane == 0) qtop[warp] = (int)top;
+      if (tid < N) qpos[tid] = tid < rows ? (row_base + tid) % p.n_q : 0x7fffffff;
+      if (tid < N * GROUPS) nm_s[tid] = 1e30f;
+      __syncthreads();
+      int t = 0;
+#pragma unroll
+      for (int k = 0; k < 4 * GROUPS; ++k) t = max(t, qtop[k]);
+      const int qe = min(max(t - 127, -100), 100);
+      // S over the queries' power of two and the codes' 2^-10, in log2 units (the key's own power comes with it)
+      base = p.scale_log2 * pow2i(qe - 3);
+      const float down = pow2i(13 - qe);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(x[e] << 16) * down;
+        f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
+      }
+      if (r < N)
+        *reinterpret_cast<uint4*>(qbuf + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+            make_uint4(pack_half2(f[0], f[4]), pack_half2(f[1], f[5]), pack_half2(f[2], f[6]), pack_half2(f[3], f[7]));
+      fence_proxy_async_smem();
+      __syncthreads();
+    }
+
+    float l[NC];                               // sums of this thread's keys' weights
+#pragma unroll
+    for (int c = 0; c < NC; ++c) l[c] = 0.f;
+    for (int t = t_first; t < n; t += GROUPS, ++i) {
+      const int s = i & 1, ph = (i >> 1) & 1, key = (tb + t) * kQtKeys + row;
+      const uint8_t* tile = my_ring + s * 2 * TILE;
+      const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
+      const int ev = vn.exponent();
+      // ---- K: this thread's key into its TMEM lane
+      {
+        const float down = pow2i(-kn.exponent()) * 0x1p14f;
         uint32_t s0[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const float ns = sc.scale(g) * down * 0x1p14f;
+          const float ns = kn.scale(g) * down;
           s0[g] = pack_half2(ns, ns);
         }
-        alive = alive && mbar_wait_warp(&full[s], (j / ST) & 1, p.status, abort_flag);
+        // the keys' V scales, laid out by (group, lane of a quad, key pair)
+        const float vdown = pow2i(-ev) * 0x1p14f;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          *reinterpret_cast<__half*>(my_scales + g * 256 + (row >> 1 & 3) * 64 + (row >> 3) * 4 + (row & 1) * 2) =
+              __float2half_rn(vn.scale(g) * vdown);
+        const int next = key + GROUPS * kQtKeys;
+        kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
+        vn.load(p.vs + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
+        alive = alive && mbar_wait_warp(&my_k_full[s], ph, p.status, abort_flag);
         uint4 w[G];
-        const uint8_t* tile = ring + s * 2 * TILE;
 #pragma unroll
         for (int g = 0; g < G; ++g)
           w[g] = *reinterpret_cast<const uint4*>(tile + (D == 128 ? row * 64 + ((g ^ (row >> 1 & 3)) << 4) : row * 32 + ((g ^ (row >> 2 & 1)) << 4)));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[s]);
-        if (j >= 2) alive = alive && mbar_wait_warp(&s_full[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
+        // (the columns' last reader was the P V before)
+        if (i > 0) alive = alive && mbar_wait_warp(&pv_done[grp], (i - 1) & 1, p.status, abort_flag);
         if (alive) {
           tc_fence_after();
 #pragma unroll
@@ -305,398 +424,265 @@ __global__ void __launch_bounds__(32 * (10 + 4 * NSG), 1) quant_tc_kernel(const 
             const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
             uint32_t out[16];                                        // element pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t hi = x[i] >> 8;
-              out[4 * i] = fma_half2(x[i] & kNibble0, s0[g], c);
-              out[4 * i + 1] = fma_half2(x[i] & kNibble1, s1, c);
-              out[4 * i + 2] = fma_half2(hi & kNibble0, s0[g], c);
-              out[4 * i + 3] = fma_half2(hi & kNibble1, s1, c);
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t hi = x[k] >> 8;
+              out[4 * k] = fma_half2(x[k] & kNibble0, s0[g], c);
+              out[4 * k + 1] = fma_half2(x[k] & kNibble1, s1, c);
+              out[4 * k + 2] = fma_half2(hi & kNibble0, s0[g], c);
+              out[4 * k + 3] = fma_half2(hi & kNibble1, s1, c);
             }
-            tc_st_16cols(t_mine + b * (D / 2) + 16 * g, out);
+            tc_st_16cols(t_kv + lanes + 16 * g, out);
           }
           tc_wait_st();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&k_full[b]);
-      }
-    });
-  } else if (warp >= kVWarp && warp < kVWarp + 4) {
-    // ---------------------------------------------------------------- V: a warp unpacks a group's 32 channels
-    const int tok = quad * 32 + lane, tig = lane & 3;
-    const uint32_t t_mine = t_v + ((uint32_t)(quad * 32) << 16);
-    const bool has_rows = quad < G;
-    segments([&](int, int kv_unit, int tb, int n, int t_unit) {
-      const int end = t_unit + p.n_q;
-      const uint16_t* src = p.vs + (size_t)kv_unit * p.t_cap * G;
-      RowScales<D> next;
-      next.load(src + (size_t)(tb * kQtKeys + tok) * G, tb * kQtKeys + tok < end);
-      for (int t = 0; t < n; ++t) {
-        const int j = job + t, s = j % ST, b = j & 1;
-        const RowScales<D> sc = next;
-        const int key = (tb + t + 1) * kQtKeys + tok;
-        next.load(src + (size_t)key * G, t + 1 < n && key < end);
-        // the keys' scales, each thread one key's, laid out by (group, lane of a quad, key pair)
-        const float down = pow2i(-sc.exponent()) * 0x1p14f;
-        uint8_t* sb = scales + b * 1024;
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-          *reinterpret_cast<__half*>(sb + g * 256 + (tok >> 1 & 3) * 64 + (tok >> 3) * 4 + (tok & 1) * 2) = __float2half_rn(sc.scale(g) * down);
-        named_bar(3, 128);
-        alive = alive && mbar_wait_warp(&full[s], (j / ST) & 1, p.status, abort_flag);
-        uint32_t w[16], sp[16];
-        if (has_rows) {
-          const uint32_t tile = smem_u32(ring + s * 2 * TILE + TILE);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int r = 32 * k + lane;
-            const uint32_t off = D == 128 ? r * 64 + ((quad ^ (r >> 1 & 3)) << 4) : r * 32 + ((quad ^ (r >> 2 & 1)) << 4);
-            ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), tile + off);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(sb + quad * 256 + tig * 64 + 16 * k);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[s]);
-        if (j >= 2) alive = alive && mbar_wait_warp(&pv_done[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
-        if (alive && has_rows) {
-          tc_fence_after();
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t lo[16], hi[16];          // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t s0 = sp[8 * h + i], s1 = mul_half2(s0, 0x2c002c00u);   // 2^-4
-              const uint32_t c = mul_half2(s0, 0x80408040u);                        // -2^-18: -8 ns 2^-7
-              const uint32_t x = w[8 * h + i] << 3, y = w[8 * h + i] >> 5;
-              lo[2 * i] = fma_half2(x & 0x00780078u, s0, c);        // c 2^-21 * ns 2^14
-              lo[2 * i + 1] = fma_half2(x & 0x07800780u, s1, c);    // c 2^-17 * ns 2^10
-              hi[2 * i] = fma_half2(y & 0x00780078u, s0, c);
-              hi[2 * i + 1] = fma_half2(y & 0x07800780u, s1, c);
-            }
-            tc_st_16x128b_8(t_mine + b * 64 + 32 * h, lo);
-            tc_st_16x128b_8(t_mine + b * 64 + 32 * h + (16u << 16), hi);
-          }
-          tc_wait_st();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&v_full[b]);
-      }
-    });
-  } else if (warp == kPWarp) {
-    // ---------------------------------------------------------------- producer
-    if (lane == 0) {
-      tma_prefetch_map(&kmap);
-      tma_prefetch_map(&vmap);
-    }
-    int issued = 0;
-    segments([&](int, int kv_unit, int tb, int n, int) {
-      if (lane == 0) {
-        for (int t = 0; t < n && alive; ++t) {
-          const int j = job + t, s = j % ST;
-          if (j >= ST) alive = mbar_wait(&empty[s], ((j / ST) & 1) ^ 1, p.status, abort_flag);
-          if (!alive) break;
-          mbar_arrive_expect_tx(&full[s], 2 * TILE);
-          tma_load_3d(ring + s * 2 * TILE, &kmap, &full[s], 0, (tb + t) * kQtKeys, kv_unit);
-          tma_load_3d(ring + s * 2 * TILE + TILE, &vmap, &full[s], 0, (tb + t) * kQtKeys, kv_unit);
-          issued = j + 1;
-        }
-      }
-    });
-    if (lane == 0 && *abort_flag) {   // no copy may land in shared memory after the CTA exits
-      for (int j = max(0, issued - ST); j < issued; ++j) mbar_wait(&full[j % ST], (j / ST) & 1, p.status, nullptr);
-    }
-    __syncwarp();
-  } else if (warp == kMWarp) {
-    // ---------------------------------------------------------------- MMA issuer (whole warp, see elect_leader)
-    const uint32_t lead = elect_leader();
-    constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
-    int seg = 0;
-    segments([&](int, int, int, int n, int) {
-      alive = alive && mbar_wait_warp(q_full, seg & 1, p.status, abort_flag);
-      for (int t = 0; t <= n && alive; ++t) {
-        if (t < n) {                                  // S of tile t
-          const int j = job + t, b = j & 1;
-          alive = mbar_wait_warp(&k_full[b], (j >> 1) & 1, p.status, abort_flag);
-          if (!alive) break;
-          tc_fence_after();
-          const uint32_t b_lo = desc_k(smem_u32(qbuf));
-#pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            tc_mma_ts_hi(lead, t_s + N * b, t_k + b * (D / 2) + 8 * ks, b_lo + ((ks >> 2) * (N * 128) + (ks & 3) * 32) / 16, kDescHi,
-                         idesc_s, ks > 0 ? 1u : 0u);
-          tc_commit(lead, &s_full[b]);
-        }
-        if (t > 0) {                                  // P V of tile t - 1
-          const int j = job + t - 1, b = j & 1;
-          if (t == 1 && seg > 0) alive = mbar_wait_warp(o_free, (seg - 1) & 1, p.status, abort_flag);
-          alive = alive && mbar_wait_warp(&v_full[b], (j >> 1) & 1, p.status, abort_flag);
-          alive = alive && mbar_wait_warp(&p_ready[b], (j >> 1) & 1, p.status, abort_flag);
-          if (!alive) break;
-          tc_fence_after();
-          const uint32_t b_lo = desc_mn(smem_u32(pbuf + b * L::P_BYTES), L::P_BYTES);
-#pragma unroll
-          for (int ks = 0; ks < kQtKeys / 16; ++ks)
-            tc_mma_ts_hi(lead, t_o, t_v + b * 64 + 8 * ks, b_lo + ks * (2 * P_ATOM / 16), kPDescHi, idesc_o,
-                         t > 1 || ks > 0 ? 1u : 0u);
-          tc_commit(lead, &pv_done[b]);
-        }
-      }
-      ++seg;
-    });
-    // every MMA this warp issued has completed before TMEM is released
-    tc_commit(lead, drain);
-    mbar_wait(drain, 0, p.status, nullptr);
-  } else {
-    // ---------------------------------------------------------------- softmax: a thread has a key, NC query rows
-    const int grp = (warp - kSWarp) >> 2, stid = tid - 32 * kSWarp, col0 = kQtRows * grp;
-    const int row = quad * 32 + lane, bar = 1 + grp;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    int* my_red = red + 4 * col0;
-    float* my_nm = nm_s + col0;
-    segments([&](int unit, int kv_unit, int tb, int n, int t_unit) {
-      const int row_base = (unit - kv_unit * p.row_chunks) * p.nq_rows;
-      const int rows = min(p.nq_rows, p.rows_total - row_base);
-      const size_t orow0 = (size_t)kv_unit * p.rows_total + row_base;
-      // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in
-      {
-        constexpr int CH = D / 8, PER = N * CH / SOFT;
-        uint4 w[PER];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int it = stid + i * SOFT, r = it / CH, c = it % CH;
-          w[i] = r < rows ? __ldg(reinterpret_cast<const uint4*>(p.q + (orow0 + r) * D + 8 * c)) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
-            top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
-          }
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        named_bar(4, SOFT);                    // (the segment before has read its own)
-        if (lane == 0) qtop[warp - kSWarp] = (int)top;
-        if (stid < N) {
-          qpos[stid] = stid < rows ? (row_base + stid) % p.n_q : 0x7fffffff;
-          nm_s[stid] = 1e30f;
-        }
-        named_bar(4, SOFT);
-        int t = 0;
-#pragma unroll
-        for (int i = 0; i < 4 * NSG; ++i) t = max(t, qtop[i]);
-        const float down = pow2i(13 - min(max(t - 127, -100), 100));
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int it = stid + i * SOFT, r = it / CH, c = it % CH;
-          const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-          float f[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f[2 * e] = __uint_as_float(x[e] << 16) * down;
-            f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
-          }
-          *reinterpret_cast<uint4*>(qbuf + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
-              make_uint4(pack_half2(f[0], f[4]), pack_half2(f[1], f[5]), pack_half2(f[2], f[6]), pack_half2(f[3], f[7]));
-        }
-      }
-      int qt = 0;
-#pragma unroll
-      for (int i = 0; i < 4 * NSG; ++i) qt = max(qt, qtop[i]);
-      // S over the queries' power of two and the codes' 2^-10, in log2 units (the key's own power comes with it)
-      const float base = p.scale_log2 * pow2i(min(max(qt - 127, -100), 100) - 3);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_full);
-
-      float l[NC];                             // sums of this thread's keys' weights
-#pragma unroll
-      for (int c = 0; c < NC; ++c) l[c] = 0.f;
-      const int end = t_unit + p.n_q;
-      const size_t src = (size_t)kv_unit * p.t_cap * G;
-      RowScales<D> kn, vn;
-      kn.load(p.ks + src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
-      vn.load(p.vs + src + (size_t)(tb * kQtKeys + row) * G, tb * kQtKeys + row < end);
-      for (int t = 0; t < n; ++t) {
-        const int j = job + t, b = j & 1, key = (tb + t) * kQtKeys + row;
-        const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
-        const int ev = vn.exponent();
-        const float e = (float)ev, el = pow2i(-ev);
-        kn.load(p.ks + src + (size_t)(key + kQtKeys) * G, t + 1 < n && key + kQtKeys < end);
-        vn.load(p.vs + src + (size_t)(key + kQtKeys) * G, t + 1 < n && key + kQtKeys < end);
-        const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
-        float y[NC];
-        // the tile's scores plus e, in log2 units, -inf where hidden
-        auto load_scores = [&]() {
-          tc_ld_cols<NC>(t_s + lanes + N * b + col0, y);
-          tc_wait_ld();
-#pragma unroll
-          for (int c = 0; c < NC; c += 2) {
-            const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
-            y[c] = r.x;
-            y[c + 1] = r.y;
-          }
-          if (masked) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) y[c] = key - t_unit <= qpos[col0 + c] ? y[c] : -INFINITY;
-          }
-        };
-        auto lower = [&]() {                   // less the running maximum
-#pragma unroll
-          for (int c = 0; c < NC; c += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(my_nm + c);
-            const float2 r0 = fadd2(make_float2(y[c], y[c + 1]), make_float2(m.x, m.y));
-            const float2 r1 = fadd2(make_float2(y[c + 2], y[c + 3]), make_float2(m.z, m.w));
-            y[c] = r0.x;
-            y[c + 1] = r0.y;
-            y[c + 2] = r1.x;
-            y[c + 3] = r1.y;
-          }
-        };
-        alive = alive && mbar_wait_warp(&s_full[b], (j >> 1) & 1, p.status, abort_flag);
-        float mx = -INFINITY;
-        if (alive) {
-          tc_fence_after();
-          load_scores();
-          lower();
-#pragma unroll
-          for (int c = 0; c < NC; ++c) mx = fmaxf(mx, y[c]);
-        }
-        if (bar_any(bar, 128, mx > kQtSlack + kQtLift)) {
-          // ---- some row's maximum grows by more than the slack: all rows take theirs
-          if (alive) {
-            load_scores();
-            int mine = 0;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
-              mine = lane == c ? r : mine;
-            }
-            if (lane < NC) my_red[4 * lane + quad] = mine;
-          }
-          named_bar(bar, 128);
-          // O holds the earlier tiles of the segment: scaled once the MMA that adds the last of them is done
-          if (t > 0) alive = alive && mbar_wait_warp(&pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, p.status, abort_flag);
-          if (alive) tc_fence_after();
-          // (a NaN score is passed over: its row is NaN all the same)
-          auto raised = [&](int c) {
-            const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * c);
-            const float top = unordered(max(max(r.x, r.y), max(r.z, r.w)));
-            return fminf(my_nm[c], top == -INFINITY ? 1e30f : kQtLift - top);
-          };
-#pragma unroll
-          for (int c = 0; c < NC; c += 8) {
-            float alpha[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              alpha[i] = fast_exp2(raised(c + i) - my_nm[c + i]);
-              l[c + i] *= alpha[i];
-            }
-            if (t > 0 && quad < G && alive) {
-              float o[8];
-              tc_ld_8(t_o + lanes + col0 + c, o);
-              tc_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] *= alpha[i];
-              tc_st_8(t_o + lanes + col0 + c, o);
-            }
-          }
-          const float m = lane < NC ? raised(lane) : 0.f;
-          named_bar(bar, 128);
-          if (quad == 0 && lane < NC) my_nm[lane] = m;
-          named_bar(bar, 128);
-          if (alive) {
-            tc_wait_st();
-            load_scores();
-            lower();
-          }
-        }
-        if (j >= 2) alive = alive && mbar_wait_warp(&pv_done[b], ((j >> 1) - 1) & 1, p.status, abort_flag);
-        if (alive) {
-          uint8_t* prow = pbuf + b * L::P_BYTES + row * P_PITCH;
-#pragma unroll
-          for (int c = 0; c < NC; c += 8) {
-            uint32_t h[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x0 = fast_exp2(y[c + 2 * i]), x1 = fast_exp2(y[c + 2 * i + 1]);
-              const float2 s = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(l[c + 2 * i], l[c + 2 * i + 1]));
-              l[c + 2 * i] = s.x;
-              l[c + 2 * i + 1] = s.y;
-              h[i] = pack_half2(x0, x1);
-            }
-            const int ch = (col0 + c) >> 3;
-            *reinterpret_cast<uint4*>(prow + ((N == 64 ? ch ^ (row & 7) : ch ^ (row >> 1 & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-          }
-        }
-        fence_proxy_async_smem();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_ready[b]);
-      }
-      // ---------------------------------------------------------------- end of the segment
-      const int last = job + n - 1;
-      alive = alive && mbar_wait_warp(&pv_done[last & 1], (last >> 1) & 1, p.status, abort_flag);
-      tc_fence_after();
-      // the rows' sums: lane c ends with column c of this warp's keys
-      float sum[32];
-#pragma unroll
-      for (int c = 0; c < 32; ++c) sum[c] = c < NC ? l[c < NC ? c : 0] : 0.f;
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-        for (int i = 0; i < off; ++i) {
-          const bool upper = (lane & off) != 0;
-          const float send = upper ? sum[i] : sum[i + off], keep = upper ? sum[i + off] : sum[i];
-          sum[i] = keep + __shfl_xor_sync(0xffffffffu, send, off);
-        }
-      named_bar(bar, 128);                     // (the maxima there have been read)
-      if (lane < NC) my_red[4 * lane + quad] = __float_as_int(sum[0]);
-      named_bar(bar, 128);
-      const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * (lane < NC ? lane : 0));
-      const float tot = (__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w));
-      const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - my_nm[lane < NC ? lane : 0]) * kLn2;
-      const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;       // (V's 2^-7; a NaN stays one)
-      const int c_first = map.owner(unit, 0), c_last = map.owner(unit, map.tiles(unit) - 1);
-      const bool whole = c_first == c_last;
-      const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first);
-      if ((int)blockIdx.x == c_first && stid == 0 && p.max_seg > 1) p.nseg[unit] = c_last - c_first + 1;
-      if (alive) {
-        if (quad == 0 && lane < NC && col0 + lane < rows) {
-          if (!whole) p.lse_part[slot * p.nq_rows + col0 + lane] = lse;
-          else if (p.lse) p.lse[orow0 + col0 + lane] = lse;
-        }
-        if (quad < G) {
-          const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);       // this lane's channel
-#pragma unroll
-          for (int c = 0; c < NC; c += 8) {
-            float o[8];
-            tc_ld_8(t_o + lanes + col0 + c, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float x = o[i] * __shfl_sync(0xffffffffu, inv, c + i);
-              const int r = col0 + c + i;
-              if (r < rows) {
-                if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(x);
-                else p.o_part[(slot * p.nq_rows + r) * D + ch] = x;
-              }
-            }
-          }
         }
       }
       tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(o_free);
-    });
-  }
+      named_bar(bar, 128);
+      if (issuer && alive) {
+        tc_fence_after();
+        const uint32_t b_lo = desc_k(smem_u32(qbuf));
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          tc_mma_ts_hi(lead, t_s, t_kv + 8 * ks, b_lo + ((ks >> 2) * (N * 128) + (ks & 3) * 32) / 16, kDescHi, idesc_s, ks > 0 ? 1u : 0u);
+        tc_commit(lead, &s_done[grp]);
+        issue_k(s);
+      }
 
+      // ---- V: a warp unpacks a group's 32 channels, while S runs
+      alive = alive && mbar_wait_warp(&my_v_full[s], ph, p.status, abort_flag);
+      {
+        const uint32_t vt = smem_u32(tile + TILE);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {         // 64 keys at a time
+          uint32_t w[8], sp[8];
+          if (has_rows) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int r = 64 * h + 32 * k + lane;
+              const uint32_t off = D == 128 ? r * 64 + ((quad ^ (r >> 1 & 3)) << 4) : r * 32 + ((quad ^ (r >> 2 & 1)) << 4);
+              ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), vt + off);
+              *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(my_scales + quad * 256 + tig * 64 + 32 * h + 16 * k);
+            }
+          }
+          if (h == 0) {
+            alive = alive && mbar_wait_warp(&s_done[grp], i & 1, p.status, abort_flag);
+            tc_fence_after();
+          }
+          if (alive && has_rows) {
+            uint32_t lo[16], hi[16];          // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t s0 = sp[k], s1 = mul_half2(s0, 0x2c002c00u);   // 2^-4
+              const uint32_t c = mul_half2(s0, 0x80408040u);                // -2^-18: -8 ns 2^-7
+              const uint32_t x = w[k] << 3, y = w[k] >> 5;
+              lo[2 * k] = fma_half2(x & 0x00780078u, s0, c);        // c 2^-21 * ns 2^14
+              lo[2 * k + 1] = fma_half2(x & 0x07800780u, s1, c);    // c 2^-17 * ns 2^10
+              hi[2 * k] = fma_half2(y & 0x00780078u, s0, c);
+              hi[2 * k + 1] = fma_half2(y & 0x07800780u, s1, c);
+            }
+            tc_st_16x128b_8(t_kv + lanes + 32 * h, lo);
+            tc_st_16x128b_8(t_kv + lanes + 32 * h + (16u << 16), hi);
+          }
+        }
+      }
+
+      // ---- softmax: this thread's key, NC query rows
+      const float e = (float)ev;
+      const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
+      float y[NC];
+      // the tile's scores plus e, in log2 units, -inf where hidden
+      auto load_scores = [&]() {
+        tc_ld_cols<NC>(t_s + lanes, y);
+        tc_wait_ld();
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) {
+          const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
+          y[c] = r.x;
+          y[c + 1] = r.y;
+        }
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c) y[c] = key - t_unit <= qpos[c] ? y[c] : -INFINITY;
+        }
+      };
+      auto lower = [&]() {                     // less the running maximum
+#pragma unroll
+        for (int c = 0; c < NC; c += 4) {
+          const float4 m = *reinterpret_cast<const float4*>(my_nm + c);
+          const float2 r0 = fadd2(make_float2(y[c], y[c + 1]), make_float2(m.x, m.y));
+          const float2 r1 = fadd2(make_float2(y[c + 2], y[c + 3]), make_float2(m.z, m.w));
+          y[c] = r0.x;
+          y[c + 1] = r0.y;
+          y[c + 2] = r1.x;
+          y[c + 3] = r1.y;
+        }
+      };
+      float mx = -INFINITY;
+      if (alive) {
+        tc_fence_after();
+        load_scores();
+        lower();
+#pragma unroll
+        for (int c = 0; c < NC; ++c) mx = fmaxf(mx, y[c]);
+      }
+      if (bar_any(bar, 128, mx > kQtSlack + kQtLift)) {
+        // ---- some row's maximum grows by more than the slack: all rows take theirs
+        if (alive) {
+          load_scores();
+          int mine = 0;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
+            mine = lane == c ? r : mine;
+          }
+          if (lane < NC) my_red[4 * lane + quad] = mine;
+        }
+        named_bar(bar, 128);
+        // (a NaN score is passed over: its row is NaN all the same)
+        auto raised = [&](int c) {
+          const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * c);
+          const float top = unordered(max(max(r.x, r.y), max(r.z, r.w)));
+          return fminf(my_nm[c], top == -INFINITY ? 1e30f : kQtLift - top);
+        };
+#pragma unroll
+        for (int c = 0; c < NC; c += 8) {
+          float alpha[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            alpha[k] = fast_exp2(raised(c + k) - my_nm[c + k]);
+            l[c + k] *= alpha[k];
+          }
+          if (t > t_first && has_rows && alive) {   // O holds the group's earlier tiles of the segment
+            float o[8];
+            tc_ld_8(t_o + lanes + c, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] *= alpha[k];
+            tc_st_8(t_o + lanes + c, o);
+          }
+        }
+        const float m = lane < NC ? raised(lane) : 0.f;
+        named_bar(bar, 128);
+        if (quad == 0 && lane < NC) my_nm[lane] = m;
+        named_bar(bar, 128);
+        if (alive) {
+          load_scores();
+          lower();
+        }
+      }
+      if (alive) {
+        const float el = pow2i(-ev);
+        uint8_t* prow = my_p + row * P_PITCH;
+#pragma unroll
+        for (int c = 0; c < NC; c += 8) {
+          uint32_t h[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x0 = fast_exp2(y[c + 2 * k]), x1 = fast_exp2(y[c + 2 * k + 1]);
+            const float2 z = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(l[c + 2 * k], l[c + 2 * k + 1]));
+            l[c + 2 * k] = z.x;
+            l[c + 2 * k + 1] = z.y;
+            h[k] = pack_half2(x0, x1);
+          }
+          *reinterpret_cast<uint4*>(prow + ((c >> 3 ^ (row >> 1 & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        tc_wait_st();
+      }
+      fence_proxy_async_smem();
+      tc_fence_before();
+      named_bar(bar, 128);
+      if (issuer && alive) {
+        tc_fence_after();
+        const uint32_t b_lo = desc_mn(smem_u32(my_p), L::P_BYTES);
+#pragma unroll
+        for (int ks = 0; ks < kQtKeys / 16; ++ks)
+          tc_mma_ts_hi(lead, t_o, t_kv + 8 * ks, b_lo + ks * (2 * P_ATOM / 16), kPDescHi, idesc_o, t > t_first || ks > 0 ? 1u : 0u);
+        tc_commit(lead, &pv_done[grp]);
+        issue_v(s);
+      }
+    }
+
+    // ---------------------------------------------------------------- end of the segment
+    job += n;
+    // the rows' sums: lane c ends with column c of this warp's keys
+    float sum[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) sum[c] = c < NC ? l[c < NC ? c : 0] : 0.f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+      for (int k = 0; k < off; ++k) {
+        const bool upper = (lane & off) != 0;
+        const float send = upper ? sum[k] : sum[k + off], keep = upper ? sum[k + off] : sum[k];
+        sum[k] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+      }
+    if (lane < NC) my_red[4 * lane + quad] = __float_as_int(sum[0]);   // (its maxima were read before the last barrier)
+    // the last P V of every group that had a tile of the segment
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int done = (job - g + GROUPS - 1) / GROUPS;        // its tiles so far (job - g > -GROUPS)
+      if (g + GROUPS * (done - 1) >= job - n) alive = alive && mbar_wait_warp(&pv_done[g], (done - 1) & 1, p.status, abort_flag);
+    }
+    tc_fence_after();
+    __syncthreads();
+    // the groups' states merged: lane c has column c's factors
+    const int mc = lane < NC ? lane : 0;
+    float f[GROUPS], tot = 0.f, nm = nm_s[mc];
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) nm = fminf(nm, nm_s[N * g + mc]);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int4 r = *reinterpret_cast<const int4*>(red + 4 * (N * g + mc));
+      f[g] = fast_exp2(nm - nm_s[N * g + mc]);
+      tot += f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w)));
+    }
+    const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - nm) * kLn2;
+    const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;         // (V's 2^-7; a NaN stays one)
+    const int c_first = map.owner(unit, 0), c_last = map.owner(unit, map.tiles(unit) - 1);
+    const bool whole = c_first == c_last;
+    const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first), orow0 = (size_t)kv_unit * p.rows_total + row_base;
+    if ((int)blockIdx.x == c_first && tid == 0 && p.max_seg > 1) p.nseg[unit] = c_last - c_first + 1;
+    if (warp == 0 && lane < NC && lane < rows && alive) {
+      if (!whole) p.lse_part[slot * p.nq_rows + lane] = lse;
+      else if (p.lse) p.lse[orow0 + lane] = lse;
+    }
+    const int c = 8 * grp;                                     // a group's block of columns
+    if (c < NC && c < rows && has_rows && alive) {
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int done = (job - g + GROUPS - 1) / GROUPS;
+        if (g + GROUPS * (done - 1) < job - n) continue;       // no tiles, O holds nothing
+        float o[8];
+        tc_ld_8(tmem + 128 * g + 96 + lanes + c, o);
+        tc_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = fmaf(o[k], __shfl_sync(0xffffffffu, f[g] * inv, c + k), x[k]);
+      }
+      const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);  // this lane's channel
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = c + k;
+        if (r < rows) {
+          if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(x[k]);
+          else p.o_part[(slot * p.nq_rows + r) * D + ch] = x[k];
+        }
+      }
+    }
+    tc_fence_before();                                         // (the next segment's barrier comes before its P V)
+  }
+  if (issuer && *abort_flag) {   // no copy may land in shared memory, no MMA write TMEM after the CTA exits
+    for (int k = max(0, ahead->k_issued - ST); k < ahead->k_issued; ++k) mbar_wait(&my_k_full[k % ST], (k / ST) & 1, p.status, nullptr);
+    for (int k = max(0, ahead->v_issued - ST); k < ahead->v_issued; ++k) mbar_wait(&my_v_full[k % ST], (k / ST) & 1, p.status, nullptr);
+    tc_commit(lead, &drain[grp]);
+    mbar_wait(&drain[grp], 0, p.status, nullptr);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == kMWarp) tmem_dealloc(tmem, 512);
+  if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
 // Merge of the segments' partials, one warp per query row of a unit (a unit of one segment was written by
@@ -768,24 +754,21 @@ namespace {
 struct QtInfo {
   const void* fn;
   size_t smem;
-  int threads;
 };
-template <int D, int NC, int NSG>
+template <int D, int NC>
 QtInfo qt_info() {
-  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC, NSG>), QuantTcSmem<D, NSG>::kTotal, 32 * (10 + 4 * NSG)};
+  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC>), QuantTcSmem<D>::kTotal};
 }
 template <int D>
 QtInfo qt_kernel(int rows) {
-  return rows <= 8 ? qt_info<D, 8, 1>() : rows <= 24 ? qt_info<D, 24, 1>() : qt_info<D, 32, 1>();
+  return rows <= 8 ? qt_info<D, 8>() : rows <= 24 ? qt_info<D, 24>() : qt_info<D, 32>();
 }
 QtInfo qt_kernel(int d, int rows) { return d == 64 ? qt_kernel<64>(rows) : qt_kernel<128>(rows); }
-
-constexpr int kQtMaxRows = 32;        // query rows of a unit
 
 }  // namespace
 
 bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
-  plan->chunks = (rows + kQtMaxRows - 1) / kQtMaxRows;
+  plan->chunks = (rows + kQtRows - 1) / kQtRows;
   plan->nq_rows = (rows + plan->chunks - 1) / plan->chunks;
   plan->smem = qt_kernel(s.head_dim, plan->nq_rows).smem;
   plan->tiles_per_unit = (int)(((long)s.t_ctx + n_q + kQtKeys - 1) / kQtKeys);
@@ -870,7 +853,7 @@ cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const Qu
   err = allow_shared_memory(k.fn);
   if (err != cudaSuccess) return err;
   void* args[] = {&p, &kmap, &vmap};
-  err = launch_kernel(k.fn, dim3(plan.grid), dim3(k.threads), plan.smem, stream, args, 0);
+  err = launch_kernel(k.fn, dim3(plan.grid), dim3(kQtThreads), plan.smem, stream, args, 0);
   if (err != cudaSuccess || plan.max_seg <= 1) return err;
   const float* op = p.o_part;
   const float* lp = p.lse_part;
