@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   const int v_total = map.vbase(p.units);
   const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
   const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
-  bool alive = true;      // false once a wait gave up; a warp then walks on without work, so that barriers still meet
+  bool alive = true;      // false once a wait gave up
 
   // ---- the warpgroup's loads, by one of its warps (another SMSP's in each): local tile i is job grp + GROUPS i of
   // the CTA's list of tiles; the list is walked ahead of the work, across segments.
@@ -323,6 +323,19 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   const int bar = 1 + grp;
   constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
 
+  // A wait that has usually been over for long: one poll and a vote.  Once one has given up the warp goes on without
+  // waiting (every address stays in bounds and every barrier meets), starts no MMA and writes no output.
+  auto wait = [&](uint64_t* b, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, mbar_test(smem_u32(b), parity))) alive = alive && mbar_wait_warp(b, parity, p.status, abort_flag);
+  };
+  // this thread's places in shared memory: its row of codes of a tile, its V scales, its weights
+  const uint32_t sw = D == 128 ? row >> 1 & 3 : row >> 2 & 1;
+  const uint8_t* k_row = my_ring + row * (D / 2);
+  const uint32_t v_rows = smem_u32(my_ring) + TILE + lane * (D / 2) + ((quad ^ (D == 128 ? lane >> 1 & 3 : lane >> 2 & 1)) << 4);
+  uint8_t* scale_at = my_scales + (row >> 1 & 3) * 64 + (row >> 3) * 4 + (row & 1) * 2;
+  uint8_t* p_row = my_p + row * P_PITCH;
+  const uint32_t p_sw = (row >> 1 & 3) << 4;
+
   int job = 0, i = 0;     // tiles of the CTA before the segment; this warpgroup's tiles so far
   for (int unit = u_first; unit <= u_last; ++unit) {
     const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
@@ -387,7 +400,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     for (int c = 0; c < NC; ++c) l[c] = 0.f;
     for (int t = t_first; t < n; t += GROUPS, ++i) {
       const int s = i & 1, ph = (i >> 1) & 1, key = (tb + t) * kQtKeys + row;
-      const uint8_t* tile = my_ring + s * 2 * TILE;
+      const uint32_t stage = s * 2 * TILE;
       const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
       const int ev = vn.exponent();
       // ---- K: this thread's key into its TMEM lane
@@ -403,22 +416,19 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         const float vdown = pow2i(-ev) * 0x1p14f;
 #pragma unroll
         for (int g = 0; g < G; ++g)
-          *reinterpret_cast<__half*>(my_scales + g * 256 + (row >> 1 & 3) * 64 + (row >> 3) * 4 + (row & 1) * 2) =
-              __float2half_rn(vn.scale(g) * vdown);
+          *reinterpret_cast<__half*>(scale_at + g * 256) = __float2half_rn(vn.scale(g) * vdown);
         const int next = key + GROUPS * kQtKeys;
         kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
         vn.load(p.vs + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
-        alive = alive && mbar_wait_warp(&my_k_full[s], ph, p.status, abort_flag);
+        wait(&my_k_full[s], ph);
         uint4 w[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-          w[g] = *reinterpret_cast<const uint4*>(tile + (D == 128 ? row * 64 + ((g ^ (row >> 1 & 3)) << 4) : row * 32 + ((g ^ (row >> 2 & 1)) << 4)));
+        for (int g = 0; g < G; ++g) w[g] = *reinterpret_cast<const uint4*>(k_row + stage + ((g ^ sw) << 4));
         // (the columns' last reader was the P V before)
-        if (i > 0) alive = alive && mbar_wait_warp(&pv_done[grp], (i - 1) & 1, p.status, abort_flag);
-        if (alive) {
-          tc_fence_after();
+        if (i > 0) wait(&pv_done[grp], (i - 1) & 1);
+        tc_fence_after();
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
+        for (int g = 0; g < G; ++g) {
             const uint32_t s1 = mul_half2(s0[g], 0x2c002c00u);       // 2^-4
             const uint32_t c = mul_half2(s0[g], 0x80088008u);        // -2^-21: -8 ns 2^-10
             const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
@@ -432,9 +442,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
               out[4 * k + 3] = fma_half2(hi & kNibble1, s1, c);
             }
             tc_st_16cols(t_kv + lanes + 16 * g, out);
-          }
-          tc_wait_st();
         }
+        tc_wait_st();
       }
       tc_fence_before();
       named_bar(bar, 128);
@@ -449,26 +458,23 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       }
 
       // ---- V: a warp unpacks a group's 32 channels, while S runs
-      alive = alive && mbar_wait_warp(&my_v_full[s], ph, p.status, abort_flag);
+      wait(&my_v_full[s], ph);
       {
-        const uint32_t vt = smem_u32(tile + TILE);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {         // 64 keys at a time
           uint32_t w[8], sp[8];
           if (has_rows) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int r = 64 * h + 32 * k + lane;
-              const uint32_t off = D == 128 ? r * 64 + ((quad ^ (r >> 1 & 3)) << 4) : r * 32 + ((quad ^ (r >> 2 & 1)) << 4);
-              ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), vt + off);
+              ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), v_rows + stage + (64 * h + 32 * k) * (D / 2));
               *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(my_scales + quad * 256 + tig * 64 + 32 * h + 16 * k);
             }
           }
           if (h == 0) {
-            alive = alive && mbar_wait_warp(&s_done[grp], i & 1, p.status, abort_flag);
+            wait(&s_done[grp], i & 1);
             tc_fence_after();
           }
-          if (alive && has_rows) {
+          if (has_rows) {
             uint32_t lo[16], hi[16];          // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -517,26 +523,21 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           y[c + 3] = r1.y;
         }
       };
-      float mx = -INFINITY;
-      if (alive) {
-        tc_fence_after();
-        load_scores();
-        lower();
+      load_scores();
+      lower();
+      float mx = y[0];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) mx = fmaxf(mx, y[c]);
-      }
+      for (int c = 1; c < NC; ++c) mx = fmaxf(mx, y[c]);
       if (bar_any(bar, 128, mx > kQtSlack + kQtLift)) {
         // ---- some row's maximum grows by more than the slack: all rows take theirs
-        if (alive) {
-          load_scores();
-          int mine = 0;
+        load_scores();
+        int mine = 0;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
-            mine = lane == c ? r : mine;
-          }
-          if (lane < NC) my_red[4 * lane + quad] = mine;
+        for (int c = 0; c < NC; ++c) {
+          const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
+          mine = lane == c ? r : mine;
         }
+        if (lane < NC) my_red[4 * lane + quad] = mine;
         named_bar(bar, 128);
         // (a NaN score is passed over: its row is NaN all the same)
         auto raised = [&](int c) {
@@ -552,7 +553,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             alpha[k] = fast_exp2(raised(c + k) - my_nm[c + k]);
             l[c + k] *= alpha[k];
           }
-          if (t > t_first && has_rows && alive) {   // O holds the group's earlier tiles of the segment
+          if (t > t_first && has_rows) {   // O holds the group's earlier tiles of the segment
             float o[8];
             tc_ld_8(t_o + lanes + c, o);
             tc_wait_ld();
@@ -565,14 +566,11 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         named_bar(bar, 128);
         if (quad == 0 && lane < NC) my_nm[lane] = m;
         named_bar(bar, 128);
-        if (alive) {
-          load_scores();
-          lower();
-        }
+        load_scores();
+        lower();
       }
-      if (alive) {
+      {
         const float el = pow2i(-ev);
-        uint8_t* prow = my_p + row * P_PITCH;
 #pragma unroll
         for (int c = 0; c < NC; c += 8) {
           uint32_t h[4];
@@ -584,7 +582,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             l[c + 2 * k + 1] = z.y;
             h[k] = pack_half2(x0, x1);
           }
-          *reinterpret_cast<uint4*>(prow + ((c >> 3 ^ (row >> 1 & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(p_row + (c * 2 ^ p_sw)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         tc_wait_st();
       }
@@ -621,7 +619,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
       const int done = (job - g + GROUPS - 1) / GROUPS;        // its tiles so far (job - g > -GROUPS)
-      if (g + GROUPS * (done - 1) >= job - n) alive = alive && mbar_wait_warp(&pv_done[g], (done - 1) & 1, p.status, abort_flag);
+      if (g + GROUPS * (done - 1) >= job - n) wait(&pv_done[g], (done - 1) & 1);
     }
     tc_fence_after();
     __syncthreads();
