@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   int* red = reinterpret_cast<int*>(smem + 1024);          // [GROUPS][N][4] a column's maximum (or sum) in each warp
   float* nm_s = reinterpret_cast<float*>(red + 4 * N * GROUPS);   // [GROUPS][N] lift - running maximum (1e30: none yet)
   int* qpos = reinterpret_cast<int*>(nm_s + N * GROUPS);   // [N] a query row's place in its block
-  int* qtop = qpos + N;                                    // [4 GROUPS]
+  float* alpha_s = reinterpret_cast<float*>(qpos + N);     // [GROUPS][N] what a maximum's last rise scales by
+  int* qtop = reinterpret_cast<int*>(alpha_s + N * GROUPS);       // [4 GROUPS]
   Ahead* ahead_s = reinterpret_cast<Ahead*>(qtop + 4 * GROUPS);   // [GROUPS]
   uint8_t* scales = smem + L::FIXED;                       // [GROUPS][4][4][16][2] fp16
   uint8_t* qbuf = scales + L::SCALES;
@@ -320,6 +321,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   uint8_t* my_p = pbuf + grp * L::P_BYTES;
   int* my_red = red + 4 * N * grp;
   float* my_nm = nm_s + N * grp;
+  float* my_alpha = alpha_s + N * grp;
   const int bar = 1 + grp;
   constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
 
@@ -496,12 +498,14 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       const float e = (float)ev;
       const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
       float y[NC];
-      // the tile's scores plus e, in log2 units, -inf where hidden
-      auto load_scores = [&]() {
+      // (one copy of the scores' code and registers: once maxima have been raised it runs again, and only once: a
+      // row that holds a NaN may still be above the slack)
+#pragma unroll 1
+      for (int pass = 0; pass < 2; ++pass) {
         tc_ld_cols<NC>(t_s + lanes, y);
         tc_wait_ld();
 #pragma unroll
-        for (int c = 0; c < NC; c += 2) {
+        for (int c = 0; c < NC; c += 2) {      // the scores plus e, in log2 units
           const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
           y[c] = r.x;
           y[c + 1] = r.y;
@@ -510,10 +514,9 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
           for (int c = 0; c < NC; ++c) y[c] = key - t_unit <= qpos[c] ? y[c] : -INFINITY;
         }
-      };
-      auto lower = [&]() {                     // less the running maximum
+        float mx = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NC; c += 4) {
+        for (int c = 0; c < NC; c += 4) {      // less the running maximum
           const float4 m = *reinterpret_cast<const float4*>(my_nm + c);
           const float2 r0 = fadd2(make_float2(y[c], y[c + 1]), make_float2(m.x, m.y));
           const float2 r1 = fadd2(make_float2(y[c + 2], y[c + 3]), make_float2(m.z, m.w));
@@ -521,53 +524,48 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           y[c + 1] = r0.y;
           y[c + 2] = r1.x;
           y[c + 3] = r1.y;
+          mx = fmaxf(fmaxf(mx, y[c]), y[c + 1]);
+          mx = fmaxf(fmaxf(mx, y[c + 2]), y[c + 3]);
         }
-      };
-      load_scores();
-      lower();
-      float mx = y[0];
-#pragma unroll
-      for (int c = 1; c < NC; ++c) mx = fmaxf(mx, y[c]);
-      if (bar_any(bar, 128, mx > kQtSlack + kQtLift)) {
+        if (pass == 1 || !bar_any(bar, 128, mx > kQtSlack + kQtLift)) break;
         // ---- some row's maximum grows by more than the slack: all rows take theirs
-        load_scores();
         int mine = 0;
+#pragma unroll 1
+        for (int c = 0; c < NC; c += 8) {
+          float z[8];
+          tc_ld_8(t_s + lanes + c, z);
+          tc_wait_ld();
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int r = __reduce_max_sync(0xffffffffu, ordered(y[c]));
-          mine = lane == c ? r : mine;
+          for (int k = 0; k < 8; ++k) {
+            const float x = masked && key - t_unit > qpos[c + k] ? -INFINITY : fmaf(z[k], a, e);
+            const int r = __reduce_max_sync(0xffffffffu, ordered(x));
+            mine = lane == c + k ? r : mine;
+          }
         }
         if (lane < NC) my_red[4 * lane + quad] = mine;
         named_bar(bar, 128);
-        // (a NaN score is passed over: its row is NaN all the same)
-        auto raised = [&](int c) {
-          const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * c);
-          const float top = unordered(max(max(r.x, r.y), max(r.z, r.w)));
-          return fminf(my_nm[c], top == -INFINITY ? 1e30f : kQtLift - top);
-        };
+        if (quad == 0 && lane < NC) {
+          const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * lane);
+          const float top = unordered(max(max(r.x, r.y), max(r.z, r.w))), old = my_nm[lane];
+          const float m = fminf(old, top == -INFINITY ? 1e30f : kQtLift - top);   // (a NaN score is passed over: its row is NaN all the same)
+          my_nm[lane] = m;
+          my_alpha[lane] = fast_exp2(m - old);
+        }
+        named_bar(bar, 128);
 #pragma unroll
-        for (int c = 0; c < NC; c += 8) {
-          float alpha[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            alpha[k] = fast_exp2(raised(c + k) - my_nm[c + k]);
-            l[c + k] *= alpha[k];
-          }
-          if (t > t_first && has_rows) {   // O holds the group's earlier tiles of the segment
+        for (int c = 0; c < NC; ++c) l[c] *= my_alpha[c];
+        if (t > t_first && has_rows) {         // O holds the group's earlier tiles of the segment
+#pragma unroll 1
+          for (int c = 0; c < NC; c += 8) {
             float o[8];
             tc_ld_8(t_o + lanes + c, o);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] *= alpha[k];
+            for (int k = 0; k < 8; ++k) o[k] *= my_alpha[c + k];
             tc_st_8(t_o + lanes + c, o);
           }
+          tc_wait_st();
         }
-        const float m = lane < NC ? raised(lane) : 0.f;
-        named_bar(bar, 128);
-        if (quad == 0 && lane < NC) my_nm[lane] = m;
-        named_bar(bar, 128);
-        load_scores();
-        lower();
       }
       {
         const float el = pow2i(-ev);
