@@ -112,7 +112,8 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # the handle alone: building the Stream object takes 3 us of a call's 9
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -279,6 +280,7 @@ class QuantCache:
                 raise ValueError("QuantCache: codes and scales must be on one device")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self._struct = BdQuantCache(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
+        self._ref = ctypes.byref(self._struct)
 
     @classmethod
     def empty(cls, batch, h_kv, t_cap, head_dim, device="cuda"):
@@ -299,34 +301,39 @@ class QuantCache:
 def _quant_cache(name, shape, cache: QuantCache):
     if (shape.batch, shape.h_kv, shape.head_dim, shape.t_cap) != (cache.batch, cache.h_kv, cache.head_dim, cache.t_cap):
         raise ValueError(f"{name}: the cache is not one of this shape: {shape}")
-    return ctypes.byref(cache._struct)
+    return cache._ref
 
 
 def _quant_rows(name, shape, k_rows, v_rows):
     """dtype code, row count and strides of a write's or read's tensors [batch, h_kv, n, head_dim]."""
-    given = [t for t in (k_rows, v_rows) if t is not None]
-    if not given:
+    first = k_rows if k_rows is not None else v_rows
+    if first is None:
         raise ValueError(f"{name}: K rows, V rows or both")
-    n = int(given[0].shape[2]) if given[0].dim() == 4 else -1
+    dtype = BD_DTYPE_BF16 if first.dtype is torch.bfloat16 else BD_DTYPE_F32
+    n = int(first.shape[2]) if first.dim() == 4 else -1
     strides = []
     for t in (k_rows, v_rows):
         if t is None:
             strides.append(None)
             continue
-        if tuple(t.shape) != (shape.batch, shape.h_kv, n, shape.head_dim):
+        if t.shape != (shape.batch, shape.h_kv, n, shape.head_dim):
             raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim], got {tuple(t.shape)}")
-        if t.dtype != given[0].dtype or t.dtype not in (torch.bfloat16, torch.float32):
+        if t.dtype is not first.dtype or t.dtype not in (torch.bfloat16, torch.float32):
             raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
-        if t.stride(3) != 1:
+        if t.is_contiguous():
+            strides.append(None)
+            continue
+        st = t.stride()
+        if st[3] != 1:
             raise ValueError(f"{name}: the elements of a row must be adjacent")
-        strides.append((ctypes.c_int64 * 3)(*t.stride()[:3]))
-    return n, BD_DTYPE_BF16 if given[0].dtype == torch.bfloat16 else BD_DTYPE_F32, strides
+        strides.append((ctypes.c_int64 * 3)(*st[:3]))
+    return n, dtype, strides
 
 
 def _dense(name, what, t, dtype, shape):
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: {what} must be a contiguous {tuple(shape)} tensor, got {tuple(t.shape)}")
 
 

@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "budgetdraft.h"
 
 namespace bd {
@@ -27,6 +29,17 @@ cudaError_t launch_kernel(const void* fn, dim3 grid, dim3 block, size_t smem, cu
 constexpr size_t kMaxSmem = 227 * 1024;
 inline cudaError_t allow_shared_memory(const void* fn, size_t static_bytes = 0) {
   return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxSmem - static_bytes));
+}
+// The same, asked for once a device (`done`: the function's own, a bit for each device below 64).
+inline cudaError_t allow_shared_memory_once(const void* fn, size_t static_bytes, std::atomic<uint64_t>* done) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done->load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  err = allow_shared_memory(fn, static_bytes);
+  if (err == cudaSuccess) done->fetch_or(bit, std::memory_order_relaxed);
+  return err;
 }
 
 // ---------------------------------------------------------------------------- workspace

@@ -3,9 +3,11 @@
 //   scale = bf16(max |x| / 7) over a group of 32, code = clamp(round(x / scale), -7, 7) + 8,
 //   value = (code - 8) * scale
 //
-// Both are one pass over the rows with nothing to reuse, bound by HBM: a thread takes eight adjacent
-// elements of a row (16 bytes of bf16, one 32-bit word of codes), so that a warp's accesses are
-// contiguous on both sides; the four threads of a group find its largest magnitude with two shuffles.
+// Both are one pass over the rows with nothing to reuse, bound by HBM: 8 x 16K rows of K and V (690 MB) are written in
+// 111 us (6.2 TB/s) and read back in 100 (6.9 TB/s).  The write is as fast only because a quotient takes three packed
+// FMAs and its code comes off the sum's last bits: with a division and a conversion an element it took 383 us.
+// A thread takes 16 adjacent elements of a row, half a group: 32 bytes of bf16, an 8-byte word of codes; a warp's
+// accesses are contiguous on both sides and the two threads of a group meet in one shuffle.
 #include <algorithm>
 
 #include "bd_internal.h"
@@ -14,6 +16,7 @@
 namespace bd {
 
 constexpr int kQThreads = 256;
+constexpr int kQPasses = 4;   // row blocks of a CTA
 
 struct QuantRows {            // one tensor of a call
   void* rows;                 // bf16 or fp32 rows (source or destination), element strides:
@@ -26,94 +29,215 @@ struct QuantParams {
   QuantRows t[2];
   const int32_t* seq_lens;    // rows start at each sequence's length (or null: at first)
   int first;                  // first row of every unit; with seq_lens the bound of the lengths
-  int n_rows, h_kv, t_cap;
-  long long items;            // (row, eight elements) pairs of one tensor
+  int n_rows, h_kv, units, t_cap;
+  int blocks;                 // CTAs of a unit's rows
+  bool wide;                  // every row is 32-byte aligned
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+
+// 32 bytes at once, or as two halves where the rows are not 32-byte aligned.  As two halves every access covers half of
+// each 32-byte sector of what a warp touches: reading 8 x 16K rows took 133 us so, 100 as one.
+__device__ __forceinline__ void load32(const void* p, bool wide, uint32_t* w) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 2; ++i) {
+      const uint4 v = __ldcs(static_cast<const uint4*>(p) + i);
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
   }
 }
+__device__ __forceinline__ void store32(void* p, bool wide, const uint32_t* w) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) static_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+
+// 16 elements as they lie.
+template <typename T>
+struct Sixteen;
 template <>
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+struct Sixteen<__nv_bfloat16> {
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool wide) { load32(p, wide, w); }
+  // the largest magnitude's bits as a float's (a NaN's are above infinity's)
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    return max(m << 16, m & 0xffff0000u);
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)); }
+};
+template <>
+struct Sixteen<float> {
+  float x[16];
+  __device__ __forceinline__ void load(const float* p, bool wide) {
+    load32(p, wide, reinterpret_cast<uint32_t*>(x));
+    load32(p + 8, wide, reinterpret_cast<uint32_t*>(x) + 8);
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(x[2 * i], x[2 * i + 1]); }
+};
+
+// Codes and scale of a group's half; top: the group's largest magnitude, as bits.
+template <typename T>
+__device__ __forceinline__ uint2 quantise(const Sixteen<T>& x, uint32_t top, uint16_t* scale) {
+  const float t = __uint_as_float(top);
+  uint32_t word[2];
+  if (top - 0x12800000u < 0x7f800000u - 0x12800000u) {   // 2^-90 <= t, finite: nothing below underflows
+    // Quotients a / b as q + (a - q b) y with y = 1 / b and q = a y, both rounded (Markstein 1990): the rounded quotient.
+    constexpr float kSeventh = 1.f / 7.f;
+    const float q7 = t * kSeventh;
+    const __nv_bfloat16 sb = __float2bfloat16_rn(fmaf(fmaf(-q7, 7.f, t), kSeventh, q7));
+    const float s = __bfloat162float(sb), y = __frcp_rn(s);
+    *scale = __bfloat16_as_ushort(sb);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // 1.5 2^23 + 8 + the quotient, rounded half to even, has the code in its last four bits (|quotient| <= 7 / (1 - 2^-8),
+      // so none needs the clamp); what the sum below carries of the rest is a constant
+      uint32_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 a = x.pair(4 * h + i), yy = make_float2(y, y), q = fmul2(a, yy);
+        const float2 r = ffma2(q, make_float2(-s, -s), a);
+        const float2 c = fadd2(ffma2(r, yy, q), make_float2(12582920.f, 12582920.f));
+        sum += __float_as_uint(c.x) << (8 * i);
+        sum += __float_as_uint(c.y) << (8 * i + 4);
+      }
+      constexpr uint32_t kBias = 0x4b400000u;
+      word[h] = sum - (kBias + (kBias << 4) + (kBias << 8) + (kBias << 12) + (kBias << 16) + (kBias << 20) + (kBias << 24) + (kBias << 28));
+    }
+    return make_uint2(word[0], word[1]);
+  }
+  // tiny groups, zeros, and groups that are not numbers
+  const bool odd = top >= 0x7f800000u;
+  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(t, 7.f));
+  const float s = __bfloat162float(sb);
+  *scale = odd ? 0x7fffu : __bfloat16_as_ushort(sb);
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    word[0] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = h ? x.pair(4 + i) : x.pair(i);
+      const bool live = !odd && s > 0.f;
+      const int c0 = live ? (int)fminf(fmaxf(rintf(__fdiv_rn(a.x, s)), -7.f), 7.f) : 0;
+      const int c1 = live ? (int)fminf(fmaxf(rintf(__fdiv_rn(a.y, s)), -7.f), 7.f) : 0;
+      word[0] |= (uint32_t)(c0 + 8) << (8 * i) | (uint32_t)(c1 + 8) << (8 * i + 4);
+    }
+    if (h == 0) word[1] = word[0];
+  }
+  return make_uint2(word[1], word[0]);
 }
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                            pack_bf16x2(x[6], x[7]));
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-}
-
-// Where item i of a tensor lies: its row's offset among the caller's rows (elements), and its cache row.
-struct ItemPlace {
-  long long at;    // first of the item's eight elements
-  long long row;   // cache row
-  int chunk;       // which eight of the row
+// A CTA's place: its tensor, unit and first row.
+struct Place {
+  const QuantRows* t;
+  long long at, cache_row;     // the unit's offset among the caller's rows; the cache row of its row 0
+  int row;
 };
 template <int D>
-__device__ __forceinline__ ItemPlace place(const QuantParams& p, const QuantRows& t, long long i) {
-  constexpr int CH = D / 8;
-  ItemPlace r;
-  r.chunk = (int)(i % CH);
-  const unsigned rr = (unsigned)(i / CH);      // (a cache has fewer than 2^31 rows)
-  const unsigned unit = rr / (unsigned)p.n_rows, n = rr - unit * (unsigned)p.n_rows;
-  const unsigned b = unit / (unsigned)p.h_kv, h = unit - b * (unsigned)p.h_kv;
+__device__ __forceinline__ Place place(const QuantParams& p) {
+  constexpr int ROWS = kQThreads / (D / 16) * kQPasses;
+  const unsigned u = blockIdx.x / (unsigned)p.blocks, b = blockIdx.x - u * (unsigned)p.blocks;
+  const int which = u >= (unsigned)p.units, unit = (int)u - which * p.units;
+  const int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
   int first = p.first;
-  if (p.seq_lens) first = min(max(p.seq_lens[b], 0), p.first);
-  r.at = b * t.sb + h * t.sh + n * t.sn + 8 * r.chunk;
-  r.row = (long long)unit * p.t_cap + first + n;
+  if (p.seq_lens) first = min(max(p.seq_lens[seq], 0), p.first);
+  Place r;
+  r.t = &p.t[which];
+  r.at = seq * r.t->sb + head * r.t->sh;
+  r.cache_row = (long long)unit * p.t_cap + first;
+  r.row = (int)b * ROWS + threadIdx.x / (D / 16);
   return r;
 }
 
 template <int D, typename T>
 __global__ void __launch_bounds__(kQThreads) quant_write_kernel(const __grid_constant__ QuantParams p) {
+  constexpr int CH = D / 16, STEP = kQThreads / CH;   // threads of a row; rows at a time
+  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;       // rows in flight: 128 bytes a thread (bf16 with 64: 123 us for 111; fp32 with 256: 95 for 86)
   grid_dependency_wait();
   allow_dependent_launch();
-  const QuantRows& t = p.t[blockIdx.y];
-  // (items come in whole rows of at least eight, and a group's four threads are adjacent lanes: a
-  // group is wholly inside or outside of the range)
-  for (long long i = (long long)blockIdx.x * kQThreads + threadIdx.x; i < p.items; i += (long long)gridDim.x * kQThreads) {
-    const ItemPlace at = place<D>(p, t, i);
-    float x[8];
-    load8(static_cast<const T*>(t.rows) + at.at, x);
-    float top = 0.f;
-    bool odd = false;                         // a NaN or an infinity among them
+  const Place at = place<D>(p);
+  const QuantRows& t = *at.t;
+  const int c = threadIdx.x % CH;
+  const T* src = static_cast<const T*>(t.rows) + at.at + 16 * c;
+#pragma unroll 1
+  for (int k = 0; k < kQPasses; k += AHEAD) {
+    if (at.row + k * STEP - (int)threadIdx.x / CH >= p.n_rows) break;      // (the whole CTA's rows are past the end)
+    Sixteen<T> x[AHEAD] = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      top = fmaxf(top, fabsf(x[e]));
-      odd |= !(fabsf(x[e]) < INFINITY);
+    for (int e = 0; e < AHEAD; ++e) {
+      const int row = at.row + (k + e) * STEP;
+      if (row < p.n_rows) x[e].load(src + (long long)row * t.sn, p.wide);
     }
-    const unsigned four = 0xfu << (threadIdx.x & 28);   // the lanes of the group
-    top = fmaxf(top, __shfl_xor_sync(four, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(four, top, 2));
-    odd = (__ballot_sync(four, odd) & four) != 0;
-    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(top, 7.f));
-    const float s = __bfloat162float(sb);
-    uint32_t word = 0x88888888u;
-    if (!odd && s > 0.f) {
-      word = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float r = fminf(fmaxf(rintf(__fdiv_rn(x[e], s)), -7.f), 7.f);
-        word |= (uint32_t)((int)r + 8) << (4 * e);
+    for (int e = 0; e < AHEAD; ++e) {
+      const int row = at.row + (k + e) * STEP;
+      uint32_t top = x[e].top();
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      if (row < p.n_rows) {
+        uint16_t scale;
+        const long long to = at.cache_row + row;
+        *reinterpret_cast<uint2*>(t.codes + to * (D / 2) + 8 * c) = quantise(x[e], top, &scale);
+        if ((c & 1) == 0) t.scales[to * (D / kQGroup) + c / 2] = scale;
       }
     }
-    *reinterpret_cast<uint32_t*>(t.codes + at.row * (D / 2) + 4 * at.chunk) = word;
-    if ((at.chunk & 3) == 0)
-      t.scales[at.row * (D / kQGroup) + at.chunk / 4] = odd ? 0x7fffu : __bfloat16_as_ushort(sb);
+  }
+}
+
+__device__ __forceinline__ uint32_t bf16x2_add(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// The eight values of a word of codes, as they are written.
+__device__ __forceinline__ void values(uint32_t w, uint32_t scale, uint32_t (&out)[4]) {
+  // 128 + c is a bf16 with c in its last bits; less 136 it is c - 8, exactly, and the product is rounded once
+  const uint32_t s2 = scale | scale << 16;
+  uint32_t v[4];                                  // element pairs (0, 4), (1, 5), (2, 6), (3, 7)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = bf16x2_mul(bf16x2_add((w >> (4 * i) & kNibble0) | 0x43004300u, 0xc308c308u), s2);
+  out[0] = __byte_perm(v[0], v[1], 0x5410);
+  out[1] = __byte_perm(v[2], v[3], 0x5410);
+  out[2] = __byte_perm(v[0], v[1], 0x7632);
+  out[3] = __byte_perm(v[2], v[3], 0x7632);
+}
+__device__ __forceinline__ void values(uint32_t w, uint32_t scale, uint32_t (&out)[8]) {
+  const float s = bf16_bits_to_float(scale);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {                // 2^23 + c, less 2^23 + 8
+    const float2 c = fadd2(make_float2(__uint_as_float((w >> (4 * i) & 15u) | 0x4b000000u), __uint_as_float((w >> (4 * i + 4) & 15u) | 0x4b000000u)),
+                           make_float2(-8388616.f, -8388616.f));
+    const float2 x = fmul2(c, make_float2(s, s));
+    out[i] = __float_as_uint(x.x);
+    out[i + 1] = __float_as_uint(x.y);
   }
 }
 
@@ -122,16 +246,35 @@ __global__ void __launch_bounds__(kQThreads) quant_write_kernel(const __grid_con
 // rows are in L2, for the copy engines' proxy too, before it ends.
 template <int D, typename T>
 __global__ void __launch_bounds__(kQThreads) quant_read_kernel(const __grid_constant__ QuantParams p) {
+  constexpr int CH = D / 16, STEP = kQThreads / CH;
   grid_dependency_wait();
-  const QuantRows& t = p.t[blockIdx.y];
-  for (long long i = (long long)blockIdx.x * kQThreads + threadIdx.x; i < p.items; i += (long long)gridDim.x * kQThreads) {
-    const ItemPlace at = place<D>(p, t, i);
-    const uint32_t word = __ldcs(reinterpret_cast<const uint32_t*>(t.codes + at.row * (D / 2) + 4 * at.chunk));
-    const float s = bf16_bits_to_float(t.scales[at.row * (D / kQGroup) + at.chunk / 4]);
-    float x[8];
+  const Place at = place<D>(p);
+  const QuantRows& t = *at.t;
+  const int c = threadIdx.x % CH;
+  T* dst = static_cast<T*>(t.rows) + at.at + 16 * c;
+  uint2 w[kQPasses];
+  uint32_t s[kQPasses];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)((int)((word >> (4 * e)) & 15u) - 8) * s;
-    store8(static_cast<T*>(t.rows) + at.at, x);
+  for (int k = 0; k < kQPasses; ++k) {
+    const int row = at.row + k * STEP;
+    const long long from = at.cache_row + row;
+    if (row < p.n_rows) {
+      w[k] = __ldcs(reinterpret_cast<const uint2*>(t.codes + from * (D / 2) + 8 * c));
+      s[k] = __ldg(t.scales + from * (D / kQGroup) + c / 2);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kQPasses; ++k) {
+    const int row = at.row + k * STEP;
+    if (row < p.n_rows) {
+      T* to = dst + (long long)row * t.sn;
+      constexpr int WORDS = sizeof(T) * 2;       // of eight elements
+      uint32_t out[2][WORDS];
+      values(w[k].x, s[k], out[0]);
+      values(w[k].y, s[k], out[1]);
+#pragma unroll
+      for (int i = 0; i < 2 * WORDS; i += 8) store32(to + i * 4 / sizeof(T), p.wide, &out[0][0] + i);
+    }
   }
   asm volatile("fence.proxy.async.global;" ::: "memory");
   __threadfence();
@@ -153,14 +296,22 @@ static cudaError_t launch_rows(const bd_shape& s, bool write, const int32_t* seq
     r.scales = static_cast<uint16_t*>(i ? c.v_scales : c.k_scales);
   }
   if (n == 1) p.t[1] = p.t[0];
+  p.wide = true;
+  for (int i = 0; i < n; ++i) {
+    const long long e = dtype == BD_DTYPE_F32 ? 4 : 2;
+    const QuantRows& r = p.t[i];
+    p.wide &= reinterpret_cast<uintptr_t>(r.rows) % 32 == 0 && r.sb * e % 32 == 0 && r.sh * e % 32 == 0 && r.sn * e % 32 == 0;
+  }
   p.seq_lens = seq_lens;
   p.first = first;
   p.n_rows = n_rows;
   p.h_kv = s.h_kv;
+  p.units = s.batch * s.h_kv;
   p.t_cap = s.t_cap;
-  p.items = (long long)s.batch * s.h_kv * n_rows * (s.head_dim / 8);
-  const long long blocks = (p.items + kQThreads - 1) / kQThreads;
-  const int most = current_sm_count() * 8;
+  const int rows = kQThreads / (s.head_dim / 16) * kQPasses;
+  p.blocks = (n_rows + rows - 1) / rows;
+  const long long grid = (long long)p.blocks * p.units * n;
+  if (grid >= (1LL << 31)) return cudaErrorInvalidConfiguration;   // (fewer than 2^31 rows in a cache: never)
   const void* fn = nullptr;
 #define BD_QR(D, CODE, T)                 \
   if (s.head_dim == D && dtype == CODE)   \
@@ -169,7 +320,7 @@ static cudaError_t launch_rows(const bd_shape& s, bool write, const int32_t* seq
   BD_QR(64, BD_DTYPE_F32, float) BD_QR(128, BD_DTYPE_F32, float)
 #undef BD_QR
   void* args[] = {&p};
-  return launch_kernel(fn, dim3((unsigned)std::min<long long>(blocks, most), n), dim3(kQThreads), 0, stream, args, 0);
+  return launch_kernel(fn, dim3((unsigned)grid), dim3(kQThreads), 0, stream, args, 0);
 }
 
 cudaError_t launch_quant_write(const bd_shape& s, int n_rows, int dtype, const bd_quant_cache& c, const QuantTensor& k,

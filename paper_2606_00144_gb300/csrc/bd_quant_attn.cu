@@ -476,12 +476,16 @@ namespace {
 struct QaInfo {
   const void* fn;
   size_t smem;
+  std::atomic<uint64_t>* allowed;
 };
+template <int D, int NT, bool GATHER>
+QaInfo qa_one() {
+  static std::atomic<uint64_t> allowed{0};
+  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER>), QaSmem<D, NT>::kTotal, &allowed};
+}
 template <int D, int NT>
 QaInfo qa_info(bool gather) {
-  return {gather ? reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, true>)
-                 : reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, false>),
-          QaSmem<D, NT>::kTotal};
+  return gather ? qa_one<D, NT, true>() : qa_one<D, NT, false>();
 }
 QaInfo qa_kernel(int d, int nt, bool gather) {
   if (d == 64) return nt == 1 ? qa_info<64, 1>(gather) : qa_info<64, 2>(gather);
@@ -535,7 +539,7 @@ cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, cons
   p.n_split = plan.n_split;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
   const QaInfo k = qa_kernel(s.head_dim, plan.nt, c.idx != nullptr);
-  cudaError_t err = allow_shared_memory(k.fn, 128);
+  cudaError_t err = allow_shared_memory_once(k.fn, 128, k.allowed);
   if (err != cudaSuccess) return err;
   void* args[] = {&p};
   return launch_kernel(k.fn, dim3(plan.n_split, s.batch * s.h_kv, plan.chunks), dim3(kQaThreads), k.smem, stream, args, 0);

@@ -750,10 +750,12 @@ namespace {
 struct QtInfo {
   const void* fn;
   size_t smem;
+  std::atomic<uint64_t>* allowed;
 };
 template <int D, int NC>
 QtInfo qt_info() {
-  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC>), QuantTcSmem<D>::kTotal};
+  static std::atomic<uint64_t> allowed{0};
+  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC>), QuantTcSmem<D>::kTotal, &allowed};
 }
 template <int D>
 QtInfo qt_kernel(int rows) {
@@ -846,7 +848,7 @@ cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const Qu
   p.vtiles_per_cta = plan.tiles_per_cta;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
   const QtInfo k = qt_kernel(s.head_dim, plan.nq_rows);
-  err = allow_shared_memory(k.fn);
+  err = allow_shared_memory_once(k.fn, 0, k.allowed);
   if (err != cudaSuccess) return err;
   void* args[] = {&p, &kmap, &vmap};
   err = launch_kernel(k.fn, dim3(plan.grid), dim3(kQtThreads), plan.smem, stream, args, 0);

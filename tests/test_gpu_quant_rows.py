@@ -127,6 +127,48 @@ def test_groups_that_are_not_numbers(dtype):
     assert (out.cpu()[0, 0, 4] - x[0, 0, 4].float()).abs().max() <= torch.finfo(BF).max / 13
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_that_are_sixteen_bytes_aligned(dtype):
+    """Rows that start on 16 but not on 32 bytes, in and out."""
+    b, h, n, d = 2, 2, 37, 64
+    off = 8 if dtype == BF else 4
+    wide = rows((b, h, n, d + 2 * off), F32, 8).to(dtype).cuda()
+    x = wide[..., off:off + d]
+    assert x.data_ptr() % 32 == 16
+    cache = bd.QuantCache.empty(b, h, n, d)
+    shape = cache.shape(h, 0)
+    bd.bd_quant_write(shape, x, x, cache)
+    qc, qs = ref.quantise(x.cpu().contiguous())
+    assert torch.equal(cache.v_codes.cpu(), qc) and torch.equal(cache.k_scales.cpu().view(torch.int16), qs.view(torch.int16))
+    out = torch.full_like(wide, 5.0)
+    bd.bd_quant_read(shape, cache, out[..., off:off + d], None, first_row=0)
+    assert torch.equal(out[..., off:off + d].cpu(), ref.values(qc, qs).float().to(dtype))
+    assert (out[..., :off] == 5).all() and (out[..., off + d:] == 5).all()
+
+
+def test_groups_of_every_scale():
+    """Scales over the whole range of bf16, subnormal ones among them, at quotients on and beside the ties."""
+    e = torch.arange(-126, 121)
+    x = torch.zeros(1, 1, len(e), 64)
+    step = torch.arange(-16, 16) / 2.0
+    step[0] = 7.0
+    for i, k in enumerate(e.tolist()):
+        x[0, 0, i, :32] = step * 2.0 ** k                       # ties: the scale is 2^k
+        x[0, 0, i, 32:] = step * (1 + 2.0 ** -7) * 2.0 ** k
+    x = x.clamp(-torch.finfo(BF).max, torch.finfo(BF).max)
+    for dtype in (BF, F32):
+        y = x.to(dtype)
+        cache = bd.QuantCache.empty(1, 1, len(e), 64)
+        shape = cache.shape(1, 0)
+        bd.bd_quant_write(shape, y.cuda(), y.cuda(), cache)
+        qc, qs = ref.quantise(y)
+        assert torch.equal(cache.k_scales.cpu().view(torch.int16), qs.view(torch.int16))
+        assert torch.equal(cache.k_codes.cpu(), qc)
+        out = torch.empty(1, 1, len(e), 64, dtype=dtype, device="cuda")
+        bd.bd_quant_read(shape, cache, out, None, first_row=0)
+        assert torch.equal(out.cpu(), ref.values(qc, qs).float().to(dtype))
+
+
 def test_an_empty_write_and_read():
     cache = bd.QuantCache.empty(2, 2, 9, 64)
     cache.k_codes.fill_(0x35)
