@@ -490,7 +490,7 @@ int bd_quant_draft_attn(const bd_shape* shape, const void* q, const bd_quant_cac
   if (!ws) return BD_ERR_WORKSPACE;
   if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
   if (ws_bytes < ws_region_offset(units) + quant_attn_bytes(s, g, qp)) return BD_ERR_WORKSPACE;
-  const QuantAttnCall call = {q, o_out, lse_out, g, 1, idx, count, budget, step_j};
+  const QuantAttnCall call = {q, o_out, lse_out, g, 1, idx, count, budget, step_j, (flags & BD_DRAFT_VIEW_READY) != 0};
   return map_cuda(launch_quant_attn(s, qp, call, *cache, region(ws, units), counters(ws), status_word(ws),
                                     static_cast<cudaStream_t>(stream)));
 }
@@ -511,7 +511,7 @@ int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd
   if (!ws) return BD_ERR_WORKSPACE;
   if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
   if (ws_bytes < ws_region_offset(units) + qp.bytes) return BD_ERR_WORKSPACE;
-  const QuantAttnCall call = {q, o_out, lse_out, (int)rows, n_q, nullptr, nullptr, 0, 0};
+  const QuantAttnCall call = {q, o_out, lse_out, (int)rows, n_q, nullptr, nullptr, 0, 0, false};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (qp.on_tc) return map_cuda(launch_quant_tc(s, qp.tc, call, *cache, region(ws, units), status_word(ws), st));
   return map_cuda(launch_quant_attn(s, qp.warps, call, *cache, region(ws, units), counters(ws), status_word(ws), st));

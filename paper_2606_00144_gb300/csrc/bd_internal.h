@@ -186,11 +186,13 @@ struct QuantAttnCall {
   const int32_t* idx;   // a drafter pass's view (null: a verify block)
   const int32_t* count;
   int budget, step_j;
+  bool view_ready;      // BD_DRAFT_VIEW_READY
 };
 struct QuantAttnPlan {
   int nt, chunks;       // n8 tiles of a CTA's query rows; chunks of a KV head's rows
-  int n_split;          // CTAs of a unit's entries
-  int most_split;       // the most that any length of this shape takes
+  int per_split;        // entries of a CTA
+  int cluster, clusters;   // CTAs of a cluster, clusters of a unit
+  int most_clusters;    // the most that any number of entries takes
 };
 // entries: the most that a unit attends to
 bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* plan);

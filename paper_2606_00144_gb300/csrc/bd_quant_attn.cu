@@ -16,11 +16,20 @@
 // ldmatrix lays a row's 16-byte group out as the A operand of S (a 32-bit word a lane), its transposed form as the
 // A operand of O^T (16-bit units of two rows in a word), so neither side needs a shuffle.
 // M is a running maximum of S + e that may trail by 2^8; each warp keeps its own, and the warps, then the CTAs
-// of a unit, are merged at the end (the last CTA to arrive merges, in the CTAs' order).
+// of a unit, are merged at the end.
+//
+// A pass is a chain of latencies, not bandwidth (64 units of 512 entries read 5 MB), so as few round trips as there are:
+// the view's first indices are fetched beside its count, every warp has a tile or two, and the CTAs of a unit are a
+// cluster that meets in the shared memory of its first (long views of few units: several clusters, whose parts the last
+// to arrive merges from global memory, in order).  ISSUED
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "bd_internal.h"
 #include "bd_quant.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace bd {
 
@@ -28,7 +37,8 @@ constexpr int kQaWarps = 4;
 constexpr int kQaThreads = 32 * kQaWarps;
 constexpr int kQaTile = 32;          // entries of a warp's tile
 constexpr int kQaStages = 3;
-constexpr int kQaMaxSplit = 32;      // CTAs of a unit
+constexpr int kQaCluster = 8;        // most CTAs of a cluster (the portable size)
+constexpr int kQaMaxParts = 8;       // clusters of a unit
 constexpr float kQaSlack = 8.f;      // log2 of how far the running maximum may trail
 constexpr float kQaLift = 6.f;       // weights are kept 2^6 higher: fp16's range is wider above 1 than P needs
 
@@ -40,14 +50,16 @@ struct QuantAttnParams {
   const __nv_bfloat16* q;      // [units][rows][D]: rows = query heads of a KV head x n_q
   __nv_bfloat16* o;
   float* lse;                  // or null
-  float* o_part;               // [units][n_split][rows][D], normalised
-  float* lse_part;             // [units][n_split][rows]
+  float* o_part;               // [units][clusters][rows][D], normalised
+  float* lse_part;             // [units][clusters][rows]
   int* counters;               // [units]
   int* status;
   const int32_t* seq_lens;
   const int32_t* idx;          // drafter pass: [units][budget]
   const int32_t* count;
-  int h_kv, t_ctx, t_cap, n_q, rows, budget, step_j, n_split;
+  int h_kv, t_ctx, t_cap, n_q, rows, budget, step_j;
+  int per_split, cluster, clusters;   // entries of a CTA; CTAs of a cluster; clusters of a unit
+  bool early;                  // BD_DRAFT_VIEW_READY
   float scale_log2;            // log2(e) / sqrt(D)
 };
 
@@ -68,7 +80,9 @@ template <int D, int NT>
 struct QaSmem {
   static constexpr size_t kRing = (size_t)kQaWarps * kQaStages * QaStage<D>::BYTES;
   static constexpr size_t kMerge = (size_t)kQaWarps * 8 * NT * (D + 4 + 2) * 4;
-  static constexpr size_t kTotal = (kRing > kMerge ? kRing : kMerge);
+  static constexpr size_t kArea = kRing > kMerge ? kRing : kMerge;
+  static constexpr size_t kSlot = (size_t)8 * NT * (D + 1) * 4;      // a CTA's part in the cluster's first
+  static size_t bytes(int cluster) { return kArea + (cluster > 1 ? cluster * kSlot : 0); }
 };
 
 __device__ __forceinline__ int quant_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
@@ -91,11 +105,23 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
   const int split = blockIdx.x, unit = blockIdx.y, row0 = blockIdx.z * NQC;
   const int rows = min(p.rows - row0, NQC);
   const int b = unit / p.h_kv;
-  grid_dependency_wait();
-  allow_dependent_launch();
+  if (!p.early) {
+    grid_dependency_wait();
+    allow_dependent_launch();
+  }
+  if (p.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this CTA has started
 
+  // slices by what a view can hold: the first tiles' indices need not wait for the count
+  const int e_begin = split * p.per_split;
+  const int32_t* iunit = GATHER ? p.idx + (size_t)unit * p.budget : nullptr;
+  auto index = [&](int tile) {                 // idx of entry `lane` of a tile, if it may be one
+    const int e = e_begin + tile * kQaTile + lane;
+    return GATHER && e < p.budget && tile * kQaTile + lane < p.per_split ? __ldg(iunit + e) : 0;
+  };
+  int spec[kQaStages];
+#pragma unroll
+  for (int i = 0; i < kQaStages; ++i) spec[i] = index(warp + i * kQaWarps);
   int* status = tid == 0 ? p.status : nullptr;
-  const int t_unit = quant_context(p.seq_lens, b, p.t_ctx, status);
   int cnt = 0;
   if (GATHER) {
     cnt = __ldg(p.count + unit);
@@ -104,58 +130,68 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
       cnt = min(max(cnt, 0), p.budget);
     }
   }
+  const int t_unit = quant_context(p.seq_lens, b, p.t_ctx, status);
   const int n_entries = GATHER ? cnt + p.step_j + 1 : t_unit + p.n_q;
-  // equal slices of whole 16-entry sub-tiles; n_seg of them hold entries
-  const int per = ((n_entries + 16 * p.n_split - 1) / (16 * p.n_split)) * 16;
-  const int n_seg = (n_entries + per - 1) / per;
-  if (split >= n_seg) return;
-  const int e_begin = split * per, e_end = min(n_entries, e_begin + per);
-  const int n_tiles = (e_end - e_begin + kQaTile - 1) / kQaTile;
+  const int e_end = min(n_entries, e_begin + p.per_split);
+  const int n_tiles = e_end > e_begin ? (e_end - e_begin + kQaTile - 1) / kQaTile : 0;
 
   const size_t base = (size_t)unit * p.t_cap;
   uint8_t* ring = smem + (size_t)warp * kQaStages * ST::BYTES;
 
-  // entry `lane` of a tile: its cache row, or -1
-  auto entry_row = [&](int tile) {
+  // entry `lane` of a tile: its cache row, or -1 (r: its index, where it has one)
+  auto entry_row = [&](int tile, int r) {
     const int e = e_begin + tile * kQaTile + lane;
     if (e >= e_end) return -1;
     if (!GATHER) return e;
     if (e >= cnt) return t_unit + (e - cnt);
-    const int r = __ldg(p.idx + (size_t)unit * p.budget + e);
     if (r < 0 || r >= t_unit) {
       record_error(p.status, BD_ERR_INVALID_ARG);
       return -1;
     }
     return r;
   };
-  // row: this lane's entry_row; returns which of the tile's entries are there (the rest are zero-filled)
-  auto fetch = [&](int row, int slot) {
+  // row: this lane's entry_row; returns which of the tile's entries are there (the rest are zero-filled).
+  // part 0: rows of the context and what is zero-filled; 1: drafted rows; 2: all
+  auto fetch = [&](int row, int slot, int part) {
     uint8_t* st = ring + slot * ST::BYTES;
     constexpr int PER = 32 / G;                // rows a pass of the warp covers, G 16-byte groups each
 #pragma unroll
     for (int it = 0; it < G; ++it) {
       const int r = it * PER + lane / G, g = lane % G;
       const int src_row = __shfl_sync(0xffffffffu, row, r);
+      if (part != 2 && (part == 1) != (src_row >= t_unit)) continue;
       const size_t src = (base + max(src_row, 0)) * (D / 2) + 16 * g;
       const uint32_t off = code_offset<D>(r, g);
       cp_async16_zfill(st + off, p.kc + src, src_row >= 0);
       cp_async16_zfill(st + ST::CODES + off, p.vc + src, src_row >= 0);
     }
-    const size_t src = (base + max(row, 0)) * G;
-    cp_async_small<2 * G>(st + 2 * ST::CODES + lane * 2 * G, p.ks + src, row >= 0);
-    cp_async_small<2 * G>(st + 2 * ST::CODES + ST::SCALES + lane * 2 * G, p.vs + src, row >= 0);
+    if (part == 2 || (part == 1) == (row >= t_unit)) {
+      const size_t src = (base + max(row, 0)) * G;
+      cp_async_small<2 * G>(st + 2 * ST::CODES + lane * 2 * G, p.ks + src, row >= 0);
+      cp_async_small<2 * G>(st + 2 * ST::CODES + ST::SCALES + lane * 2 * G, p.vs + src, row >= 0);
+    }
     return __ballot_sync(0xffffffffu, row >= 0);
   };
 
   // this warp's tiles: warp, warp + kQaWarps, ...
   const int mine = n_tiles > warp ? (n_tiles - warp + kQaWarps - 1) / kQaWarps : 0;
-  uint32_t live[kQaStages] = {};                    // of this iteration's tile and the next ones
+  uint32_t live[kQaStages] = {};               // of this iteration's tile and the next ones
+  int at_row[kQaStages];
+#pragma unroll
+  for (int i = 0; i < kQaStages; ++i) at_row[i] = i < mine ? entry_row(warp + i * kQaWarps, spec[i]) : -1;
+  if (p.early) {                               // the view is older than the kernel before; its drafted rows are not
+#pragma unroll
+    for (int i = 0; i < kQaStages - 1; ++i)
+      if (i < mine) fetch(at_row[i], i, 0);
+    grid_dependency_wait();
+    allow_dependent_launch();
+  }
 #pragma unroll
   for (int i = 0; i < kQaStages - 1; ++i) {
-    if (i < mine) live[i] = fetch(entry_row(warp + i * kQaWarps), i);
+    if (i < mine) live[i] = fetch(at_row[i], i, p.early ? 1 : 2);
     cp_async_commit();
   }
-  int next_row = kQaStages - 1 < mine ? entry_row(warp + (kQaStages - 1) * kQaWarps) : -1;
+  int next_row = at_row[kQaStages - 1];
 
   // ---- the query rows as B operands: fp16 over a power of two of their own, odd elements over 16 more
   uint32_t bq[NT][G][4];
@@ -233,9 +269,9 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
   for (int i = 0; i < mine; ++i) {
     const int tile = warp + i * kQaWarps;
     // the tile two further on, its rows looked up an iteration ago
-    if (i + kQaStages - 1 < mine) live[kQaStages - 1] = fetch(next_row, (i + kQaStages - 1) % kQaStages);
+    if (i + kQaStages - 1 < mine) live[kQaStages - 1] = fetch(next_row, (i + kQaStages - 1) % kQaStages, 2);
     cp_async_commit();
-    if (i + kQaStages < mine) next_row = entry_row(tile + kQaStages * kQaWarps);
+    if (i + kQaStages < mine) next_row = entry_row(tile + kQaStages * kQaWarps, index(tile + kQaStages * kQaWarps));
     cp_async_wait<kQaStages - 1>();
     __syncwarp();
     const uint8_t* st = ring + (i % kQaStages) * ST::BYTES;
@@ -401,8 +437,29 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
     }
   __syncthreads();
   const size_t out0 = (size_t)unit * p.rows + row0;
-  const size_t part0 = ((size_t)unit * p.n_split + split) * p.rows + row0;
-  const bool whole = n_seg == 1;
+  const int C = p.cluster, part = split / C;
+  float* slots = reinterpret_cast<float*>(smem + QaSmem<D, NT>::kArea);   // [C][NQC][D], then [C][NQC] lse (in the first CTA)
+  float* lses = slots + (size_t)C * NQC * D;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = C > 1 ? (int)cluster.block_rank() : 0;
+  float* my_slot = slots + (size_t)rank * NQC * D;
+  float* my_lse = lses + rank * NQC;
+  if (C > 1) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");           // every CTA is running
+    my_slot = cluster.map_shared_rank(my_slot, 0);
+    my_lse = cluster.map_shared_rank(my_lse, 0);
+  }
+  // a row's final values, or with several clusters its part's
+  auto emit = [&](int r, int d, float4 a, float lse) {
+    if (p.clusters == 1) {
+      *reinterpret_cast<uint2*>(p.o + (out0 + r) * D + d) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+      if (d == 0 && p.lse) p.lse[out0 + r] = lse;
+    } else {
+      const size_t at = ((size_t)unit * p.clusters + part) * p.rows + row0 + r;
+      *reinterpret_cast<float4*>(p.o_part + at * D + d) = a;
+      if (d == 0) p.lse_part[at] = lse;
+    }
+  };
   for (int i = tid; i < rows * (D / 4); i += kQaThreads) {
     const int r = i / (D / 4), d = i % (D / 4) * 4;
     float mx = -INFINITY, tot = 0.f;
@@ -424,42 +481,75 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
     const float inv = tot == 0.f ? 0.f : 1.f / tot;            // (a NaN stays one)
     a.x *= inv, a.y *= inv, a.z *= inv, a.w *= inv;
     const float lse = tot == 0.f ? -INFINITY : (mx + log2f(tot)) * kLn2;
-    if (whole) {
-      *reinterpret_cast<uint2*>(p.o + (out0 + r) * D + d) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
-      if (d == 0 && p.lse) p.lse[out0 + r] = lse;
+    if (C == 1) {
+      emit(r, d, a, lse);
     } else {
-      *reinterpret_cast<float4*>(p.o_part + (part0 + r) * D + d) = a;
-      if (d == 0) p.lse_part[part0 + r] = lse;
+      *reinterpret_cast<float4*>(my_slot + r * D + d) = a;
+      if (d == 0) my_lse[r] = lse;
     }
   }
-  if (whole) return;
+  if (C > 1) {
+    // ---------------------------------------------------------------- the cluster's parts, in its first CTA
+    cluster.sync();                            // all parts have landed
+    if (rank != 0) return;
+    for (int i = tid; i < rows * (D / 4); i += kQaThreads) {
+      const int r = i / (D / 4), d = i % (D / 4) * 4;
+      float ls[kQaCluster], mx = -INFINITY, tot = 0.f;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kQaCluster; ++k) {
+        ls[k] = k < C ? lses[k * NQC + r] : -INFINITY;
+        mx = fmaxf(mx, ls[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kQaCluster; ++k) {
+        if (k >= C || ls[k] == -INFINITY) continue;            // (an empty part's slot holds zeros; a NaN stays one)
+        const float f = fast_exp2((ls[k] - mx) * kLog2e);
+        const float4 v = *reinterpret_cast<const float4*>(slots + ((size_t)k * NQC + r) * D + d);
+        tot += f;
+        a.x = fmaf(f, v.x, a.x);
+        a.y = fmaf(f, v.y, a.y);
+        a.z = fmaf(f, v.z, a.z);
+        a.w = fmaf(f, v.w, a.w);
+      }
+      const float inv = tot == 0.f ? 0.f : 1.f / tot;
+      a.x *= inv, a.y *= inv, a.z *= inv, a.w *= inv;
+      emit(r, d, a, tot == 0.f ? -INFINITY : mx + logf(tot));
+    }
+  }
+  if (p.clusters == 1) return;
 
-  // ---------------------------------------------------------------- the unit's last CTA merges
+  // ---------------------------------------------------------------- the unit's last cluster to arrive merges
   __shared__ int last;
   __threadfence();
   __syncthreads();
-  if (tid == 0) last = atomicAdd(&p.counters[unit], 1) == n_seg * (int)gridDim.z - 1;
+  if (tid == 0) last = atomicAdd(&p.counters[unit], 1) == p.clusters * (int)gridDim.z - 1;
   __syncthreads();
   if (!last) return;
   __threadfence();
-  const float* part = p.o_part + (size_t)unit * p.n_split * p.rows * D;
-  const float* lses = p.lse_part + (size_t)unit * p.n_split * p.rows;
+  const float* parts = p.o_part + (size_t)unit * p.clusters * p.rows * D;
+  const float* part_lse = p.lse_part + (size_t)unit * p.clusters * p.rows;
   for (int i = tid; i < p.rows * (D / 4); i += kQaThreads) {
     const int r = i / (D / 4), d = i % (D / 4) * 4;
-    float mx = -INFINITY, tot = 0.f;
-    for (int sp = 0; sp < n_seg; ++sp) mx = fmaxf(mx, __ldcg(lses + (size_t)sp * p.rows + r));
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int sp = 0; sp < n_seg; ++sp) {
-      const float ls = __ldcg(lses + (size_t)sp * p.rows + r);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(part + ((size_t)sp * p.rows + r) * D + d));
-      if (ls == -INFINITY) continue;
-      const float f = fast_exp2((ls - mx) * kLog2e);
+    float ls[kQaMaxParts], mx = -INFINITY, tot = 0.f;
+    float4 v[kQaMaxParts], a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kQaMaxParts; ++k) {    // every part requested at once
+      const size_t at = (size_t)k * p.rows + r;
+      ls[k] = k < p.clusters ? __ldcg(part_lse + at) : -INFINITY;
+      v[k] = k < p.clusters ? __ldcg(reinterpret_cast<const float4*>(parts + at * D + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kQaMaxParts; ++k) mx = fmaxf(mx, ls[k]);
+#pragma unroll
+    for (int k = 0; k < kQaMaxParts; ++k) {
+      if (ls[k] == -INFINITY) continue;
+      const float f = fast_exp2((ls[k] - mx) * kLog2e);
       tot += f;
-      a.x = fmaf(f, v.x, a.x);
-      a.y = fmaf(f, v.y, a.y);
-      a.z = fmaf(f, v.z, a.z);
-      a.w = fmaf(f, v.w, a.w);
+      a.x = fmaf(f, v[k].x, a.x);
+      a.y = fmaf(f, v[k].y, a.y);
+      a.z = fmaf(f, v[k].z, a.z);
+      a.w = fmaf(f, v[k].w, a.w);
     }
     const float inv = tot == 0.f ? 0.f : 1.f / tot;
     *reinterpret_cast<uint2*>(p.o + ((size_t)unit * p.rows + r) * D + d) =
@@ -475,13 +565,13 @@ namespace {
 
 struct QaInfo {
   const void* fn;
-  size_t smem;
+  size_t (*smem)(int cluster);
   std::atomic<uint64_t>* allowed;
 };
 template <int D, int NT, bool GATHER>
 QaInfo qa_one() {
   static std::atomic<uint64_t> allowed{0};
-  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER>), QaSmem<D, NT>::kTotal, &allowed};
+  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER>), &QaSmem<D, NT>::bytes, &allowed};
 }
 template <int D, int NT>
 QaInfo qa_info(bool gather) {
@@ -499,16 +589,21 @@ bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* p
   plan->nt = rows <= 8 ? 1 : 2;
   plan->chunks = (rows + 8 * plan->nt - 1) / (8 * plan->nt);
   if (units > 65535 || plan->chunks > 65535) return false;
-  // two CTAs an SM in one wave, none with fewer than 64 entries
-  const long slots = 2L * current_sm_count();
-  plan->most_split = (int)std::min<long>(kQaMaxSplit, std::max(1L, slots / (units * plan->chunks)));
-  plan->n_split = (int)std::max(1L, std::min<long>(plan->most_split, (entries + 63) / 64));
+  // A tile for every warp while one wave holds the CTAs (three an SM; of a cluster, the shared memory of two), and
+  // never more than kQaMaxParts clusters of a unit.
+  const long slots = std::max(1L, 2L * current_sm_count() / (units * plan->chunks));
+  const long want = std::max(1L, std::min<long>(slots, (entries + kQaWarps * kQaTile - 1) / (kQaWarps * kQaTile)));
+  plan->clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
+  plan->cluster = (int)std::min<long>(kQaCluster, (want + plan->clusters - 1) / plan->clusters);
+  const long ctas = (long)plan->cluster * plan->clusters;
+  plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);
+  plan->most_clusters = (int)std::min<long>(kQaMaxParts, (slots + kQaCluster - 1) / kQaCluster);
   return true;
 }
 
 size_t quant_attn_bytes(const bd_shape& s, int rows, const QuantAttnPlan& plan) {
-  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.most_split * rows;
-  return plan.most_split > 1 ? align_up(part_rows * s.head_dim * 4, 256) + align_up(part_rows * 4, 256) : 0;
+  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.most_clusters * rows;
+  return plan.most_clusters > 1 ? align_up(part_rows * s.head_dim * 4, 256) + align_up(part_rows * 4, 256) : 0;
 }
 
 cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
@@ -522,7 +617,7 @@ cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, cons
   p.o = static_cast<__nv_bfloat16*>(c.o_out);
   p.lse = c.lse_out;
   p.rows = c.rows;
-  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.n_split * c.rows;
+  const size_t part_rows = (size_t)s.batch * s.h_kv * plan.clusters * c.rows;
   p.o_part = static_cast<float*>(ws_region);
   p.lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws_region) + align_up(part_rows * s.head_dim * 4, 256));
   p.counters = counters;
@@ -536,13 +631,17 @@ cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, cons
   p.n_q = c.n_q;
   p.budget = c.budget;
   p.step_j = c.step_j;
-  p.n_split = plan.n_split;
+  p.per_split = plan.per_split;
+  p.cluster = plan.cluster;
+  p.clusters = plan.clusters;
+  p.early = c.view_ready;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
   const QaInfo k = qa_kernel(s.head_dim, plan.nt, c.idx != nullptr);
   cudaError_t err = allow_shared_memory_once(k.fn, 128, k.allowed);
   if (err != cudaSuccess) return err;
   void* args[] = {&p};
-  return launch_kernel(k.fn, dim3(plan.n_split, s.batch * s.h_kv, plan.chunks), dim3(kQaThreads), k.smem, stream, args, 0);
+  return launch_kernel(k.fn, dim3(plan.cluster * plan.clusters, s.batch * s.h_kv, plan.chunks), dim3(kQaThreads),
+                       k.smem(plan.cluster), stream, args, plan.cluster > 1 ? plan.cluster : 0);
 }
 
 }  // namespace bd
