@@ -190,7 +190,7 @@ struct QuantAttnCall {
 };
 struct QuantAttnPlan {
   int nt, chunks;       // n8 tiles of a CTA's query rows; chunks of a KV head's rows
-  int per_split;        // entries of a CTA
+  int per_split, warps; // entries and warps of a CTA
   int cluster, clusters;   // CTAs of a cluster, clusters of a unit
   int most_clusters;    // the most that any number of entries takes
 };

@@ -33,10 +33,7 @@ namespace cg = cooperative_groups;
 
 namespace bd {
 
-constexpr int kQaWarps = 4;
-constexpr int kQaThreads = 32 * kQaWarps;
 constexpr int kQaTile = 32;          // entries of a warp's tile
-constexpr int kQaStages = 3;
 constexpr int kQaCluster = 8;        // most CTAs of a cluster (the portable size)
 constexpr int kQaMaxParts = 8;       // clusters of a unit
 constexpr float kQaSlack = 8.f;      // log2 of how far the running maximum may trail
@@ -76,10 +73,12 @@ __device__ __forceinline__ uint32_t code_offset(int r, int g) {
   return D == 128 ? r * 64 + ((g ^ (r >> 1 & 3)) << 4) : r * 32 + ((g ^ (r >> 2 & 1)) << 4);
 }
 
-template <int D, int NT>
+// WARPS: 4 with three tiles in flight each, or 8 with two for slices of more than a tile a warp.
+template <int D, int NT, int WARPS>
 struct QaSmem {
-  static constexpr size_t kRing = (size_t)kQaWarps * kQaStages * QaStage<D>::BYTES;
-  static constexpr size_t kMerge = (size_t)kQaWarps * 8 * NT * (D + 4 + 2) * 4;
+  static constexpr int kStages = WARPS == 4 ? 3 : 2;
+  static constexpr size_t kRing = (size_t)WARPS * kStages * QaStage<D>::BYTES;
+  static constexpr size_t kMerge = (size_t)WARPS * 8 * NT * (D + 4 + 2) * 4;
   static constexpr size_t kArea = kRing > kMerge ? kRing : kMerge;
   static constexpr size_t kSlot = (size_t)8 * NT * (D + 1) * 4;      // a CTA's part in the cluster's first
   static size_t bytes(int cluster) { return kArea + (cluster > 1 ? cluster * kSlot : 0); }
@@ -96,9 +95,10 @@ __device__ __forceinline__ int quant_context(const int32_t* seq_lens, int b, int
 }
 
 // NT: n8 tiles of query rows; GATHER: entries come from idx (and the drafted rows), else entry = cache row.
-template <int D, int NT, bool GATHER>
-__global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_constant__ QuantAttnParams p) {
+template <int D, int NT, bool GATHER, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_attn_kernel(const __grid_constant__ QuantAttnParams p) {
   using ST = QaStage<D>;
+  constexpr int kQaWarps = WARPS, kQaThreads = 32 * WARPS, kQaStages = QaSmem<D, NT, WARPS>::kStages;
   constexpr int G = D / 32, NQC = 8 * NT;
   extern __shared__ __align__(128) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kQaThreads) quant_attn_kernel(const __grid_con
   __syncthreads();
   const size_t out0 = (size_t)unit * p.rows + row0;
   const int C = p.cluster, part = split / C;
-  float* slots = reinterpret_cast<float*>(smem + QaSmem<D, NT>::kArea);   // [C][NQC][D], then [C][NQC] lse (in the first CTA)
+  float* slots = reinterpret_cast<float*>(smem + QaSmem<D, NT, WARPS>::kArea);   // [C][NQC][D], then [C][NQC] lse (in the first CTA)
   float* lses = slots + (size_t)C * NQC * D;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = C > 1 ? (int)cluster.block_rank() : 0;
@@ -568,18 +568,18 @@ struct QaInfo {
   size_t (*smem)(int cluster);
   std::atomic<uint64_t>* allowed;
 };
-template <int D, int NT, bool GATHER>
+template <int D, int NT, bool GATHER, int WARPS>
 QaInfo qa_one() {
   static std::atomic<uint64_t> allowed{0};
-  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER>), &QaSmem<D, NT>::bytes, &allowed};
+  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER, WARPS>), &QaSmem<D, NT, WARPS>::bytes, &allowed};
 }
-template <int D, int NT>
-QaInfo qa_info(bool gather) {
-  return gather ? qa_one<D, NT, true>() : qa_one<D, NT, false>();
+template <int D, bool GATHER>
+QaInfo qa_info(int nt, int warps) {
+  return nt == 2 ? qa_one<D, 2, GATHER, 4>() : warps == 4 ? qa_one<D, 1, GATHER, 4>() : qa_one<D, 1, GATHER, 8>();
 }
-QaInfo qa_kernel(int d, int nt, bool gather) {
-  if (d == 64) return nt == 1 ? qa_info<64, 1>(gather) : qa_info<64, 2>(gather);
-  return nt == 1 ? qa_info<128, 1>(gather) : qa_info<128, 2>(gather);
+QaInfo qa_kernel(int d, int nt, int warps, bool gather) {
+  if (d == 64) return gather ? qa_info<64, true>(nt, warps) : qa_info<64, false>(nt, warps);
+  return gather ? qa_info<128, true>(nt, warps) : qa_info<128, false>(nt, warps);
 }
 
 }  // namespace
@@ -589,14 +589,15 @@ bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* p
   plan->nt = rows <= 8 ? 1 : 2;
   plan->chunks = (rows + 8 * plan->nt - 1) / (8 * plan->nt);
   if (units > 65535 || plan->chunks > 65535) return false;
-  // A tile for every warp while one wave holds the CTAs (three an SM; of a cluster, the shared memory of two), and
-  // never more than kQaMaxParts clusters of a unit.
+  // A tile for every one of four warps while one wave holds the CTAs (two an SM: what a cluster's shared memory leaves),
+  // eight warps where a slice is longer, and never more than kQaMaxParts clusters of a unit.
   const long slots = std::max(1L, 2L * current_sm_count() / (units * plan->chunks));
-  const long want = std::max(1L, std::min<long>(slots, (entries + kQaWarps * kQaTile - 1) / (kQaWarps * kQaTile)));
+  const long want = std::max(1L, std::min<long>(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile)));
   plan->clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
   plan->cluster = (int)std::min<long>(kQaCluster, (want + plan->clusters - 1) / plan->clusters);
   const long ctas = (long)plan->cluster * plan->clusters;
   plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);
+  plan->warps = plan->nt == 1 && plan->per_split > 4 * kQaTile ? 8 : 4;
   plan->most_clusters = (int)std::min<long>(kQaMaxParts, (slots + kQaCluster - 1) / kQaCluster);
   return true;
 }
@@ -636,11 +637,11 @@ cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, cons
   p.clusters = plan.clusters;
   p.early = c.view_ready;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
-  const QaInfo k = qa_kernel(s.head_dim, plan.nt, c.idx != nullptr);
+  const QaInfo k = qa_kernel(s.head_dim, plan.nt, plan.warps, c.idx != nullptr);
   cudaError_t err = allow_shared_memory_once(k.fn, 128, k.allowed);
   if (err != cudaSuccess) return err;
   void* args[] = {&p};
-  return launch_kernel(k.fn, dim3(plan.cluster * plan.clusters, s.batch * s.h_kv, plan.chunks), dim3(kQaThreads),
+  return launch_kernel(k.fn, dim3(plan.cluster * plan.clusters, s.batch * s.h_kv, plan.chunks), dim3(32 * plan.warps),
                        k.smem(plan.cluster), stream, args, plan.cluster > 1 ? plan.cluster : 0);
 }
 
