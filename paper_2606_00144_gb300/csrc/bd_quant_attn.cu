@@ -593,7 +593,10 @@ bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* p
   // eight warps where a slice is longer, and never more than kQaMaxParts clusters of a unit.
   const long slots = std::max(1L, 2L * current_sm_count() / (units * plan->chunks));
   const long want = std::max(1L, std::min<long>(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile)));
+  // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA: one, unless its
+  // slices would be longer by more than that.
   plan->clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
+  if (entries / kQaCluster - entries / want <= 320) plan->clusters = 1;
   plan->cluster = (int)std::min<long>(kQaCluster, (want + plan->clusters - 1) / plan->clusters);
   const long ctas = (long)plan->cluster * plan->clusters;
   plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);

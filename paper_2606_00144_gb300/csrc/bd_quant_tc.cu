@@ -802,16 +802,22 @@ size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
   return align_up(rows * s.head_dim * 4, 256) + align_up(rows * 4, 256) + align_up(units * 4, 256);
 }
 
+// The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast, as long as one cluster
+// holds a unit; beyond, its tensor pipe and its second merge cost more.  mma.sync / tcgen05, us, d 128: 8 units of 1K, 4
+// rows 5.2 / 9.6, 16 rows 9.7 / 11.6, 24 rows 14.4 / 11.8; of 4K (several clusters), 4 rows 11.3 / 10.6; 64 units of 1K, 4K, 8K,
+// 16K, 4 rows 8.9 / 12.3, 16.0 / 20.4, 25.0 / 27.2, 43.0 / 41.5, 16 rows of 16K 59.7 / 47.7, 24 rows 108 / 48; 8 units of 0.4K,
+// 24 rows 7.7 / 10.1; d 64: 64 units of 16K, 4 rows 26.6 / 35.2, 8 units of 128K 37.4 / 33.0, 2 units of 1K, 24 rows 6.4 / 9.7.
+static bool warps_suit(const bd_shape& s, int rows, const QuantAttnPlan& w) {
+  if (w.clusters > 1) return false;
+  if (rows <= 8) return w.per_split <= (s.head_dim == 128 ? 3072 : 5120);
+  return w.per_split <= 160 && (long)s.batch * s.h_kv * w.chunks * w.cluster <= 64;
+}
+
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
-  // One n8 tile of query rows at head_dim 64 stays on mma.sync: half of quant_tc_kernel's V warps have no channels
-  // there (64 units of 16K, 4 rows: 35 us, 44 on quant_tc_kernel; 24 rows: 100 / 55; d 128: 63 / 49 and 115 / 58).
-  plan->on_tc = !(s.head_dim == 64 && rows <= 8) && quant_tc_plan(s, rows, n_q, &plan->tc);
-  if (plan->on_tc) {
-    plan->bytes = quant_tc_bytes(s, plan->tc);
-    return true;
-  }
-  if (!quant_attn_plan(s, rows, (long)s.t_ctx + n_q, &plan->warps)) return false;
-  plan->bytes = quant_attn_bytes(s, rows, plan->warps);
+  const bool w = quant_attn_plan(s, rows, (long)s.t_ctx + n_q, &plan->warps);
+  plan->on_tc = !(w && warps_suit(s, rows, plan->warps)) && quant_tc_plan(s, rows, n_q, &plan->tc);
+  if (!plan->on_tc && !w) return false;
+  plan->bytes = plan->on_tc ? quant_tc_bytes(s, plan->tc) : quant_attn_bytes(s, rows, plan->warps);
   return true;
 }
 
