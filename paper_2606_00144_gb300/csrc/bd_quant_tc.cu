@@ -14,7 +14,10 @@
 // Four warpgroups take the tiles in turn, each through the whole chain with buffers of its own: unpack K, start S,
 // unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
 // warps, with two buffers between them) left every warp a chain of waits: 1700 cycles a tile, of which its work
-// was 600; the issue slots of the whole chain come to about 700.
+// was 600.  As it is a tile takes 1200 cycles of an SM's 740 issue slots each (64 units of 16K, 24 rows: 48 us).
+// Blocks of more than 32 query rows run on two groups of two warpgroups: those share a tile's unpacking and halve its
+// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 68 -> 53 us; 64
+// units, 64 rows 66 us, 84 rows 88).
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
 #include <algorithm>
@@ -26,10 +29,8 @@
 namespace bd {
 
 constexpr int kQtKeys = 128;          // keys of a tile
-constexpr int kQtGroups = 4;          // warpgroups
-constexpr int kQtThreads = 128 * kQtGroups;
-constexpr int kQtStages = 2;          // tiles of codes in flight for each of them
-constexpr int kQtRows = 32;           // query rows of a unit: the MMAs' N side
+constexpr int kQtThreads = 512;
+constexpr int kQtStages = 2;          // tiles of codes in flight for each group
 constexpr float kQtSlack = 8.f;       // log2 of how far a running maximum may trail
 constexpr float kQtLift = 6.f;        // weights are kept 2^6 higher (fp16 reaches further above 1 than P needs)
 
@@ -49,14 +50,19 @@ struct QuantTcParams {
   float scale_log2;            // log2(e) / sqrt(D)
 };
 
-template <int D>
+// H warpgroups a group, each of which takes NC columns of query rows.
+template <int D, int NC, int H>
 struct QuantTcSmem {
-  static constexpr int N = kQtRows;
+  static constexpr int N = H == 1 ? 32 : H * NC;               // the MMAs' N side
+  static constexpr int GROUPS = 4 / H;
   static constexpr uint32_t TILE = kQtKeys * D / 2;            // codes of one tensor
   static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = kQtKeys * N * 2;
-  static constexpr uint32_t SCALES = kQtGroups * 1024;         // a tile's V scales: 4 groups x 128 keys, fp16
-  static constexpr uint32_t FIXED = 1024 + 5120;               // barriers | exchange
-  static constexpr size_t kTotal = 1024 + FIXED + SCALES + Q_BYTES + kQtGroups * P_BYTES + kQtGroups * kQtStages * 2 * TILE;
+  static constexpr uint32_t FIXED = 2048;                      // the CTA's flags, places of the query rows; then its queries
+  // A group's area, everything at a constant offset from its start: barriers and loads, exchange, a tile's V scales
+  // (4 groups x 128 keys, fp16), weights, codes.
+  static constexpr uint32_t EXCHANGE = 256, SCALES = 4096, WEIGHTS = 5120, CODES = WEIGHTS + P_BYTES;
+  static constexpr uint32_t GROUP = CODES + kQtStages * 2 * TILE;
+  static constexpr size_t kTotal = 1024 + FIXED + Q_BYTES + GROUPS * GROUP;
 };
 
 template <int N>
@@ -94,6 +100,13 @@ __device__ __forceinline__ void tc_st_16x128b_8(uint32_t taddr, const uint32_t (
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+
+__device__ __forceinline__ void tc_st_16x128b(uint32_t taddr, const uint32_t (&r)[16]) { tc_st_16x128b_8(taddr, r); }
+__device__ __forceinline__ void tc_st_16x128b(uint32_t taddr, const uint32_t (&r)[8]) {   // 16 columns
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 
 // MMA with A in tensor memory, B in shared memory; desc_hi: B's high descriptor word.
@@ -158,7 +171,10 @@ struct RowScales {
     for (int i = 0; i < D / 64; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
     return scale_exponent(top);
   }
-  __device__ __forceinline__ float scale(int g) const { return __uint_as_float(g & 1 ? w[g >> 1] & 0xffff0000u : w[g >> 1] << 16); }
+  __device__ __forceinline__ float scale(int g) const {
+    const uint32_t x = g < 2 ? w[0] : w[D / 64 - 1];
+    return __uint_as_float(g & 1 ? x & 0xffff0000u : x << 16);
+  }
 };
 
 __device__ __forceinline__ int quant_tc_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
@@ -178,50 +194,45 @@ struct Ahead {
   int v_unit[kQtStages], v_key[kQtStages];
 };
 
-// NC: columns of query rows that a softmax takes.
-template <int D, int NC>
+// A thread's columns of query rows: NB blocks of BC.
+template <int D, int BC, int NB, int H>
 __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_constant__ QuantTcParams p,
                                                                 const __grid_constant__ CUtensorMap kmap,
                                                                 const __grid_constant__ CUtensorMap vmap) {
-  using L = QuantTcSmem<D>;
-  constexpr int N = L::N, G = D / 32, ST = kQtStages, GROUPS = kQtGroups;
+  constexpr int NC = BC * NB;
+  constexpr bool EARLY = NB == 1 || D == 128;              // a tile's scales loaded a tile ahead (else no registers are left)
+  using L = QuantTcSmem<D, NC, H>;
+  constexpr int N = L::N, G = D / 32, ST = kQtStages, GROUPS = L::GROUPS, GT = 128 * H;
   constexpr uint32_t TILE = L::TILE;
-  // B of P V: MN-major, the N weights of a key in one row of a 64-byte swizzle atom of 8 keys
-  constexpr uint32_t P_PITCH = N * 2, P_ATOM = 8 * P_PITCH;
+  // B of P V: MN-major, 32 weights of a key in one row of a 64-byte swizzle atom of 8 keys, blocks of 32 one after another
+  constexpr uint32_t P_PITCH = 64, P_ATOM = 8 * P_PITCH, P_BLOCK = kQtKeys * P_PITCH;
   constexpr uint32_t kPDescHi = (P_ATOM >> 4) | (1u << 14) | (4u << 29);
+  constexpr uint32_t TM = 512 / GROUPS;                    // TMEM columns of a group: K's, then V's operand (64), S (N), O (N)
+  static_assert(64 + 2 * N <= TM, "a group's tensor memory");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem);    // [GROUPS][ST] codes of K, of V have arrived
-  uint64_t* v_full = k_full + GROUPS * ST;
-  uint64_t* s_done = v_full + GROUPS * ST;                 // [GROUPS] S is in TMEM, K's columns are free
-  uint64_t* pv_done = s_done + GROUPS;                     // [GROUPS] O is up to date, V's columns and P are free
-  uint64_t* drain = pv_done + GROUPS;                      // [GROUPS]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + GROUPS);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* red = reinterpret_cast<int*>(smem + 1024);          // [GROUPS][N][4] a column's maximum (or sum) in each warp
-  float* nm_s = reinterpret_cast<float*>(red + 4 * N * GROUPS);   // [GROUPS][N] lift - running maximum (1e30: none yet)
-  int* qpos = reinterpret_cast<int*>(nm_s + N * GROUPS);   // [N] a query row's place in its block
-  float* alpha_s = reinterpret_cast<float*>(qpos + N);     // [GROUPS][N] what a maximum's last rise scales by
-  int* qtop = reinterpret_cast<int*>(alpha_s + N * GROUPS);       // [4 GROUPS]
-  Ahead* ahead_s = reinterpret_cast<Ahead*>(qtop + 4 * GROUPS);   // [GROUPS]
-  uint8_t* scales = smem + L::FIXED;                       // [GROUPS][4][4][16][2] fp16
-  uint8_t* qbuf = scales + L::SCALES;
-  uint8_t* pbuf = qbuf + L::Q_BYTES;                       // [GROUPS]
-  uint8_t* ring = pbuf + GROUPS * L::P_BYTES;              // [GROUPS][ST][K, V]
-  int* pref = reinterpret_cast<int*>(ring + GROUPS * ST * 2 * TILE);
-  static_assert((L::FIXED + L::SCALES) % 1024 == 0 && L::Q_BYTES % 1024 == 0 && L::P_BYTES % 1024 == 0, "aligned tiles");
+  int* qtop = reinterpret_cast<int*>(smem + 64);           // [16]
+  int* wtot = reinterpret_cast<int*>(smem + 128);          // [16]
+  int* qpos = reinterpret_cast<int*>(smem + 1024);         // [N] a query row's place in its block
+  uint8_t* qbuf = smem + L::FIXED;
+  uint8_t* groups = qbuf + L::Q_BYTES;
+  int* pref = reinterpret_cast<int*>(groups + GROUPS * L::GROUP);
+  static_assert(L::Q_BYTES % 1024 == 0 && L::P_BYTES % 1024 == 0 && L::GROUP % 1024 == 0, "aligned tiles");
+  static_assert(L::EXCHANGE + N * 16 + N * 8 <= L::SCALES, "exchange");
 
-  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31, quad = warp & 3, grp = warp >> 2;
+  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31, quad = warp & 3, set = warp >> 2;
+  const int grp = set / H, half = set % H;                 // the warpgroup's group, and which of its columns and unpacking
+  // a group's barriers
+  auto k_full = [&](int g, int st) { return reinterpret_cast<uint64_t*>(groups + g * L::GROUP) + st; };   // codes of K,
+  auto v_full = [&](int g, int st) { return k_full(g, ST + st); };                                        // of V have arrived
+  auto s_done = [&](int g) { return k_full(g, 2 * ST); };          // S is in TMEM, K's columns are free
+  auto pv_done = [&](int g) { return k_full(g, 2 * ST + 1); };     // O is up to date, V's columns and P are free
+  auto drain = [&](int g) { return k_full(g, 2 * ST + 2); };
   if (tid == 0) {
-    for (int i = 0; i < GROUPS * ST; ++i) {
-      mbar_init(&k_full[i], 1);
-      mbar_init(&v_full[i], 1);
-    }
-    for (int i = 0; i < GROUPS; ++i) {
-      mbar_init(&s_done[i], 1);
-      mbar_init(&pv_done[i], 1);
-      mbar_init(&drain[i], 1);
-    }
+    for (int g = 0; g < GROUPS; ++g)
+      for (int i = 0; i < 2 * ST + 3; ++i) mbar_init(k_full(g, i), 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_map(&kmap);
@@ -232,14 +243,14 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     tmem_relinquish();
   }
   // P's columns past the query rows are never written again
-  for (uint32_t i = tid; i < GROUPS * L::P_BYTES / 16; i += kQtThreads) reinterpret_cast<uint4*>(pbuf)[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (uint32_t i = tid % GT; i < L::P_BYTES / 16; i += GT)
+    reinterpret_cast<uint4*>(groups + grp * L::GROUP + L::WEIGHTS)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  // a warpgroup's columns: K's, then V's operand (64), S (32), O (32)
   const uint32_t tmem = *tmem_slot, lanes = (uint32_t)(quad * 32) << 16;
-  const uint32_t t_kv = tmem + 128 * grp, t_s = t_kv + 64, t_o = t_kv + 96;
+  const uint32_t t_kv = tmem + TM * grp, t_s = t_kv + 64, t_o = t_s + N;
 
   grid_dependency_wait();
   allow_dependent_launch();
@@ -247,7 +258,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   if (p.seq_lens) {
     lay_out_spans<kQtThreads>(p.units, [&](int u) {
       return (quant_tc_context(p.seq_lens, u / p.row_chunks / p.h_kv, p.t_ctx, nullptr) + p.n_q + kQtKeys - 1) / kQtKeys + p.seg_cost;
-    }, reinterpret_cast<int*>(smem + 512), pref);
+    }, wtot, pref);
     map.pref = pref;
     map.vtpc = max((pref[p.units] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
   }
@@ -256,14 +267,13 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
   bool alive = true;      // false once a wait gave up
 
-  // ---- the warpgroup's loads, by one of its warps (another SMSP's in each): local tile i is job grp + GROUPS i of
+  // ---- the group's loads, by one of its warps (another SMSP's in each): local tile i is job grp + GROUPS i of
   // the CTA's list of tiles; the list is walked ahead of the work, across segments.
-  const bool issuer = quad == grp;
+  const bool issuer = quad == grp && half == 0;
   const uint32_t lead = elect_leader();
-  uint64_t* my_k_full = k_full + grp * ST;
-  uint64_t* my_v_full = v_full + grp * ST;
-  uint8_t* my_ring = ring + grp * ST * 2 * TILE;
-  Ahead* ahead = ahead_s + grp;                // (in shared memory: it is the issuing warp's alone and seldom used)
+  uint8_t* mine = groups + grp * L::GROUP;
+  uint8_t* my_ring = mine + L::CODES;
+  Ahead* ahead = reinterpret_cast<Ahead*>(mine + 64 + 8 * (2 * ST));                // (in shared memory: it is the issuing warp's alone and seldom used)
   if (issuer) {
     if (lane == 0) *ahead = Ahead{u_first - 1, 0, 0, 0, 0, 0, {}, {}};
     __syncwarp();
@@ -281,8 +291,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     const bool found = j < st.job + st.n;
     const int unit = st.unit / p.row_chunks, key = (st.tb + j - st.job) * kQtKeys;
     if (found && lead) {
-      mbar_arrive_expect_tx(&my_k_full[s], TILE);
-      tma_load_3d(my_ring + s * 2 * TILE, &kmap, &my_k_full[s], 0, key, unit);
+      mbar_arrive_expect_tx(k_full(grp, s), TILE);
+      tma_load_3d(my_ring + s * 2 * TILE, &kmap, k_full(grp, s), 0, key, unit);
     }
     __syncwarp();
     if (lane == 0) {
@@ -300,8 +310,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     const int v_issued = ahead->v_issued;
     if (v_issued >= ahead->k_issued) return;
     if (lead) {
-      mbar_arrive_expect_tx(&my_v_full[s], TILE);
-      tma_load_3d(my_ring + s * 2 * TILE + TILE, &vmap, &my_v_full[s], 0, ahead->v_key[s], ahead->v_unit[s]);
+      mbar_arrive_expect_tx(v_full(grp, s), TILE);
+      tma_load_3d(my_ring + s * 2 * TILE + TILE, &vmap, v_full(grp, s), 0, ahead->v_key[s], ahead->v_unit[s]);
     }
     __syncwarp();
     if (lane == 0) ahead->v_issued = v_issued + 1;
@@ -316,12 +326,15 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   }
 
   const int row = quad * 32 + lane, tig = lane & 3;   // this thread's key of a tile
+  const int col0 = half * NC;                         // and its columns of query rows
   const bool has_rows = quad < G;                     // this warp has channels of V (and of O)
-  uint8_t* my_scales = scales + grp * 1024;
-  uint8_t* my_p = pbuf + grp * L::P_BYTES;
-  int* my_red = red + 4 * N * grp;
-  float* my_nm = nm_s + N * grp;
-  float* my_alpha = alpha_s + N * grp;
+  uint8_t* my_scales = mine + L::SCALES;                   // [4][4][16][2] fp16
+  uint8_t* my_p = mine + L::WEIGHTS;
+  auto red_of = [&](int g) { return reinterpret_cast<int*>(groups + g * L::GROUP + L::EXCHANGE); };   // [N][4] a column's maximum
+  auto nm_of = [&](int g) { return reinterpret_cast<float*>(red_of(g) + 4 * N); };   // (or sum) in each warp; [N] lift - running
+  int* my_red = red_of(grp) + 4 * col0;                    // maximum (1e30: none yet); [N] what its last rise scales by
+  float* my_nm = nm_of(grp) + col0;
+  float* my_alpha = my_nm + N;
   const int bar = 1 + grp;
   constexpr uint32_t idesc_s = umma_idesc_f16(128, N), idesc_o = idesc_s | kIdescBMnMajor;
 
@@ -330,14 +343,6 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   auto wait = [&](uint64_t* b, uint32_t parity) {
     if (!__all_sync(0xffffffffu, mbar_test(smem_u32(b), parity))) alive = alive && mbar_wait_warp(b, parity, p.status, abort_flag);
   };
-  // this thread's places in shared memory: its row of codes of a tile, its V scales, its weights
-  const uint32_t sw = D == 128 ? row >> 1 & 3 : row >> 2 & 1;
-  const uint8_t* k_row = my_ring + row * (D / 2);
-  const uint32_t v_rows = smem_u32(my_ring) + TILE + lane * (D / 2) + ((quad ^ (D == 128 ? lane >> 1 & 3 : lane >> 2 & 1)) << 4);
-  uint8_t* scale_at = my_scales + (row >> 1 & 3) * 64 + (row >> 3) * 4 + (row & 1) * 2;
-  uint8_t* p_row = my_p + row * P_PITCH;
-  const uint32_t p_sw = (row >> 1 & 3) << 4;
-
   int job = 0, i = 0;     // tiles of the CTA before the segment; this warpgroup's tiles so far
   for (int unit = u_first; unit <= u_last; ++unit) {
     const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
@@ -359,40 +364,53 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in
     float base;
     {
-      constexpr int CH = D / 8;
-      static_assert(N * CH <= kQtThreads, "a thread has eight elements at most");
-      const int r = tid / CH, c = tid % CH;
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows) w = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)kv_unit * p.rows_total + row_base + r) * D + 8 * c));
-      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+      constexpr int CH = D / 8, PER = (N * CH + kQtThreads - 1) / kQtThreads, STEP = kQtThreads / CH;
+      const int r0 = tid / CH, c = tid % CH;
+      uint4 w[PER];
       uint32_t top = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
-        top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+      for (int k = 0; k < PER; ++k) {
+        const int r = r0 + k * STEP;
+        w[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) w[k] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)kv_unit * p.rows_total + row_base + r) * D + 8 * c));
+      }
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
+          top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+        }
       }
       top = __reduce_max_sync(0xffffffffu, top);
       __syncthreads();                         // (the segment before has read its own)
       if (lane == 0) qtop[warp] = (int)top;
       if (tid < N) qpos[tid] = tid < rows ? (row_base + tid) % p.n_q : 0x7fffffff;
-      if (tid < N * GROUPS) nm_s[tid] = 1e30f;
+      if (tid < N)
+        for (int g = 0; g < GROUPS; ++g) nm_of(g)[tid] = 1e30f;
       __syncthreads();
       int t = 0;
 #pragma unroll
-      for (int k = 0; k < 4 * GROUPS; ++k) t = max(t, qtop[k]);
+      for (int k = 0; k < 16; ++k) t = max(t, qtop[k]);
       const int qe = min(max(t - 127, -100), 100);
       // S over the queries' power of two and the codes' 2^-10, in log2 units (the key's own power comes with it)
       base = p.scale_log2 * pow2i(qe - 3);
       const float down = pow2i(13 - qe);
-      float f[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[2 * e] = __uint_as_float(x[e] << 16) * down;
-        f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
+      for (int k = 0; k < PER; ++k) {
+        const int r = r0 + k * STEP;
+        const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[2 * e] = __uint_as_float(x[e] << 16) * down;
+          f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u) * down;
+        }
+        if (r < N)
+          *reinterpret_cast<uint4*>(qbuf + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+              make_uint4(pack_half2(f[0], f[4]), pack_half2(f[1], f[5]), pack_half2(f[2], f[6]), pack_half2(f[3], f[7]));
       }
-      if (r < N)
-        *reinterpret_cast<uint4*>(qbuf + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
-            make_uint4(pack_half2(f[0], f[4]), pack_half2(f[1], f[5]), pack_half2(f[2], f[6]), pack_half2(f[3], f[7]));
       fence_proxy_async_smem();
       __syncthreads();
     }
@@ -403,34 +421,50 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     for (int t = t_first; t < n; t += GROUPS, ++i) {
       const int s = i & 1, ph = (i >> 1) & 1, key = (tb + t) * kQtKeys + row;
       const uint32_t stage = s * 2 * TILE;
+      // this thread's places in shared memory: its row of codes of a tile, its V scales, its weights (with several blocks of
+      // columns worked out anew in every tile: their sums need the registers)
+      int at_row = row;
+      if (NB > 1) asm volatile("" : "+r"(at_row));
+      const uint32_t sw = D == 128 ? at_row >> 1 & 3 : at_row >> 2 & 1, p_sw = (at_row >> 1 & 3) << 4;
+      const uint8_t* k_row = my_ring + at_row * (D / 2);
+      const uint32_t v_rows = smem_u32(my_ring) + TILE + (at_row & 31) * (D / 2) + ((quad ^ (D == 128 ? at_row >> 1 & 3 : at_row >> 2 & 1)) << 4);
+      uint8_t* scale_at = my_scales + (at_row >> 1 & 3) * 64 + (at_row >> 3) * 4 + (at_row & 1) * 2;
+      uint8_t* p_row = my_p + at_row * P_PITCH;
+      if (!EARLY) {
+        kn.load(p.ks + (size_t)(row0 + key) * G, key < end);
+        vn.load(p.vs + (size_t)(row0 + key) * G, key < end);
+      }
       const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
       const int ev = vn.exponent();
       // ---- K: this thread's key into its TMEM lane
       {
         const float down = pow2i(-kn.exponent()) * 0x1p14f;
-        uint32_t s0[G];
+        constexpr int KG = G / H;              // groups of 32 elements that this warpgroup unpacks
+        uint32_t s0[KG];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const float ns = kn.scale(g) * down;
+        for (int g = 0; g < KG; ++g) {
+          const float ns = kn.scale(half * KG + g) * down;
           s0[g] = pack_half2(ns, ns);
         }
         // the keys' V scales, laid out by (group, lane of a quad, key pair)
         const float vdown = pow2i(-ev) * 0x1p14f;
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-          *reinterpret_cast<__half*>(scale_at + g * 256) = __float2half_rn(vn.scale(g) * vdown);
-        const int next = key + GROUPS * kQtKeys;
-        kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
-        vn.load(p.vs + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
-        wait(&my_k_full[s], ph);
-        uint4 w[G];
+        for (int g = 0; g < KG; ++g)
+          *reinterpret_cast<__half*>(scale_at + (half * KG + g) * 256) = __float2half_rn(vn.scale(half * KG + g) * vdown);
+        if (EARLY) {
+          const int next = key + GROUPS * kQtKeys;
+          kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
+          vn.load(p.vs + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
+        }
+        wait(k_full(grp, s), ph);
+        uint4 w[KG];
 #pragma unroll
-        for (int g = 0; g < G; ++g) w[g] = *reinterpret_cast<const uint4*>(k_row + stage + ((g ^ sw) << 4));
+        for (int g = 0; g < KG; ++g) w[g] = *reinterpret_cast<const uint4*>(k_row + stage + (((half * KG + g) ^ sw) << 4));
         // (the columns' last reader was the P V before)
-        if (i > 0) wait(&pv_done[grp], (i - 1) & 1);
+        if (i > 0) wait(pv_done(grp), (i - 1) & 1);
         tc_fence_after();
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
+        for (int g = 0; g < KG; ++g) {
             const uint32_t s1 = mul_half2(s0[g], 0x2c002c00u);       // 2^-4
             const uint32_t c = mul_half2(s0[g], 0x80088008u);        // -2^-21: -8 ns 2^-10
             const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
@@ -443,43 +477,45 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
               out[4 * k + 2] = fma_half2(hi & kNibble0, s0[g], c);
               out[4 * k + 3] = fma_half2(hi & kNibble1, s1, c);
             }
-            tc_st_16cols(t_kv + lanes + 16 * g, out);
+            tc_st_16cols(t_kv + lanes + 16 * (half * KG + g), out);
         }
         tc_wait_st();
       }
       tc_fence_before();
-      named_bar(bar, 128);
+      named_bar(bar, GT);
       if (issuer && alive) {
         tc_fence_after();
         const uint32_t b_lo = desc_k(smem_u32(qbuf));
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
           tc_mma_ts_hi(lead, t_s, t_kv + 8 * ks, b_lo + ((ks >> 2) * (N * 128) + (ks & 3) * 32) / 16, kDescHi, idesc_s, ks > 0 ? 1u : 0u);
-        tc_commit(lead, &s_done[grp]);
+        tc_commit(lead, s_done(grp));
         issue_k(s);
       }
 
       // ---- V: a warp unpacks a group's 32 channels, while S runs
-      wait(&my_v_full[s], ph);
+      wait(v_full(grp, s), ph);
       {
+        constexpr int VK = NB > 1 ? 4 : 8;    // key pairs of a lane at a time (four where the sums leave few registers)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {         // 64 keys at a time
-          uint32_t w[8], sp[8];
+        for (int hh = 0; hh < 16 / (VK * H); ++hh) {
+          const int h = H == 1 ? hh : half * (16 / (VK * H)) + hh;
+          uint32_t w[VK], sp[VK];
           if (has_rows) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), v_rows + stage + (64 * h + 32 * k) * (D / 2));
-              *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(my_scales + quad * 256 + tig * 64 + 32 * h + 16 * k);
+            for (int k = 0; k < VK / 4; ++k) {
+              ldmatrix_x4_trans(*reinterpret_cast<uint32_t(*)[4]>(&w[4 * k]), v_rows + stage + (8 * VK * h + 32 * k) * (D / 2));
+              *reinterpret_cast<uint4*>(&sp[4 * k]) = *reinterpret_cast<const uint4*>(my_scales + quad * 256 + tig * 64 + 4 * VK * h + 16 * k);
             }
           }
-          if (h == 0) {
-            wait(&s_done[grp], i & 1);
+          if (hh == 0) {
+            wait(s_done(grp), i & 1);
             tc_fence_after();
           }
           if (has_rows) {
-            uint32_t lo[16], hi[16];          // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
+            uint32_t lo[2 * VK], hi[2 * VK];  // lanes 0-15: codes 0 and 1 of a unit; 16-31: codes 2 and 3
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < VK; ++k) {
               const uint32_t s0 = sp[k], s1 = mul_half2(s0, 0x2c002c00u);   // 2^-4
               const uint32_t c = mul_half2(s0, 0x80408040u);                // -2^-18: -8 ns 2^-7
               const uint32_t x = w[k] << 3, y = w[k] >> 5;
@@ -488,8 +524,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
               hi[2 * k] = fma_half2(y & 0x00780078u, s0, c);
               hi[2 * k + 1] = fma_half2(y & 0x07800780u, s1, c);
             }
-            tc_st_16x128b_8(t_kv + lanes + 32 * h, lo);
-            tc_st_16x128b_8(t_kv + lanes + 32 * h + (16u << 16), hi);
+            tc_st_16x128b(t_kv + lanes + 4 * VK * h, lo);
+            tc_st_16x128b(t_kv + lanes + 4 * VK * h + (16u << 16), hi);
           }
         }
       }
@@ -497,27 +533,24 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       // ---- softmax: this thread's key, NC query rows
       const float e = (float)ev;
       const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
-      float y[NC];
-      // (one copy of the scores' code and registers: once maxima have been raised it runs again, and only once: a
-      // row that holds a NaN may still be above the slack)
-#pragma unroll 1
-      for (int pass = 0; pass < 2; ++pass) {
-        tc_ld_cols<NC>(t_s + lanes, y);
+      float y[BC];
+      // a block of the tile's scores plus e less the running maximum, in log2 units
+      auto scores = [&](int c0, float& mx) {
+        tc_ld_cols<BC>(t_s + lanes + col0 + c0, y);
         tc_wait_ld();
 #pragma unroll
-        for (int c = 0; c < NC; c += 2) {      // the scores plus e, in log2 units
+        for (int c = 0; c < BC; c += 2) {
           const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
           y[c] = r.x;
           y[c + 1] = r.y;
         }
         if (masked) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) y[c] = key - t_unit <= qpos[c] ? y[c] : -INFINITY;
+          for (int c = 0; c < BC; ++c) y[c] = key - t_unit <= qpos[col0 + c0 + c] ? y[c] : -INFINITY;
         }
-        float mx = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NC; c += 4) {      // less the running maximum
-          const float4 m = *reinterpret_cast<const float4*>(my_nm + c);
+        for (int c = 0; c < BC; c += 4) {
+          const float4 m = *reinterpret_cast<const float4*>(my_nm + c0 + c);
           const float2 r0 = fadd2(make_float2(y[c], y[c + 1]), make_float2(m.x, m.y));
           const float2 r1 = fadd2(make_float2(y[c + 2], y[c + 3]), make_float2(m.z, m.w));
           y[c] = r0.x;
@@ -527,42 +560,52 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           mx = fmaxf(fmaxf(mx, y[c]), y[c + 1]);
           mx = fmaxf(fmaxf(mx, y[c + 2]), y[c + 3]);
         }
-        if (pass == 1 || !bar_any(bar, 128, mx > kQtSlack + kQtLift)) break;
+      };
+      // (one copy of that code for one block: once maxima have been raised it runs again, and only once: a
+      // row that holds a NaN may still be above the slack)
+#pragma unroll 1
+      for (int pass = 0; pass < 2; ++pass) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) scores(BC * nb, mx);
+        if (pass == 1 || !bar_any(bar, GT, mx > kQtSlack + kQtLift)) break;
         // ---- some row's maximum grows by more than the slack: all rows take theirs
-        int mine = 0;
 #pragma unroll 1
         for (int c = 0; c < NC; c += 8) {
           float z[8];
-          tc_ld_8(t_s + lanes + c, z);
+          int top = 0;
+          tc_ld_8(t_s + lanes + col0 + c, z);
           tc_wait_ld();
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float x = masked && key - t_unit > qpos[c + k] ? -INFINITY : fmaf(z[k], a, e);
+            const float x = masked && key - t_unit > qpos[col0 + c + k] ? -INFINITY : fmaf(z[k], a, e);
             const int r = __reduce_max_sync(0xffffffffu, ordered(x));
-            mine = lane == c + k ? r : mine;
+            top = lane == k ? r : top;
+          }
+          if (lane < 8) my_red[4 * (c + lane) + quad] = top;
+        }
+        named_bar(bar, GT);
+        if (quad == 0) {
+          for (int c = lane; c < NC; c += 32) {
+            const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * c);
+            const float top = unordered(max(max(r.x, r.y), max(r.z, r.w))), old = my_nm[c];
+            const float m = fminf(old, top == -INFINITY ? 1e30f : kQtLift - top);   // (a NaN score is passed over: its row is NaN all the same)
+            my_nm[c] = m;
+            my_alpha[c] = fast_exp2(m - old);
           }
         }
-        if (lane < NC) my_red[4 * lane + quad] = mine;
-        named_bar(bar, 128);
-        if (quad == 0 && lane < NC) {
-          const int4 r = *reinterpret_cast<const int4*>(my_red + 4 * lane);
-          const float top = unordered(max(max(r.x, r.y), max(r.z, r.w))), old = my_nm[lane];
-          const float m = fminf(old, top == -INFINITY ? 1e30f : kQtLift - top);   // (a NaN score is passed over: its row is NaN all the same)
-          my_nm[lane] = m;
-          my_alpha[lane] = fast_exp2(m - old);
-        }
-        named_bar(bar, 128);
+        named_bar(bar, GT);
 #pragma unroll
         for (int c = 0; c < NC; ++c) l[c] *= my_alpha[c];
         if (t > t_first && has_rows) {         // O holds the group's earlier tiles of the segment
 #pragma unroll 1
           for (int c = 0; c < NC; c += 8) {
             float o[8];
-            tc_ld_8(t_o + lanes + c, o);
+            tc_ld_8(t_o + lanes + col0 + c, o);
             tc_wait_ld();
 #pragma unroll
             for (int k = 0; k < 8; ++k) o[k] *= my_alpha[c + k];
-            tc_st_8(t_o + lanes + c, o);
+            tc_st_8(t_o + lanes + col0 + c, o);
           }
           tc_wait_st();
         }
@@ -570,80 +613,94 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       {
         const float el = pow2i(-ev);
 #pragma unroll
-        for (int c = 0; c < NC; c += 8) {
-          uint32_t h[4];
+        for (int nb = 0; nb < NB; ++nb) {
+          float mx = 0.f;
+          if (NB > 1) scores(BC * nb, mx);     // (a single block is still there)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float x0 = fast_exp2(y[c + 2 * k]), x1 = fast_exp2(y[c + 2 * k + 1]);
-            const float2 z = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(l[c + 2 * k], l[c + 2 * k + 1]));
-            l[c + 2 * k] = z.x;
-            l[c + 2 * k + 1] = z.y;
-            h[k] = pack_half2(x0, x1);
+          for (int c = 0; c < BC; c += 8) {
+            uint32_t h[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float* lc = l + BC * nb + c + 2 * k;
+              const float x0 = fast_exp2(y[c + 2 * k]), x1 = fast_exp2(y[c + 2 * k + 1]);
+              const float2 z = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(lc[0], lc[1]));
+              lc[0] = z.x;
+              lc[1] = z.y;
+              h[k] = pack_half2(x0, x1);
+            }
+            const int at = col0 + BC * nb + c;
+            *reinterpret_cast<uint4*>(p_row + (H == 1 ? c * 2 ^ p_sw : (at >> 5) * P_BLOCK + ((at & 31) * 2 ^ p_sw))) =
+                make_uint4(h[0], h[1], h[2], h[3]);
           }
-          *reinterpret_cast<uint4*>(p_row + (c * 2 ^ p_sw)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         tc_wait_st();
       }
       fence_proxy_async_smem();
       tc_fence_before();
-      named_bar(bar, 128);
+      named_bar(bar, GT);
       if (issuer && alive) {
         tc_fence_after();
-        const uint32_t b_lo = desc_mn(smem_u32(my_p), L::P_BYTES);
+        const uint32_t b_lo = desc_mn(smem_u32(my_p), P_BLOCK);
 #pragma unroll
         for (int ks = 0; ks < kQtKeys / 16; ++ks)
           tc_mma_ts_hi(lead, t_o, t_kv + 8 * ks, b_lo + ks * (2 * P_ATOM / 16), kPDescHi, idesc_o, t > t_first || ks > 0 ? 1u : 0u);
-        tc_commit(lead, &pv_done[grp]);
+        tc_commit(lead, pv_done(grp));
         issue_v(s);
       }
     }
 
     // ---------------------------------------------------------------- end of the segment
     job += n;
-    // the rows' sums: lane c ends with column c of this warp's keys
-    float sum[32];
+    // the rows' sums over this warp's keys: lane c ends with column 32 k + c (their maxima were read before the last barrier)
 #pragma unroll
-    for (int c = 0; c < 32; ++c) sum[c] = c < NC ? l[c < NC ? c : 0] : 0.f;
+    for (int c0 = 0; c0 < NC; c0 += 32) {
+      float sum[32];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
+      for (int c = 0; c < 32; ++c) sum[c] = c0 + c < NC ? l[c0 + c < NC ? c0 + c : 0] : 0.f;
 #pragma unroll
-      for (int k = 0; k < off; ++k) {
-        const bool upper = (lane & off) != 0;
-        const float send = upper ? sum[k] : sum[k + off], keep = upper ? sum[k + off] : sum[k];
-        sum[k] = keep + __shfl_xor_sync(0xffffffffu, send, off);
-      }
-    if (lane < NC) my_red[4 * lane + quad] = __float_as_int(sum[0]);   // (its maxima were read before the last barrier)
+      for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < off; ++k) {
+          const bool upper = (lane & off) != 0;
+          const float send = upper ? sum[k] : sum[k + off], keep = upper ? sum[k + off] : sum[k];
+          sum[k] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+        }
+      if (c0 + lane < NC) my_red[4 * (c0 + lane) + quad] = __float_as_int(sum[0]);
+    }
     // the last P V of every group that had a tile of the segment
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
       const int done = (job - g + GROUPS - 1) / GROUPS;        // its tiles so far (job - g > -GROUPS)
-      if (g + GROUPS * (done - 1) >= job - n) wait(&pv_done[g], (done - 1) & 1);
+      if (g + GROUPS * (done - 1) >= job - n) wait(pv_done(g), (done - 1) & 1);
     }
     tc_fence_after();
     __syncthreads();
-    // the groups' states merged: lane c has column c's factors
-    const int mc = lane < NC ? lane : 0;
-    float f[GROUPS], tot = 0.f, nm = nm_s[mc];
-#pragma unroll
-    for (int g = 1; g < GROUPS; ++g) nm = fminf(nm, nm_s[N * g + mc]);
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int4 r = *reinterpret_cast<const int4*>(red + 4 * (N * g + mc));
-      f[g] = fast_exp2(nm - nm_s[N * g + mc]);
-      tot += f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w)));
-    }
-    const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - nm) * kLn2;
-    const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;         // (V's 2^-7; a NaN stays one)
-    const int c_first = map.owner(unit, 0), c_last = map.owner(unit, map.tiles(unit) - 1);
-    const bool whole = c_first == c_last;
+    const int c_first = map.owner(unit, 0), n_seg = map.owner(unit, map.tiles(unit) - 1) - c_first + 1;
+    const bool whole = n_seg == 1;
     const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first), orow0 = (size_t)kv_unit * p.rows_total + row_base;
-    if ((int)blockIdx.x == c_first && tid == 0 && p.max_seg > 1) p.nseg[unit] = c_last - c_first + 1;
-    if (warp == 0 && lane < NC && lane < rows && alive) {
-      if (!whole) p.lse_part[slot * p.nq_rows + lane] = lse;
-      else if (p.lse) p.lse[orow0 + lane] = lse;
-    }
-    const int c = 8 * grp;                                     // a group's block of columns
-    if (c < NC && c < rows && has_rows && alive) {
+    if ((int)blockIdx.x == c_first && tid == 0 && p.max_seg > 1) p.nseg[unit] = n_seg;
+    const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);   // this lane's channel
+    // the groups' states merged, eight columns at a time, the blocks dealt out over the warpgroups: lane k has column c + k
+#pragma unroll 1
+    for (int c = 8 * set; c < rows; c += 32) {
+      const int mc = c + (lane & 7);
+      float f[GROUPS], tot = 0.f, nm = nm_of(0)[mc];
+#pragma unroll
+      for (int g = 1; g < GROUPS; ++g) nm = fminf(nm, nm_of(g)[mc]);
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int4 r = *reinterpret_cast<const int4*>(red_of(g) + 4 * mc);
+        f[g] = fast_exp2(nm - nm_of(g)[mc]);
+        tot += f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w)));
+      }
+      const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;       // (V's 2^-7; a NaN stays one)
+      if (!alive) continue;
+      if (quad == 0 && lane < 8 && mc < rows) {
+        const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - nm) * kLn2;
+        if (!whole) p.lse_part[slot * p.nq_rows + mc] = lse;
+        else if (p.lse) p.lse[orow0 + mc] = lse;
+      }
+      if (!has_rows) continue;
       float x[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = 0.f;
@@ -652,12 +709,11 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         const int done = (job - g + GROUPS - 1) / GROUPS;
         if (g + GROUPS * (done - 1) < job - n) continue;       // no tiles, O holds nothing
         float o[8];
-        tc_ld_8(tmem + 128 * g + 96 + lanes + c, o);
+        tc_ld_8(tmem + TM * g + 64 + N + lanes + c, o);
         tc_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = fmaf(o[k], __shfl_sync(0xffffffffu, f[g] * inv, c + k), x[k]);
+        for (int k = 0; k < 8; ++k) x[k] = fmaf(o[k], __shfl_sync(0xffffffffu, f[g] * inv, k), x[k]);
       }
-      const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);  // this lane's channel
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int r = c + k;
@@ -670,10 +726,10 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     tc_fence_before();                                         // (the next segment's barrier comes before its P V)
   }
   if (issuer && *abort_flag) {   // no copy may land in shared memory, no MMA write TMEM after the CTA exits
-    for (int k = max(0, ahead->k_issued - ST); k < ahead->k_issued; ++k) mbar_wait(&my_k_full[k % ST], (k / ST) & 1, p.status, nullptr);
-    for (int k = max(0, ahead->v_issued - ST); k < ahead->v_issued; ++k) mbar_wait(&my_v_full[k % ST], (k / ST) & 1, p.status, nullptr);
-    tc_commit(lead, &drain[grp]);
-    mbar_wait(&drain[grp], 0, p.status, nullptr);
+    for (int k = max(0, ahead->k_issued - ST); k < ahead->k_issued; ++k) mbar_wait(k_full(grp, k % ST), (k / ST) & 1, p.status, nullptr);
+    for (int k = max(0, ahead->v_issued - ST); k < ahead->v_issued; ++k) mbar_wait(v_full(grp, k % ST), (k / ST) & 1, p.status, nullptr);
+    tc_commit(lead, drain(grp));
+    mbar_wait(drain(grp), 0, p.status, nullptr);
   }
   tc_fence_before();
   __syncthreads();
@@ -752,21 +808,24 @@ struct QtInfo {
   size_t smem;
   std::atomic<uint64_t>* allowed;
 };
-template <int D, int NC>
+template <int D, int BC, int NB, int H>
 QtInfo qt_info() {
   static std::atomic<uint64_t> allowed{0};
-  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, NC>), QuantTcSmem<D>::kTotal, &allowed};
+  return {reinterpret_cast<const void*>(&quant_tc_kernel<D, BC, NB, H>), QuantTcSmem<D, BC * NB, H>::kTotal, &allowed};
 }
 template <int D>
 QtInfo qt_kernel(int rows) {
-  return rows <= 8 ? qt_info<D, 8>() : rows <= 24 ? qt_info<D, 24>() : qt_info<D, 32>();
+  return rows <= 8 ? qt_info<D, 8, 1, 1>() : rows <= 24 ? qt_info<D, 24, 1, 1>() : rows <= 32 ? qt_info<D, 32, 1, 1>()
+         : rows <= 64 ? qt_info<D, 32, 1, 2>() : qt_info<D, 8, 6, 2>();
 }
 QtInfo qt_kernel(int d, int rows) { return d == 64 ? qt_kernel<64>(rows) : qt_kernel<128>(rows); }
+
+constexpr int kQtMaxRows = 96;        // query rows of a unit
 
 }  // namespace
 
 bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
-  plan->chunks = (rows + kQtRows - 1) / kQtRows;
+  plan->chunks = (rows + kQtMaxRows - 1) / kQtMaxRows;
   plan->nq_rows = (rows + plan->chunks - 1) / plan->chunks;
   plan->smem = qt_kernel(s.head_dim, plan->nq_rows).smem;
   plan->tiles_per_unit = (int)(((long)s.t_ctx + n_q + kQtKeys - 1) / kQtKeys);
