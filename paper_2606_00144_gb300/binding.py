@@ -8,6 +8,7 @@ the library is not built, or an argument is rejected, these functions raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -281,6 +282,7 @@ class QuantCache:
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self._struct = BdQuantCache(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
         self._ref = ctypes.byref(self._struct)
+        self.is_cuda = k_codes.is_cuda
 
     @classmethod
     def empty(cls, batch, h_kv, t_cap, head_dim, device="cuda"):
@@ -298,92 +300,121 @@ class QuantCache:
         return sum(t.numel() * t.element_size() for t in (self.k_codes, self.k_scales, self.v_codes, self.v_scales))
 
 
-def _quant_cache(name, shape, cache: QuantCache):
-    if (shape.batch, shape.h_kv, shape.head_dim, shape.t_cap) != (cache.batch, cache.h_kv, cache.head_dim, cache.t_cap):
-        raise ValueError(f"{name}: the cache is not one of this shape: {shape}")
-    return cache._ref
+# The calls below are small next to a launch, so what they check is checked once, in one place, and told apart
+# (_refuse_rows, _refuse) only when something does not fit.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
-def _quant_rows(name, shape, k_rows, v_rows):
-    """dtype code, row count and strides of a write's or read's tensors [batch, h_kv, n, head_dim]."""
+@functools.lru_cache(maxsize=256)
+def _stride_array(sb, sh, sn):
+    return (ctypes.c_int64 * 3)(sb, sh, sn)
+
+
+def _refuse_cache(name, shape):
+    raise ValueError(f"{name}: the cache is not one of this shape: {shape}")
+
+
+def _refuse_rows(name, want, dtype, t):
+    if t.shape != want:
+        raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim] = {want}, got {tuple(t.shape)}")
+    if t.dtype is not dtype or dtype not in (_BF16, _F32):
+        raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    raise ValueError(f"{name}: the rows and the cache must be on the GPU")
+
+
+def _quant_rows(name, shape, cache, k_rows, v_rows):
+    """Checks a write's or read's cache and tensors [batch, h_kv, n, head_dim]: n, the dtype's code, the tensors'
+    pointers and strides (None where they are dense)."""
     first = k_rows if k_rows is not None else v_rows
     if first is None:
         raise ValueError(f"{name}: K rows, V rows or both")
-    dtype = BD_DTYPE_BF16 if first.dtype is torch.bfloat16 else BD_DTYPE_F32
-    n = int(first.shape[2]) if first.dim() == 4 else -1
-    strides = []
+    b, h, d = shape.batch, shape.h_kv, shape.head_dim
+    if not (b == cache.batch and h == cache.h_kv and d == cache.head_dim and shape.t_cap == cache.t_cap):
+        _refuse_cache(name, shape)
+    dtype = first.dtype
+    want = (b, h, first.shape[2] if first.dim() == 4 else -1, d)
+    out = []
     for t in (k_rows, v_rows):
         if t is None:
-            strides.append(None)
+            out += None, None
             continue
-        if t.shape != (shape.batch, shape.h_kv, n, shape.head_dim):
-            raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim], got {tuple(t.shape)}")
-        if t.dtype is not first.dtype or t.dtype not in (torch.bfloat16, torch.float32):
-            raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
+        if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.is_cuda and cache.is_cuda
+                and (t.is_contiguous() or t.stride(3) == 1)):
+            _refuse_rows(name, want, dtype, t)
         if t.is_contiguous():
-            strides.append(None)
+            out += t.data_ptr(), None
             continue
-        st = t.stride()
-        if st[3] != 1:
-            raise ValueError(f"{name}: the elements of a row must be adjacent")
-        strides.append((ctypes.c_int64 * 3)(*st[:3]))
-    return n, dtype, strides
+        out += t.data_ptr(), _stride_array(*t.stride()[:3])
+    return want[2], BD_DTYPE_BF16 if dtype is _BF16 else BD_DTYPE_F32, out
 
 
-def _dense(name, what, t, dtype, shape):
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: {what} must be a contiguous {tuple(shape)} tensor, got {tuple(t.shape)}")
+def _refuse(name, **tensors):
+    for what, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
+        if t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: {what} must be a contiguous {shape} tensor, got {tuple(t.shape)}")
+        if not t.is_cuda:
+            raise ValueError(f"{name}: {what} must be on the GPU")
+    raise ValueError(f"{name}: the cache must be on the GPU")
+
+
+def _quant_attn(name, shape, cache, q, o_out, lse_out, want):
+    """Checks the cache, the queries and the outputs of an attention; want: the queries' shape."""
+    if not (shape.batch == cache.batch and shape.h_kv == cache.h_kv and shape.head_dim == cache.head_dim
+            and shape.t_cap == cache.t_cap):
+        _refuse_cache(name, shape)
+    if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
+            and o_out.is_contiguous() and q.is_cuda and o_out.is_cuda and cache.is_cuda
+            and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
+                                     and lse_out.is_cuda))):
+        _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]))
 
 
 def bd_quant_write(shape, k_rows, v_rows, cache: QuantCache, stream=None):
     """Quantises rows [batch, h_kv, n, head_dim] (bf16 or fp32; any strides of whole 16 bytes; either may
     be None) into the cache, behind the context (each sequence's length, if the shape has lengths)."""
-    n, dtype, (ks, vs) = _quant_rows("bd_quant_write", shape, k_rows, v_rows)
-    st = library().bd_quant_write(ctypes.byref(shape), n, dtype, _ptr(k_rows), ks, _ptr(v_rows), vs,
-                                  _quant_cache("bd_quant_write", shape, cache), _stream(stream))
+    n, dtype, (k, ks, v, vs) = _quant_rows("bd_quant_write", shape, cache, k_rows, v_rows)
+    st = library().bd_quant_write(ctypes.byref(shape), n, dtype, k, ks, v, vs, cache._ref, _stream(stream))
     _check("bd_quant_write", st)
 
 
 def bd_quant_read(shape, cache: QuantCache, k_out, v_out=None, first_row=None, stream=None):
     """Reads the cache's rows first_row .. first_row + n - 1 (None: those behind the context) into
     [batch, h_kv, n, head_dim] tensors, bf16 or fp32; either may be None."""
-    n, dtype, (ks, vs) = _quant_rows("bd_quant_read", shape, k_out, v_out)
-    if first_row is not None and first_row < 0:
+    n, dtype, (k, ks, v, vs) = _quant_rows("bd_quant_read", shape, cache, k_out, v_out)
+    if first_row is None:
+        first_row = BD_QUANT_BLOCK_ROWS
+    elif first_row < 0:
         raise ValueError("bd_quant_read: first_row must not be negative")
-    st = library().bd_quant_read(ctypes.byref(shape), BD_QUANT_BLOCK_ROWS if first_row is None else int(first_row), n,
-                                 dtype, _quant_cache("bd_quant_read", shape, cache), _ptr(k_out), ks, _ptr(v_out), vs,
-                                 _stream(stream))
+    st = library().bd_quant_read(ctypes.byref(shape), first_row, n, dtype, cache._ref, k, ks, v, vs, _stream(stream))
     _check("bd_quant_read", st)
 
 
 def bd_quant_draft_attn(shape, q, cache: QuantCache, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
                         stream=None, flags=0):
     """bd_draft_attn over a 4-bit cache."""
-    name = "bd_quant_draft_attn"
-    _dense(name, "q", q, torch.bfloat16, (shape.batch, shape.h_q, shape.head_dim))
-    _dense(name, "o_out", o_out, torch.bfloat16, q.shape)
-    _dense(name, "idx", idx, torch.int32, (shape.batch, shape.h_kv, int(budget)))
-    _dense(name, "count", count, torch.int32, (shape.batch, shape.h_kv))
-    if lse_out is not None:
-        _dense(name, "lse_out", lse_out, torch.float32, q.shape[:2])
-    st = library().bd_quant_draft_attn(ctypes.byref(shape), _ptr(q), _quant_cache(name, shape, cache), _ptr(idx),
-                                       _ptr(count), int(budget), int(step_j), int(flags), _ptr(o_out), _ptr(lse_out),
-                                       ws.ptr, ws.nbytes, _stream(stream))
-    _check(name, st)
+    _quant_attn("bd_quant_draft_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, shape.head_dim))
+    units = (cache.batch, cache.h_kv)
+    if not (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (*units, budget) and count.shape == units
+            and idx.is_contiguous() and count.is_contiguous() and idx.is_cuda and count.is_cuda):
+        _refuse("bd_quant_draft_attn", idx=(idx, _I32, (*units, budget)), count=(count, _I32, units))
+    st = library().bd_quant_draft_attn(ctypes.byref(shape), q.data_ptr(), cache._ref, idx.data_ptr(), count.data_ptr(),
+                                       budget, step_j, flags, o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes,
+                                       _stream(stream))
+    _check("bd_quant_draft_attn", st)
 
 
 def bd_quant_verify_attn(shape, q, n_q, cache: QuantCache, o_out, lse_out, ws: Workspace, stream=None):
     """bd_verify_attn over a 4-bit cache; n_q = 1 decodes one token."""
-    name = "bd_quant_verify_attn"
-    _dense(name, "q", q, torch.bfloat16, (shape.batch, shape.h_q, int(n_q), shape.head_dim))
-    _dense(name, "o_out", o_out, torch.bfloat16, q.shape)
-    if lse_out is not None:
-        _dense(name, "lse_out", lse_out, torch.float32, q.shape[:3])
-    st = library().bd_quant_verify_attn(ctypes.byref(shape), _ptr(q), int(n_q), _quant_cache(name, shape, cache),
-                                        _ptr(o_out), _ptr(lse_out), ws.ptr, ws.nbytes, _stream(stream))
-    _check(name, st)
+    _quant_attn("bd_quant_verify_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, n_q, shape.head_dim))
+    st = library().bd_quant_verify_attn(ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, o_out.data_ptr(), _ptr(lse_out),
+                                        ws.ptr, ws.nbytes, _stream(stream))
+    _check("bd_quant_verify_attn", st)
 
 
 def bd_check_wait_timeout(ws: Workspace, limit_us: int, stream=None):

@@ -194,3 +194,19 @@ def test_the_binding_refuses_tensors_that_do_not_fit(lib):
         bd.bd_quant_draft_attn(s, q[:, :, 0].contiguous(), c, idx, count, 9, 0, q[:, :, 0].contiguous(), None, ws)
     with pytest.raises(TypeError):
         bd.bd_quant_draft_attn(s, q[:, :, 0].contiguous(), c, idx.long(), count, 8, 0, q[:, :, 0].contiguous(), None, ws)
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_the_gpu(lib):
+    """All of them fit but for where they are: no call reaches the library with a host pointer."""
+    c = cpu_cache()
+    s = c.shape(4, 10)
+    rows = torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
+    ws = type("W", (), dict(ptr=A, nbytes=1 << 30))()
+    q, lse = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), torch.zeros(2, 4, 3)
+    q1 = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    idx, count = torch.zeros(2, 2, 8, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)
+    for call in (lambda: bd.bd_quant_write(s, rows, rows, c), lambda: bd.bd_quant_read(s, c, rows, None, first_row=0),
+                 lambda: bd.bd_quant_verify_attn(s, q, 3, c, q, lse, ws),
+                 lambda: bd.bd_quant_draft_attn(s, q1, c, idx, count, 8, 0, q1, None, ws)):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call()
