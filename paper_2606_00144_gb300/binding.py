@@ -314,13 +314,14 @@ def _refuse_cache(name, shape):
     raise ValueError(f"{name}: the cache is not one of this shape: {shape}")
 
 
-def _refuse_rows(name, want, dtype, t):
-    if t.shape != want:
-        raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim] = {want}, got {tuple(t.shape)}")
-    if t.dtype is not dtype or dtype not in (_BF16, _F32):
-        raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
-    if t.stride(3) != 1:
-        raise ValueError(f"{name}: the elements of a row must be adjacent")
+def _refuse_rows(name, want, dtype, *rows):
+    for t in (x for x in rows if x is not None):
+        if t.shape != want:
+            raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim] = {want}, got {tuple(t.shape)}")
+        if t.dtype is not dtype or dtype not in (_BF16, _F32):
+            raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
+        if not t.is_contiguous() and t.stride(3) != 1:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
     raise ValueError(f"{name}: the rows and the cache must be on the GPU")
 
 
@@ -342,7 +343,7 @@ def _quant_rows(name, shape, cache, k_rows, v_rows):
             continue
         if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.is_cuda and cache.is_cuda
                 and (t.is_contiguous() or t.stride(3) == 1)):
-            _refuse_rows(name, want, dtype, t)
+            _refuse_rows(name, want, dtype, k_rows, v_rows)
         if t.is_contiguous():
             out += t.data_ptr(), None
             continue
