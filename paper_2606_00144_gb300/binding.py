@@ -353,27 +353,28 @@ def _quant_rows(name, shape, cache, k_rows, v_rows):
 
 def _refuse(name, **tensors):
     for what, (t, dtype, shape) in tensors.items():
-        if t is None:
-            continue
-        if t.dtype is not dtype:
+        if t is not None and t.dtype is not dtype:
             raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
-        if t.shape != shape or not t.is_contiguous():
+        if t is not None and (t.shape != shape or not t.is_contiguous()):
             raise ValueError(f"{name}: {what} must be a contiguous {shape} tensor, got {tuple(t.shape)}")
-        if not t.is_cuda:
-            raise ValueError(f"{name}: {what} must be on the GPU")
-    raise ValueError(f"{name}: the cache must be on the GPU")
+    raise ValueError(f"{name}: every tensor must be on the GPU")
 
 
-def _quant_attn(name, shape, cache, q, o_out, lse_out, want):
-    """Checks the cache, the queries and the outputs of an attention; want: the queries' shape."""
+def _quant_attn(name, shape, cache, q, o_out, lse_out, want, idx=None, count=None, budget=0):
+    """Checks the cache, the queries, the outputs and a drafter pass's view; want: the queries' shape."""
     if not (shape.batch == cache.batch and shape.h_kv == cache.h_kv and shape.head_dim == cache.head_dim
             and shape.t_cap == cache.t_cap):
         _refuse_cache(name, shape)
+    units = (cache.batch, cache.h_kv)
     if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
             and o_out.is_contiguous() and q.is_cuda and o_out.is_cuda and cache.is_cuda
             and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
-                                     and lse_out.is_cuda))):
-        _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]))
+                                     and lse_out.is_cuda))
+            and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (*units, budget)
+                                 and count.shape == units and idx.is_contiguous() and count.is_contiguous()
+                                 and idx.is_cuda and count.is_cuda))):
+        _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]),
+                idx=(idx, _I32, (*units, budget)), count=(count, _I32, units))
 
 
 def bd_quant_write(shape, k_rows, v_rows, cache: QuantCache, stream=None):
@@ -399,11 +400,8 @@ def bd_quant_read(shape, cache: QuantCache, k_out, v_out=None, first_row=None, s
 def bd_quant_draft_attn(shape, q, cache: QuantCache, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
                         stream=None, flags=0):
     """bd_draft_attn over a 4-bit cache."""
-    _quant_attn("bd_quant_draft_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, shape.head_dim))
-    units = (cache.batch, cache.h_kv)
-    if not (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (*units, budget) and count.shape == units
-            and idx.is_contiguous() and count.is_contiguous() and idx.is_cuda and count.is_cuda):
-        _refuse("bd_quant_draft_attn", idx=(idx, _I32, (*units, budget)), count=(count, _I32, units))
+    _quant_attn("bd_quant_draft_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, shape.head_dim), idx, count,
+                budget)
     st = library().bd_quant_draft_attn(ctypes.byref(shape), q.data_ptr(), cache._ref, idx.data_ptr(), count.data_ptr(),
                                        budget, step_j, flags, o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes,
                                        _stream(stream))
