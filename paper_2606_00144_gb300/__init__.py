@@ -45,4 +45,4 @@ from .binding import (  # noqa: F401
 )
 from .build import LIB_PATH, build  # noqa: F401
 from .hostio import HostStepIO  # noqa: F401
-from .step import SpecStep  # noqa: F401
+from .step import QuantSpecStep, SpecStep  # noqa: F401

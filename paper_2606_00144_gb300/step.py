@@ -22,7 +22,7 @@ class SpecStep:
         self.shape = B.make_shape(batch, h_q, h_kv, head_dim, t_ctx, t_cap, seq_lens)
         self.budget, self.n_sink, self.n_recent = budget, n_sink, n_recent
         self.window, self.gamma, self.chunk = window, gamma, chunk
-        self.ws = B.Workspace.for_step(self.shape, budget, window, gamma, device)
+        self.ws = self._workspace(device)
         dev = torch.device(device)
         self.idx = torch.empty(batch, h_kv, budget, dtype=torch.int32, device=dev)
         self.count = torch.empty(batch, h_kv, dtype=torch.int32, device=dev)
@@ -30,6 +30,9 @@ class SpecStep:
         self.draft_lse = torch.empty(gamma, batch, h_q, dtype=torch.float32, device=dev)
         self.verify_o = torch.empty(batch, h_q, gamma + 1, head_dim, dtype=torch.bfloat16, device=dev)
         self.verify_lse = torch.empty(batch, h_q, gamma + 1, dtype=torch.float32, device=dev)
+
+    def _workspace(self, device):
+        return B.Workspace.for_step(self.shape, self.budget, self.window, self.gamma, device)
 
     def bind_outputs(self, idx, count, draft_o, draft_lse, verify_o, verify_lse):
         """Directs the following calls' results into these tensors (same shapes and dtypes as
@@ -105,3 +108,59 @@ class SpecStep:
         ws = B.Workspace(size, k_cache.device, units=s.batch * s.h_kv if size > 1 << 20 else None)
         B.bd_verify_attn(sh, q_win, self.window, k_cache, None, None, out, ws, stream)
         return out
+
+
+class QuantSpecStep(SpecStep):
+    """A step over a 4-bit cache (QuantCache) of one layer: bd_quant_write for new rows, bd_quant_draft_attn and
+    bd_quant_verify_attn in place of the bf16 attentions.
+
+    The selection and the window's normalisers rank keys on the tensor cores as bf16: the context's keys are
+    read back (bd_quant_read) into one bf16 buffer [batch, h_kv, t_cap, head_dim], made at the first such call
+    and shared by every layer that the object serves."""
+
+    def __init__(self, *args, **kw):
+        self._keys = None
+        super().__init__(*args, **kw)
+
+    def _workspace(self, device):
+        s = self.shape
+        sizes = [B.bd_workspace_size(s, B.BD_OP_SELECT, self.budget, self.window),
+                 B.bd_workspace_size(s, B.BD_OP_QUANT_DRAFT, self.budget, self.gamma),
+                 B.bd_workspace_size(s, B.BD_OP_QUANT_VERIFY, 0, self.gamma + 1)]
+        if min(sizes[1:]) == 0:
+            raise B.BudgetDraftError("bd_workspace_size", -1)
+        return B.Workspace(max(sizes), device)
+
+    def keys(self, cache, stream=None):
+        """The context's keys as bf16, in the step's own buffer (rows past t_ctx are not read)."""
+        s = self.shape
+        if self._keys is None:
+            self._keys = torch.empty(s.batch, s.h_kv, s.t_cap, s.head_dim, dtype=torch.bfloat16,
+                                     device=cache.k_codes.device)
+            if stream is not None:
+                self._keys.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+        B.bd_quant_read(s, cache, self._keys[:, :, :s.t_ctx], first_row=0, stream=stream)
+        return self._keys
+
+    def write(self, k_rows, v_rows, cache, stream=None):
+        """Quantises the block's rows [batch, h_kv, n, head_dim] into the cache, behind the context."""
+        B.bd_quant_write(self.shape, k_rows, v_rows, cache, stream)
+
+    def select(self, cache, q_win, window_lse=None, stream=None, window_ready=False):
+        super().select(self.keys(cache, stream), q_win, window_lse, stream, window_ready)
+
+    def draft(self, j, q_j, cache, stream=None, view_ready=False):
+        B.bd_quant_draft_attn(self.shape, q_j, cache, self.idx, self.count, self.budget, j, self.draft_o[j],
+                              self.draft_lse[j], self.ws, stream, flags=B.BD_DRAFT_VIEW_READY if view_ready else 0)
+
+    def verify(self, q_verify, cache, stream=None):
+        B.bd_quant_verify_attn(self.shape, q_verify, self.gamma + 1, cache, self.verify_o, self.verify_lse, self.ws, stream)
+
+    def run(self, cache, q_win, q_draft, q_verify, window_lse=None, stream=None):
+        self.select(cache, q_win, window_lse, stream)
+        for j in range(self.gamma):
+            self.draft(j, q_draft[j], cache, stream, view_ready=j > 0)
+        self.verify(q_verify, cache, stream)
+
+    def window_lse(self, cache, q_win, out=None, stream=None):
+        return super().window_lse(self.keys(cache, stream), q_win, out, stream)
