@@ -187,13 +187,6 @@ __device__ __forceinline__ int quant_tc_context(const int32_t* seq_lens, int b, 
   return t;
 }
 
-// Where a warpgroup's loads are: the segment of the next one (its unit, first tile and tiles, the CTA's tiles before it),
-// the loads made, and the place of each stage's tile.
-struct Ahead {
-  int unit, job, n, tb, k_issued, v_issued;
-  int v_unit[kQtStages], v_key[kQtStages];
-};
-
 // A thread's columns of query rows: NB blocks of BC.
 template <int D, int BC, int NB, int H>
 __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_constant__ QuantTcParams p,
@@ -267,62 +260,35 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
   bool alive = true;      // false once a wait gave up
 
-  // ---- the group's loads, by one of its warps (another SMSP's in each): local tile i is job grp + GROUPS i of
-  // the CTA's list of tiles; the list is walked ahead of the work, across segments.
-  const bool issuer = quad == grp && half == 0;
+  // ---- the group's MMAs and its loads are started by a warp each (other groups' on other SMSPs).  Local tile i is job
+  // grp + GROUPS i of the CTA's list of tiles.
+  const bool issuer = quad == grp && half == 0, loader = quad == (grp ^ 2) && half == H - 1;
   const uint32_t lead = elect_leader();
   uint8_t* mine = groups + grp * L::GROUP;
   uint8_t* my_ring = mine + L::CODES;
-  Ahead* ahead = reinterpret_cast<Ahead*>(mine + 64 + 8 * (2 * ST));                // (in shared memory: it is the issuing warp's alone and seldom used)
-  if (issuer) {
-    if (lane == 0) *ahead = Ahead{u_first - 1, 0, 0, 0, 0, 0, {}, {}};
-    __syncwarp();
-  }
-  // K of the next tile, if there is one, into stage s; then the V of the tile there
-  auto issue_k = [&](int s) {
-    Ahead st = *ahead;
-    const int j = grp + GROUPS * st.k_issued;
-    while (j >= st.job + st.n && st.unit < u_last) {
-      st.job += st.n;
-      ++st.unit;
-      st.tb = map.first_tile(st.unit, v0);
-      st.n = max(0, map.end_tile(st.unit, v1) - st.tb);
+  int* issued = reinterpret_cast<int*>(mine + 128);        // K's, V's loads so far (for a CTA that gives up)
+  // Job j's K or V into stage s: u is a unit of the list, its segment the tiles tb, .. of which the first is job `from`;
+  // j lies in it or, seldom, further on.
+  auto load = [&](int which, int s, int j, int u, int kv_unit, int tb, int n, int from) {
+    while (j >= from + n) {
+      if (u >= u_last) return;
+      from += n;
+      ++u;
+      kv_unit = u / p.row_chunks;
+      tb = map.first_tile(u, v0);
+      n = max(0, map.end_tile(u, v1) - tb);
     }
-    const bool found = j < st.job + st.n;
-    const int unit = st.unit / p.row_chunks, key = (st.tb + j - st.job) * kQtKeys;
-    if (found && lead) {
-      mbar_arrive_expect_tx(k_full(grp, s), TILE);
-      tma_load_3d(my_ring + s * 2 * TILE, &kmap, k_full(grp, s), 0, key, unit);
-    }
-    __syncwarp();
-    if (lane == 0) {
-      ahead->unit = st.unit;
-      ahead->job = st.job;
-      ahead->n = st.n;
-      ahead->tb = st.tb;
-      ahead->k_issued = st.k_issued + found;
-      ahead->v_unit[s] = unit;
-      ahead->v_key[s] = key;
-    }
-    __syncwarp();
-  };
-  auto issue_v = [&](int s) {
-    const int v_issued = ahead->v_issued;
-    if (v_issued >= ahead->k_issued) return;
     if (lead) {
-      mbar_arrive_expect_tx(v_full(grp, s), TILE);
-      tma_load_3d(my_ring + s * 2 * TILE + TILE, &vmap, v_full(grp, s), 0, ahead->v_key[s], ahead->v_unit[s]);
+      uint64_t* full = which ? v_full(grp, s) : k_full(grp, s);
+      mbar_arrive_expect_tx(full, TILE);
+      tma_load_3d(my_ring + (2 * s + which) * TILE, which ? &vmap : &kmap, full, 0, (tb + j - from) * kQtKeys, kv_unit);
+      issued[which] = j / GROUPS + 1;
     }
-    __syncwarp();
-    if (lane == 0) ahead->v_issued = v_issued + 1;
-    __syncwarp();
   };
-  if (issuer) {
-#pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      issue_k(s);
-      issue_v(s);
-    }
+  if (loader) {
+    if (lead) issued[0] = issued[1] = 0;
+#pragma unroll 1
+    for (int k = 0; k < 2 * ST; ++k) load(k & 1, k >> 1, grp + GROUPS * (k >> 1), u_first - 1, 0, 0, 0, 0);
   }
 
   const int row = quad * 32 + lane, tig = lane & 3;   // this thread's key of a tile
@@ -490,8 +456,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         for (int ks = 0; ks < D / 16; ++ks)
           tc_mma_ts_hi(lead, t_s, t_kv + 8 * ks, b_lo + ((ks >> 2) * (N * 128) + (ks & 3) * 32) / 16, kDescHi, idesc_s, ks > 0 ? 1u : 0u);
         tc_commit(lead, s_done(grp));
-        issue_k(s);
       }
+      if (loader) load(0, s, job + t + GROUPS * ST, unit, kv_unit, tb, n, job);
 
       // ---- V: a warp unpacks a group's 32 channels, while S runs
       wait(v_full(grp, s), ph);
@@ -645,8 +611,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         for (int ks = 0; ks < kQtKeys / 16; ++ks)
           tc_mma_ts_hi(lead, t_o, t_kv + 8 * ks, b_lo + ks * (2 * P_ATOM / 16), kPDescHi, idesc_o, t > t_first || ks > 0 ? 1u : 0u);
         tc_commit(lead, pv_done(grp));
-        issue_v(s);
       }
+      if (loader) load(1, s, job + t + GROUPS * ST, unit, kv_unit, tb, n, job);
     }
 
     // ---------------------------------------------------------------- end of the segment
@@ -725,11 +691,15 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     }
     tc_fence_before();                                         // (the next segment's barrier comes before its P V)
   }
-  if (issuer && *abort_flag) {   // no copy may land in shared memory, no MMA write TMEM after the CTA exits
-    for (int k = max(0, ahead->k_issued - ST); k < ahead->k_issued; ++k) mbar_wait(k_full(grp, k % ST), (k / ST) & 1, p.status, nullptr);
-    for (int k = max(0, ahead->v_issued - ST); k < ahead->v_issued; ++k) mbar_wait(v_full(grp, k % ST), (k / ST) & 1, p.status, nullptr);
-    tc_commit(lead, drain(grp));
-    mbar_wait(drain(grp), 0, p.status, nullptr);
+  if (*abort_flag) {   // no copy may land in shared memory, no MMA write to TMEM after the CTA exits
+    if (loader)
+      for (int w = 0; w < 2; ++w)
+        for (int k = max(0, issued[w] - ST); k < issued[w]; ++k)
+          mbar_wait(w ? v_full(grp, k % ST) : k_full(grp, k % ST), (k / ST) & 1, p.status, nullptr);
+    if (issuer) {
+      tc_commit(lead, drain(grp));
+      mbar_wait(drain(grp), 0, p.status, nullptr);
+    }
   }
   tc_fence_before();
   __syncthreads();
