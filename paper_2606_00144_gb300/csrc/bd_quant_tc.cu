@@ -14,10 +14,11 @@
 // Four warpgroups take the tiles in turn, each through the whole chain with buffers of its own: unpack K, start S,
 // unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
 // warps, with two buffers between them) left every warp a chain of waits: 1700 cycles a tile, of which its work
-// was 600.  As it is a tile takes 1200 cycles of an SM's 740 issue slots each (64 units of 16K, 24 rows: 48 us).
+// was 600.  As it is a tile takes 1200 cycles of an SM, of which each scheduler issues in 740 (64 units of 16K, 24 rows:
+// 44.2 us, 3.4 TB/s; one row 37.3 us, 4.1 TB/s).
 // Blocks of more than 32 query rows run on two groups of two warpgroups: those share a tile's unpacking and halve its
-// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 68 -> 53 us; 64
-// units, 64 rows 66 us, 84 rows 88).
+// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 49.6 us, 68 on
+// four groups; 64 units, 64 rows 69 us, 84 rows 84).
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
 #include <algorithm>
@@ -285,11 +286,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       issued[which] = j / GROUPS + 1;
     }
   };
-  if (loader) {
-    if (lead) issued[0] = issued[1] = 0;
-#pragma unroll 1
-    for (int k = 0; k < 2 * ST; ++k) load(k & 1, k >> 1, grp + GROUPS * (k >> 1), u_first - 1, 0, 0, 0, 0);
-  }
+  if (loader && lead) issued[0] = issued[1] = 0;
 
   const int row = quad * 32 + lane, tig = lane & 3;   // this thread's key of a tile
   const int col0 = half * NC;                         // and its columns of query rows
@@ -340,6 +337,10 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         w[k] = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows) w[k] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)kv_unit * p.rows_total + row_base + r) * D + 8 * c));
       }
+      if (job == 0 && loader) {                // the first tiles, while the queries and scales arrive
+#pragma unroll 1
+        for (int k = 0; k < 2 * ST; ++k) load(k & 1, k >> 1, grp + GROUPS * (k >> 1), unit, kv_unit, tb, n, 0);
+      }
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
         const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         }
       }
       top = __reduce_max_sync(0xffffffffu, top);
-      __syncthreads();                         // (the segment before has read its own)
+      if (job > 0) __syncthreads();            // (the segment before has read its own)
       if (lane == 0) qtop[warp] = (int)top;
       if (tid < N) qpos[tid] = tid < rows ? (row_base + tid) % p.n_q : 0x7fffffff;
       if (tid < N)
@@ -800,7 +801,9 @@ bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
   plan->smem = qt_kernel(s.head_dim, plan->nq_rows).smem;
   plan->tiles_per_unit = (int)(((long)s.t_ctx + n_q + kQtKeys - 1) / kQtKeys);
   const long units = (long)s.batch * s.h_kv * plan->chunks, ctas = std::max(1, current_sm_count());
-  const int tpu = plan->tiles_per_unit, a = 6;
+  // a: what a segment's start and end cost, in tiles (3, 6, 8, 11: 64 units of 16K, 24 rows 47.7, 46.5, 46.3, 46.0 us; 64
+  // units of 4K 24.1, 22.9, 22.5, 22.6)
+  const int tpu = plan->tiles_per_unit, a = 8;
   const long vtotal = units * (tpu + a);
   if (vtotal >= (1L << 31)) return false;
   long vtpc = (vtotal + ctas - 1) / ctas;
