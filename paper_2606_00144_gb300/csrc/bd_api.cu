@@ -218,7 +218,7 @@ size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
     case BD_OP_QUANT_DRAFT: {
       const int g = s.h_q / s.h_kv;
       QuantAttnPlan qp;
-      if (n_q < 1 || budget < 1 || !group_supported_by_draft(g) || !quant_attn_plan(s, g, (long)budget + n_q, &qp)) return 0;
+      if (n_q < 1 || budget < 1 || !group_supported_by_draft(g) || !quant_attn_plan(s, g, (long)budget + n_q, true, &qp)) return 0;
       return ws_region_offset(units) + quant_attn_bytes(s, g, qp);
     }
     case BD_OP_QUANT_VERIFY: {
@@ -485,7 +485,7 @@ int bd_quant_draft_attn(const bd_shape* shape, const void* q, const bd_quant_cac
   const int g = s.h_q / s.h_kv, units = s.batch * s.h_kv;
   QuantAttnPlan qp;
   if (!group_supported_by_draft(g) || (long long)budget + step_j >= (1LL << 30) ||
-      !quant_attn_plan(s, g, (long)budget + step_j + 1, &qp))
+      !quant_attn_plan(s, g, (long)budget + step_j + 1, true, &qp))
     return BD_ERR_UNSUPPORTED;
   if (!ws) return BD_ERR_WORKSPACE;
   if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;

@@ -194,8 +194,8 @@ struct QuantAttnPlan {
   int cluster, clusters;   // CTAs of a cluster, clusters of a unit
   int most_clusters;    // the most that any number of entries takes
 };
-// entries: the most that a unit attends to
-bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* plan);
+// entries: the most that a unit attends to; gather: they come from a view
+bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, QuantAttnPlan* plan);
 // Op region for any number of entries with this many query rows.
 size_t quant_attn_bytes(const bd_shape& s, int rows, const QuantAttnPlan& plan);
 cudaError_t launch_quant_attn(const bd_shape& s, const QuantAttnPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,

@@ -18,10 +18,11 @@
 // M is a running maximum of S + e that may trail by 2^8; each warp keeps its own, and the warps, then the CTAs
 // of a unit, are merged at the end.
 //
-// A pass is a chain of latencies, not bandwidth (64 units of 512 entries read 5 MB), so as few round trips as there are:
-// the view's first indices are fetched beside its count, every warp has a tile or two, and the CTAs of a unit are a
-// cluster that meets in the shared memory of its first (long views of few units: several clusters, whose parts the last
-// to arrive merges from global memory, in order).  ISSUED
+// A pass is a chain of latencies, not bandwidth (64 units of 512 entries read 5 MB, 0.7 us of HBM), so as few round trips as
+// there are: the view's first indices are fetched beside its count, every warp has a tile or two, and the CTAs of a unit
+// are a cluster that meets in shared memory (long views of few units: several clusters, whose parts the last CTA to
+// arrive merges from global memory, in order).  64 units of 512 entries take 6.8 us, of 2048 13.7, 16 of 2048 9.1, 2 of 256
+// (d 64) 3.5.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -80,8 +81,10 @@ struct QaSmem {
   static constexpr size_t kRing = (size_t)WARPS * kStages * QaStage<D>::BYTES;
   static constexpr size_t kMerge = (size_t)WARPS * 8 * NT * (D + 4 + 2) * 4;
   static constexpr size_t kArea = kRing > kMerge ? kRing : kMerge;
-  static constexpr size_t kSlot = (size_t)8 * NT * (D + 1) * 4;      // a CTA's part in the cluster's first
-  static size_t bytes(int cluster) { return kArea + (cluster > 1 ? cluster * kSlot : 0); }
+  // A cluster's parts: CTA k merges rows k, k + cluster, ... of every CTA, so that the slots of all are little more than
+  // one CTA's rows (all of them in the first CTA took 33 (66) KB of each, which halved the CTAs of an SM).
+  __host__ __device__ static constexpr int slot_rows(int cluster) { return (8 * NT + cluster - 1) / cluster; }
+  static size_t bytes(int cluster) { return kArea + (cluster > 1 ? (size_t)cluster * slot_rows(cluster) * (D + 1) * 4 : 0); }
 };
 
 __device__ __forceinline__ int quant_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
@@ -438,17 +441,12 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
   __syncthreads();
   const size_t out0 = (size_t)unit * p.rows + row0;
   const int C = p.cluster, part = split / C;
-  float* slots = reinterpret_cast<float*>(smem + QaSmem<D, NT, WARPS>::kArea);   // [C][NQC][D], then [C][NQC] lse (in the first CTA)
-  float* lses = slots + (size_t)C * NQC * D;
+  const int slot_rows = QaSmem<D, NT, WARPS>::slot_rows(C);
+  float* slots = reinterpret_cast<float*>(smem + QaSmem<D, NT, WARPS>::kArea);   // [C][slot_rows][D], then [C][slot_rows] lse
+  float* lses = slots + (size_t)C * slot_rows * D;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = C > 1 ? (int)cluster.block_rank() : 0;
-  float* my_slot = slots + (size_t)rank * NQC * D;
-  float* my_lse = lses + rank * NQC;
-  if (C > 1) {
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");           // every CTA is running
-    my_slot = cluster.map_shared_rank(my_slot, 0);
-    my_lse = cluster.map_shared_rank(my_lse, 0);
-  }
+  if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA is running
   // a row's final values, or with several clusters its part's
   auto emit = [&](int r, int d, float4 a, float lse) {
     if (p.clusters == 1) {
@@ -484,28 +482,29 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     if (C == 1) {
       emit(r, d, a, lse);
     } else {
-      *reinterpret_cast<float4*>(my_slot + r * D + d) = a;
-      if (d == 0) my_lse[r] = lse;
+      const int to = r % C, at = rank * slot_rows + r / C;
+      *reinterpret_cast<float4*>(cluster.map_shared_rank(slots + (size_t)at * D + d, to)) = a;
+      if (d == 0) *cluster.map_shared_rank(lses + at, to) = lse;
     }
   }
   if (C > 1) {
-    // ---------------------------------------------------------------- the cluster's parts, in its first CTA
-    cluster.sync();                            // all parts have landed
-    if (rank != 0) return;
-    for (int i = tid; i < rows * (D / 4); i += kQaThreads) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4;
+    // ---------------------------------------------------------------- the cluster's parts of this CTA's rows
+    cluster.sync();                            // all have landed
+    for (int i = tid; i < slot_rows * (D / 4); i += kQaThreads) {
+      const int at = i / (D / 4), r = at * C + rank, d = i % (D / 4) * 4;
+      if (r >= rows) break;
       float ls[kQaCluster], mx = -INFINITY, tot = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kQaCluster; ++k) {
-        ls[k] = k < C ? lses[k * NQC + r] : -INFINITY;
+        ls[k] = k < C ? lses[k * slot_rows + at] : -INFINITY;
         mx = fmaxf(mx, ls[k]);
       }
 #pragma unroll
       for (int k = 0; k < kQaCluster; ++k) {
         if (k >= C || ls[k] == -INFINITY) continue;            // (an empty part's slot holds zeros; a NaN stays one)
         const float f = fast_exp2((ls[k] - mx) * kLog2e);
-        const float4 v = *reinterpret_cast<const float4*>(slots + ((size_t)k * NQC + r) * D + d);
+        const float4 v = *reinterpret_cast<const float4*>(slots + ((size_t)k * slot_rows + at) * D + d);
         tot += f;
         a.x = fmaf(f, v.x, a.x);
         a.y = fmaf(f, v.y, a.y);
@@ -519,11 +518,11 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
   }
   if (p.clusters == 1) return;
 
-  // ---------------------------------------------------------------- the unit's last cluster to arrive merges
+  // ---------------------------------------------------------------- the unit's last CTA to arrive merges
   __shared__ int last;
   __threadfence();
   __syncthreads();
-  if (tid == 0) last = atomicAdd(&p.counters[unit], 1) == p.clusters * (int)gridDim.z - 1;
+  if (tid == 0) last = atomicAdd(&p.counters[unit], 1) == (int)(gridDim.x * gridDim.z) - 1;
   __syncthreads();
   if (!last) return;
   __threadfence();
@@ -565,13 +564,15 @@ namespace {
 
 struct QaInfo {
   const void* fn;
+  int id;                      // 0 .. 11
   size_t (*smem)(int cluster);
   std::atomic<uint64_t>* allowed;
 };
 template <int D, int NT, bool GATHER, int WARPS>
 QaInfo qa_one() {
   static std::atomic<uint64_t> allowed{0};
-  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER, WARPS>), &QaSmem<D, NT, WARPS>::bytes, &allowed};
+  constexpr int id = (D == 128 ? 6 : 0) + (GATHER ? 3 : 0) + (NT == 2 ? 2 : WARPS == 8);
+  return {reinterpret_cast<const void*>(&quant_attn_kernel<D, NT, GATHER, WARPS>), id, &QaSmem<D, NT, WARPS>::bytes, &allowed};
 }
 template <int D, bool GATHER>
 QaInfo qa_info(int nt, int warps) {
@@ -582,25 +583,71 @@ QaInfo qa_kernel(int d, int nt, int warps, bool gather) {
   return gather ? qa_info<128, true>(nt, warps) : qa_info<128, false>(nt, warps);
 }
 
+// Clusters of c CTAs that the device holds at once (a GPC's SMs are shared out by whole clusters).  Asked once per instance
+// and c.
+long clusters_held(const QaInfo& k, int warps, int c) {
+  static thread_local int cache_dev = -1;
+  static thread_local int cache[12][kQaCluster + 1];
+  int dev = 0;
+  const long guess = 2L * current_sm_count() / c;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return guess;
+  }
+  if (dev != cache_dev) {
+    std::fill_n(&cache[0][0], sizeof(cache) / sizeof(int), -1);
+    cache_dev = dev;
+  }
+  int& held = cache[k.id][c];
+  if (held < 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(c);
+    cfg.blockDim = dim3(32 * warps);
+    cfg.dynamicSmemBytes = k.smem(c);
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)c;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (allow_shared_memory_once(k.fn, 128, k.allowed) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k.fn, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      n = (int)guess;
+    }
+    held = n;
+  }
+  return held;
+}
+
 }  // namespace
 
-bool quant_attn_plan(const bd_shape& s, int rows, long entries, QuantAttnPlan* plan) {
+bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, QuantAttnPlan* plan) {
   const long units = (long)s.batch * s.h_kv;
   plan->nt = rows <= 8 ? 1 : 2;
   plan->chunks = (rows + 8 * plan->nt - 1) / (8 * plan->nt);
   if (units > 65535 || plan->chunks > 65535) return false;
-  // A tile for every one of four warps while one wave holds the CTAs (two an SM: what a cluster's shared memory leaves),
-  // eight warps where a slice is longer, and never more than kQaMaxParts clusters of a unit.
-  const long slots = std::max(1L, 2L * current_sm_count() / (units * plan->chunks));
-  const long want = std::max(1L, std::min<long>(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile)));
-  // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA: one, unless its
-  // slices would be longer by more than that.
-  plan->clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
-  if (entries / kQaCluster - entries / want <= 320) plan->clusters = 1;
-  plan->cluster = (int)std::min<long>(kQaCluster, (want + plan->clusters - 1) / plan->clusters);
-  const long ctas = (long)plan->cluster * plan->clusters;
-  plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);
-  plan->warps = plan->nt == 1 && plan->per_split > 4 * kQaTile ? 8 : 4;
+  // A tile for every one of four warps, eight warps where a slice is longer, as long as one wave holds the CTAs: a second
+  // one repeats the whole chain of latencies (32 units of 1024 entries, 16 rows: 23.7 us in clusters of eight that waited for
+  // another's end, 12.3; 40 units, 8 rows 12.3 / 9.3).
+  const long blocks = units * plan->chunks, slots = std::max(1L, 2L * current_sm_count() / blocks);
+  const int most = (int)std::min<long>(kQaCluster, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
+  auto take = [&](int cluster, int clusters) {
+    const long ctas = (long)cluster * clusters;
+    plan->cluster = cluster;
+    plan->clusters = clusters;
+    plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);
+    plan->warps = plan->nt == 1 && plan->per_split > 4 * kQaTile ? 8 : 4;
+    return blocks * clusters <= clusters_held(qa_kernel(s.head_dim, plan->nt, plan->warps, gather), plan->warps, cluster);
+  };
+  // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA.
+  const long want = std::min(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
+  int clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
+  if (entries / kQaCluster - entries / want <= 320) clusters = 1;
+  bool held = false;
+  for (; clusters > 1 && !held; --clusters) held = take((int)std::min<long>(kQaCluster, (want + clusters - 1) / clusters), clusters);
+  for (int c = most; c > 0 && !held; --c) held = take(c, 1);
   plan->most_clusters = (int)std::min<long>(kQaMaxParts, (slots + kQaCluster - 1) / kQaCluster);
   return true;
 }

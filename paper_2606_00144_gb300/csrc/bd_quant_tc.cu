@@ -846,7 +846,7 @@ static bool warps_suit(const bd_shape& s, int rows, const QuantAttnPlan& w) {
 }
 
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
-  const bool w = quant_attn_plan(s, rows, (long)s.t_ctx + n_q, &plan->warps);
+  const bool w = quant_attn_plan(s, rows, (long)s.t_ctx + n_q, false, &plan->warps);
   plan->on_tc = !(w && warps_suit(s, rows, plan->warps)) && quant_tc_plan(s, rows, n_q, &plan->tc);
   if (!plan->on_tc && !w) return false;
   plan->bytes = plan->on_tc ? quant_tc_bytes(s, plan->tc) : quant_attn_bytes(s, rows, plan->warps);
