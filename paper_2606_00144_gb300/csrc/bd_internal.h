@@ -193,6 +193,7 @@ struct QuantAttnPlan {
   int per_split, warps; // entries and warps of a CTA
   int cluster, clusters;   // CTAs of a cluster, clusters of a unit
   int most_clusters;    // the most that any number of entries takes
+  bool one_wave;        // the device holds every CTA at once
 };
 // entries: the most that a unit attends to; gather: they come from a view
 bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, QuantAttnPlan* plan);

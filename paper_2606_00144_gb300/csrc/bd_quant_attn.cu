@@ -639,15 +639,18 @@ bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, Qua
     plan->clusters = clusters;
     plan->per_split = (int)(((entries + ctas - 1) / ctas + 15) / 16 * 16);
     plan->warps = plan->nt == 1 && plan->per_split > 4 * kQaTile ? 8 : 4;
-    return blocks * clusters <= clusters_held(qa_kernel(s.head_dim, plan->nt, plan->warps, gather), plan->warps, cluster);
+    // (above seven eighths of what the device holds, launches of 16 rows do take a second wave: 96 of 97 clusters 14.5 us,
+    // 10.8 as pairs; 32 of 36 12.3)
+    const long held = clusters_held(qa_kernel(s.head_dim, plan->nt, plan->warps, gather), plan->warps, cluster);
+    return plan->one_wave = blocks * clusters <= (plan->nt == 2 ? held * 7 / 8 : held);
   };
   // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA.
   const long want = std::min(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
   int clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
   if (entries / kQaCluster - entries / want <= 320) clusters = 1;
-  bool held = false;
-  for (; clusters > 1 && !held; --clusters) held = take((int)std::min<long>(kQaCluster, (want + clusters - 1) / clusters), clusters);
-  for (int c = most; c > 0 && !held; --c) held = take(c, 1);
+  plan->one_wave = false;
+  for (; clusters > 1 && !plan->one_wave; --clusters) take((int)std::min<long>(kQaCluster, (want + clusters - 1) / clusters), clusters);
+  for (int c = most; c > 0 && !plan->one_wave; --c) take(c, 1);
   plan->most_clusters = (int)std::min<long>(kQaMaxParts, (slots + kQaCluster - 1) / kQaCluster);
   return true;
 }

@@ -834,15 +834,16 @@ size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
   return align_up(rows * s.head_dim * 4, 256) + align_up(rows * 4, 256) + align_up(units * 4, 256);
 }
 
-// The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast, as long as one cluster
-// holds a unit; beyond, its tensor pipe and its second merge cost more.  mma.sync / tcgen05, us, d 128: 8 units of 1K, 4
-// rows 5.2 / 9.6, 16 rows 9.7 / 11.6, 24 rows 14.4 / 11.8; of 4K (several clusters), 4 rows 11.3 / 10.6; 64 units of 1K, 4K, 8K,
-// 16K, 4 rows 8.9 / 12.3, 16.0 / 20.4, 25.0 / 27.2, 43.0 / 41.5, 16 rows of 16K 59.7 / 47.7, 24 rows 108 / 48; 8 units of 0.4K,
-// 24 rows 7.7 / 10.1; d 64: 64 units of 16K, 4 rows 26.6 / 35.2, 8 units of 128K 37.4 / 33.0, 2 units of 1K, 24 rows 6.4 / 9.7.
+// The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast; its chunks of 16 rows each
+// read the cache and use the tensor pipe anew.  So it takes short slices, the longer the fewer instructions a row costs (d 64,
+// few rows).  mma.sync / tcgen05, us, d 128, 4 rows: 8 units of 1K 5.4 / 9.0, 64 of 4K 16.2 / 18.0, of 8K 25.2 / 24.5, of 16K
+// 43.2 / 37.4, 8 of 8K (four clusters) 11.2 / 11.9, of 64K 27.3 / 24.0; 16 rows: 64 of 2K 15.6 / 16.9, of 4K 22.3 / 21.6;
+// 24 rows: 64 of 0.5K 12.1 / 13.2, of 1K 15.4 / 14.7; 84 rows: 16 of 1K 15.2 / 17.0, 32 of 1K 20.2 / 19.0; d 64: 64 of 16K,
+// 4 rows 26.8 / 33.2, of 4K, 16 rows 15.2 / 20.9, 24 rows 22.3 / 21.1.
 static bool warps_suit(const bd_shape& s, int rows, const QuantAttnPlan& w) {
-  if (w.clusters > 1) return false;
-  if (rows <= 8) return w.per_split <= (s.head_dim == 128 ? 3072 : 5120);
-  return w.per_split <= 160 && (long)s.batch * s.h_kv * w.chunks * w.cluster <= 64;
+  const int wide = s.head_dim == 128 ? 1 : 2;
+  if (rows <= 8) return w.per_split <= (s.head_dim == 64 ? 5120 : w.clusters == 1 ? 3072 : 640);
+  return w.clusters == 1 && w.one_wave && w.per_split <= (rows > 16 && rows <= 32 ? 320 : 640) * wide;
 }
 
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
