@@ -500,11 +500,14 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       // ---- softmax: this thread's key, NC query rows
       const float e = (float)ev;
       const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
-      float y[BC];
+      float ys[NB > 1 ? 2 : 1][BC];            // (of several blocks the next is on its way while one is worked on)
+      auto fetch = [&](int nb) { tc_ld_cols<BC>(t_s + lanes + col0 + BC * nb, ys[nb & 1]); };
       // a block of the tile's scores plus e less the running maximum, in log2 units
-      auto scores = [&](int c0, float& mx) {
-        tc_ld_cols<BC>(t_s + lanes + col0 + c0, y);
+      auto scores = [&](int nb, float& mx) {
+        const int c0 = BC * nb;
+        float* y = ys[nb & 1];
         tc_wait_ld();
+        if (nb + 1 < NB) fetch(nb + 1);
 #pragma unroll
         for (int c = 0; c < BC; c += 2) {
           const float2 r = ffma2(make_float2(y[c], y[c + 1]), make_float2(a, a), make_float2(e, e));
@@ -533,8 +536,9 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
         float mx = -INFINITY;
+        fetch(0);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) scores(BC * nb, mx);
+        for (int nb = 0; nb < NB; ++nb) scores(nb, mx);
         if (pass == 1 || !bar_any(bar, GT, mx > kQtSlack + kQtLift)) break;
         // ---- some row's maximum grows by more than the slack: all rows take theirs
 #pragma unroll 1
@@ -579,10 +583,12 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       }
       {
         const float el = pow2i(-ev);
+        if (NB > 1) fetch(0);                  // (a single block is still there)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           float mx = 0.f;
-          if (NB > 1) scores(BC * nb, mx);     // (a single block is still there)
+          if (NB > 1) scores(nb, mx);
+          const float* y = ys[nb & 1];
 #pragma unroll
           for (int c = 0; c < BC; c += 8) {
             uint32_t h[4];
