@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -114,7 +115,7 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         # the handle alone: building the Stream object takes 3 us of a call's 9
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -280,6 +281,7 @@ class QuantCache:
             if codes.device != k_codes.device or scales.device != k_codes.device:
                 raise ValueError("QuantCache: codes and scales must be on one device")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self._rows = (self.batch, self.h_kv, self.head_dim, self.t_cap)
         self._struct = BdQuantCache(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
         self._ref = ctypes.byref(self._struct)
         self.is_cuda = k_codes.is_cuda
@@ -303,6 +305,7 @@ class QuantCache:
 # The calls below are small next to a launch, so what they check is checked once, in one place, and told apart
 # (_refuse_rows, _refuse) only when something does not fit.
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_shape_ints = struct.Struct("6i").unpack_from      # a shape's sizes at once
 
 
 @functools.lru_cache(maxsize=256)
@@ -331,8 +334,8 @@ def _quant_rows(name, shape, cache, k_rows, v_rows):
     first = k_rows if k_rows is not None else v_rows
     if first is None:
         raise ValueError(f"{name}: K rows, V rows or both")
-    b, h, d = shape.batch, shape.h_kv, shape.head_dim
-    if not (b == cache.batch and h == cache.h_kv and d == cache.head_dim and shape.t_cap == cache.t_cap):
+    b, _, h, d, _, cap = _shape_ints(shape)
+    if (b, h, d, cap) != cache._rows:
         _refuse_cache(name, shape)
     dtype = first.dtype
     want = (b, h, first.shape[2] if first.dim() == 4 else -1, d)
@@ -341,13 +344,15 @@ def _quant_rows(name, shape, cache, k_rows, v_rows):
         if t is None:
             out += None, None
             continue
-        if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.is_cuda and cache.is_cuda
-                and (t.is_contiguous() or t.stride(3) == 1)):
+        if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.is_cuda and cache.is_cuda):
             _refuse_rows(name, want, dtype, k_rows, v_rows)
         if t.is_contiguous():
             out += t.data_ptr(), None
             continue
-        out += t.data_ptr(), _stride_array(*t.stride()[:3])
+        sb, sh, sn, one = t.stride()
+        if one != 1:
+            _refuse_rows(name, want, dtype, k_rows, v_rows)
+        out += t.data_ptr(), _stride_array(sb, sh, sn)
     return want[2], BD_DTYPE_BF16 if dtype is _BF16 else BD_DTYPE_F32, out
 
 
@@ -360,17 +365,18 @@ def _refuse(name, **tensors):
     raise ValueError(f"{name}: every tensor must be on the GPU")
 
 
-def _quant_attn(name, shape, cache, q, o_out, lse_out, want, idx=None, count=None, budget=0):
-    """Checks the cache, the queries, the outputs and a drafter pass's view; want: the queries' shape."""
-    if not (shape.batch == cache.batch and shape.h_kv == cache.h_kv and shape.head_dim == cache.head_dim
-            and shape.t_cap == cache.t_cap):
+def _quant_attn(name, shape, cache, q, o_out, lse_out, n_q, idx=None, count=None, budget=0):
+    """Checks the cache, the queries (of a drafter pass where n_q is None), the outputs and a drafter pass's view."""
+    b, h_q, h, d, _, cap = _shape_ints(shape)
+    if (b, h, d, cap) != cache._rows:
         _refuse_cache(name, shape)
-    units = (cache.batch, cache.h_kv)
+    want = (b, h_q, d) if n_q is None else (b, h_q, n_q, d)
+    units = (b, h)
     if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
             and o_out.is_contiguous() and q.is_cuda and o_out.is_cuda and cache.is_cuda
             and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
                                      and lse_out.is_cuda))
-            and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (*units, budget)
+            and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (b, h, budget)
                                  and count.shape == units and idx.is_contiguous() and count.is_contiguous()
                                  and idx.is_cuda and count.is_cuda))):
         _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]),
@@ -381,7 +387,7 @@ def bd_quant_write(shape, k_rows, v_rows, cache: QuantCache, stream=None):
     """Quantises rows [batch, h_kv, n, head_dim] (bf16 or fp32; any strides of whole 16 bytes; either may
     be None) into the cache, behind the context (each sequence's length, if the shape has lengths)."""
     n, dtype, (k, ks, v, vs) = _quant_rows("bd_quant_write", shape, cache, k_rows, v_rows)
-    st = library().bd_quant_write(ctypes.byref(shape), n, dtype, k, ks, v, vs, cache._ref, _stream(stream))
+    st = (_lib or library()).bd_quant_write(ctypes.byref(shape), n, dtype, k, ks, v, vs, cache._ref, _stream(stream))
     _check("bd_quant_write", st)
 
 
@@ -393,26 +399,25 @@ def bd_quant_read(shape, cache: QuantCache, k_out, v_out=None, first_row=None, s
         first_row = BD_QUANT_BLOCK_ROWS
     elif first_row < 0:
         raise ValueError("bd_quant_read: first_row must not be negative")
-    st = library().bd_quant_read(ctypes.byref(shape), first_row, n, dtype, cache._ref, k, ks, v, vs, _stream(stream))
+    st = (_lib or library()).bd_quant_read(ctypes.byref(shape), first_row, n, dtype, cache._ref, k, ks, v, vs, _stream(stream))
     _check("bd_quant_read", st)
 
 
 def bd_quant_draft_attn(shape, q, cache: QuantCache, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
                         stream=None, flags=0):
     """bd_draft_attn over a 4-bit cache."""
-    _quant_attn("bd_quant_draft_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, shape.head_dim), idx, count,
-                budget)
-    st = library().bd_quant_draft_attn(ctypes.byref(shape), q.data_ptr(), cache._ref, idx.data_ptr(), count.data_ptr(),
-                                       budget, step_j, flags, o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes,
-                                       _stream(stream))
+    _quant_attn("bd_quant_draft_attn", shape, cache, q, o_out, lse_out, None, idx, count, budget)
+    st = (_lib or library()).bd_quant_draft_attn(ctypes.byref(shape), q.data_ptr(), cache._ref, idx.data_ptr(), count.data_ptr(),
+                                                 budget, step_j, flags, o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes,
+                                                 _stream(stream))
     _check("bd_quant_draft_attn", st)
 
 
 def bd_quant_verify_attn(shape, q, n_q, cache: QuantCache, o_out, lse_out, ws: Workspace, stream=None):
     """bd_verify_attn over a 4-bit cache; n_q = 1 decodes one token."""
-    _quant_attn("bd_quant_verify_attn", shape, cache, q, o_out, lse_out, (shape.batch, shape.h_q, n_q, shape.head_dim))
-    st = library().bd_quant_verify_attn(ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, o_out.data_ptr(), _ptr(lse_out),
-                                        ws.ptr, ws.nbytes, _stream(stream))
+    _quant_attn("bd_quant_verify_attn", shape, cache, q, o_out, lse_out, n_q)
+    st = (_lib or library()).bd_quant_verify_attn(ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, o_out.data_ptr(), _ptr(lse_out),
+                                                  ws.ptr, ws.nbytes, _stream(stream))
     _check("bd_quant_verify_attn", st)
 
 
