@@ -625,13 +625,18 @@ long clusters_held(const QaInfo& k, int warps, int c) {
 
 bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, QuantAttnPlan* plan) {
   const long units = (long)s.batch * s.h_kv;
-  plan->nt = rows <= 8 ? 1 : 2;
-  plan->chunks = (rows + 8 * plan->nt - 1) / (8 * plan->nt);
+  long blocks = 0;             // units x chunks
+  auto tiles = [&](int nt) {
+    plan->nt = nt;
+    plan->chunks = (rows + 8 * nt - 1) / (8 * nt);
+    blocks = units * plan->chunks;
+  };
+  tiles(rows <= 8 ? 1 : 2);
   if (units > 65535 || plan->chunks > 65535) return false;
   // A tile for every one of four warps, eight warps where a slice is longer, as long as one wave holds the CTAs: a second
   // one repeats the whole chain of latencies (32 units of 1024 entries, 16 rows: 23.7 us in clusters of eight that waited for
   // another's end, 12.3; 40 units, 8 rows 12.3 / 9.3).
-  const long blocks = units * plan->chunks, slots = std::max(1L, 2L * current_sm_count() / blocks);
+  const long slots = std::max(1L, 2L * current_sm_count() / blocks);
   const int most = (int)std::min<long>(kQaCluster, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
   auto take = [&](int cluster, int clusters) {
     const long ctas = (long)cluster * clusters;
@@ -644,14 +649,26 @@ bool quant_attn_plan(const bd_shape& s, int rows, long entries, bool gather, Qua
     const long held = clusters_held(qa_kernel(s.head_dim, plan->nt, plan->warps, gather), plan->warps, cluster);
     return plan->one_wave = blocks * clusters <= (plan->nt == 2 ? held * 7 / 8 : held);
   };
-  // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA.
-  const long want = std::min(slots, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
-  int clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
-  if (entries / kQaCluster - entries / want <= 320) clusters = 1;
-  plan->one_wave = false;
-  for (; clusters > 1 && !plan->one_wave; --clusters) take((int)std::min<long>(kQaCluster, (want + clusters - 1) / clusters), clusters);
-  for (int c = most; c > 0 && !plan->one_wave; --c) take(c, 1);
   plan->most_clusters = (int)std::min<long>(kQaMaxParts, (slots + kQaCluster - 1) / kQaCluster);
+  // Several clusters of a unit cost a merge through global memory, as long as some 320 entries of a CTA.
+  auto cut = [&] {
+    const long room = std::max(1L, 2L * current_sm_count() / blocks);
+    const long want = std::min(room, (entries + 4 * kQaTile - 1) / (4 * kQaTile));
+    int clusters = (int)std::min<long>(kQaMaxParts, (want + kQaCluster - 1) / kQaCluster);
+    if (entries / kQaCluster - entries / want <= 320) clusters = 1;
+    plan->one_wave = false;
+    for (; clusters > 1 && !plan->one_wave; --clusters) take((int)std::min<long>(kQaCluster, (want + clusters - 1) / clusters), clusters);
+    for (int c = most; c > 0 && !plan->one_wave; --c) take(c, 1);
+  };
+  // Chunks of 8 rows while the device holds them all at once, else of 16.  A CTA's chain is a third shorter with one n8 tile, and
+  // what the chunks read again is in L2 (2 units of 1K, d 64, 24 rows: 6.3 us as chunks of 16, 4.2; 64 units of 0.5K, 24 rows 12.1 / 9.9;
+  // drafter pass of 8 units of 1024, 16 rows 8.2 / 6.7).
+  tiles(1);
+  cut();
+  if (rows > 8 && !plan->one_wave) {
+    tiles(2);
+    cut();
+  }
   return true;
 }
 

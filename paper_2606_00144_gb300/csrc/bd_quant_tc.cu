@@ -840,21 +840,21 @@ size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
   return align_up(rows * s.head_dim * 4, 256) + align_up(rows * 4, 256) + align_up(units * 4, 256);
 }
 
-// The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast; its chunks of 16 rows each
-// read the cache and use the tensor pipe anew.  So it takes short slices, the longer the fewer instructions a row costs (d 64,
-// few rows).  mma.sync / tcgen05, us, d 128, 4 rows: 8 units of 1K 5.4 / 9.0, 64 of 4K 16.2 / 18.0, of 8K 25.2 / 24.5, of 16K
-// 43.2 / 37.4, 8 of 8K (four clusters) 11.2 / 11.9, of 64K 27.3 / 24.0; 16 rows: 64 of 2K 15.6 / 16.9, of 4K 22.3 / 21.6;
-// 24 rows: 64 of 0.5K 12.1 / 13.2, of 1K 15.4 / 14.7; 84 rows: 16 of 1K 15.2 / 17.0, 32 of 1K 20.2 / 19.0; d 64: 64 of 16K,
-// 4 rows 26.8 / 33.2, of 4K, 16 rows 15.2 / 20.9, 24 rows 22.3 / 21.1.
-static bool warps_suit(const bd_shape& s, int rows, const QuantAttnPlan& w) {
-  const int wide = s.head_dim == 128 ? 1 : 2;
+// The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast; every chunk of 8 rows
+// reads the cache and unpacks it anew.  So it takes short slices, and of more rows what an SM is soon done with.  mma.sync /
+// tcgen05, us, d 128, 4 rows: 8 units of 1K 5.4 / 9.0, 64 of 4K 16.2 / 18.0, of 8K 25.2 / 24.5, of 16K 43.2 / 37.4, 8 of 8K (four
+// clusters) 11.2 / 11.9, of 64K 27.3 / 24.0; 16 rows: 64 of 1K 11.3 / 14.7, of 4K 25.0 / 21.9; 24 rows: 8 of 1K 6.9 / 11.1, 64 of
+// 0.5K 10.0 / 13.3, of 1K 14.5 / 14.8, 16 of 4K 13.9 / 13.4; 84 rows: 8 of 1K 9.2 / 16.6, 32 of 1K 20.3 / 19.1; d 64: 64 of 16K,
+// 4 rows 26.8 / 33.2, of 4K, 16 rows 15.9 / 21.1, 24 rows 25.6 / 21.3, 8 of 2K, 84 rows 8.6 / 16.0.
+static bool warps_suit(const bd_shape& s, int rows, int n_q, const QuantAttnPlan& w) {
   if (rows <= 8) return w.per_split <= (s.head_dim == 64 ? 5120 : w.clusters == 1 ? 3072 : 640);
-  return w.clusters == 1 && w.one_wave && w.per_split <= (rows > 16 && rows <= 32 ? 320 : 640) * wide;
+  const long work = (long)s.batch * s.h_kv * ((rows + 7) / 8) * ((long)s.t_ctx + n_q);   // key and chunk pairs
+  return w.one_wave && work <= (s.head_dim == 64 ? 3000L : 1300L) * current_sm_count();
 }
 
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
   const bool w = quant_attn_plan(s, rows, (long)s.t_ctx + n_q, false, &plan->warps);
-  plan->on_tc = !(w && warps_suit(s, rows, plan->warps)) && quant_tc_plan(s, rows, n_q, &plan->tc);
+  plan->on_tc = !(w && warps_suit(s, rows, n_q, plan->warps)) && quant_tc_plan(s, rows, n_q, &plan->tc);
   if (!plan->on_tc && !w) return false;
   plan->bytes = plan->on_tc ? quant_tc_bytes(s, plan->tc) : quant_attn_bytes(s, rows, plan->warps);
   return true;
