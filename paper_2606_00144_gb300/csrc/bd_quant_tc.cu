@@ -17,8 +17,8 @@
 // was 600.  As it is a tile takes 1200 cycles of an SM, of which each scheduler issues in 740 (64 units of 16K, 24 rows:
 // 44.2 us, 3.4 TB/s; one row 37.3 us, 4.1 TB/s).
 // Blocks of more than 32 query rows run on two groups of two warpgroups: those share a tile's unpacking and halve its
-// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 49.6 us, 68 on
-// four groups; 64 units, 64 rows 69 us, 84 rows 84).
+// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 48.8 us, 68 on
+// four groups; 64 units, 64 rows 69 us, 84 rows 82).
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
 #include <algorithm>
