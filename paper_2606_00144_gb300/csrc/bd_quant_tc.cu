@@ -715,26 +715,34 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 }
 
 // Merge of the segments' partials, one warp per query row of a unit (a unit of one segment was written by
-// quant_tc_kernel itself).  A lane takes four adjacent channels (at D 64 half of the segments); the parts' loads
-// are all in flight before their weights are known.
+// quant_tc_kernel itself).  A lane takes four adjacent channels (at D 64 half of the segments).
 template <int D>
 __global__ void __launch_bounds__(128) quant_merge_kernel(const float* o_part, const float* lse_part, const int* nseg, int max_seg,
                                                           int nq_rows, int rows_total, int row_chunks, __nv_bfloat16* o, float* lse) {
-  constexpr int Q = D / 4, NG = 32 / Q, AT = 8;          // lanes of a row's channels; segment groups; parts at a time
+  // lanes of a row's channels; segment groups; a group's parts at a time, and those asked for before their number is known
+  constexpr int Q = D / 4, NG = 32 / Q, AT = 16, AHEAD = 4;
   grid_dependency_wait();
   allow_dependent_launch();
   const int unit = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int kv_unit = unit / row_chunks, row_base = (unit - kv_unit * row_chunks) * nq_rows;
-  const int n = min(__ldcg(nseg + unit), max_seg);
-  if (n <= 1 || r >= min(nq_rows, rows_total - row_base)) return;
+  if (r >= min(nq_rows, rows_total - row_base)) return;
   const size_t base = (size_t)unit * max_seg;
   const int q = lane % Q, g = lane / Q;
   const float* lp = lse_part + base * nq_rows + r;
   const float4* op = reinterpret_cast<const float4*>(o_part + (base * nq_rows + r) * D) + q;
-  float mx = -INFINITY;
-  const float l0 = lane < n ? __ldcg(lp + (size_t)lane * nq_rows) : -INFINITY;
-  const float l1 = lane + 32 < n ? __ldcg(lp + (size_t)(lane + 32) * nq_rows) : -INFINITY;
-  mx = fmaxf(l0, l1);
+  // one round trip for the segments' number, their lse and the first parts (what lies past the number is not used): 64 units of
+  // 16K 44.3 -> 43.0 us; all 16 parts so: 40 units of 84 rows 36.8 -> 39.4
+  auto part = [&](int s, int end) { return s < end ? __ldcg(op + (size_t)s * nq_rows * Q) : make_float4(0.f, 0.f, 0.f, 0.f); };
+  float4 v[AT];
+#pragma unroll
+  for (int i = 0; i < AT; ++i) v[i] = part(i * NG + g, i < AHEAD ? max_seg : 0);
+  float l0 = lane < max_seg ? __ldcg(lp + (size_t)lane * nq_rows) : -INFINITY;
+  float l1 = lane + 32 < max_seg ? __ldcg(lp + (size_t)(lane + 32) * nq_rows) : -INFINITY;
+  const int n = min(__ldcg(nseg + unit), max_seg);
+  if (n <= 1) return;
+  l0 = lane < n ? l0 : -INFINITY;
+  l1 = lane + 32 < n ? l1 : -INFINITY;
+  float mx = fmaxf(l0, l1);
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
   // (empty parts weigh nothing; a NaN stays one)
@@ -744,11 +752,10 @@ __global__ void __launch_bounds__(128) quant_merge_kernel(const float* o_part, c
   for (int off = 16; off > 0; off >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, off);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s0 = 0; s0 < n; s0 += AT * NG) {
-    float4 v[AT];
+    if (s0 > 0 || n > AHEAD * NG) {
 #pragma unroll
-    for (int i = 0; i < AT; ++i) {
-      const int s = s0 + i * NG + g;
-      v[i] = s < n ? __ldcg(op + (size_t)s * nq_rows * Q) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < AT; ++i)
+        if (s0 > 0 || i >= AHEAD) v[i] = part(s0 + i * NG + g, n);
     }
 #pragma unroll
     for (int i = 0; i < AT; ++i) {
