@@ -250,15 +250,20 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   allow_dependent_launch();
   VerifyMap map{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
   if (p.seq_lens) {
+    int last_u = -1, last = 0;               // (asked for twice; a thread has one unit as a rule)
     lay_out_spans<kQtThreads>(p.units, [&](int u) {
-      return (quant_tc_context(p.seq_lens, u / p.row_chunks / p.h_kv, p.t_ctx, nullptr) + p.n_q + kQtKeys - 1) / kQtKeys + p.seg_cost;
+      if (u != last_u) last = (quant_tc_context(p.seq_lens, u / p.row_chunks / p.h_kv, p.t_ctx, nullptr) + p.n_q + kQtKeys - 1) / kQtKeys + p.seg_cost;
+      last_u = u;
+      return last;
     }, wtot, pref);
     map.pref = pref;
     map.vtpc = max((pref[p.units] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
   }
   const int v_total = map.vbase(p.units);
   const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
-  const int u_first = v0 < v1 ? map.unit_of(v0) : 0, u_last = v0 < v1 ? map.unit_of(v1 - 1) : -1;
+  const int u_first = v0 < v1 ? map.unit_of(v0) : 0;
+  int u_last = v0 < v1 ? u_first : -1;       // (a unit more or two)
+  while (u_last >= 0 && u_last + 1 < p.units && map.vbase(u_last + 1) < v1) ++u_last;
   bool alive = true;      // false once a wait gave up
 
   // ---- the group's MMAs and its loads are started by a warp each (other groups' on other SMSPs).  Local tile i is job
