@@ -15,9 +15,10 @@
 // unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
 // warps, with two buffers between them) left every warp a chain of waits: 1700 cycles a tile, of which its work
 // was 600.  As it is a tile takes 1200 cycles of an SM, of which each scheduler issues in 740 (64 units of 16K, 24 rows:
-// 44.2 us, 3.4 TB/s; one row 37.3 us, 4.1 TB/s).
+// 42.5 us, 3.6 TB/s; one row 35.8 us, 4.2 TB/s).  A fifth group (up to 8 rows, 96 registers a thread) made that
+// 38.4: more warps to fill the waits are not what it lacks.
 // Blocks of more than 32 query rows run on two groups of two warpgroups: those share a tile's unpacking and halve its
-// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 48.8 us, 68 on
+// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 48.1 us, 68 on
 // four groups; 64 units, 64 rows 69 us, 84 rows 82).
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
@@ -853,15 +854,18 @@ size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
 }
 
 // The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast; every chunk of 8 rows
-// reads the cache and unpacks it anew.  So it takes short slices, and of more rows what an SM is soon done with.  mma.sync /
-// tcgen05, us, d 128, 4 rows: 8 units of 1K 5.4 / 9.0, 64 of 4K 16.2 / 18.0, of 8K 25.2 / 24.5, of 16K 43.2 / 37.4, 8 of 8K (four
-// clusters) 11.2 / 11.9, of 64K 27.3 / 24.0; 16 rows: 64 of 1K 11.3 / 14.7, of 4K 25.0 / 21.9; 24 rows: 8 of 1K 6.9 / 11.1, 64 of
-// 0.5K 10.0 / 13.3, of 1K 14.5 / 14.8, 16 of 4K 13.9 / 13.4; 84 rows: 8 of 1K 9.2 / 16.6, 32 of 1K 20.3 / 19.1; d 64: 64 of 16K,
-// 4 rows 26.8 / 33.2, of 4K, 16 rows 15.9 / 21.1, 24 rows 25.6 / 21.3, 8 of 2K, 84 rows 8.6 / 16.0.
+// reads the cache and unpacks it anew, several clusters of a unit meet in global memory.  So it takes short slices, and of
+// more rows what an SM is soon done with.  mma.sync / tcgen05, us, d 128, 4 rows: 8 units of 1K 5.3 / 7.9, 64 of 4K 16.2 / 17.0, of
+// 8K 25.2 / 23.3, 256 of 2K 24.5 / 28.8, 8 of 8K (four clusters) 11.1 / 10.3; 16 rows: 64 of 1K 11.3 / 13.4, of 4K 25.0 / 20.2, 8 of
+// 8K 14.1 / 12.6; 24 rows: 8 of 1K 7.0 / 9.8, 64 of 0.5K 10.0 / 12.5, of 1K 14.5 / 13.7; 84 rows: 8 of 1K 9.2 / 15.0, 32 of 1K
+// 20.3 / 17.9; d 64: 64 of 16K, 4 rows 26.7 / 31.3, of 4K, 16 rows 15.8 / 19.0, 24 rows 25.6 / 19.4, 8 of 2K, 84 rows 8.5 / 15.7, of
+// 16K, 16 rows 13.0 / 12.2.
 static bool warps_suit(const bd_shape& s, int rows, int n_q, const QuantAttnPlan& w) {
-  if (rows <= 8) return w.per_split <= (s.head_dim == 64 ? 5120 : w.clusters == 1 ? 3072 : 640);
-  const long work = (long)s.batch * s.h_kv * ((rows + 7) / 8) * ((long)s.t_ctx + n_q);   // key and chunk pairs
-  return w.one_wave && work <= (s.head_dim == 64 ? 3000L : 1300L) * current_sm_count();
+  const bool wide = s.head_dim == 128, one = w.clusters == 1;
+  const long keys = (long)s.t_ctx + n_q;
+  if (rows <= 8) return wide ? one && keys <= 6144 : w.per_split <= 5120;
+  const long most = wide ? (one ? 1100 : 450) : (one ? 2700 : 1300);      // keys x chunks of an SM
+  return w.one_wave && (long)s.batch * s.h_kv * ((rows + 7) / 8) * keys <= most * current_sm_count();
 }
 
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan) {
