@@ -489,6 +489,7 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
   }
   if (C > 1) {
     // ---------------------------------------------------------------- the cluster's parts of this CTA's rows
+    __syncwarp();
     cluster.sync();                            // all have landed
     for (int i = tid; i < slot_rows * (D / 4); i += kQaThreads) {
       const int at = i / (D / 4), r = at * C + rank, d = i % (D / 4) * 4;

@@ -570,6 +570,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             my_nm[c] = m;
             my_alpha[c] = fast_exp2(m - old);
           }
+          __syncwarp();                        // (lanes leave the loop apart; what follows is for whole warps)
         }
         named_bar(bar, GT);
 #pragma unroll
@@ -679,6 +680,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         if (!whole) p.lse_part[slot * p.nq_rows + mc] = lse;
         else if (p.lse) p.lse[orow0 + mc] = lse;
       }
+      __syncwarp();
       if (!has_rows) continue;
       float x[8];
 #pragma unroll
