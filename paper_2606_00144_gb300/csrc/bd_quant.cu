@@ -4,7 +4,7 @@
 //   value = (code - 8) * scale
 //
 // Both are one pass over the rows with nothing to reuse, bound by HBM: 8 x 16K rows of K and V (690 MB) are written in
-// 111 us (6.2 TB/s) and read back in 100 (6.9 TB/s).  The write is as fast only because a quotient takes three packed
+// 109 us (6.3 TB/s) and read back in 100 (6.9 TB/s).  The write is as fast only because a quotient takes three packed
 // FMAs and its code comes off the sum's last bits: with a division and a conversion an element it took 383 us.
 // A thread takes 16 adjacent elements of a row, half a group: 32 bytes of bf16, an 8-byte word of codes; a warp's
 // accesses are contiguous on both sides and the two threads of a group meet in one shuffle.
@@ -76,12 +76,13 @@ template <>
 struct Sixteen<__nv_bfloat16> {
   uint32_t w[8];
   __device__ __forceinline__ void load(const __nv_bfloat16* p, bool wide) { load32(p, wide, w); }
-  // the largest magnitude's bits as a float's (a NaN's are above infinity's)
+  // the largest magnitude's bits as a float's (a NaN's are above infinity's); one instruction for two elements, their signs
+  // left to the end (with a mask and an integer maximum 8 x 16K rows took 111 us, 109 so)
   __device__ __forceinline__ uint32_t top() const {
-    uint32_t m = 0;
+    uint32_t m = w[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-    return max(m << 16, m & 0xffff0000u);
+    for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
+    return max(m << 16 & 0x7fff0000u, m & 0x7fff0000u);
   }
   __device__ __forceinline__ float2 pair(int i) const { return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)); }
 };
@@ -177,7 +178,7 @@ __device__ __forceinline__ Place place(const QuantParams& p) {
 template <int D, typename T>
 __global__ void __launch_bounds__(kQThreads) quant_write_kernel(const __grid_constant__ QuantParams p) {
   constexpr int CH = D / 16, STEP = kQThreads / CH;   // threads of a row; rows at a time
-  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;       // rows in flight: 128 bytes a thread (bf16 with 64: 123 us for 111; fp32 with 256: 95 for 86)
+  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;       // rows in flight: 128 bytes a thread (bf16 with 64: 1.1 times the time; fp32 with 256: 95 us for 86)
   grid_dependency_wait();
   allow_dependent_launch();
   const Place at = place<D>(p);
