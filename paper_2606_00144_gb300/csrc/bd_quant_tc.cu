@@ -647,14 +647,12 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         }
       if (c0 + lane < NC) my_red[4 * (c0 + lane) + quad] = __float_as_int(sum[0]);
     }
-    // the last P V of every group that had a tile of the segment
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int done = (job - g + GROUPS - 1) / GROUPS;        // its tiles so far (job - g > -GROUPS)
-      if (g + GROUPS * (done - 1) >= job - n) wait(pv_done(g), (done - 1) & 1);
-    }
-    tc_fence_after();
+    // Every group's last P V: its own warps wait for it (a parity does not tell another group's phases apart), the barrier
+    // passes that on, and the fence behind the barrier orders the reads of the groups' O below.
+    if (t_first < n) wait(pv_done(grp), (i - 1) & 1);
+    tc_fence_before();
     __syncthreads();
+    tc_fence_after();
     const int c_first = map.owner(unit, 0), n_seg = map.owner(unit, map.tiles(unit) - 1) - c_first + 1;
     const bool whole = n_seg == 1;
     const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first), orow0 = (size_t)kv_unit * p.rows_total + row_base;
