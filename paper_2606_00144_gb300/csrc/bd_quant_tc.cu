@@ -233,6 +233,9 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     tma_prefetch_map(&kmap);
     tma_prefetch_map(&vmap);
   }
+  // Branches that single lanes take end in a __syncwarp() where an instruction for whole warps follows (tcgen05.alloc, .ld,
+  // .st, bar): nothing else promises that the lanes are together again.
+  __syncwarp();
   if (warp == 0) {
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
@@ -291,6 +294,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       tma_load_3d(my_ring + (2 * s + which) * TILE, which ? &vmap : &kmap, full, 0, (tb + j - from) * kQtKeys, kv_unit);
       issued[which] = j / GROUPS + 1;
     }
+    __syncwarp();
   };
   if (loader && lead) issued[0] = issued[1] = 0;
 
@@ -560,6 +564,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             top = lane == k ? r : top;
           }
           if (lane < 8) my_red[4 * (c + lane) + quad] = top;
+          __syncwarp();
         }
         named_bar(bar, GT);
         if (quad == 0) {
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             my_nm[c] = m;
             my_alpha[c] = fast_exp2(m - old);
           }
-          __syncwarp();                        // (lanes leave the loop apart; what follows is for whole warps)
+          __syncwarp();                        // (lanes leave the loop apart)
         }
         named_bar(bar, GT);
 #pragma unroll
@@ -647,6 +652,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         }
       if (c0 + lane < NC) my_red[4 * (c0 + lane) + quad] = __float_as_int(sum[0]);
     }
+    __syncwarp();
     // Every group's last P V: its own warps wait for it (a parity does not tell another group's phases apart), the barrier
     // passes that on, and the fence behind the barrier orders the reads of the groups' O below.
     if (t_first < n) wait(pv_done(grp), (i - 1) & 1);

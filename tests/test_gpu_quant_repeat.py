@@ -8,7 +8,7 @@ import torch
 import paper_2606_00144_gb300 as bd
 from tests import quant_reference as ref
 from tests.test_gpu_quant_attn import BF, check_verify
-from tests.test_gpu_quant_attn_long import room
+from tests.test_gpu_quant_attn_long import room, run
 
 pytestmark = pytest.mark.gpu
 REPEATS = 60
@@ -47,3 +47,21 @@ def test_every_call_gives_the_same_bits(d, G, n, grow):
     assert ws.status() == 0
     assert same.item()
     check_verify(tensors, q, lens, n, first[0], first[1])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n", [(1, 8), (4, 6), (4, 8), (8, 8), (4, 21)])
+def test_maxima_that_grow_with_every_tile(d, G, n):
+    """Every tile raises some row's maximum by more than it may trail, in every instance: the path that single lanes
+    write from."""
+    t = 2600
+    g = torch.Generator().manual_seed(G + n)
+    k, v = torch.randn(2, 1, t + n, d, generator=g) * 0.1, torch.randn(2, 1, t + n, d, generator=g)
+    q = torch.randn(2, G, n, d, generator=g)
+    q[..., 0] = 8.0
+    k[..., 0] = torch.arange(t + n) // 128 * 6.5 * d ** 0.5 / 8        # 6.5 nats a tile: 9.4 in log2 units
+    k[..., 1:32] = 0                                         # (a scale's group of its own)
+    tensors = [x for y in (k, v) for x in ref.quantise(y.to(BF))]
+    q = q.to(BF)
+    o, lse = run(tensors, q, [t, t - 700], n)
+    check_verify(tensors, q, [t, t - 700], n, o, lse)
