@@ -153,8 +153,13 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     }
     return r;
   };
+  // Scales come through L1 (a cp.async of 4 or 8 bytes has no other way), a line of many rows'.  A row whose line may also
+  // hold a drafted row's (the context's last rows; the first ones, next to the unit before) must not bring that line in
+  // before the drafted rows are there, or their scales could be read stale: it is asked for with the drafted rows.
+  constexpr int kNear = 128 / (2 * G);         // rows of a line's scales
+  auto late = [&](int row) { return row < kNear || row + kNear > t_unit; };
   // row: this lane's entry_row; returns which of the tile's entries are there (the rest are zero-filled).
-  // part 0: rows of the context and what is zero-filled; 1: drafted rows; 2: all
+  // part 0: rows that are not late; 1: those that are, and what is zero-filled; 2: all
   auto fetch = [&](int row, int slot, int part) {
     uint8_t* st = ring + slot * ST::BYTES;
     constexpr int PER = 32 / G;                // rows a pass of the warp covers, G 16-byte groups each
@@ -162,13 +167,13 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     for (int it = 0; it < G; ++it) {
       const int r = it * PER + lane / G, g = lane % G;
       const int src_row = __shfl_sync(0xffffffffu, row, r);
-      if (part != 2 && (part == 1) != (src_row >= t_unit)) continue;
+      if (part != 2 && (part == 1) != late(src_row)) continue;
       const size_t src = (base + max(src_row, 0)) * (D / 2) + 16 * g;
       const uint32_t off = code_offset<D>(r, g);
       cp_async16_zfill(st + off, p.kc + src, src_row >= 0);
       cp_async16_zfill(st + ST::CODES + off, p.vc + src, src_row >= 0);
     }
-    if (part == 2 || (part == 1) == (row >= t_unit)) {
+    if (part == 2 || (part == 1) == late(row)) {
       const size_t src = (base + max(row, 0)) * G;
       cp_async_small<2 * G>(st + 2 * ST::CODES + lane * 2 * G, p.ks + src, row >= 0);
       cp_async_small<2 * G>(st + 2 * ST::CODES + ST::SCALES + lane * 2 * G, p.vs + src, row >= 0);
@@ -182,7 +187,7 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
   int at_row[kQaStages];
 #pragma unroll
   for (int i = 0; i < kQaStages; ++i) at_row[i] = i < mine ? entry_row(warp + i * kQaWarps, spec[i]) : -1;
-  if (p.early) {                               // the view is older than the kernel before; its drafted rows are not
+  if (p.early) {                               // the view is older than the kernel before; the drafted rows are not
 #pragma unroll
     for (int i = 0; i < kQaStages - 1; ++i)
       if (i < mine) fetch(at_row[i], i, 0);
