@@ -116,7 +116,8 @@ class QuantSpecStep(SpecStep):
 
     The selection and the window's normalisers rank keys on the tensor cores as bf16: the context's keys are
     read back (bd_quant_read) into one bf16 buffer [batch, h_kv, t_cap, head_dim], made at the first such call
-    and shared by every layer that the object serves."""
+    and shared by every layer that the object serves.  Like the outputs and the workspace it is one for all
+    calls: those on different streams are the caller's to order."""
 
     def __init__(self, *args, **kw):
         self._keys = None
@@ -134,11 +135,14 @@ class QuantSpecStep(SpecStep):
     def keys(self, cache, stream=None):
         """The context's keys as bf16, in the step's own buffer (rows past t_ctx are not read)."""
         s = self.shape
+        ts = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream or torch.cuda.current_stream()
         if self._keys is None:
-            self._keys = torch.empty(s.batch, s.h_kv, s.t_cap, s.head_dim, dtype=torch.bfloat16,
-                                     device=cache.k_codes.device)
-            if stream is not None:
-                self._keys.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+            with torch.cuda.stream(ts):          # memory that what is queued on the stream is done with, on no other
+                self._keys = torch.empty(s.batch, s.h_kv, s.t_cap, s.head_dim, dtype=torch.bfloat16,
+                                         device=cache.k_codes.device)
+            self._keys_stream = ts.cuda_stream
+        elif ts.cuda_stream != self._keys_stream:
+            self._keys.record_stream(ts)
         B.bd_quant_read(s, cache, self._keys[:, :, :s.t_ctx], first_row=0, stream=stream)
         return self._keys
 
