@@ -109,7 +109,9 @@ enum { BD_OP_SELECT = 1, BD_OP_DRAFT = 2, BD_OP_VERIFY = 3, BD_OP_QUANT_DRAFT = 
  *   BD_OP_VERIFY: budget ignored, n_q = queries per head in the block, or the most that
  *                 will be passed (with or without an output);
  *   BD_OP_QUANT_DRAFT, BD_OP_QUANT_VERIFY: like BD_OP_DRAFT and BD_OP_VERIFY, for
- *                 bd_quant_draft_attn and bd_quant_verify_attn (t_ctx may be 0).
+ *                 bd_quant_draft_attn and bd_quant_verify_attn (t_ctx may be 0).  These sizes serve a
+ *                 shape's calls at every t_ctx up to its t_cap, not its own alone (with per-sequence
+ *                 lengths or without, as here).
  * The size depends on the current device's SM count.  Sizes for different ops may
  * be satisfied by one buffer of the largest of them.
  */

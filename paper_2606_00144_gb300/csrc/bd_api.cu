@@ -228,7 +228,7 @@ size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
       for (int n = 1; n <= n_q; ++n) {       // (a shorter block may need more partials than a longer one)
         QuantVerifyPlan qp;
         if (!quant_verify_plan(s, (int)g * n, n, &qp)) return 0;
-        bytes = std::max(bytes, qp.bytes);
+        bytes = std::max(bytes, quant_verify_room(s, (int)g * n));
       }
       return ws_region_offset(units) + bytes;
     }

@@ -221,6 +221,8 @@ struct QuantVerifyPlan {
   size_t bytes;         // op region
 };
 bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* plan);
+// Op region for this many query rows behind any context: the kernel that takes them and how a unit is cut follow the context.
+size_t quant_verify_room(const bd_shape& s, int rows);
 
 // ---------------------------------------------------------------------------- TMA maps
 // 3-D map over a [units, rows_total (stride t_cap), head_dim] bf16 cache: only rows

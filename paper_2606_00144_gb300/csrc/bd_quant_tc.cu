@@ -820,9 +820,13 @@ constexpr int kQtMaxRows = 96;        // query rows of a unit
 
 }  // namespace
 
-bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
+static void cut_rows(int rows, QuantTcPlan* plan) {
   plan->chunks = (rows + kQtMaxRows - 1) / kQtMaxRows;
   plan->nq_rows = (rows + plan->chunks - 1) / plan->chunks;
+}
+
+bool quant_tc_plan(const bd_shape& s, int rows, int n_q, QuantTcPlan* plan) {
+  cut_rows(rows, plan);
   plan->smem = qt_kernel(s.head_dim, plan->nq_rows).smem;
   plan->tiles_per_unit = (int)(((long)s.t_ctx + n_q + kQtKeys - 1) / kQtKeys);
   const long units = (long)s.batch * s.h_kv * plan->chunks, ctas = std::max(1, current_sm_count());
@@ -880,6 +884,17 @@ bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* pl
   if (!plan->on_tc && !w) return false;
   plan->bytes = plan->on_tc ? quant_tc_bytes(s, plan->tc) : quant_attn_bytes(s, rows, plan->warps);
   return true;
+}
+
+size_t quant_verify_room(const bd_shape& s, int rows) {
+  // A unit's tpu tiles lie in at most ceil(tpu / vtpc) + 1 ranges of vtpc >= units (tpu + a) / ctas.
+  QuantTcPlan tc = {};
+  cut_rows(rows, &tc);
+  const long units = (long)s.batch * s.h_kv * tc.chunks, ctas = std::max(1, current_sm_count());
+  tc.max_seg = s.seq_lens ? kVMaxSeg : (int)std::min<long>(kVMaxSeg, (ctas + units - 1) / units + 1);
+  QuantAttnPlan w;
+  const bool on_warps = quant_attn_plan(s, rows, 1, false, &w);   // (its partials do not depend on the entries)
+  return std::max(quant_tc_bytes(s, tc), on_warps ? quant_attn_bytes(s, rows, w) : 0);
 }
 
 cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,

@@ -124,12 +124,17 @@ class QuantSpecStep(SpecStep):
         super().__init__(*args, **kw)
 
     def _workspace(self, device):
+        # for every context up to t_cap: the loop that the step is for grows it (self.shape)
         s = self.shape
-        sizes = [B.bd_workspace_size(s, B.BD_OP_SELECT, self.budget, self.window),
-                 B.bd_workspace_size(s, B.BD_OP_QUANT_DRAFT, self.budget, self.gamma),
+        sizes = [B.bd_workspace_size(s, B.BD_OP_QUANT_DRAFT, self.budget, self.gamma),
                  B.bd_workspace_size(s, B.BD_OP_QUANT_VERIFY, 0, self.gamma + 1)]
-        if min(sizes[1:]) == 0:
+        if min(sizes) == 0:
             raise B.BudgetDraftError("bd_workspace_size", -1)
+        longer = B.BdShape.from_buffer_copy(s)
+        # (a selection's scores grow with the context, the partials of its normalisers with how its 128-key tiles are cut)
+        for t in (s.t_ctx, *range(-(-s.t_ctx // 128) * 128, s.t_cap, 128), s.t_cap):
+            longer.t_ctx = t
+            sizes.append(B.bd_workspace_size(longer, B.BD_OP_SELECT, self.budget, self.window))
         return B.Workspace(max(sizes), device)
 
     def keys(self, cache, stream=None):
