@@ -74,6 +74,13 @@ __device__ __forceinline__ uint32_t code_offset(int r, int g) {
   return D == 128 ? r * 64 + ((g ^ (r >> 1 & 3)) << 4) : r * 32 + ((g ^ (r >> 2 & 1)) << 4);
 }
 
+// Ones in the half of each number that is negative.
+__device__ __forceinline__ uint32_t signs(float lo, float hi) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, 0xffbb;" : "=r"(r) : "r"(__float_as_uint(lo)), "r"(__float_as_uint(hi)));
+  return r;
+}
+
 // WARPS: 4 with three tiles in flight each, or 8 with two for slices of more than a tile a warp.
 template <int D, int NT, int WARPS>
 struct QaSmem {
@@ -380,7 +387,8 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
         for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float w = fast_exp2(s[sub][nt][2 * h + e] + nm);
+            float w = fast_exp2(s[sub][nt][2 * h + e] + nm);
+            if (!GATHER && masked && s[sub][nt][2 * h + e] == -INFINITY) w = -0.f;   // hidden (below)
             s[sub][nt][2 * h + e] = w;
             l[nt][e] = fmaf(w, pow2i(-(int)ve[sub][h]), l[nt][e]);
           }
@@ -404,8 +412,14 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
           const float* w = s[sub][nt];
-          const uint32_t b0 = movmatrix_trans(pack_half2(w[0] * vn[sub][0][g], w[1] * vn[sub][0][g]));
-          const uint32_t b1 = movmatrix_trans(pack_half2(w[2] * vn[sub][1][g], w[3] * vn[sub][1][g]));
+          uint32_t b0 = pack_half2(w[0] * vn[sub][0][g], w[1] * vn[sub][0][g]);
+          uint32_t b1 = pack_half2(w[2] * vn[sub][1][g], w[3] * vn[sub][1][g]);
+          if (!GATHER) {                        // a hidden entry's weight is -0: its product is 0, also with a scale that is no number
+            b0 &= ~signs(w[0], w[1]);
+            b1 &= ~signs(w[2], w[3]);
+          }
+          b0 = movmatrix_trans(b0);
+          b1 = movmatrix_trans(b1);
           const uint32_t w0 = vw[sub][2 * g], w1 = vw[sub][2 * g + 1], x0 = w0 >> 8, x1 = w1 >> 8;
           mma_16816_f16(o[2 * g][nt], centred0(w0), centred1(w0), centred0(w1), centred1(w1), b0, b1);
           mma_16816_f16(o[2 * g + 1][nt], centred0(x0), centred1(x0), centred0(x1), centred1(x1), b0, b1);

@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* qtop = reinterpret_cast<int*>(smem + 64);           // [16]
   int* wtot = reinterpret_cast<int*>(smem + 128);          // [16]
+  int* nan_from = reinterpret_cast<int*>(smem + 192);      // [4] first row of the block (from 1 on) whose V is no number, by group
   int* qpos = reinterpret_cast<int*>(smem + 1024);         // [N] a query row's place in its block
   uint8_t* qbuf = smem + L::FIXED;
   uint8_t* groups = qbuf + L::Q_BYTES;
@@ -363,6 +364,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       top = __reduce_max_sync(0xffffffffu, top);
       if (job > 0) __syncthreads();            // (the segment before has read its own)
       if (lane == 0) qtop[warp] = (int)top;
+      if (tid < 4) nan_from[tid] = 0x7fffffff;
       if (tid < N) qpos[tid] = tid < rows ? (row_base + tid) % p.n_q : 0x7fffffff;
       if (tid < N)
         for (int g = 0; g < GROUPS; ++g) nm_of(g)[tid] = 1e30f;
@@ -411,6 +413,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         kn.load(p.ks + (size_t)(row0 + key) * G, key < end);
         vn.load(p.vs + (size_t)(row0 + key) * G, key < end);
       }
+      const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
       const float a = fminf(base * pow2i(kn.exponent()), 3e38f);
       const int ev = vn.exponent();
       // ---- K: this thread's key into its TMEM lane
@@ -428,6 +431,17 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
         for (int g = 0; g < KG; ++g)
           *reinterpret_cast<__half*>(scale_at + (half * KG + g) * 256) = __float2half_rn(vn.scale(half * KG + g) * vdown);
+        if (masked && key > t_unit) {          // (rare: one tile or two of a unit)
+          // A row of the block that is no number may be hidden from some of the queries, to whom 0 times it would be NaN: it
+          // counts as zeros here, and the queries that see it have NaN written at the segment's end.
+#pragma unroll
+          for (int g = 0; g < KG; ++g)
+            if (!(vn.scale(half * KG + g) < INFINITY)) {
+              *reinterpret_cast<uint16_t*>(scale_at + (half * KG + g) * 256) = 0;
+              atomicMin(nan_from + half * KG + g, key - t_unit);
+            }
+        }
+        __syncwarp();
         if (EARLY) {
           const int next = key + GROUPS * kQtKeys;
           kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
@@ -509,7 +523,6 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 
       // ---- softmax: this thread's key, NC query rows
       const float e = (float)ev;
-      const bool masked = (tb + t + 1) * kQtKeys - 1 > t_unit;
       float ys[NB > 1 ? 2 : 1][BC];            // (of several blocks the next is on its way while one is worked on)
       auto fetch = [&](int nb) { tc_ld_cols<BC>(t_s + lanes + col0 + BC * nb, ys[nb & 1]); };
       // a block of the tile's scores plus e less the running maximum, in log2 units
@@ -664,6 +677,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
     const size_t slot = (size_t)unit * p.max_seg + ((int)blockIdx.x - c_first), orow0 = (size_t)kv_unit * p.rows_total + row_base;
     if ((int)blockIdx.x == c_first && tid == 0 && p.max_seg > 1) p.nseg[unit] = n_seg;
     const int ch = 32 * quad + 4 * (lane & 7) + (lane >> 3);   // this lane's channel
+    const int no_number = nan_from[quad];
     // the groups' states merged, eight columns at a time, the blocks dealt out over the warpgroups: lane k has column c + k
 #pragma unroll 1
     for (int c = 8 * set; c < rows; c += 32) {
@@ -703,8 +717,9 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       for (int k = 0; k < 8; ++k) {
         const int r = c + k;
         if (r < rows) {
-          if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(x[k]);
-          else p.o_part[(slot * p.nq_rows + r) * D + ch] = x[k];
+          const float y = qpos[r] >= no_number ? NAN : x[k];
+          if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(y);
+          else p.o_part[(slot * p.nq_rows + r) * D + ch] = y;
         }
       }
     }
