@@ -62,10 +62,12 @@ __device__ __forceinline__ void cp_async_small(void* dst, const void* src, bool 
 // The exponent that normalises a cache row's V scales: floor(log2) of the largest, within [-100, 126].
 // Scales are taken to fp16 as scale * 2^-e (the largest in [1, 2)) and 2^e joins the row's softmax
 // weight, so that V of any size keeps its precision in fp16.  A row of zeros (or smaller than
-// 2^-100) has -100; a row with a NaN scale 0 (its products are NaN whatever e is).
+// 2^-100) has -100.
 __device__ __forceinline__ int scale_exponent(uint32_t largest_bits) {
-  const int e = (int)((largest_bits >> 7) & 0xffu);
-  return e == 255 ? 0 : min(max(e - 127, -100), 126);
+  return min(max((int)(largest_bits >> 7) - 127, -100), 126);
 }
+// A scale that is no number makes its own group NaN and says nothing about the row's other groups: the largest is that of
+// the numbers.  bits: a scale's, without its sign.
+__device__ __forceinline__ uint32_t if_number(uint32_t bits) { return bits < 0x7f80u ? bits : 0u; }
 
 }  // namespace bd

@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
           kscale[h][g] = bf16_bits_to_float(ksm[r * G + g]);
           const uint32_t v = vsm[r * G + g];
           vn[sub][h][g] = bf16_bits_to_float(v);
-          top = max(top, v & 0x7fffu);
+          top = max(top, if_number(v & 0x7fffu));
         }
         const int e = scale_exponent(top);
         ve[sub][h] = (float)e;

@@ -171,6 +171,11 @@ struct RowScales {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+    if (top >= 0x7f80u) {                      // (rare)
+      top = 0;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) top = max(top, max(if_number(w[i] & 0x7fffu), if_number(w[i] >> 16 & 0x7fffu)));
+    }
     return scale_exponent(top);
   }
   __device__ __forceinline__ float scale(int g) const {
