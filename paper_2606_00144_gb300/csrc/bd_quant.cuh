@@ -63,11 +63,42 @@ __device__ __forceinline__ void cp_async_small(void* dst, const void* src, bool 
 // Scales are taken to fp16 as scale * 2^-e (the largest in [1, 2)) and 2^e joins the row's softmax
 // weight, so that V of any size keeps its precision in fp16.  A row of zeros (or smaller than
 // 2^-100) has -100.
-__device__ __forceinline__ int scale_exponent(uint32_t largest_bits) {
-  return min(max((int)(largest_bits >> 7) - 127, -100), 126);
-}
-// A scale that is no number makes its own group NaN and says nothing about the row's other groups: the largest is that of
-// the numbers.  bits: a scale's, without its sign.
-__device__ __forceinline__ uint32_t if_number(uint32_t bits) { return bits < 0x7f80u ? bits : 0u; }
+__device__ __forceinline__ int scale_exponent(int largest_bits) { return min(max((largest_bits >> 7) - 127, -100), 126); }
+
+// A cache row's scales as they lie: D / 32 bf16.
+template <int D>
+struct RowScales {
+  uint32_t w[D / 64];
+  // from global memory, zero where there is no row
+  __device__ __forceinline__ void load(const uint16_t* p, bool valid) {
+    if constexpr (D == 128) {
+      const uint2 v = valid ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      w[0] = valid ? __ldg(reinterpret_cast<const uint32_t*>(p)) : 0u;
+    }
+  }
+  __device__ __forceinline__ void load_shared(const uint16_t* p) {
+    if constexpr (D == 128) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+  }
+  // scale_exponent of the largest that is a number: one that is not makes its own group NaN and says nothing about the
+  // others (a unit more in the exponent takes it below all numbers, as a signed 16-bit value)
+  __device__ __forceinline__ int exponent() const {
+    uint32_t t = (w[0] & 0x7fff7fffu) + 0x00800080u;
+    if constexpr (D == 128) asm("max.s16x2 %0, %0, %1;" : "+r"(t) : "r"((w[D / 64 - 1] & 0x7fff7fffu) + 0x00800080u));
+    return scale_exponent(max((int)t >> 16, (int)(int16_t)t) - 0x80);
+  }
+  __device__ __forceinline__ float scale(int g) const {
+    const uint32_t x = g < 2 ? w[0] : w[D / 64 - 1];
+    return __uint_as_float(g & 1 ? x & 0xffff0000u : x << 16);
+  }
+};
 
 }  // namespace bd

@@ -311,19 +311,17 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = 16 * sub + 8 * h + gid;
-        uint32_t top = 0;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          kscale[h][g] = bf16_bits_to_float(ksm[r * G + g]);
-          const uint32_t v = vsm[r * G + g];
-          vn[sub][h][g] = bf16_bits_to_float(v);
-          top = max(top, if_number(v & 0x7fffu));
-        }
-        const int e = scale_exponent(top);
+        RowScales<D> ks, vs;
+        ks.load_shared(ksm + r * G);
+        vs.load_shared(vsm + r * G);
+        const int e = vs.exponent();
         ve[sub][h] = (float)e;
         const float down = pow2i(-e);
 #pragma unroll
-        for (int g = 0; g < G; ++g) vn[sub][h][g] *= down;
+        for (int g = 0; g < G; ++g) {
+          kscale[h][g] = ks.scale(g);
+          vn[sub][h][g] = vs.scale(g) * down;
+        }
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {

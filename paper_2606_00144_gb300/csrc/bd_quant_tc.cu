@@ -154,36 +154,6 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// A cache row's scales as they lie (D / 32 bf16), zero where there is no row.
-template <int D>
-struct RowScales {
-  uint32_t w[D / 64];
-  __device__ __forceinline__ void load(const uint16_t* p, bool valid) {
-    if constexpr (D == 128) {
-      const uint2 v = valid ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0u, 0u);
-      w[0] = v.x;
-      w[1] = v.y;
-    } else {
-      w[0] = valid ? __ldg(reinterpret_cast<const uint32_t*>(p)) : 0u;
-    }
-  }
-  __device__ __forceinline__ int exponent() const {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-    if (top >= 0x7f80u) {                      // (rare)
-      top = 0;
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) top = max(top, max(if_number(w[i] & 0x7fffu), if_number(w[i] >> 16 & 0x7fffu)));
-    }
-    return scale_exponent(top);
-  }
-  __device__ __forceinline__ float scale(int g) const {
-    const uint32_t x = g < 2 ? w[0] : w[D / 64 - 1];
-    return __uint_as_float(g & 1 ? x & 0xffff0000u : x << 16);
-  }
-};
-
 __device__ __forceinline__ int quant_tc_context(const int32_t* seq_lens, int b, int t_ctx, int* status) {
   if (seq_lens == nullptr) return t_ctx;
   int t = seq_lens[b];
@@ -446,7 +416,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
               atomicMin(nan_from + half * KG + g, key - t_unit);
             }
         }
-        __syncwarp();
+        if (masked) __syncwarp();
         if (EARLY) {
           const int next = key + GROUPS * kQtKeys;
           kn.load(p.ks + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
@@ -718,13 +688,16 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = fmaf(o[k], __shfl_sync(0xffffffffu, f[g] * inv, k), x[k]);
       }
+      if (no_number != 0x7fffffff) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = qpos[c + k] >= no_number ? NAN : x[k];
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int r = c + k;
         if (r < rows) {
-          const float y = qpos[r] >= no_number ? NAN : x[k];
-          if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(y);
-          else p.o_part[(slot * p.nq_rows + r) * D + ch] = y;
+          if (whole) p.o[(orow0 + r) * D + ch] = __float2bfloat16_rn(x[k]);
+          else p.o_part[(slot * p.nq_rows + r) * D + ch] = x[k];
         }
       }
     }
