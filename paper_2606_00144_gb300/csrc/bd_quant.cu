@@ -34,15 +34,6 @@ struct QuantParams {
   bool wide;                  // every row is 32-byte aligned
 };
 
-__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
-  float2 r;
-  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
-      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-
 // 32 bytes at once, or as two halves where the rows are not 32-byte aligned.  As two halves every access covers half of
 // each 32-byte sector of what a warp touches: reading 8 x 16K rows took 133 us so, 100 as one.
 __device__ __forceinline__ void load32(const void* p, bool wide, uint32_t* w) {

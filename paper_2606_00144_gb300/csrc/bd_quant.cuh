@@ -29,6 +29,15 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 // 2^e for -126 <= e <= 127.
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }
 
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+
 __device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                               uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -62,8 +71,16 @@ __device__ __forceinline__ void cp_async_small(void* dst, const void* src, bool 
 // The exponent that normalises a cache row's V scales: floor(log2) of the largest, within [-100, 126].
 // Scales are taken to fp16 as scale * 2^-e (the largest in [1, 2)) and 2^e joins the row's softmax
 // weight, so that V of any size keeps its precision in fp16.  A row of zeros (or smaller than
-// 2^-100) has -100.
-__device__ __forceinline__ int scale_exponent(int largest_bits) { return min(max((largest_bits >> 7) - 127, -100), 126); }
+// 2^-90) has -90.
+__device__ __forceinline__ int scale_exponent(int largest_bits) { return min(max((largest_bits >> 7) - 127, -90), 126); }
+// The normaliser counts a key by its score alone, 2^S: a row of zeros whose exponent of -90 went into the weight's would be
+// flushed (ex2 ends at 2^-126) beside rows of 2^40 although it may have the highest score.  So only what is above
+// kWeightExponent joins the weight before the sum:
+//   t = 2^(S - M + max(e, -16)),  sum += t 2^-max(e, -16),  weight = t 2^min(e + 16, 0)
+// With V up to 2^92 no key is lost to the sum whose 2^S is above 2^-24 of the largest key's; a sum stays below 2^128 for
+// 2^24 keys of zeros that all trail the maximum by the slack (2^14 2^90 each).  A factor between two maxima may span as
+// much, so it is applied to a sum as two halves.
+constexpr int kWeightExponent = -16;
 
 // A cache row's scales as they lie: D / 32 bf16.
 template <int D>

@@ -7,7 +7,7 @@
 //                                                  group's products leave the MMA centred;
 //   S     = sum_g scale_g D_g                      fp32, exact products of a 4-bit and an 8-bit number;
 //   P_g   = 2^(S - M + e) ns_g                     fp16, ns_g the row's V scale of group g over 2^e
-//                                                  (scale_exponent): 11 bits, where bf16 would keep 8; a
+//                                                  (scale_exponent, kWeightExponent): 11 bits, where bf16 would keep 8; a
 //                                                  weight below 2^-30 of the largest is lost;
 //   O^T_g += (V_codes - 8)^T P_g                   centred before the MMA (one FMA for two codes): with the
 //                                                  offset in, an element whose heavy rows hold zeros is
@@ -296,7 +296,9 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     const int e0 = e_begin + tile * kQaTile;
 
     // ---------------------------------------------------------------- S of two 16-entry sub-tiles
-    float s[2][NT][4], vn[2][2][G], ve[2][2];   // scores; V scales over 2^ve of rows gid, gid + 8
+    // scores; of rows gid, gid + 8: V's exponents e, 2^-u (u = max(e, kWeightExponent)), V scales over 2^u
+    float s[2][NT][4], ve[2][2], un[2][2], vn[2][2][G];
+    bool low = false;                           // some u is above its e
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
       uint32_t kw[2 * G];                       // [group][row half]
@@ -316,11 +318,12 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
         vs.load_shared(vsm + r * G);
         const int e = vs.exponent();
         ve[sub][h] = (float)e;
-        const float down = pow2i(-e);
+        un[sub][h] = pow2i(-max(e, kWeightExponent));
+        low |= e < kWeightExponent;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           kscale[h][g] = ks.scale(g);
-          vn[sub][h][g] = vs.scale(g) * down;
+          vn[sub][h][g] = vs.scale(g) * un[sub][h];
         }
       }
 #pragma unroll
@@ -366,13 +369,26 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
           mx = fmaxf(mx, m[nt][e]);
-          const float alpha = mx == -INFINITY ? 1.f : fast_exp2(m[nt][e] - mx);
+          const float root = mx == -INFINITY ? 1.f : fast_exp2(0.5f * (m[nt][e] - mx)), alpha = root * root;
           m[nt][e] = mx;
-          l[nt][e] *= alpha;
+          l[nt][e] = l[nt][e] * root * root;
 #pragma unroll
           for (int mt = 0; mt < 2 * G; ++mt) {
             o[mt][nt][e] *= alpha;
             o[mt][nt][e + 2] *= alpha;
+          }
+        }
+    }
+    if (__any_sync(0xffffffffu, low)) {         // (rare)
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float rest = fmaxf(ve[sub][h], kWeightExponent) - ve[sub][h];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            s[sub][nt][2 * h] += rest;
+            s[sub][nt][2 * h + 1] += rest;
           }
         }
     }
@@ -388,7 +404,7 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
             float w = fast_exp2(s[sub][nt][2 * h + e] + nm);
             if (!GATHER && masked && s[sub][nt][2 * h + e] == -INFINITY) w = -0.f;   // hidden (below)
             s[sub][nt][2 * h + e] = w;
-            l[nt][e] = fmaf(w, pow2i(-(int)ve[sub][h]), l[nt][e]);
+            l[nt][e] = fmaf(w, un[sub][h], l[nt][e]);
           }
       }
 
@@ -485,9 +501,9 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     for (int w = 0; w < kQaWarps; ++w) {
       const float mw = m_s[w * NQC + r], lw = l_s[w * NQC + r];
       if (mw == -INFINITY && lw == 0.f) continue;              // a warp without entries for this row
-      const float f = fast_exp2(mw - mx);
+      const float root = fast_exp2(0.5f * (mw - mx)), f = root * root;
       const float4 v = *reinterpret_cast<const float4*>(o_s + (size_t)(w * NQC + r) * OP + d);
-      tot = fmaf(f, lw, tot);
+      tot = fmaf(root * lw, root, tot);
       a.x = fmaf(f, v.x, a.x);
       a.y = fmaf(f, v.y, a.y);
       a.z = fmaf(f, v.z, a.z);

@@ -4,7 +4,7 @@
 // around it: both MMAs take the unpacked cache as their A operand from TENSOR MEMORY, written there straight
 // from the registers it is unpacked in, and the few query rows are the N side.
 //   S^T = K Q^T      M = 128 keys, N = 32 (64) query rows, K = D.  A thread unpacks a key's row: lane = key.
-//   P^T = 2^(S^T - M + e), one thread per key; e the exponent of the key's V scales (scale_exponent)
+//   P^T = 2^(S^T - M + e), one thread per key; e the exponent of the key's V scales (scale_exponent, kWeightExponent)
 //   O^T += V^T P^T   M = D, N = query rows, K = 128 keys.  ldmatrix.trans lays a group's 32 channels of two keys
 //                    out as the 16-lane halves of a 16x128b store: lane = channel, column = key pair.
 // Unpacking is a mask and one packed FMA for two codes (bd_quant.cuh): c * 2^-k * scale + (-8 scale 2^-j), rounded
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   uint8_t* my_p = mine + L::WEIGHTS;
   auto red_of = [&](int g) { return reinterpret_cast<int*>(groups + g * L::GROUP + L::EXCHANGE); };   // [N][4] a column's maximum
   auto nm_of = [&](int g) { return reinterpret_cast<float*>(red_of(g) + 4 * N); };   // (or sum) in each warp; [N] lift - running
-  int* my_red = red_of(grp) + 4 * col0;                    // maximum (1e30: none yet); [N] what its last rise scales by
+  int* my_red = red_of(grp) + 4 * col0;                    // maximum (1e30: none yet); [N] the root of what its last rise scales by
   float* my_nm = nm_of(grp) + col0;
   float* my_alpha = my_nm + N;
   const int bar = 1 + grp;
@@ -497,7 +497,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       }
 
       // ---- softmax: this thread's key, NC query rows
-      const float e = (float)ev;
+      const int eu = max(ev, kWeightExponent);  // what joins the weights before their sum (a row below may raise maxima in vain)
+      const float e = (float)eu;
       float ys[NB > 1 ? 2 : 1][BC];            // (of several blocks the next is on its way while one is worked on)
       auto fetch = [&](int nb) { tc_ld_cols<BC>(t_s + lanes + col0 + BC * nb, ys[nb & 1]); };
       // a block of the tile's scores plus e less the running maximum, in log2 units
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           tc_wait_ld();
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float x = masked && key - t_unit > qpos[col0 + c + k] ? -INFINITY : fmaf(z[k], a, e);
+            const float x = masked && key - t_unit > qpos[col0 + c + k] ? -INFINITY : fmaf(z[k], a, (float)ev);
             const int r = __reduce_max_sync(0xffffffffu, ordered(x));
             top = lane == k ? r : top;
           }
@@ -561,13 +562,13 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             const float top = unordered(max(max(r.x, r.y), max(r.z, r.w))), old = my_nm[c];
             const float m = fminf(old, top == -INFINITY ? 1e30f : kQtLift - top);   // (a NaN score is passed over: its row is NaN all the same)
             my_nm[c] = m;
-            my_alpha[c] = fast_exp2(m - old);
+            my_alpha[c] = fast_exp2(0.5f * (m - old));
           }
           __syncwarp();                        // (lanes leave the loop apart)
         }
         named_bar(bar, GT);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) l[c] *= my_alpha[c];
+        for (int c = 0; c < NC; ++c) l[c] = l[c] * my_alpha[c] * my_alpha[c];
         if (t > t_first && has_rows) {         // O holds the group's earlier tiles of the segment
 #pragma unroll 1
           for (int c = 0; c < NC; c += 8) {
@@ -575,14 +576,14 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
             tc_ld_8(t_o + lanes + col0 + c, o);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] *= my_alpha[c + k];
+            for (int k = 0; k < 8; ++k) o[k] *= my_alpha[c + k] * my_alpha[c + k];
             tc_st_8(t_o + lanes + col0 + c, o);
           }
           tc_wait_st();
         }
       }
       {
-        const float el = pow2i(-ev);
+        const float el = pow2i(-eu), rest = pow2i(ev - eu);   // (the rest of ev: multiplied in always, a branch around it took longer)
         if (NB > 1) fetch(0);                  // (a single block is still there)
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -599,7 +600,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
               const float2 z = ffma2(make_float2(x0, x1), make_float2(el, el), make_float2(lc[0], lc[1]));
               lc[0] = z.x;
               lc[1] = z.y;
-              h[k] = pack_half2(x0, x1);
+              const float2 w = fmul2(make_float2(x0, x1), make_float2(rest, rest));
+              h[k] = pack_half2(w.x, w.y);
             }
             const int at = col0 + BC * nb + c;
             *reinterpret_cast<uint4*>(p_row + (H == 1 ? c * 2 ^ p_sw : (at >> 5) * P_BLOCK + ((at & 31) * 2 ^ p_sw))) =
@@ -663,8 +665,9 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
         const int4 r = *reinterpret_cast<const int4*>(red_of(g) + 4 * mc);
-        f[g] = fast_exp2(nm - nm_of(g)[mc]);
-        tot += f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w)));
+        f[g] = fast_exp2(0.5f * (nm - nm_of(g)[mc]));
+        tot += f[g] * (f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w))));
+        f[g] *= f[g];
       }
       const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;       // (V's 2^-7; a NaN stays one)
       if (!alive) continue;
