@@ -348,9 +348,12 @@ int bd_write_block_rows(const bd_shape* shape, int n_rows, const void* k_rows, c
  *     value = (code - 8) * scale
  * A scale of 0 (a group of zeros, or too small for bf16) gives codes of 8; a group that holds a
  * NaN or an infinity has the scale NaN, and all its values are NaN.
- * Any code 0 .. 15 and any scale >= 0 may be in a cache that something else wrote.
+ * Any code 0 .. 15 and any scale of 0 up to 2^127, or NaN, may be in a cache that something else wrote.
  *   k_codes, v_codes    uint8 [batch, h_kv, t_cap, head_dim / 2]
  *   k_scales, v_scales  bf16  [batch, h_kv, t_cap, head_dim / 32]
+ * bd_quant_read gives these values.  The attentions take a group's values to within 2^-19 of the largest scale in its
+ * row, exactly where the group's scale is at least 2^-8 of that; their weights are rounded to 11 bits and end at
+ * 2^-30 of the largest product of a key's weight and its row's largest V scale.
  * All four 16-byte aligned, dense.  The struct is read during a call only.  Rows hold what the
  * rows of a bf16 cache of the same bd_shape hold, and bd_shape means the same; t_ctx, and a
  * sequence's own length, may also be 0 (an empty cache).

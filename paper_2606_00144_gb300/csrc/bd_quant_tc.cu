@@ -8,8 +8,10 @@
 //   O^T += V^T P^T   M = D, N = query rows, K = 128 keys.  ldmatrix.trans lays a group's 32 channels of two keys
 //                    out as the 16-lane halves of a 16x128b store: lane = channel, column = key pair.
 // Unpacking is a mask and one packed FMA for two codes (bd_quant.cuh): c * 2^-k * scale + (-8 scale 2^-j), rounded
-// once, exact but where a group's scale is below 2^-7 of its row's largest.  Each row's scales are divided by a
-// power of two of its own, which joins the scores (K) or the weights (V): fp16 holds any cache.
+// once.  Each row's scales are divided by a power of two of its own, which joins the scores (K) or the weights (V), so that
+// the row's largest fits fp16 whatever it is; a value is off by 2^-19 of that at most, and not at all where its own group's
+// scale is at least 2^-8 of it.  (Exact down to 2^-23, with c - 8 formed before it is multiplied: 24 rows of 64 units of 16K
+// 47.5 us for 43.0, one row 42.1 for 37.3; codes 0 and 2 left where they lie in K, with 2^-16 in place of 2^-19: 42.5, 36.8.)
 //
 // Four warpgroups take the tiles in turn, each through the whole chain with buffers of its own: unpack K, start S,
 // unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
@@ -34,6 +36,8 @@ constexpr int kQtKeys = 128;          // keys of a tile
 constexpr int kQtThreads = 512;
 constexpr int kQtStages = 2;          // tiles of codes in flight for each group
 constexpr float kQtSlack = 8.f;       // log2 of how far a running maximum may trail
+constexpr float kQtScale = 0x1p15f;                  // where a row's largest scale is put in fp16, whose end is 2^16,
+constexpr float kQtOperand = kQtScale * 0x1p-21f;    // and where that leaves a code of 1 times it
 constexpr float kQtLift = 6.f;        // weights are kept 2^6 higher (fp16 reaches further above 1 than P needs)
 
 struct QuantTcParams {
@@ -348,8 +352,8 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < 16; ++k) t = max(t, qtop[k]);
       const int qe = min(max(t - 127, -100), 100);
-      // S over the queries' power of two and the codes' 2^-10, in log2 units (the key's own power comes with it)
-      base = p.scale_log2 * pow2i(qe - 3);
+      // S over the queries' power of two and the operand's, in log2 units (the key's own power comes with it)
+      base = p.scale_log2 / kQtOperand * pow2i(qe - 13);
       const float down = pow2i(13 - qe);
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
@@ -393,7 +397,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       const int ev = vn.exponent();
       // ---- K: this thread's key into its TMEM lane
       {
-        const float down = pow2i(-kn.exponent()) * 0x1p14f;
+        const float down = pow2i(-kn.exponent()) * kQtScale;
         constexpr int KG = G / H;              // groups of 32 elements that this warpgroup unpacks
         uint32_t s0[KG];
 #pragma unroll
@@ -402,7 +406,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           s0[g] = pack_half2(ns, ns);
         }
         // the keys' V scales, laid out by (group, lane of a quad, key pair)
-        const float vdown = pow2i(-ev) * 0x1p14f;
+        const float vdown = pow2i(-ev) * kQtScale;
 #pragma unroll
         for (int g = 0; g < KG; ++g)
           *reinterpret_cast<__half*>(scale_at + (half * KG + g) * 256) = __float2half_rn(vn.scale(half * KG + g) * vdown);
@@ -423,25 +427,28 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
           vn.load(p.vs + (size_t)(row0 + next) * G, next < end && t + GROUPS < n);
         }
         wait(k_full(grp, s), ph);
-        uint4 w[KG];
+        uint4 w[KG];                           // (with several blocks of columns read where they are used: 93 us for 86.5 at 84 rows)
+        auto read = [&](int g) { w[g] = *reinterpret_cast<const uint4*>(k_row + stage + (((half * KG + g) ^ sw) << 4)); };
 #pragma unroll
-        for (int g = 0; g < KG; ++g) w[g] = *reinterpret_cast<const uint4*>(k_row + stage + (((half * KG + g) ^ sw) << 4));
+        for (int g = 0; g < KG; ++g)
+          if (NB == 1) read(g);
         // (the columns' last reader was the P V before)
         if (i > 0) wait(pv_done(grp), (i - 1) & 1);
         tc_fence_after();
 #pragma unroll
         for (int g = 0; g < KG; ++g) {
             const uint32_t s1 = mul_half2(s0[g], 0x2c002c00u);       // 2^-4
-            const uint32_t c = mul_half2(s0[g], 0x80088008u);        // -2^-21: -8 ns 2^-10
+            const uint32_t c = mul_half2(s0[g], 0x80408040u);        // -2^-18: -8 of 2^-21
+            if (NB > 1) read(g);
             const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
             uint32_t out[16];                                        // element pairs (0, 4), (1, 5), (2, 6), (3, 7) of eight
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const uint32_t hi = x[k] >> 8;
-              out[4 * k] = fma_half2(x[k] & kNibble0, s0[g], c);
-              out[4 * k + 1] = fma_half2(x[k] & kNibble1, s1, c);
-              out[4 * k + 2] = fma_half2(hi & kNibble0, s0[g], c);
-              out[4 * k + 3] = fma_half2(hi & kNibble1, s1, c);
+              const uint32_t lo = x[k] << 3, hi = x[k] >> 5;
+              out[4 * k] = fma_half2(lo & 0x00780078u, s0[g], c);    // c 2^-21 * s
+              out[4 * k + 1] = fma_half2(lo & 0x07800780u, s1, c);   // c 2^-17 * s / 16
+              out[4 * k + 2] = fma_half2(hi & 0x00780078u, s0[g], c);
+              out[4 * k + 3] = fma_half2(hi & 0x07800780u, s1, c);
             }
             tc_st_16cols(t_kv + lanes + 16 * (half * KG + g), out);
         }
@@ -483,10 +490,10 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
             for (int k = 0; k < VK; ++k) {
               const uint32_t s0 = sp[k], s1 = mul_half2(s0, 0x2c002c00u);   // 2^-4
-              const uint32_t c = mul_half2(s0, 0x80408040u);                // -2^-18: -8 ns 2^-7
+              const uint32_t c = mul_half2(s0, 0x80408040u);                // -2^-18
               const uint32_t x = w[k] << 3, y = w[k] >> 5;
-              lo[2 * k] = fma_half2(x & 0x00780078u, s0, c);        // c 2^-21 * ns 2^14
-              lo[2 * k + 1] = fma_half2(x & 0x07800780u, s1, c);    // c 2^-17 * ns 2^10
+              lo[2 * k] = fma_half2(x & 0x00780078u, s0, c);
+              lo[2 * k + 1] = fma_half2(x & 0x07800780u, s1, c);
               hi[2 * k] = fma_half2(y & 0x00780078u, s0, c);
               hi[2 * k + 1] = fma_half2(y & 0x07800780u, s1, c);
             }
@@ -669,7 +676,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
         tot += f[g] * (f[g] * ((__int_as_float(r.x) + __int_as_float(r.y)) + (__int_as_float(r.z) + __int_as_float(r.w))));
         f[g] *= f[g];
       }
-      const float inv = tot == 0.f ? 0.f : 0x1p7f / tot;       // (V's 2^-7; a NaN stays one)
+      const float inv = tot == 0.f ? 0.f : 1.f / (kQtOperand * tot);   // (a NaN stays one)
       if (!alive) continue;
       if (quad == 0 && lane < 8 && mc < rows) {
         const float lse = tot == 0.f ? -INFINITY : (log2f(tot) - nm) * kLn2;
