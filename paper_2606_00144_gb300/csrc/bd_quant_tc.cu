@@ -190,7 +190,10 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
   int* qtop = reinterpret_cast<int*>(smem + 64);           // [16]
   int* wtot = reinterpret_cast<int*>(smem + 128);          // [16]
   int* nan_from = reinterpret_cast<int*>(smem + 192);      // [4] first row of the block (from 1 on) whose V is no number, by group
+  int* lifted = reinterpret_cast<int*>(smem + 208);        // whether some query row has a power of two of its own,
   int* qpos = reinterpret_cast<int*>(smem + 1024);         // [N] a query row's place in its block
+  float* qdown = reinterpret_cast<float*>(smem + 1536);    // [N] and what that takes its scores by
+  static_assert(N <= 128, "a row's place and factor");
   uint8_t* qbuf = smem + L::FIXED;
   uint8_t* groups = qbuf + L::Q_BYTES;
   int* pref = reinterpret_cast<int*>(groups + GROUPS * L::GROUP);
@@ -314,13 +317,16 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       kn.load(p.ks + (size_t)(row0 + key) * G, t_first < n && key < end);
       vn.load(p.vs + (size_t)(row0 + key) * G, t_first < n && key < end);
     }
-    // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in
+    // ---- the query rows as B of S: fp16 over one power of two, in the order the codes are unpacked in.  A row whose largest
+    // is below 2^-12 of the block's has its own besides, which its scores are multiplied by: one row's size costs no other
+    // its digits.
     float base;
+    bool own_sizes;
     {
       constexpr int CH = D / 8, PER = (N * CH + kQtThreads - 1) / kQtThreads, STEP = kQtThreads / CH;
       const int r0 = tid / CH, c = tid % CH;
       uint4 w[PER];
-      uint32_t top = 0;
+      uint32_t top = 0, row_top[PER];
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
         const int r = r0 + k * STEP;
@@ -334,16 +340,21 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
         const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        row_top[k] = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t lo = x[e] >> 7 & 0xffu, hi = x[e] >> 23 & 0xffu;
-          top = max(top, max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
+          row_top[k] = max(row_top[k], max(lo == 255 ? 0u : lo, hi == 255 ? 0u : hi));
         }
+#pragma unroll
+        for (int off = 1; off < CH; off *= 2) row_top[k] = max(row_top[k], __shfl_xor_sync(0xffffffffu, row_top[k], off));
+        top = max(top, row_top[k]);
       }
       top = __reduce_max_sync(0xffffffffu, top);
       if (job > 0) __syncthreads();            // (the segment before has read its own)
       if (lane == 0) qtop[warp] = (int)top;
       if (tid < 4) nan_from[tid] = 0x7fffffff;
+      if (tid == 0) *lifted = 0;
       if (tid < N) qpos[tid] = tid < rows ? (row_base + tid) % p.n_q : 0x7fffffff;
       if (tid < N)
         for (int g = 0; g < GROUPS; ++g) nm_of(g)[tid] = 1e30f;
@@ -354,10 +365,13 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       const int qe = min(max(t - 127, -100), 100);
       // S over the queries' power of two and the operand's, in log2 units (the key's own power comes with it)
       base = p.scale_log2 / kQtOperand * pow2i(qe - 13);
-      const float down = pow2i(13 - qe);
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
         const int r = r0 + k * STEP;
+        const int below = qe - ((int)row_top[k] - 127), lift = row_top[k] > 0 && below > 12 ? min(below, min(126, 114 + qe)) : 0;
+        const float down = pow2i(13 - qe + lift);
+        if (c == 0 && r < N) qdown[r] = pow2i(-lift);
+        if (lift > 0) *lifted = 1;
         const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
         float f[8];
 #pragma unroll
@@ -371,6 +385,7 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       }
       fence_proxy_async_smem();
       __syncthreads();
+      own_sizes = *lifted != 0;
     }
 
     float l[NC];                               // sums of this thread's keys' weights
@@ -504,6 +519,19 @@ __global__ void __launch_bounds__(kQtThreads, 1) quant_tc_kernel(const __grid_co
       }
 
       // ---- softmax: this thread's key, NC query rows
+      // (rare; asked of shared memory anew where the sums leave no register for it)
+      if (NB > 1 ? *reinterpret_cast<volatile int*>(lifted) != 0 : own_sizes) {
+#pragma unroll 1
+        for (int c = 0; c < NC; c += 8) {
+          float z[8];
+          tc_ld_8(t_s + lanes + col0 + c, z);
+          tc_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) z[k] *= qdown[col0 + c + k];
+          tc_st_8(t_s + lanes + col0 + c, z);
+        }
+        tc_wait_st();
+      }
       const int eu = max(ev, kWeightExponent);  // what joins the weights before their sum (a row below may raise maxima in vain)
       const float e = (float)eu;
       float ys[NB > 1 ? 2 : 1][BC];            // (of several blocks the next is on its way while one is worked on)
