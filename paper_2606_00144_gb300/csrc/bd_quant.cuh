@@ -5,8 +5,8 @@
 //
 // Codes reach the tensor cores without a conversion: a code in the low bits of an fp16's mantissa
 // is the subnormal c * 2^-24, exactly, and the next one, left where it lies four bits higher, 16 c *
-// 2^-24.  One AND of a 32-bit word that holds two 16-bit units so makes two operands, and four
-// ANDs and a shift unpack eight codes.
+// 2^-24.  One AND of a 32-bit word that holds two 16-bit units and one packed FMA, which brings them
+// to normal numbers less the offset of 8, so make two operands.
 #pragma once
 
 #include <cuda_fp16.h>

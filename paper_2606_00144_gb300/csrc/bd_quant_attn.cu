@@ -2,17 +2,18 @@
 // (bd_quant_draft_attn), and verify blocks (bd_quant_verify_attn).
 //
 // A warp takes tiles of 32 entries of its CTA's slice; K is the A operand (16 entries x 16 elements), the
-// query rows the n8 side, as in the bf16 kernels, and the codes become fp16 operands by masking (bd_quant.cuh):
-//   D_g   = sum over group g of c q - 8 sum q      the -8 sum is the accumulator's first value, so the
-//                                                  group's products leave the MMA centred;
-//   S     = sum_g scale_g D_g                      fp32, exact products of a 4-bit and an 8-bit number;
+// query rows the n8 side, as in the bf16 kernels, and the codes become fp16 operands by a mask and an FMA (bd_quant.cuh):
+//   D_g   = sum over group g of (c - 8) q          exact products of a 4-bit and an 8-bit number;
+//   S     = sum_g scale_g D_g                      fp32;
 //   P_g   = 2^(S - M + e) ns_g                     fp16, ns_g the row's V scale of group g over 2^e
 //                                                  (scale_exponent, kWeightExponent): 11 bits, where bf16 would keep 8; a
 //                                                  weight below 2^-30 of the largest is lost;
-//   O^T_g += (V_codes - 8)^T P_g                   centred before the MMA (one FMA for two codes): with the
-//                                                  offset in, an element whose heavy rows hold zeros is
-//                                                  what is left of a cancellation, to 2^-17 of the weights
-//                                                  (the MMA aligns a subnormal as if its leading zeros counted).
+//   O^T_g += (V_codes - 8)^T P_g                   both centred before the MMA (one FMA for two codes), which aligns
+//                                                  a subnormal as if its leading zeros counted: with the codes
+//                                                  as such and 8 times the rest subtracted, an element whose
+//                                                  heavy rows hold zeros is what is left of a cancellation, to
+//                                                  2^-17 of the weights, and a score is off by 2^-21 of
+//                                                  sum |q k| (2^-24 so).
 // ldmatrix lays a row's 16-byte group out as the A operand of S (a 32-bit word a lane), its transposed form as the
 // A operand of O^T (16-bit units of two rows in a word), so neither side needs a shuffle.
 // M is a running maximum of S + e that may trail by 2^8; each warp keeps its own, and the warps, then the CTAs
@@ -208,9 +209,9 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
   }
   int next_row = at_row[kQaStages - 1];
 
-  // ---- the query rows as B operands: fp16 over a power of two of their own, odd elements over 16 more
+  // ---- the query rows as B operands: fp16 over a power of two of their own
   uint32_t bq[NT][G][4];
-  float bias[NT][G][2], mult[NT][2];
+  float mult[NT][2];
   int lim[NT][2];                              // last visible entry of this lane's columns
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -234,7 +235,6 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int qe = min(max((int)top - 127, -100), 100);        // the row's elements are below 2^(qe + 1)
     const float down = pow2i(13 - qe);                         // to fp16: below 2^14
-    float sums[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const uint32_t x[4] = {w[g].x, w[g].y, w[g].z, w[g].w};
@@ -246,26 +246,15 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
       }
       // element pairs (0, 4), (1, 5), (2, 6), (3, 7): the codes that one mask of a word leaves
       bq[nt][g][0] = pack_half2(f[0], f[4]);
-      bq[nt][g][1] = pack_half2(f[1] * 0.0625f, f[5] * 0.0625f);
+      bq[nt][g][1] = pack_half2(f[1], f[5]);
       bq[nt][g][2] = pack_half2(f[2], f[6]);
-      bq[nt][g][3] = pack_half2(f[3] * 0.0625f, f[7] * 0.0625f);
-      float s = 0.f;                           // of what the MMA will multiply
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&bq[nt][g][e]));
-        s += (h.x + h.y) * (e & 1 ? 16.f : 1.f);
-      }
-      s += __shfl_xor_sync(0xffffffffu, s, 1);
-      s += __shfl_xor_sync(0xffffffffu, s, 2);
-      sums[g] = s;
+      bq[nt][g][3] = pack_half2(f[3], f[7]);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {              // this lane's accumulator columns
       const int src = 4 * (2 * tig + e), col = 8 * nt + 2 * tig + e;
-#pragma unroll
-      for (int g = 0; g < G; ++g) bias[nt][g][e] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], src);
-      // S over the products' 2^-24 and the row's own power of two, in log2 units
-      mult[nt][e] = p.scale_log2 * 0x1p11f * pow2i(__shfl_sync(0xffffffffu, qe, src));
+      // S over the codes' 2^-10 and the row's own power of two, in log2 units
+      mult[nt][e] = p.scale_log2 * pow2i(__shfl_sync(0xffffffffu, qe, src) - 3);
       lim[nt][e] = GATHER || col >= rows ? 0x7fffffff : t_unit + (row0 + col) % p.n_q;
     }
   }
@@ -333,9 +322,9 @@ __global__ void __launch_bounds__(32 * WARPS, NT == 1 ? 16 / WARPS : 1) quant_at
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const uint32_t w0 = kw[2 * g], w1 = kw[2 * g + 1], x0 = w0 >> 8, x1 = w1 >> 8;
-          float d[4] = {bias[nt][g][0], bias[nt][g][1], bias[nt][g][0], bias[nt][g][1]};
-          mma_16816_f16(d, w0 & kNibble0, w1 & kNibble0, w0 & kNibble1, w1 & kNibble1, bq[nt][g][0], bq[nt][g][1]);
-          mma_16816_f16(d, x0 & kNibble0, x1 & kNibble0, x0 & kNibble1, x1 & kNibble1, bq[nt][g][2], bq[nt][g][3]);
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_16816_f16(d, centred0(w0), centred0(w1), centred1(w0), centred1(w1), bq[nt][g][0], bq[nt][g][1]);
+          mma_16816_f16(d, centred0(x0), centred0(x1), centred1(x0), centred1(x1), bq[nt][g][2], bq[nt][g][3]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) s[sub][nt][c] = fmaf(d[c], kscale[c >> 1][g], s[sub][nt][c]);
         }
