@@ -371,7 +371,7 @@ typedef struct bd_quant_cache {
  * prefill's.
  *   dtype           BD_DTYPE_BF16 or BD_DTYPE_F32, of both tensors;
  *   k_rows, v_rows  [batch, h_kv, n_rows, head_dim]; either may be NULL (that tensor of the
- *                   cache is left alone), not both.  16-byte aligned;
+ *                   cache is left alone), not both unless n_rows is 0.  16-byte aligned;
  *   k_strides, v_strides  elements from one sequence, KV head and row to the next (HOST int64
  *                   [3]), or NULL for dense rows; multiples of 16 bytes, not negative; the
  *                   elements of a row are adjacent.  E.g. a projection's [batch, row, head, d].

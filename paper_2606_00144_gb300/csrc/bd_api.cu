@@ -444,7 +444,7 @@ int bd_quant_write(const bd_shape* shape, int n_rows, int dtype, const void* k_r
                    const void* v_rows, const int64_t* v_strides, const bd_quant_cache* cache, void* stream) {
   BD_TRY(check_shape(shape, 0));
   const bd_shape& s = *shape;
-  if (n_rows < 0 || (long long)s.t_ctx + n_rows > s.t_cap || (!k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (n_rows < 0 || (long long)s.t_ctx + n_rows > s.t_cap || (n_rows > 0 && !k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
   if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
   BD_TRY(check_quant_cache(cache, k_rows != nullptr, v_rows != nullptr));
   QuantTensor k, v;
@@ -459,7 +459,7 @@ int bd_quant_read(const bd_shape* shape, int first_row, int n_rows, int dtype, c
   BD_TRY(check_shape(shape, 0));
   const bd_shape& s = *shape;
   const long long first = first_row == BD_QUANT_BLOCK_ROWS ? s.t_ctx : first_row;
-  if (first < 0 || n_rows < 0 || first + n_rows > s.t_cap || (!k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (first < 0 || n_rows < 0 || first + n_rows > s.t_cap || (n_rows > 0 && !k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
   if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
   BD_TRY(check_quant_cache(cache, k_rows != nullptr, v_rows != nullptr));
   QuantTensor k, v;
