@@ -285,6 +285,7 @@ class QuantCache:
         self._struct = BdQuantCache(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
         self._ref = ctypes.byref(self._struct)
         self.is_cuda = k_codes.is_cuda
+        self._gpu = k_codes.get_device() if self.is_cuda else None   # (what no tensor's get_device() equals where it is none)
 
     @classmethod
     def empty(cls, batch, h_kv, t_cap, head_dim, device="cuda"):
@@ -325,7 +326,7 @@ def _refuse_rows(name, want, dtype, *rows):
             raise TypeError(f"{name}: rows must be bf16 or fp32, K and V alike, got {t.dtype}")
         if not t.is_contiguous() and t.stride(3) != 1:
             raise ValueError(f"{name}: the elements of a row must be adjacent")
-    raise ValueError(f"{name}: the rows and the cache must be on the GPU")
+    raise ValueError(f"{name}: the rows and the cache must be on the GPU, the same one")
 
 
 def _quant_rows(name, shape, cache, k_rows, v_rows):
@@ -339,12 +340,12 @@ def _quant_rows(name, shape, cache, k_rows, v_rows):
         _refuse_cache(name, shape)
     dtype = first.dtype
     want = (b, h, first.shape[2] if first.dim() == 4 else -1, d)
-    out = []
+    out, gpu = [], cache._gpu
     for t in (k_rows, v_rows):
         if t is None:
             out += None, None
             continue
-        if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.is_cuda and cache.is_cuda):
+        if not (t.shape == want and t.dtype is dtype and (dtype is _BF16 or dtype is _F32) and t.get_device() == gpu):
             _refuse_rows(name, want, dtype, k_rows, v_rows)
         if t.is_contiguous():
             out += t.data_ptr(), None
@@ -362,7 +363,7 @@ def _refuse(name, **tensors):
             raise TypeError(f"{name}: {what} must be {dtype}, got {t.dtype}")
         if t is not None and (t.shape != shape or not t.is_contiguous()):
             raise ValueError(f"{name}: {what} must be a contiguous {shape} tensor, got {tuple(t.shape)}")
-    raise ValueError(f"{name}: every tensor must be on the GPU")
+    raise ValueError(f"{name}: every tensor must be on the GPU of the cache")
 
 
 def _quant_attn(name, shape, cache, q, o_out, lse_out, n_q, idx=None, count=None, budget=0):
@@ -371,14 +372,14 @@ def _quant_attn(name, shape, cache, q, o_out, lse_out, n_q, idx=None, count=None
     if (b, h, d, cap) != cache._rows:
         _refuse_cache(name, shape)
     want = (b, h_q, d) if n_q is None else (b, h_q, n_q, d)
-    units = (b, h)
+    units, gpu = (b, h), cache._gpu
     if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
-            and o_out.is_contiguous() and q.is_cuda and o_out.is_cuda and cache.is_cuda
+            and o_out.is_contiguous() and q.get_device() == gpu and o_out.get_device() == gpu
             and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
-                                     and lse_out.is_cuda))
+                                     and lse_out.get_device() == gpu))
             and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (b, h, budget)
                                  and count.shape == units and idx.is_contiguous() and count.is_contiguous()
-                                 and idx.is_cuda and count.is_cuda))):
+                                 and idx.get_device() == gpu and count.get_device() == gpu))):
         _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]),
                 idx=(idx, _I32, (*units, budget)), count=(count, _I32, units))
 
