@@ -340,7 +340,9 @@ int bd_write_block_rows(const bd_shape* shape, int n_rows, const void* k_rows, c
 
 /*
  * A 4-bit KV cache (no counterpart in the paper): 3.6 times as many positions in the same
- * memory as bf16, and as much less to read for the attention over it.  A row of head_dim
+ * memory as bf16, and as much less to read for the attention over it (which is some 2 times faster where
+ * reading bounds it, long contexts and up to 32 query rows a KV head, and not where it does not: blocks
+ * of more rows, short contexts and views of some hundred rows take up to half as long again).  A row of head_dim
  * elements x is held as codes, two to a byte (element 2 j in the low half of byte j), and
  * one scale for each group of 32 elements:
  *     scale = bf16(max |x| / 7)

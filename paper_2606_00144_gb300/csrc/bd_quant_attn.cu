@@ -22,8 +22,7 @@
 // A pass is a chain of latencies, not bandwidth (64 units of 512 entries read 5 MB, 0.7 us of HBM), so as few round trips as
 // there are: the view's first indices are fetched beside its count, every warp has a tile or two, and the CTAs of a unit
 // are a cluster that meets in shared memory (long views of few units: several clusters, whose parts the last CTA to
-// arrive merges from global memory, in order).  64 units of 512 entries take 6.8 us, of 2048 13.7, 16 of 2048 9.1, 2 of 256
-// (d 64) 3.5.
+// arrive merges from global memory, in order).  64 units of 512 entries take 6.6 us, of 2048 13.8, 2 of 256 (d 64) 3.6.
 #include <cooperative_groups.h>
 
 #include <algorithm>

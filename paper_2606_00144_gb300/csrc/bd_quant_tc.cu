@@ -16,12 +16,13 @@
 // Four warpgroups take the tiles in turn, each through the whole chain with buffers of its own: unpack K, start S,
 // unpack V while S runs (into K's columns once it is done), softmax, start P V.  Roles of their own (K, V, softmax
 // warps, with two buffers between them) left every warp a chain of waits: 1700 cycles a tile, of which its work
-// was 600.  As it is a tile takes 1200 cycles of an SM, of which each scheduler issues in 740 (64 units of 16K, 24 rows:
-// 42.5 us, 3.6 TB/s; one row 35.8 us, 4.2 TB/s).  A fifth group (up to 8 rows, 96 registers a thread) made that
-// 38.4: more warps to fill the waits are not what it lacks.
+// was 600.  As it is a tile takes some 1240 cycles of an SM, of which each scheduler issues in some 780 (64 units of 16K,
+// 24 rows: 43.7 us, 3.5 TB/s; one row 37.5 us, 4.0 TB/s).  No unit is full (the issue slots 62 %, the ALU pipe 47 %, DRAM
+// 44 %): the rest is waiting along each group's chain, where V takes K's columns once S is done and the next K V's once P V
+// is.  A fifth group of the same chain (up to 8 rows, 96 registers a thread: 38.4 us for 36.2) did not fill it.
 // Blocks of more than 32 query rows run on two groups of two warpgroups: those share a tile's unpacking and halve its
-// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 48.1 us, 68 on
-// four groups; 64 units, 64 rows 69 us, 84 rows 82).
+// columns, so that K and V are unpacked once for up to 96 rows (16 units of 16K, 168 rows in two chunks: 48 us, 68 on
+// four groups, when that was tried; 51 now; 64 units, 64 rows 73 us, 84 rows 86).
 // Work is cut as in verify_kernel (bd_verify.cuh): one list of (unit, 128-key tile) pairs in equal ranges, one CTA
 // per SM, partials merged by quant_merge_kernel.
 #include <algorithm>
@@ -889,11 +890,11 @@ size_t quant_tc_bytes(const bd_shape& s, const QuantTcPlan& plan) {
 
 // The mma.sync kernel starts in a third of the time and streams up to one n8 tile of rows as fast; every chunk of 8 rows
 // reads the cache and unpacks it anew, several clusters of a unit meet in global memory.  So it takes short slices, and of
-// more rows what an SM is soon done with.  mma.sync / tcgen05, us, d 128, 4 rows: 8 units of 1K 5.3 / 7.9, 64 of 4K 16.2 / 17.0, of
-// 8K 25.2 / 23.3, 256 of 2K 24.5 / 28.8, 8 of 8K (four clusters) 11.1 / 10.3; 16 rows: 64 of 1K 11.3 / 13.4, of 4K 25.0 / 20.2, 8 of
-// 8K 14.1 / 12.6; 24 rows: 8 of 1K 7.0 / 9.8, 64 of 0.5K 10.0 / 12.5, of 1K 14.5 / 13.7; 84 rows: 8 of 1K 9.2 / 15.0, 32 of 1K
-// 20.3 / 17.9; d 64: 64 of 16K, 4 rows 26.7 / 31.3, of 4K, 16 rows 15.8 / 19.0, 24 rows 25.6 / 19.4, 8 of 2K, 84 rows 8.5 / 15.7, of
-// 16K, 16 rows 13.0 / 12.2.
+// more rows what an SM is soon done with.  mma.sync / tcgen05, us, d 128, 4 rows: 8 units of 1K 5.3 / 8.2, 64 of 4K 16.3 / 17.9, of
+// 8K 25.6 / 24.3, 256 of 2K 24.8 / 30.6, 8 of 8K (four clusters) 11.3 / 10.6; 16 rows: 64 of 1K 11.3 / 13.6, of 4K 25.4 / 21.0, 8 of
+// 8K 14.2 / 12.9; 24 rows: 8 of 1K 6.9 / 10.1, 64 of 0.5K 10.1 / 12.8, of 1K 14.8 / 14.1; 84 rows: 8 of 1K 9.0 / 15.5, 32 of 1K
+// 21.4 / 18.8; d 64: 64 of 16K, 4 rows 28.0 / 32.8, of 4K, 16 rows 16.6 / 19.7, 24 rows 26.8 / 20.1, 8 of 2K, 84 rows 8.7 / 15.9, of
+// 16K, 16 rows 13.4 / 12.6.
 static bool warps_suit(const bd_shape& s, int rows, int n_q, const QuantAttnPlan& w) {
   const bool wide = s.head_dim == 128, one = w.clusters == 1;
   const long keys = (long)s.t_ctx + n_q;
