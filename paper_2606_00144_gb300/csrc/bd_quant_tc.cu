@@ -799,7 +799,7 @@ __global__ void __launch_bounds__(128) quant_merge_kernel(const float* o_part, c
       const int s = s0 + i * NG + g;
       const float wl = __shfl_sync(0xffffffffu, w0, s & 31), wh = __shfl_sync(0xffffffffu, w1, s & 31);
       const float w = s < 32 ? wl : wh;
-      if (s < n && w != 0.f) {
+      if (s < n) {                             // (an empty part holds zeros; a NaN stays one however little its part weighs)
         a.x = fmaf(w, v[i].x, a.x);
         a.y = fmaf(w, v[i].y, a.y);
         a.z = fmaf(w, v[i].z, a.z);

@@ -69,3 +69,27 @@ def test_draft(d, G, size):
                            budget, j, o, lse, ws)
     rows = torch.cat([idx[0, 0].long(), t + torch.arange(j + 1)])
     check_healthy([x[0, 0] for x in tensors], group, q[0], rows, torch.ones(G, len(rows), dtype=torch.bool), o[0], lse[0], "draft")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n", [(1, 1), (4, 6), (4, 21)])
+@pytest.mark.parametrize("long", [False, True])
+def test_a_row_of_next_to_no_weight(d, G, n, long):
+    """A context row that is NaN is seen by every query, also where another part of the context has all the weight."""
+    t, group = 2000, 1
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(2, 1, t + n, d, generator=g) * 0.1 for _ in range(2))
+    k[:, :, 1700, 0] = 40.0
+    q = torch.randn(2, G, n, d, generator=g) * 0.1
+    q[..., 0] = 100.0                                        # 4000 / sqrt(d): hundreds of nats above the others
+    tensors = [x for y in (k, v) for x in ref.quantise(y.to(BF))]
+    q = q.to(BF)
+    tensors[3][:, 0, 45, group] = math.nan
+    if long:
+        cap = room(G * n, d) + n
+        o, lse = run_lens(widened(tensors, cap), q, cap - n, n, torch.tensor([t, t], dtype=torch.int32, device="cuda"))
+    else:
+        o, lse = run_verify_nan(tensors, q, t, n)
+    visible = torch.arange(t + n)[None, :] <= (t + torch.arange(n).repeat(G))[:, None]
+    for i in range(2):
+        check_healthy([x[i, 0] for x in tensors], group, q[i], slice(0, t + n), visible, o[i], lse[i], f"seq {i}")
