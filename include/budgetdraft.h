@@ -350,7 +350,7 @@ int bd_write_block_rows(const bd_shape* shape, int n_rows, const void* k_rows, c
  *     value = (code - 8) * scale
  * A scale of 0 (a group of zeros, or too small for bf16) gives codes of 8; a group that holds a
  * NaN or an infinity has the scale NaN, and all its values are NaN.
- * Any code 0 .. 15 and any scale of 0 up to 2^127, or NaN, may be in a cache that something else wrote.
+ * Any code 0 .. 15 and any scale from 0 to below 2^127, or NaN, may be in a cache that something else wrote.
  *   k_codes, v_codes    uint8 [batch, h_kv, t_cap, head_dim / 2]
  *   k_scales, v_scales  bf16  [batch, h_kv, t_cap, head_dim / 32]
  * bd_quant_read gives these values.  The attentions take a group's values to within 2^-19 of the largest scale in its
