@@ -23,6 +23,10 @@
  * and a 4-bit form of the caches in four more:
  *   bd_quant_write / bd_quant_read  quantise rows into a 4-bit cache and read them back;
  *   bd_quant_draft_attn / bd_quant_verify_attn  the two attentions over it.
+ * and a paged form of the caches in four more:
+ *   bd_paged_append   rotates new rows to their positions and writes them into their pages;
+ *   bd_paged_read     reads rows back as a dense tensor;
+ *   bd_paged_verify_attn / bd_paged_draft_attn  the two attentions over it.
  * Around them: bd_workspace_size / bd_workspace_status (scratch and device-side
  * errors), bd_draft_attn_static / bd_draft_static_status (bd_draft_attn without a
  * workspace, and its error word),
@@ -96,11 +100,19 @@ typedef struct bd_shape {
   const int32_t* seq_lens;  /* per-sequence lengths [batch] or NULL  */
 } bd_shape;
 
-/* Element types of bd_argmax logits and of the rows bd_quant_write takes and bd_quant_read gives. */
+/* Element types of bd_argmax logits and of the rows bd_quant_write and bd_paged_append take and bd_quant_read gives. */
 enum { BD_DTYPE_BF16 = 1, BD_DTYPE_F32 = 2 };
 
 /* Operation codes for bd_workspace_size. */
-enum { BD_OP_SELECT = 1, BD_OP_DRAFT = 2, BD_OP_VERIFY = 3, BD_OP_QUANT_DRAFT = 4, BD_OP_QUANT_VERIFY = 5 };
+enum {
+  BD_OP_SELECT = 1,
+  BD_OP_DRAFT = 2,
+  BD_OP_VERIFY = 3,
+  BD_OP_QUANT_DRAFT = 4,
+  BD_OP_QUANT_VERIFY = 5,
+  BD_OP_PAGED_DRAFT = 6,
+  BD_OP_PAGED_VERIFY = 7
+};
 
 /*
  * Workspace bytes needed by one operation on `shape` (0 on invalid input).
@@ -111,7 +123,8 @@ enum { BD_OP_SELECT = 1, BD_OP_DRAFT = 2, BD_OP_VERIFY = 3, BD_OP_QUANT_DRAFT = 
  *   BD_OP_QUANT_DRAFT, BD_OP_QUANT_VERIFY: like BD_OP_DRAFT and BD_OP_VERIFY, for
  *                 bd_quant_draft_attn and bd_quant_verify_attn (t_ctx may be 0).  These sizes serve a
  *                 shape's calls at every t_ctx up to its t_cap, not its own alone (with per-sequence
- *                 lengths or without, as here).
+ *                 lengths or without, as here);
+ *   BD_OP_PAGED_DRAFT, BD_OP_PAGED_VERIFY: the same for bd_paged_draft_attn and bd_paged_verify_attn.
  * The size depends on the current device's SM count.  Sizes for different ops may
  * be satisfied by one buffer of the largest of them.
  */
@@ -414,6 +427,110 @@ int bd_quant_draft_attn(const bd_shape* shape, const void* q, const bd_quant_cac
  */
 int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_quant_cache* cache, void* o_out,
                          float* lse_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A paged KV cache (the paper has no counterpart): sequences take memory a page at a time, as they grow.  K and V are
+ * pools of pages, each page page_size rows of every KV head, and a table says which page holds which rows: position p of
+ * sequence b is row p % page_size of page table[b, p / page_size].
+ *   k, v       bf16 pools, 16-byte aligned; the elements of a row are adjacent.
+ *   k_strides, v_strides  elements from one page, KV head and row to the next: [n_pages, h_kv, page_size, head_dim] has
+ *              {h_kv * page_size * head_dim, page_size * head_dim, head_dim}, [n_pages, page_size, h_kv, head_dim] the last
+ *              two the other way round.  Multiples of 8, at least head_dim and below 2^39 where there is more than one.
+ *   page_size  a power of two, at least 16;  n_pages * page_size < 2^31.
+ * The struct is read during a call only.  Calls take the table beside it:
+ *   table      int32 [batch, table_pages] on the device, t_cap <= table_pages * page_size; entries past the pages that a
+ *              call's positions need are not read.
+ * A negative entry stands for a page that is not there (given back, say, behind a sliding window): its positions are
+ * hidden from the attentions, read back as zeros, and not written.  An entry of n_pages or more does the same, and the
+ * attentions record it in the status word (BD_ERR_INVALID_ARG).  Sequences may share pages that are only read.
+ * bd_shape means what it means elsewhere (t_cap: the most positions of a sequence, up to 2^30); t_ctx, and a
+ * sequence's own length, may also be 0, and batch * h_kv may be anything below 2^20, per-sequence lengths or not.  What a
+ * call reads may have been written by the kernel just before it on the stream: no call here starts reading early, but for
+ * BD_DRAFT_VIEW_READY.
+ */
+typedef struct bd_paged_cache {
+  void* k;
+  void* v;
+  int64_t k_strides[3];
+  int64_t v_strides[3];
+  int32_t n_pages;
+  int32_t page_size;
+} bd_paged_cache;
+
+/*
+ * The rotation of queries and keys to their positions (rotary embedding): pair j of a row, j < dim / 2, turns by p
+ * times its frequency at position p, and is multiplied by `scale` (1, or a long-context method's factor).
+ *   turns       uint64 [dim / 2] on the device, 8-byte aligned: pair j's turns a position, a full turn being 2^64; i.e.
+ *               its angular frequency / (2 pi) * 2^64, modulo 2^64.  Angles are p * turns modulo 2^64: exact for
+ *               any position.
+ *   dim         elements of a row that are rotated, the first ones: a multiple of 16 up to head_dim;
+ *   interleaved 0: pair j is elements j and j + dim / 2;  1: elements 2 j and 2 j + 1.
+ */
+typedef struct bd_rope {
+  const uint64_t* turns;
+  int32_t dim;
+  int32_t interleaved;
+  float scale;
+} bd_rope;
+
+/*
+ * New tokens join a paged cache: token i of sequence b has position t_ctx + i (T_b + i with per-sequence lengths).  Its
+ * query and key rows are rotated to that position in fp32 and rounded to bf16 once, its value row is rounded to bf16; the
+ * key and value rows go to their pages, the query rows to q_out.
+ *   dtype      BD_DTYPE_BF16 or BD_DTYPE_F32, of the three sources;
+ *   q_rows, k_rows, v_rows  [batch, heads, n_rows, head_dim], h_q heads of q and h_kv of k and v; any may be NULL (not all,
+ *              unless n_rows is 0).  16-byte aligned;
+ *   *_strides  elements from one sequence, head and row to the next (HOST int64 [3]), or NULL for dense rows; multiples of 16
+ *              bytes, not negative; the elements of a row are adjacent.  E.g. slices of a projection's [token, heads, d];
+ *   row_starts NULL, or int32 [batch + 1] on the device: prompts of unequal lengths, packed.  The tensors are then
+ *              [heads, n_rows, head_dim] (their sequence strides are not used), sequence b has rows row_starts[b] ..
+ *              row_starts[b + 1] - 1, ascending from 0 on.  Rows before the first and behind the last sequence are neither read
+ *              nor written, nor is the row of a position of t_cap or more;
+ *   rope       NULL: rows are written as they are;
+ *   q_out      bf16, of q_rows' shape, 16-byte aligned, q_out_strides as above (between different rows at least head_dim);
+ *              NULL exactly if q_rows is.  It may be q_rows itself, with the same strides.
+ * A T_b outside [0, t_ctx] is clamped.  Constraints: n_rows >= 0 (0 is a no-op); t_ctx + n_rows <= t_cap without
+ * row_starts; batch * n_rows < 2^31 (n_rows with row_starts).  Two tokens must not share a row of the pool.  No workspace.
+ */
+int bd_paged_append(const bd_shape* shape, int n_rows, int dtype, const void* q_rows, const int64_t* q_strides,
+                    const void* k_rows, const int64_t* k_strides, const void* v_rows, const int64_t* v_strides,
+                    const int32_t* row_starts, const bd_rope* rope, const bd_paged_cache* cache, const int32_t* table,
+                    int table_pages, void* q_out, const int64_t* q_out_strides, void* stream);
+
+enum { BD_PAGED_BLOCK_ROWS = -1 };
+
+/*
+ * Reads the context's rows first_row .. first_row + n_rows - 1 of every (sequence, KV head) as bf16 [batch, h_kv, n_rows,
+ * head_dim]; output rows of positions at or past a sequence's length are left as they were.  With first_row =
+ * BD_PAGED_BLOCK_ROWS the rows behind the context, t_ctx (T_b) .. + n_rows - 1.
+ *   k_rows, v_rows  16-byte aligned, either may be NULL, not both unless n_rows is 0; strides as of bd_paged_append, between
+ *              different rows at least head_dim.
+ * Constraints: n_rows >= 0, first_row + n_rows <= t_cap (t_ctx + n_rows for the rows behind the context).  No workspace.
+ */
+int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_paged_cache* cache, const int32_t* table,
+                  int table_pages, void* k_rows, const int64_t* k_strides, void* v_rows, const int64_t* v_strides,
+                  void* stream);
+
+/*
+ * bd_verify_attn over a paged cache (n_q = 1: decoding one token): query i of head h attends to the keys of [0, t_ctx + i]
+ * whose pages are there; one that sees none has o = 0 and lse = -inf.
+ *   q        bf16 [batch, h_q, n_q, d];  o_out bf16 [batch, h_q, n_q, d];
+ *   lse_out  fp32 [batch, h_q, n_q] (may be NULL).
+ * Constraints: 1 <= n_q, t_ctx + n_q <= t_cap, (h_q/h_kv)*n_q <= 768; ws of at least bd_workspace_size(BD_OP_PAGED_VERIFY)
+ * bytes; with per-sequence lengths batch <= 2048.  What a query does not see (rows past its position in its block or in a page, pages that
+ * are not its sequence's) may hold anything, NaN included.  An infinite V element that is seen may count as NaN.
+ */
+int bd_paged_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_paged_cache* cache, const int32_t* table,
+                         int table_pages, void* o_out, float* lse_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * bd_draft_attn over a paged cache: the same arguments, results and constraints, and ws of at least
+ * bd_workspace_size(BD_OP_PAGED_DRAFT) bytes.  Entries of the view whose pages are not there are skipped.  With
+ * BD_DRAFT_VIEW_READY the table is as old as the view.
+ */
+int bd_paged_draft_attn(const bd_shape* shape, const void* q, const bd_paged_cache* cache, const int32_t* table,
+                        int table_pages, const int32_t* idx, const int32_t* count, int budget, int step_j, unsigned flags,
+                        void* o_out, float* lse_out, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Diagnostic of the device-side error path (the paper has no counterpart): launches one

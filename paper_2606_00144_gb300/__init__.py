@@ -13,13 +13,17 @@ from .binding import (  # noqa: F401
     BD_DTYPE_BF16,
     BD_DTYPE_F32,
     BD_OP_DRAFT,
+    BD_OP_PAGED_DRAFT,
+    BD_OP_PAGED_VERIFY,
     BD_OP_QUANT_DRAFT,
     BD_OP_QUANT_VERIFY,
     BD_OP_SELECT,
     BD_OP_VERIFY,
     BdShape,
     BudgetDraftError,
+    PagedCache,
     QuantCache,
+    Rope,
     Workspace,
     bd_accept,
     bd_advance,
@@ -29,6 +33,10 @@ from .binding import (  # noqa: F401
     bd_draft_attn,
     bd_draft_attn_static,
     bd_draft_static_status,
+    bd_paged_append,
+    bd_paged_draft_attn,
+    bd_paged_read,
+    bd_paged_verify_attn,
     bd_quant_draft_attn,
     bd_quant_read,
     bd_quant_verify_attn,
@@ -45,4 +53,4 @@ from .binding import (  # noqa: F401
 )
 from .build import LIB_PATH, build  # noqa: F401
 from .hostio import HostStepIO  # noqa: F401
-from .step import QuantSpecStep, SpecStep  # noqa: F401
+from .step import PagedSpecStep, QuantSpecStep, SpecStep  # noqa: F401

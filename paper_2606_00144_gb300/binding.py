@@ -8,7 +8,9 @@ the library is not built, or an argument is rejected, these functions raise.
 from __future__ import annotations
 
 import ctypes
+import fractions
 import functools
+import math
 import os
 import struct
 
@@ -19,6 +21,8 @@ from .build import LIB_PATH
 BD_OK = 0
 BD_ERR_CUDA = -5
 BD_OP_SELECT, BD_OP_DRAFT, BD_OP_VERIFY, BD_OP_QUANT_DRAFT, BD_OP_QUANT_VERIFY = 1, 2, 3, 4, 5
+BD_OP_PAGED_DRAFT, BD_OP_PAGED_VERIFY = 6, 7
+BD_PAGED_BLOCK_ROWS = -1
 BD_QUANT_BLOCK_ROWS = -1
 BD_QUANT_GROUP = 32
 BD_DRAFT_VIEW_READY = 1
@@ -41,6 +45,16 @@ class BdQuantCache(ctypes.Structure):
                 ("v_scales", ctypes.c_void_p)]
 
 
+class BdPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_strides", ctypes.c_int64 * 3),
+                ("v_strides", ctypes.c_int64 * 3), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class BdRope(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 class BudgetDraftError(RuntimeError):
     def __init__(self, func, status):
         self.status = status
@@ -52,6 +66,8 @@ _P = ctypes.c_void_p
 _SHAPE = ctypes.POINTER(BdShape)
 _QCACHE = ctypes.POINTER(BdQuantCache)
 _STRIDES = ctypes.POINTER(ctypes.c_int64)
+_PCACHE = ctypes.POINTER(BdPagedCache)
+_ROPE = ctypes.POINTER(BdRope)
 _SIGNATURES = {
     "bd_workspace_size": (ctypes.c_size_t, [_SHAPE, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
     "bd_select_budget": (ctypes.c_int, [_SHAPE, _P, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int,
@@ -75,6 +91,14 @@ _SIGNATURES = {
     "bd_quant_draft_attn": (ctypes.c_int, [_SHAPE, _P, _QCACHE, _P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_uint, _P,
                                            _P, _P, ctypes.c_size_t, _P]),
     "bd_quant_verify_attn": (ctypes.c_int, [_SHAPE, _P, ctypes.c_int, _QCACHE, _P, _P, _P, ctypes.c_size_t, _P]),
+    "bd_paged_append": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, _P, _STRIDES, _P, _STRIDES, _P, _STRIDES, _P,
+                                       _ROPE, _PCACHE, _P, ctypes.c_int, _P, _STRIDES, _P]),
+    "bd_paged_read": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, _PCACHE, _P, ctypes.c_int, _P, _STRIDES, _P,
+                                     _STRIDES, _P]),
+    "bd_paged_verify_attn": (ctypes.c_int, [_SHAPE, _P, ctypes.c_int, _PCACHE, _P, ctypes.c_int, _P, _P, _P,
+                                            ctypes.c_size_t, _P]),
+    "bd_paged_draft_attn": (ctypes.c_int, [_SHAPE, _P, _PCACHE, _P, ctypes.c_int, _P, _P, ctypes.c_int, ctypes.c_int,
+                                           ctypes.c_uint, _P, _P, _P, ctypes.c_size_t, _P]),
     "bd_check_wait_timeout": (ctypes.c_int, [_P, ctypes.c_size_t, ctypes.c_int, _P]),
     "bd_workspace_status": (ctypes.c_int, [_P, _P]),
     "bd_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -420,6 +444,213 @@ def bd_quant_verify_attn(shape, q, n_q, cache: QuantCache, o_out, lse_out, ws: W
     st = (_lib or library()).bd_quant_verify_attn(ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, o_out.data_ptr(), _ptr(lse_out),
                                                   ws.ptr, ws.nbytes, _stream(stream))
     _check("bd_quant_verify_attn", st)
+
+
+class PagedCache:
+    """A pool of pages (the header has the layout): bf16 K and V tensors [n_pages, h_kv, page_size, head_dim] of any strides
+    of whole 16 bytes whose rows' elements are adjacent, e.g. x.transpose(1, 2) of an [n_pages, page_size, h_kv, head_dim]
+    pool.  The tensors stay the caller's.  Calls take the batch's table of pages beside it: int32 [batch, pages] on the same
+    GPU, dense, negative where a page is not there."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape:
+            raise ValueError("PagedCache: K and V must be [n_pages, h_kv, page_size, head_dim], alike")
+        if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+            raise TypeError("PagedCache: K and V are bf16")
+        if k.device != v.device:
+            raise ValueError("PagedCache: K and V must be on one device")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("PagedCache: the elements of a row must be adjacent")
+        self.n_pages, self.h_kv, self.page_size, self.head_dim = (int(x) for x in k.shape)
+        if self.head_dim not in (64, 128):
+            raise ValueError("PagedCache: head_dim must be 64 or 128")
+        if self.page_size < 16 or self.page_size & (self.page_size - 1):
+            raise ValueError("PagedCache: page_size must be a power of two, at least 16")
+        self.k, self.v = k, v
+        self._struct = BdPagedCache(k.data_ptr(), v.data_ptr(), (ctypes.c_int64 * 3)(*k.stride()[:3]),
+                                    (ctypes.c_int64 * 3)(*v.stride()[:3]), self.n_pages, self.page_size)
+        self._ref = ctypes.byref(self._struct)
+        self.is_cuda = k.is_cuda
+        self._gpu = k.get_device() if self.is_cuda else None
+
+    @classmethod
+    def empty(cls, n_pages, h_kv, page_size, head_dim, device="cuda"):
+        """A pool whose pages are not written yet."""
+        return cls(*(torch.empty(n_pages, h_kv, page_size, head_dim, dtype=torch.bfloat16, device=device) for _ in "kv"))
+
+    def shape(self, batch: int, h_q: int, t_ctx: int, t_cap: int, seq_lens=None) -> BdShape:
+        return make_shape(batch, h_q, self.h_kv, self.head_dim, t_ctx, t_cap, seq_lens)
+
+    @property
+    def nbytes(self) -> int:
+        return 2 * self.k.numel() * 2
+
+
+class Rope:
+    """The rotation of rows to their positions (the header's bd_rope).  inv_freq: the angular frequency of each pair of a
+    row's first 2 * len(inv_freq) elements (a tensor or a sequence, taken in 64 bits); interleaved: pairs are elements
+    (2 j, 2 j + 1), else (j, j + dim / 2); scale: a factor on the rotated rows (a long-context method's)."""
+
+    def __init__(self, inv_freq, interleaved=False, scale=1.0, device=None):
+        if device is None:
+            device = inv_freq.device if isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda else "cuda"
+        freq = torch.as_tensor(inv_freq, dtype=torch.float64).cpu()
+        if freq.dim() != 1 or freq.numel() == 0 or freq.numel() % 8 or freq.numel() > 64:
+            raise ValueError("Rope: inv_freq must hold a frequency for each of 8, 16, ... 64 pairs")
+        if not torch.isfinite(freq).all() or not math.isfinite(scale):
+            raise ValueError("Rope: frequencies and scale must be finite")
+        turns = [round(fractions.Fraction(w) / _TWO_PI * 2**64) % 2**64 for w in freq.tolist()]
+        self.turns = torch.tensor([x - 2**64 if x >= 2**63 else x for x in turns], dtype=torch.int64, device=device)
+        self.dim, self.interleaved, self.scale = 2 * freq.numel(), bool(interleaved), float(scale)
+        self._struct = BdRope(self.turns.data_ptr(), self.dim, int(self.interleaved), self.scale)
+        self._ref = ctypes.byref(self._struct)
+        self._gpu = self.turns.get_device() if self.turns.is_cuda else None
+
+    @classmethod
+    def of_base(cls, dim, base=10000.0, **kw):
+        """Pair j of dim / 2 turns by base^(-2 j / dim) a position."""
+        return cls([base ** (-2.0 * j / dim) for j in range(dim // 2)], **kw)
+
+
+# 2 pi to 35 digits: a frequency of 64 bits keeps all of them
+_TWO_PI = fractions.Fraction(628318530717958647692528676655900577, 10**35)
+
+
+def _paged_call(name, gpu, stream, fn, *args):
+    if torch._C._cuda_getDevice() == gpu:
+        st = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(gpu):
+            st = fn(*args, _stream(stream))
+    _check(name, st)
+
+
+def _paged_table(name, shape, cache, table):
+    """Checks the cache and the table; the shape's sizes."""
+    b, h_q, h, d, t_ctx, t_cap = _shape_ints(shape)
+    if (h, d) != (cache.h_kv, cache.head_dim):
+        _refuse_cache(name, shape)
+    if not (table.dtype is _I32 and table.dim() == 2 and table.shape[0] == b and table.is_contiguous()
+            and table.get_device() == cache._gpu):
+        if table.dtype is not _I32:
+            raise TypeError(f"{name}: the table must be int32, got {table.dtype}")
+        if table.dim() != 2 or table.shape[0] != b or not table.is_contiguous():
+            raise ValueError(f"{name}: the table must be a contiguous [{b}, pages] tensor, got {tuple(table.shape)}")
+        raise ValueError(f"{name}: every tensor must be on the GPU of the cache")
+    return b, h_q, h, d
+
+
+def _paged_rows(name, cache, t, want, *dtypes):
+    """Checks rows of this shape (None: any); their pointer and strides (None where they are dense)."""
+    if t is None:
+        return None, None
+    if not (t.shape == want and t.dtype in dtypes and t.get_device() == cache._gpu and (t.is_contiguous() or t.stride(-1) == 1)):
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name}: rows must be {' or '.join(str(x) for x in dtypes)}, got {t.dtype}")
+        if t.shape != want:
+            raise ValueError(f"{name}: rows must be {tuple(want)}, got {tuple(t.shape)}")
+        if t.get_device() != cache._gpu:
+            raise ValueError(f"{name}: every tensor must be on the GPU of the cache")
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if t.is_contiguous():
+        return t.data_ptr(), None
+    st = t.stride()
+    return t.data_ptr(), _stride_array(*(st[:3] if len(st) == 4 else (0, st[0], st[1])))
+
+
+def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, table, q_out, row_starts=None, stream=None):
+    """New tokens join a paged cache behind each sequence's context: queries and keys are rotated to their positions (rope: a
+    Rope, or None), keys and values written into their pages, queries into q_out (bf16).  Rows are [batch, heads, n,
+    head_dim], or with row_starts (int32 [batch + 1] on the GPU) packed [heads, rows, head_dim]; bf16 or fp32, any strides
+    of whole 16 bytes; any of q_rows (with q_out), k_rows and v_rows may be None."""
+    name = "bd_paged_append"
+    b, h_q, h, d = _paged_table(name, shape, cache, table)
+    first = next((t for t in (q_rows, k_rows, v_rows) if t is not None), None)
+    if first is None:
+        raise ValueError(f"{name}: rows of queries, keys or values")
+    if (q_rows is None) != (q_out is None):
+        raise ValueError(f"{name}: q_rows and q_out come together")
+    dtype = first.dtype
+    if dtype is not _BF16 and dtype is not _F32:
+        raise TypeError(f"{name}: rows must be bf16 or fp32, got {dtype}")
+    if row_starts is None:
+        if first.dim() != 4:
+            raise ValueError(f"{name}: rows must be [batch, heads, n, head_dim], got {tuple(first.shape)}")
+        n = first.shape[2]
+        want_q, want_kv = (b, h_q, n, d), (b, h, n, d)
+    else:
+        if first.dim() != 3:
+            raise ValueError(f"{name}: packed rows must be [heads, rows, head_dim], got {tuple(first.shape)}")
+        n = first.shape[1]
+        want_q, want_kv = (h_q, n, d), (h, n, d)
+        if not (row_starts.dtype is _I32 and row_starts.shape == (b + 1,) and row_starts.is_contiguous()
+                and row_starts.get_device() == cache._gpu):
+            _refuse(name, row_starts=(row_starts, _I32, (b + 1,)))
+    q, qs = _paged_rows(name, cache, q_rows, want_q, dtype)
+    k, ks = _paged_rows(name, cache, k_rows, want_kv, dtype)
+    v, vs = _paged_rows(name, cache, v_rows, want_kv, dtype)
+    o, os_ = _paged_rows(name, cache, q_out, want_q, _BF16)
+    if rope is not None and (rope._gpu != cache._gpu or rope.dim > d):
+        raise ValueError(f"{name}: the rotation must be of at most head_dim elements, on the GPU of the cache")
+    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_append, ctypes.byref(shape), n,
+                BD_DTYPE_BF16 if dtype is _BF16 else BD_DTYPE_F32, q, qs, k, ks, v, vs, _ptr(row_starts),
+                None if rope is None else rope._ref, cache._ref, table.data_ptr(), table.shape[1], o, os_)
+
+
+def bd_paged_read(shape, cache: PagedCache, table, k_out, v_out=None, first_row=None, stream=None):
+    """Reads the context's rows first_row .. first_row + n - 1 (None: those behind the context) into bf16 [batch, h_kv, n,
+    head_dim] tensors; either may be None.  Rows of positions at or past a sequence's length are left as they were, those whose
+    page is not there are zeros."""
+    name = "bd_paged_read"
+    b, _, h, d = _paged_table(name, shape, cache, table)
+    first = k_out if k_out is not None else v_out
+    if first is None:
+        raise ValueError(f"{name}: K rows, V rows or both")
+    if first_row is None:
+        first_row = BD_PAGED_BLOCK_ROWS
+    elif first_row < 0:
+        raise ValueError(f"{name}: first_row must not be negative")
+    if first.dim() != 4:
+        raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim], got {tuple(first.shape)}")
+    n = first.shape[2]
+    k, ks = _paged_rows(name, cache, k_out, (b, h, n, d), _BF16)
+    v, vs = _paged_rows(name, cache, v_out, (b, h, n, d), _BF16)
+    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_read, ctypes.byref(shape), first_row, n, cache._ref,
+                table.data_ptr(), table.shape[1], k, ks, v, vs)
+
+
+def _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, n_q, idx=None, count=None, budget=0):
+    """Checks an attention's tensors (of a drafter pass where n_q is None)."""
+    b, h_q, h, d = _paged_table(name, shape, cache, table)
+    want = (b, h_q, d) if n_q is None else (b, h_q, n_q, d)
+    gpu = cache._gpu
+    if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
+            and o_out.is_contiguous() and q.get_device() == gpu and o_out.get_device() == gpu and ws.buf.get_device() == gpu
+            and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
+                                     and lse_out.get_device() == gpu))
+            and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (b, h, budget)
+                                 and count.shape == (b, h) and idx.is_contiguous() and count.is_contiguous()
+                                 and idx.get_device() == gpu and count.get_device() == gpu))):
+        _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]),
+                idx=(idx, _I32, (b, h, budget)), count=(count, _I32, (b, h)))
+
+
+def bd_paged_verify_attn(shape, q, n_q, cache: PagedCache, table, o_out, lse_out, ws: Workspace, stream=None):
+    """bd_verify_attn over a paged cache; n_q = 1 decodes one token."""
+    name = "bd_paged_verify_attn"
+    _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, n_q)
+    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_verify_attn, ctypes.byref(shape), q.data_ptr(), n_q, cache._ref,
+                table.data_ptr(), table.shape[1], o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes)
+
+
+def bd_paged_draft_attn(shape, q, cache: PagedCache, table, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
+                        stream=None, flags=0):
+    """bd_draft_attn over a paged cache."""
+    name = "bd_paged_draft_attn"
+    _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, None, idx, count, budget)
+    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_draft_attn, ctypes.byref(shape), q.data_ptr(), cache._ref,
+                table.data_ptr(), table.shape[1], idx.data_ptr(), count.data_ptr(), budget, step_j, flags, o_out.data_ptr(),
+                _ptr(lse_out), ws.ptr, ws.nbytes)
 
 
 def bd_check_wait_timeout(ws: Workspace, limit_us: int, stream=None):

@@ -94,6 +94,24 @@ cudaError_t make_codes_map(CUtensorMap* map, const void* base, int units, int t_
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t make_paged_map(CUtensorMap* map, const void* base, const int64_t* strides, int head_dim, int h_kv, int page_size,
+                           int n_pages, int box_rows, int box_halves) {
+  auto fn = encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t halves = (cuuint64_t)head_dim / 64;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)page_size, halves, (cuuint64_t)h_kv, (cuuint64_t)n_pages};
+  // (the stride of a dimension of one is never used, but has to be one)
+  const cuuint64_t row = 2 * (cuuint64_t)strides[2], head = h_kv > 1 ? 2 * (cuuint64_t)strides[1] : 256,
+                   page = n_pages > 1 ? 2 * (cuuint64_t)strides[0] : 256;
+  const cuuint64_t bytes[4] = {row, 128, head, page};
+  const cuuint32_t box[5] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_halves, 1, 1};
+  const cuuint32_t estride[5] = {1, 1, 1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, bytes, box, estride,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 cudaError_t make_rows_map(CUtensorMap* map, const void* base, long long n_rows, int head_dim, int box_rows) {
   auto fn = encode_fn();
   if (!fn) return cudaErrorNotSupported;
@@ -183,11 +201,87 @@ int quant_rows(const bd_shape& s, const void* rows, const int64_t* strides, int 
   return check_tensor(rows, 16);
 }
 
+// ---- paged caches
+
+constexpr int kPagedMaxRows = 768;        // query rows of a KV head in one block
+
+int check_paged_shape(const bd_shape* s) {
+  if (!s) return BD_ERR_INVALID_ARG;
+  if (s->batch < 1 || s->h_q < 1 || s->h_kv < 1 || s->h_q % s->h_kv != 0 || s->t_ctx < 0 || s->t_cap < s->t_ctx)
+    return BD_ERR_INVALID_ARG;
+  if (s->head_dim != 64 && s->head_dim != 128) return BD_ERR_UNSUPPORTED;
+  if (s->t_cap > (1 << 30) || (long long)s->batch * s->h_kv >= 1 << 20 || s->h_q >= 1 << 16) return BD_ERR_UNSUPPORTED;
+  if (s->seq_lens && !aligned(s->seq_lens, 4)) return BD_ERR_MISALIGNED;
+  return BD_OK;
+}
+
+// A pool's tensors, of K and / or V, and the table.
+int check_paged_cache(const bd_shape& s, const bd_paged_cache* c, const int32_t* table, int table_pages, bool k, bool v) {
+  if (!c) return BD_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->page_size < 1 || table_pages < 1) return BD_ERR_INVALID_ARG;
+  if (c->page_size < 16 || (c->page_size & (c->page_size - 1)) != 0 || (long long)c->n_pages * c->page_size >= 1LL << 31)
+    return BD_ERR_UNSUPPORTED;
+  if ((long long)table_pages * c->page_size < s.t_cap) return BD_ERR_INVALID_ARG;
+  const int size[3] = {c->n_pages, s.h_kv, c->page_size};
+  for (int w = 0; w < 2; ++w) {
+    if (!(w ? v : k)) continue;
+    BD_TRY(check_tensor(w ? c->v : c->k, 16));
+    const int64_t* st = w ? c->v_strides : c->k_strides;
+    for (int i = 0; i < 3; ++i) {
+      if (size[i] == 1) continue;
+      if (st[i] < s.head_dim || st[i] >= (int64_t)1 << 39) return BD_ERR_INVALID_ARG;
+      if (st[i] % 8 != 0) return BD_ERR_MISALIGNED;
+    }
+  }
+  return check_tensor(table, 4);
+}
+
+// The rows of one tensor of an append or a read: [batch, heads, n_rows, d], or packed [heads, n_rows, d]; dense where strides is
+// null.  Different rows of a destination must not overlap.
+int paged_rows(const bd_shape& s, int heads, const void* rows, const int64_t* strides, int n_rows, int elem_bytes, bool packed,
+               bool written, RowTensor* t) {
+  t->rows = const_cast<void*>(rows);
+  t->sb = t->sh = t->sn = 0;
+  if (!rows) return BD_OK;
+  const int64_t d = s.head_dim, n = std::max(n_rows, 1), dense[3] = {heads * n * d, n * d, d};
+  const int64_t* st = strides ? strides : dense;
+  const int64_t vec = 16 / elem_bytes, size[3] = {packed ? 1 : s.batch, heads, n_rows};
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] <= 1) continue;
+    if (st[i] < 0 || st[i] >= (int64_t)1 << 40 || (written && st[i] < d)) return BD_ERR_INVALID_ARG;
+    if (st[i] % vec != 0) return BD_ERR_MISALIGNED;
+  }
+  t->sb = size[0] > 1 ? st[0] : 0;
+  t->sh = size[1] > 1 ? st[1] : 0;
+  t->sn = size[2] > 1 ? st[2] : 0;
+  return check_tensor(rows, 16);
+}
+
+size_t paged_workspace(const bd_shape* shape, int op, int budget, int n_q) {
+  if (check_paged_shape(shape) != BD_OK || n_q < 1) return 0;
+  const bd_shape& s = *shape;
+  const long long g = s.h_q / s.h_kv, units = (long long)s.batch * s.h_kv;
+  if (op == BD_OP_PAGED_DRAFT) {
+    DraftPlan dp;
+    if (budget < 1 || units > 65535 || !draft_plan(s, budget, n_q, SIZE_MAX, &dp)) return 0;
+    return ws_region_offset((int)units) + draft_region_bytes(s);
+  }
+  if (g * n_q > kPagedMaxRows) return 0;
+  size_t bytes = 0;
+  for (int n = 1; n <= n_q; ++n) {           // (a shorter block may need more partials than a longer one)
+    PagedVerifyPlan pp;
+    if (!paged_verify_plan(s, (int)g * n, n, &pp)) return 0;
+    bytes = std::max(bytes, paged_verify_room(s, (int)g * n));
+  }
+  return ws_region_offset((int)units) + bytes;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t bd_workspace_size(const bd_shape* shape, int op, int budget, int n_q) {
+  if (op == BD_OP_PAGED_DRAFT || op == BD_OP_PAGED_VERIFY) return paged_workspace(shape, op, budget, n_q);
   if (check_shape(shape, op == BD_OP_QUANT_VERIFY || op == BD_OP_QUANT_DRAFT ? 0 : 1) != BD_OK) return 0;
   const bd_shape& s = *shape;
   const int units = s.batch * s.h_kv;
@@ -515,6 +609,97 @@ int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (qp.on_tc) return map_cuda(launch_quant_tc(s, qp.tc, call, *cache, region(ws, units), status_word(ws), st));
   return map_cuda(launch_quant_attn(s, qp.warps, call, *cache, region(ws, units), counters(ws), status_word(ws), st));
+}
+
+int bd_paged_append(const bd_shape* shape, int n_rows, int dtype, const void* q_rows, const int64_t* q_strides,
+                    const void* k_rows, const int64_t* k_strides, const void* v_rows, const int64_t* v_strides,
+                    const int32_t* row_starts, const bd_rope* rope, const bd_paged_cache* cache, const int32_t* table,
+                    int table_pages, void* q_out, const int64_t* q_out_strides, void* stream) {
+  BD_TRY(check_paged_shape(shape));
+  const bd_shape& s = *shape;
+  const bool packed = row_starts != nullptr;
+  if (n_rows < 0 || (n_rows > 0 && !q_rows && !k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (!packed && (long long)s.t_ctx + n_rows > s.t_cap) return BD_ERR_INVALID_ARG;
+  if (!packed && (long long)s.batch * n_rows >= 1LL << 31) return BD_ERR_UNSUPPORTED;
+  if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
+  if ((q_rows == nullptr) != (q_out == nullptr)) return BD_ERR_INVALID_ARG;
+  if (packed && !aligned(row_starts, 4)) return BD_ERR_MISALIGNED;
+  if (rope) {
+    if (rope->dim < 16 || rope->dim > s.head_dim || rope->dim % 16 != 0 || (rope->interleaved != 0 && rope->interleaved != 1))
+      return BD_ERR_INVALID_ARG;
+    BD_TRY(check_tensor(rope->turns, 8));
+  }
+  BD_TRY(check_paged_cache(s, cache, table, table_pages, k_rows != nullptr, v_rows != nullptr));
+  const int bytes = dtype == BD_DTYPE_F32 ? 4 : 2;
+  RowTensor q, k, v, o;
+  BD_TRY(paged_rows(s, s.h_q, q_rows, q_strides, n_rows, bytes, packed, false, &q));
+  BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, bytes, packed, false, &k));
+  BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, bytes, packed, false, &v));
+  BD_TRY(paged_rows(s, s.h_q, q_out, q_out_strides, n_rows, 2, packed, true, &o));
+  if (n_rows == 0) return BD_OK;
+  return map_cuda(launch_paged_append(s, n_rows, dtype, q, k, v, row_starts, rope, *cache, table, table_pages, o,
+                                      static_cast<cudaStream_t>(stream)));
+}
+
+int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_paged_cache* cache, const int32_t* table,
+                  int table_pages, void* k_rows, const int64_t* k_strides, void* v_rows, const int64_t* v_strides,
+                  void* stream) {
+  BD_TRY(check_paged_shape(shape));
+  const bd_shape& s = *shape;
+  const long long first = first_row == BD_PAGED_BLOCK_ROWS ? s.t_ctx : first_row;
+  if (first < 0 || n_rows < 0 || first + n_rows > s.t_cap || (n_rows > 0 && !k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  BD_TRY(check_paged_cache(s, cache, table, table_pages, k_rows != nullptr, v_rows != nullptr));
+  RowTensor k, v;
+  BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, 2, false, true, &k));
+  BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, 2, false, true, &v));
+  if ((n_rows / 128 + 1LL) * s.batch * s.h_kv * 2 >= 1LL << 31) return BD_ERR_UNSUPPORTED;   // (CTAs)
+  if (n_rows == 0) return BD_OK;
+  return map_cuda(launch_paged_read(s, first_row, n_rows, *cache, table, table_pages, k, v, static_cast<cudaStream_t>(stream)));
+}
+
+int bd_paged_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_paged_cache* cache, const int32_t* table,
+                         int table_pages, void* o_out, float* lse_out, void* ws, size_t ws_bytes, void* stream) {
+  BD_TRY(check_paged_shape(shape));
+  const bd_shape& s = *shape;
+  BD_TRY(check_tensor(q, 16));
+  BD_TRY(check_tensor(o_out, 16));
+  if (lse_out) BD_TRY(check_tensor(lse_out, 4));
+  if (n_q < 1 || (long long)s.t_ctx + n_q > s.t_cap) return BD_ERR_INVALID_ARG;
+  BD_TRY(check_paged_cache(s, cache, table, table_pages, true, true));
+  const long long rows = (long long)(s.h_q / s.h_kv) * n_q;
+  const int units = s.batch * s.h_kv;
+  PagedVerifyPlan pp;
+  if (rows > kPagedMaxRows || !paged_verify_plan(s, (int)rows, n_q, &pp)) return BD_ERR_UNSUPPORTED;
+  if (!ws) return BD_ERR_WORKSPACE;
+  if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
+  if (ws_bytes < ws_region_offset(units) + paged_verify_bytes(s, pp)) return BD_ERR_WORKSPACE;
+  return map_cuda(launch_paged_verify(s, pp, (int)rows, n_q, q, *cache, table, table_pages, o_out, lse_out, region(ws, units),
+                                      status_word(ws), static_cast<cudaStream_t>(stream)));
+}
+
+int bd_paged_draft_attn(const bd_shape* shape, const void* q, const bd_paged_cache* cache, const int32_t* table,
+                        int table_pages, const int32_t* idx, const int32_t* count, int budget, int step_j, unsigned flags,
+                        void* o_out, float* lse_out, void* ws, size_t ws_bytes, void* stream) {
+  BD_TRY(check_paged_shape(shape));
+  const bd_shape& s = *shape;
+  BD_TRY(check_tensor(q, 16));
+  BD_TRY(check_tensor(idx, 4));
+  BD_TRY(check_tensor(count, 4));
+  BD_TRY(check_tensor(o_out, 16));
+  if (lse_out) BD_TRY(check_tensor(lse_out, 4));
+  if (budget < 1 || step_j < 0 || (long long)s.t_ctx + step_j >= s.t_cap) return BD_ERR_INVALID_ARG;
+  if (flags & ~BD_DRAFT_VIEW_READY) return BD_ERR_INVALID_ARG;
+  BD_TRY(check_paged_cache(s, cache, table, table_pages, true, true));
+  const int units = s.batch * s.h_kv;
+  if (!group_supported_by_draft(s.h_q / s.h_kv) || units > 65535) return BD_ERR_UNSUPPORTED;
+  DraftPlan dp;
+  const size_t base = ws_region_offset(units);
+  if (!draft_plan(s, budget, step_j + 1, ws_bytes > base ? ws_bytes - base : 0, &dp)) return BD_ERR_UNSUPPORTED;
+  if (!ws) return BD_ERR_WORKSPACE;
+  if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
+  if (ws_bytes < base) return BD_ERR_WORKSPACE;
+  return map_cuda(launch_paged_draft(s, dp, q, *cache, table, table_pages, idx, count, budget, step_j, flags, o_out, lse_out,
+                                     region(ws, units), counters(ws), status_word(ws), static_cast<cudaStream_t>(stream)));
 }
 
 int bd_check_wait_timeout(void* ws, size_t ws_bytes, int limit_us, void* stream) {

@@ -237,7 +237,8 @@ __device__ __forceinline__ void merge_warps_and_store(const float* m_s, const fl
 // the WK warps' (m, l) (broadcast shared-memory loads), so no barrier separates the
 // factors from the output.  o_dst rows are D wide (bf16 if OUT_BF16 else fp32, written
 // 8 or 16 bytes at a time: o_dst must be 16-byte aligned); lse_dst[r] in natural log.
-template <int D, int WK, bool OUT_BF16>
+// KEEP_NAN: a row whose sum is NaN has an lse of NaN (else -inf).
+template <int D, int WK, bool OUT_BF16, bool KEEP_NAN = false>
 __device__ __forceinline__ void merge_warps_flat(const float* m_s, const float* l_s, const float* o_s, int nqc,
                                                  int n_cols, float* lse_dst, void* o_dst, int tid, int n_threads) {
   constexpr int OP = D + 4;
@@ -269,7 +270,7 @@ __device__ __forceinline__ void merge_warps_flat(const float* m_s, const float* 
     a.y *= inv;
     a.z *= inv;
     a.w *= inv;
-    if (d == 0 && lse_dst) lse_dst[col] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+    if (d == 0 && lse_dst) lse_dst[col] = L > 0.f || (KEEP_NAN && L != 0.f) ? (M_use + log2f(L)) * kLn2 : -INFINITY;
     if (OUT_BF16) {
       uint2 packed;
       packed.x = pack_bf16x2(a.x, a.y);

@@ -29,6 +29,7 @@
 #include "bd_attn_warp.cuh"
 #include "bd_common.cuh"
 #include "bd_internal.h"
+#include "bd_paged.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -67,6 +68,14 @@ struct DraftLongParams : DraftParams {
   int* counters;               // [units] arrivals of the unit's clusters (left zero)
 };
 
+// A pass over a paged cache (k, v and t_cap are not used).
+struct DraftPagedParams : DraftLongParams {
+  PagedTensor pk, pv;
+  PageTable pages;
+};
+template <bool LONG, bool PAGED>
+using DraftParamsOf = std::conditional_t<PAGED, DraftPagedParams, std::conditional_t<LONG, DraftLongParams, DraftParams>>;
+
 template <int D, int G, bool LONG>
 struct DraftSmem {
   static constexpr int ROWS = LONG ? kDLongRows : kDRows;
@@ -88,7 +97,7 @@ struct DraftSmem {
 // The unit's last cluster to arrive merges the clusters' partials: part [n][g_rows][D + 4] (a
 // normalised row, its lse), by the threads of its leading CTA.  Every part of an item is requested at
 // once.  `arrived` is left at zero.
-template <int D, int THREADS>
+template <int D, int THREADS, bool KEEP_NAN>
 __device__ __forceinline__ void merge_clusters(const float* part, int n, int g_rows, int* arrived, __nv_bfloat16* o,
                                                float* lse, int tid) {
   __shared__ int last;
@@ -125,7 +134,7 @@ __device__ __forceinline__ void merge_clusters(const float* part, int n, int g_r
     const float inv = tot > 0.f ? 1.f / tot : 0.f;
     *reinterpret_cast<uint2*>(o + (size_t)g * D + d) =
         make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-    if (d == 0 && lse) lse[g] = mx == -INFINITY ? -INFINITY : mx + logf(tot);
+    if (d == 0 && lse) lse[g] = (KEEP_NAN ? tot == 0.f : mx == -INFINITY) ? -INFINITY : mx + logf(tot);
   }
   if (tid == 0) *arrived = 0;
 }
@@ -135,8 +144,10 @@ __device__ __forceinline__ void merge_clusters(const float* part, int n, int g_r
 // several clusters per unit where SMs are left.  4 units of 8K rows (d 128, groups of 8): 16.2 us
 // a pass in 32 CTAs of five warps, 12.5 with ten, 7.7 over all SMs; traced, 1 us of that is the
 // dependency wait, 2.5 the tiles, 2 the cluster's merge and 2 the clusters'.
-template <int D, int G, bool LONG>
-__global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(const std::conditional_t<LONG, DraftLongParams, DraftParams> p) {
+// PAGED: positions are looked up in the sequence's pages; an entry whose page is not there is skipped.  A NaN reaches the
+// lse too.
+template <int D, int G, bool LONG, bool PAGED>
+__global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(const DraftParamsOf<LONG, PAGED> p) {
   using L = DraftSmem<D, G, LONG>;
   constexpr int kRows = L::ROWS, kWarps = L::WARPS, kThreads = L::THREADS;
   constexpr int NT = (G + 7) / 8, NQC = L::NQC;   // the group's query heads in n8 tiles
@@ -182,20 +193,41 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
   }
   // the unit's context length (like idx and count, written before the preceding kernel
   // when the view is ready, so it may be read before the dependency wait)
-  const int t_unit = unit_context(p.seq_lens, unit, p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
+  int t_unit;
+  if constexpr (PAGED) t_unit = paged_context(p.seq_lens, unit / p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
+  else t_unit = unit_context(p.seq_lens, unit, p.h_kv, p.t_ctx, tid == 0 ? p.status : nullptr);
   const int n_entries = cnt + p.step_j + 1;
   const int e_end = min(e_begin + p.rows_per_split, n_entries);
   const int n_tiles = e_end > e_begin ? (e_end - e_begin + kRows - 1) / kRows : 0;
-  const __nv_bfloat16* kunit = p.k + (size_t)unit * p.t_cap * D;
-  const __nv_bfloat16* vunit = p.v + (size_t)unit * p.t_cap * D;
+  const __nv_bfloat16 *kunit, *vunit;
+  if constexpr (PAGED) {
+    kunit = p.pk.base + unit % p.h_kv * p.pk.sh;
+    vunit = p.pv.base + unit % p.h_kv * p.pv.sh;
+  } else {
+    kunit = p.k + (size_t)unit * p.t_cap * D;
+    vunit = p.v + (size_t)unit * p.t_cap * D;
+  }
+  // a position's row: of the unit, or of the pool (all pages' rows counted through), -1 where its page is not there
+  auto row_of = [&](int pos) -> int {
+    if constexpr (PAGED) {
+      const int e = p.pages.entry(unit / p.h_kv, pos);
+      if (!p.pages.there(e)) {
+        if (e >= 0) record_error(p.status, BD_ERR_INVALID_ARG);
+        return -1;
+      }
+      return (e << p.pages.shift) | (pos & ((1 << p.pages.shift) - 1));
+    } else {
+      return pos;
+    }
+  };
 
   auto position = [&](int e, int idx_value) -> int {
-    if (e >= cnt) return t_unit + (e - cnt);             // a drafted row
+    if (e >= cnt) return row_of(t_unit + (e - cnt));     // a drafted row
     if (idx_value < 0 || idx_value >= t_unit) {
       record_error(p.status, BD_ERR_INVALID_ARG);
       return -1;                                         // skipped
     }
-    return idx_value;
+    return row_of(idx_value);
   };
   // the row of every entry of the slice, up front: tile 0 from the prefetched indices, the
   // later tiles' loads all in flight together (no index round trip between tiles)
@@ -216,9 +248,17 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
       const int r = c / CH, ch = c % CH;
       const int pos = rowpos[tile * kRows + r];
       const bool live = r < nrows && pos >= 0;   // others zero-filled (0 * garbage could be NaN in P V)
-      const bool drafted = live && pos >= t_unit;
+      bool drafted;
+      if constexpr (PAGED) drafted = live && e_begin + tile * kRows + r >= cnt;
+      else drafted = live && pos >= t_unit;
       if ((part == 0 && drafted) || (part == 1 && !drafted)) continue;
       const uint32_t off = sw128_offset(r, ch * 8, HALF_BYTES);
+      if constexpr (PAGED) {
+        const long long page = live ? pos >> p.pages.shift : 0, row = live ? pos & ((1 << p.pages.shift) - 1) : 0;
+        cp_async16_zfill(kt + off, kunit + page * p.pk.sp + row * p.pk.sn + ch * 8, live);
+        cp_async16_zfill(vt + off, vunit + page * p.pv.sp + row * p.pv.sn + ch * 8, live);
+        continue;
+      }
       const size_t src = live ? (size_t)pos * D + ch * 8 : 0;   // slots past the slice are not initialised
       cp_async16_zfill(kt + off, kunit + src, live);
       cp_async16_zfill(vt + off, vunit + src, live);
@@ -268,8 +308,8 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
   __syncthreads();
   const size_t row0 = (size_t)unit * p.g;
   if (p.n_split == 1) {
-    merge_warps_flat<D, kWarps, true>(m_s, l_s, o_s, NQC, p.g, p.lse ? p.lse + row0 : nullptr, p.o + row0 * D, tid,
-                                       kThreads);
+    merge_warps_flat<D, kWarps, true, PAGED>(m_s, l_s, o_s, NQC, p.g, p.lse ? p.lse + row0 : nullptr, p.o + row0 * D, tid,
+                                             kThreads);
     return;
   }
   // ---------------------------------------------------------------- cluster merge (DSMEM)
@@ -279,7 +319,7 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
   const int rank = (int)cluster.block_rank();
   float* slot = cluster.map_shared_rank(parts, 0) + (size_t)rank * SLOT;   // in rank 0
   asm volatile("barrier.cluster.wait.aligned;" ::: "memory");          // every CTA is running
-  merge_warps_flat<D, kWarps, false>(m_s, l_s, o_s, NQC, G, slot + G * D, slot, tid, kThreads);
+  merge_warps_flat<D, kWarps, false, PAGED>(m_s, l_s, o_s, NQC, G, slot + G * D, slot, tid, kThreads);
   cluster.sync();                                  // all partials have landed in rank 0
   if (rank != 0) return;
   // each thread: four output columns of one head, its merge weights derived in place
@@ -297,7 +337,7 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
 #pragma unroll
     for (int r = 0; r < kDMaxCluster; ++r) {
       if (r < C) {
-        const float w = mx == -INFINITY ? 0.f : fast_exp2((lr[r] - mx) * kLog2e);
+        const float w = (PAGED ? lr[r] : mx) == -INFINITY ? 0.f : fast_exp2((lr[r] - mx) * kLog2e);
         const float4 v = *reinterpret_cast<const float4*>(parts + r * SLOT + g * D + d);
         tot += w;
         a.x += w * v.x;
@@ -307,11 +347,12 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
       }
     }
     const float inv = tot > 0.f ? 1.f / tot : 0.f;
+    const float lse = (PAGED ? tot == 0.f : mx == -INFINITY) ? -INFINITY : mx + logf(tot);
     if constexpr (LONG) {
       if (p.n_clusters > 1) {
         float* own = p.o_part + (((size_t)unit * p.n_clusters + split / C) * p.g + g) * (D + 4);
         *reinterpret_cast<float4*>(own + d) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-        if (d == 0) own[D] = mx == -INFINITY ? -INFINITY : mx + logf(tot);
+        if (d == 0) own[D] = lse;
         continue;
       }
     }
@@ -319,11 +360,11 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
     packed.x = pack_bf16x2(a.x * inv, a.y * inv);
     packed.y = pack_bf16x2(a.z * inv, a.w * inv);
     *reinterpret_cast<uint2*>(p.o + (row0 + g) * D + d) = packed;
-    if (d == 0 && p.lse) p.lse[row0 + g] = mx == -INFINITY ? -INFINITY : mx + logf(tot);
+    if (d == 0 && p.lse) p.lse[row0 + g] = lse;
   }
   if constexpr (LONG) {
     if (p.n_clusters > 1)
-      merge_clusters<D, kThreads>(p.o_part + (size_t)unit * p.n_clusters * p.g * (D + 4), p.n_clusters, p.g,
+      merge_clusters<D, kThreads, PAGED>(p.o_part + (size_t)unit * p.n_clusters * p.g * (D + 4), p.n_clusters, p.g,
                                   &p.counters[unit], p.o + row0 * D, p.lse ? p.lse + row0 : nullptr, tid);
   }
 }
@@ -332,10 +373,12 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
 
 namespace {
 using DraftFn = void*;
+template <bool PAGED = false>
 DraftFn pick(int d, int g, bool longs) {
-#define BD_DK(DD, GG)                                                              \
-  if (d == DD && g == GG)                                                          \
-    return longs ? reinterpret_cast<void*>(&draft_kernel<DD, GG, true>) : reinterpret_cast<void*>(&draft_kernel<DD, GG, false>);
+#define BD_DK(DD, GG)                                                                       \
+  if (d == DD && g == GG)                                                                   \
+    return longs ? reinterpret_cast<void*>(&draft_kernel<DD, GG, true, PAGED>)              \
+                 : reinterpret_cast<void*>(&draft_kernel<DD, GG, false, PAGED>);
   BD_DK(64, 1) BD_DK(64, 2) BD_DK(64, 4) BD_DK(64, 8) BD_DK(64, 16)
   BD_DK(128, 1) BD_DK(128, 2) BD_DK(128, 4) BD_DK(128, 8) BD_DK(128, 16)
 #undef BD_DK
@@ -501,15 +544,13 @@ bool draft_plan(const bd_shape& s, int budget, int n_steps, size_t room, DraftPl
                                    draft_pos_slots(*plan)) <= kMaxSmem;
 }
 
-cudaError_t launch_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const void* k_cache,
-                         const void* v_cache, const int32_t* idx, const int32_t* count, int budget,
-                         int step_j, unsigned flags, void* o_out, float* lse_out, void* ws_region,
-                         int* counters, int* status, cudaStream_t stream) {
+// p: what the caller's cache needs is set; the rest is set here.  (A short instance takes the first part of DraftLongParams.)
+static cudaError_t launch_instance(const bd_shape& s, const DraftPlan& plan, const void* q, const int32_t* idx,
+                                   const int32_t* count, int budget, int step_j, unsigned flags, void* o_out, float* lse_out,
+                                   void* ws_region, int* counters, int* status, cudaStream_t stream, DraftFn fn,
+                                   DraftLongParams& p) {
   const int units = s.batch * s.h_kv;
-  DraftLongParams p;             // (a short instance takes its first part)
   p.q = static_cast<const __nv_bfloat16*>(q);
-  p.k = static_cast<const __nv_bfloat16*>(k_cache);
-  p.v = static_cast<const __nv_bfloat16*>(v_cache);
   p.idx = idx;
   p.count = count;
   p.o = static_cast<__nv_bfloat16*>(o_out);
@@ -533,7 +574,6 @@ cudaError_t launch_draft(const bd_shape& s, const DraftPlan& plan, const void* q
   const int g = s.h_q / s.h_kv;
   const int g_kernel = draft_group_instance(g);
   p.g = g;
-  void* fn = pick(s.head_dim, g_kernel, plan.longs);
   const size_t smem = smem_bytes(s.head_dim, g_kernel, plan.longs, p.n_stage, plan.n_split, p.pos_slots);
   cudaError_t err = allow_shared_memory(fn, plan.longs ? kDLongStatic : 0);
   if (err != cudaSuccess) return err;
@@ -542,6 +582,30 @@ cudaError_t launch_draft(const bd_shape& s, const DraftPlan& plan, const void* q
   return launch_kernel(fn, dim3(plan.n_split * plan.n_clusters, units),
                        dim3(2 * (plan.longs ? kDLongRows : kDRows)), smem, stream, args,
                        plan.n_split > 1 ? plan.n_split : 0);
+}
+
+cudaError_t launch_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const void* k_cache,
+                         const void* v_cache, const int32_t* idx, const int32_t* count, int budget,
+                         int step_j, unsigned flags, void* o_out, float* lse_out, void* ws_region,
+                         int* counters, int* status, cudaStream_t stream) {
+  DraftLongParams p;
+  p.k = static_cast<const __nv_bfloat16*>(k_cache);
+  p.v = static_cast<const __nv_bfloat16*>(v_cache);
+  return launch_instance(s, plan, q, idx, count, budget, step_j, flags, o_out, lse_out, ws_region, counters, status, stream,
+                         pick(s.head_dim, draft_group_instance(s.h_q / s.h_kv), plan.longs), p);
+}
+
+cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const bd_paged_cache& c,
+                               const int32_t* table, int table_pages, const int32_t* idx, const int32_t* count, int budget,
+                               int step_j, unsigned flags, void* o_out, float* lse_out, void* ws_region, int* counters,
+                               int* status, cudaStream_t stream) {
+  DraftPagedParams p;
+  p.k = p.v = nullptr;
+  p.pk = {static_cast<__nv_bfloat16*>(c.k), c.k_strides[0], c.k_strides[1], c.k_strides[2]};
+  p.pv = {static_cast<__nv_bfloat16*>(c.v), c.v_strides[0], c.v_strides[1], c.v_strides[2]};
+  p.pages = {table, table_pages, c.n_pages, page_shift(c)};
+  return launch_instance(s, plan, q, idx, count, budget, step_j, flags, o_out, lse_out, ws_region, counters, status, stream,
+                         pick<true>(s.head_dim, draft_group_instance(s.h_q / s.h_kv), plan.longs), p);
 }
 
 // ============================================================================ allocation-free variant

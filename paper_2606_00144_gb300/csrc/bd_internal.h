@@ -224,7 +224,56 @@ bool quant_verify_plan(const bd_shape& s, int rows, int n_q, QuantVerifyPlan* pl
 // Op region for this many query rows behind any context: the kernel that takes them and how a unit is cut follow the context.
 size_t quant_verify_room(const bd_shape& s, int rows);
 
+// Merge of partials laid out [units][max_seg][nq_rows][head_dim] (lse_part [units][max_seg][nq_rows]), nseg[unit] of them,
+// into the rows of units that have more than one.
+struct RowMerge {
+  const float* o_part;
+  const float* lse_part;
+  const int* nseg;
+  int max_seg, nq_rows, rows_total, row_chunks, units;
+  void* o;
+  float* lse;
+};
+cudaError_t launch_row_merge(int head_dim, const RowMerge& m, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------- paged caches
+using RowTensor = QuantTensor;
+inline int page_shift(const bd_paged_cache& c) {
+  int n = 0;
+  while (1 << n < c.page_size) ++n;
+  return n;
+}
+cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const RowTensor& q, const RowTensor& k, const RowTensor& v,
+                                const int32_t* row_starts, const bd_rope* rope, const bd_paged_cache& c, const int32_t* table,
+                                int table_pages, const RowTensor& q_out, cudaStream_t stream);
+cudaError_t launch_paged_read(const bd_shape& s, int first_row, int n_rows, const bd_paged_cache& c, const int32_t* table,
+                              int table_pages, const RowTensor& k, const RowTensor& v, cudaStream_t stream);
+
+cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const bd_paged_cache& c,
+                               const int32_t* table, int table_pages, const int32_t* idx, const int32_t* count, int budget,
+                               int step_j, unsigned flags, void* o_out, float* lse_out, void* ws_region, int* counters,
+                               int* status, cudaStream_t stream);
+
+// Verify blocks.
+struct PagedVerifyPlan {
+  int nt;               // n8 tiles of a unit's query rows
+  int chunks, nq_rows;  // chunks of a KV head's query rows, rows of one: units = batch * h_kv * chunks
+  int tiles_per_unit, tiles_per_cta, seg_cost, grid, max_seg;   // as in VerifyPlan
+  size_t smem;
+};
+bool paged_verify_plan(const bd_shape& s, int rows, int n_q, PagedVerifyPlan* plan);
+size_t paged_verify_bytes(const bd_shape& s, const PagedVerifyPlan& plan);
+// Op region for this many query rows behind any context.
+size_t paged_verify_room(const bd_shape& s, int rows);
+cudaError_t launch_paged_verify(const bd_shape& s, const PagedVerifyPlan& plan, int rows, int n_q, const void* q,
+                                const bd_paged_cache& c, const int32_t* table, int table_pages, void* o_out, float* lse_out,
+                                void* ws_region, int* status, cudaStream_t stream);
+
 // ---------------------------------------------------------------------------- TMA maps
+// 5-D map over one tensor of a pool: 64 columns x rows of a page x 64-column halves of a row x KV heads x pages, 128-byte
+// swizzle.  Box = 64 columns x box_rows rows x box_halves halves; pages that the pool has not read as zero.
+cudaError_t make_paged_map(CUtensorMap* map, const void* base, const int64_t* strides, int head_dim, int h_kv, int page_size,
+                           int n_pages, int box_rows, int box_halves);
 // 3-D map over a [units, rows_total (stride t_cap), head_dim] bf16 cache: only rows
 // [0, n_rows) of each unit are addressable (the rest reads as zero).  Box = 64 columns x
 // box_rows rows x 1 unit, 128-byte swizzle.

@@ -922,6 +922,18 @@ size_t quant_verify_room(const bd_shape& s, int rows) {
   return std::max(quant_tc_bytes(s, tc), on_warps ? quant_attn_bytes(s, rows, w) : 0);
 }
 
+cudaError_t launch_row_merge(int head_dim, const RowMerge& m, cudaStream_t stream) {
+  const float* op = m.o_part;
+  const float* lp = m.lse_part;
+  const int* ns = m.nseg;
+  int max_seg = m.max_seg, nq = m.nq_rows, total = m.rows_total, chunks = m.row_chunks;
+  __nv_bfloat16* o = static_cast<__nv_bfloat16*>(m.o);
+  float* l = m.lse;
+  void* args[] = {&op, &lp, &ns, &max_seg, &nq, &total, &chunks, &o, &l};
+  const void* fn = head_dim == 64 ? reinterpret_cast<const void*>(&quant_merge_kernel<64>) : reinterpret_cast<const void*>(&quant_merge_kernel<128>);
+  return launch_kernel(fn, dim3(m.units, (nq + 3) / 4), dim3(128), 0, stream, args, 0);
+}
+
 cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const QuantAttnCall& c, const bd_quant_cache& cache,
                             void* ws_region, int* status, cudaStream_t stream) {
   const int kv_units = s.batch * s.h_kv;
@@ -960,15 +972,7 @@ cudaError_t launch_quant_tc(const bd_shape& s, const QuantTcPlan& plan, const Qu
   void* args[] = {&p, &kmap, &vmap};
   err = launch_kernel(k.fn, dim3(plan.grid), dim3(kQtThreads), plan.smem, stream, args, 0);
   if (err != cudaSuccess || plan.max_seg <= 1) return err;
-  const float* op = p.o_part;
-  const float* lp = p.lse_part;
-  const int* ns = p.nseg;
-  int max_seg = plan.max_seg, nq = plan.nq_rows, total = c.rows, chunks = plan.chunks;
-  __nv_bfloat16* o = p.o;
-  float* l = p.lse;
-  void* margs[] = {&op, &lp, &ns, &max_seg, &nq, &total, &chunks, &o, &l};
-  const void* mfn = s.head_dim == 64 ? reinterpret_cast<const void*>(&quant_merge_kernel<64>) : reinterpret_cast<const void*>(&quant_merge_kernel<128>);
-  return launch_kernel(mfn, dim3(p.units, (nq + 3) / 4), dim3(128), 0, stream, margs, 0);
+  return launch_row_merge(s.head_dim, {p.o_part, p.lse_part, p.nseg, plan.max_seg, plan.nq_rows, c.rows, plan.chunks, p.units, p.o, p.lse}, stream);
 }
 
 }  // namespace bd

@@ -110,24 +110,21 @@ class SpecStep:
         return out
 
 
-class QuantSpecStep(SpecStep):
-    """A step over a 4-bit cache (QuantCache) of one layer: bd_quant_write for new rows, bd_quant_draft_attn and
-    bd_quant_verify_attn in place of the bf16 attentions.
-
-    The selection and the window's normalisers rank keys on the tensor cores as bf16: the context's keys are
-    read back (bd_quant_read) into one bf16 buffer [batch, h_kv, t_cap, head_dim], made at the first such call
-    and shared by every layer that the object serves.  Like the outputs and the workspace it is one for all
-    calls: those on different streams are the caller's to order."""
+class _ReadBackStep(SpecStep):
+    """A step over a cache of another form.  The selection and the window's normalisers rank keys on the tensor cores as bf16:
+    the context's keys are read back into one bf16 buffer [batch, h_kv, t_cap, head_dim], made at the first such call and
+    shared by every layer that the object serves.  Like the outputs and the workspace it is one for all calls: those on
+    different streams are the caller's to order."""
 
     def __init__(self, *args, **kw):
         self._keys = None
         super().__init__(*args, **kw)
 
-    def _workspace(self, device):
+    def _workspace_for(self, device, draft_op, verify_op):
         # for every context up to t_cap: the loop that the step is for grows it (self.shape)
         s = self.shape
-        sizes = [B.bd_workspace_size(s, B.BD_OP_QUANT_DRAFT, self.budget, self.gamma),
-                 B.bd_workspace_size(s, B.BD_OP_QUANT_VERIFY, 0, self.gamma + 1)]
+        sizes = [B.bd_workspace_size(s, draft_op, self.budget, self.gamma),
+                 B.bd_workspace_size(s, verify_op, 0, self.gamma + 1)]
         if min(sizes) == 0:
             raise B.BudgetDraftError("bd_workspace_size", -1)
         longer = B.BdShape.from_buffer_copy(s)
@@ -137,19 +134,31 @@ class QuantSpecStep(SpecStep):
             sizes.append(B.bd_workspace_size(longer, B.BD_OP_SELECT, self.budget, self.window))
         return B.Workspace(max(sizes), device)
 
-    def keys(self, cache, stream=None):
-        """The context's keys as bf16, in the step's own buffer (rows past t_ctx are not read)."""
+    def _read_keys(self, device, read, stream):
+        """The context's keys as bf16, in the step's own buffer (rows past t_ctx are not read): read(rows) fills it."""
         s = self.shape
         ts = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream or torch.cuda.current_stream()
         if self._keys is None:
             with torch.cuda.stream(ts):          # memory that what is queued on the stream is done with, on no other
-                self._keys = torch.empty(s.batch, s.h_kv, s.t_cap, s.head_dim, dtype=torch.bfloat16,
-                                         device=cache.k_codes.device)
+                self._keys = torch.empty(s.batch, s.h_kv, s.t_cap, s.head_dim, dtype=torch.bfloat16, device=device)
             self._keys_stream = ts.cuda_stream
         elif ts.cuda_stream != self._keys_stream:
             self._keys.record_stream(ts)
-        B.bd_quant_read(s, cache, self._keys[:, :, :s.t_ctx], first_row=0, stream=stream)
+        read(self._keys[:, :, :s.t_ctx])
         return self._keys
+
+
+class QuantSpecStep(_ReadBackStep):
+    """A step over a 4-bit cache (QuantCache) of one layer: bd_quant_write for new rows, bd_quant_draft_attn and
+    bd_quant_verify_attn in place of the bf16 attentions; bd_quant_read gives the selection its keys."""
+
+    def _workspace(self, device):
+        return self._workspace_for(device, B.BD_OP_QUANT_DRAFT, B.BD_OP_QUANT_VERIFY)
+
+    def keys(self, cache, stream=None):
+        """The context's keys as bf16, in the step's own buffer (rows past t_ctx are not read)."""
+        return self._read_keys(cache.k_codes.device,
+                               lambda rows: B.bd_quant_read(self.shape, cache, rows, first_row=0, stream=stream), stream)
 
     def write(self, k_rows, v_rows, cache, stream=None):
         """Quantises the block's rows [batch, h_kv, n, head_dim] into the cache, behind the context."""
@@ -173,3 +182,42 @@ class QuantSpecStep(SpecStep):
 
     def window_lse(self, cache, q_win, out=None, stream=None):
         return super().window_lse(self.keys(cache, stream), q_win, out, stream)
+
+
+class PagedSpecStep(_ReadBackStep):
+    """A step over a paged cache (PagedCache) of one layer: bd_paged_append for new tokens, bd_paged_draft_attn and
+    bd_paged_verify_attn in place of the bf16 attentions; bd_paged_read gives the selection its keys.  Every call takes the
+    batch's table of pages, int32 [batch, pages].  The selection does not know of pages that are not there: a position on one
+    reads as a key of zeros, and is skipped by the passes if it is kept."""
+
+    def _workspace(self, device):
+        return self._workspace_for(device, B.BD_OP_PAGED_DRAFT, B.BD_OP_PAGED_VERIFY)
+
+    def keys(self, cache, table, stream=None):
+        """The context's keys as bf16, in the step's own buffer (rows past a sequence's length are not read)."""
+        return self._read_keys(cache.k.device,
+                               lambda rows: B.bd_paged_read(self.shape, cache, table, rows, first_row=0, stream=stream), stream)
+
+    def append(self, q_rows, k_rows, v_rows, rope, cache, table, q_out, stream=None):
+        """New tokens behind the context: rows [batch, heads, n, head_dim] rotated by rope to their positions, keys and values
+        into their pages, queries into q_out."""
+        B.bd_paged_append(self.shape, q_rows, k_rows, v_rows, rope, cache, table, q_out, stream=stream)
+
+    def select(self, cache, table, q_win, window_lse=None, stream=None, window_ready=False):
+        super().select(self.keys(cache, table, stream), q_win, window_lse, stream, window_ready)
+
+    def draft(self, j, q_j, cache, table, stream=None, view_ready=False):
+        B.bd_paged_draft_attn(self.shape, q_j, cache, table, self.idx, self.count, self.budget, j, self.draft_o[j],
+                              self.draft_lse[j], self.ws, stream, flags=B.BD_DRAFT_VIEW_READY if view_ready else 0)
+
+    def verify(self, q_verify, cache, table, stream=None):
+        B.bd_paged_verify_attn(self.shape, q_verify, self.gamma + 1, cache, table, self.verify_o, self.verify_lse, self.ws, stream)
+
+    def run(self, cache, table, q_win, q_draft, q_verify, window_lse=None, stream=None):
+        self.select(cache, table, q_win, window_lse, stream)
+        for j in range(self.gamma):
+            self.draft(j, q_draft[j], cache, table, stream, view_ready=j > 0)
+        self.verify(q_verify, cache, table, stream)
+
+    def window_lse(self, cache, table, q_win, out=None, stream=None):
+        return super().window_lse(self.keys(cache, table, stream), q_win, out, stream)
