@@ -282,7 +282,8 @@ __device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, 
 // Shared-memory matrix descriptors of operands in the 128-byte swizzled layout (8-row x
 // 128-byte atoms): a low word with the address and the leading byte offset, a constant high
 // word (stride byte offset 1024, descriptor version 1, swizzle 128 B).
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__host__ __device__ constexpr uint32_t desc_hi(uint32_t stride) { return (stride >> 4) | (1u << 14) | (2u << 29); }
+constexpr uint32_t kDescHi = desc_hi(1024);
 // K-major: atoms stacked every 1024 bytes along M/N (the leading byte offset is unused).
 __device__ __forceinline__ uint32_t desc_k(uint32_t smem_addr) { return ((smem_addr & 0x3FFFFu) >> 4) | (1u << 16); }
 // MN-major: 8 K-rows of 64 MN elements per atom, atoms every 1024 bytes along K and every
@@ -293,28 +294,29 @@ __device__ __forceinline__ uint32_t desc_mn(uint32_t smem_addr, uint32_t mn_stri
 
 // D[tmem] (+)= A * B^T, bf16 inputs, fp32 accumulate, issued by the lane with lead != 0.  A and
 // B in shared memory (low descriptor words):
+// (b_hi: where B's atoms are not 1024 bytes apart)
 __device__ __forceinline__ void tc_mma_ss(uint32_t lead, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
-                                          uint32_t accumulate) {
+                                          uint32_t accumulate, uint32_t b_hi = kDescHi) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
       "setp.ne.b32 q, %0, 0;\n\t"
       "setp.ne.b32 p, %5, 0;\n\t"
       "mov.b64 da, {%2, %6};\n\t"
-      "mov.b64 db, {%3, %6};\n\t"
+      "mov.b64 db, {%3, %7};\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%1], da, db, %4, p;\n\t}" ::"r"(lead),
-      "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"(b_hi)
       : "memory");
 }
 // A in tensor memory:
 __device__ __forceinline__ void tc_mma_ts(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo,
-                                          uint32_t idesc, uint32_t accumulate) {
+                                          uint32_t idesc, uint32_t accumulate, uint32_t b_hi = kDescHi) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
       "setp.ne.b32 q, %0, 0;\n\t"
       "setp.ne.b32 p, %5, 0;\n\t"
       "mov.b64 db, {%3, %6};\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], db, %4, p;\n\t}" ::"r"(lead),
-      "r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      "r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(b_hi)
       : "memory");
 }
 // Arrive on `bar` once every tcgen05 operation the leader issued so far has completed.

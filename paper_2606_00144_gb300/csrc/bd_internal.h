@@ -256,7 +256,8 @@ cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const v
 
 // Verify blocks.
 struct PagedVerifyPlan {
-  int nt;               // n8 tiles of a unit's query rows
+  int q_tiles;          // M tiles of a unit's query rows on the tcgen05 kernel, 0: the mma.sync kernel
+  int nt;               // mma.sync: n8 tiles of a unit's query rows
   int chunks, nq_rows;  // chunks of a KV head's query rows, rows of one: units = batch * h_kv * chunks
   int tiles_per_unit, tiles_per_cta, seg_cost, grid, max_seg;   // as in VerifyPlan
   size_t smem;

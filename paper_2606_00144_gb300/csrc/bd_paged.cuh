@@ -2,6 +2,7 @@
 #pragma once
 
 #include "bd_common.cuh"
+#include "bd_verify.cuh"
 
 namespace bd {
 
@@ -42,5 +43,83 @@ __device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map,
 }
 // What other kernels wrote is read through the async proxy from here on (after the dependency wait).
 __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
+
+// The virtual tile list of a verify block (as VerifyMap): unit u's `a` virtual tiles, then its real ones.  A sequence's units
+// (KV heads x chunks) are alike, so the table for per-sequence lengths, pref, only says where each sequence's units begin
+// (null: every unit has span0 - a tiles).
+struct PagedMap {
+  const int* pref;
+  int span0, a, per_seq, batch, vtpc;
+  __device__ __forceinline__ int seq_of(int u) const { return u / per_seq; }
+  __device__ __forceinline__ int seq_base(int b) const { return pref ? pref[b] : b * per_seq * span0; }
+  __device__ __forceinline__ int span(int b) const { return pref ? (pref[b + 1] - pref[b]) / per_seq : span0; }
+  __device__ __forceinline__ int real_base(int u) const {    // the unit's first real tile
+    const int b = seq_of(u);
+    return seq_base(b) + (u - b * per_seq) * span(b) + a;
+  }
+  __device__ __forceinline__ int tiles(int u) const { return span(seq_of(u)) - a; }
+  __device__ __forceinline__ int first_tile(int u, int v0) const { return max(0, v0 - real_base(u)); }
+  __device__ __forceinline__ int end_tile(int u, int v1) const { return min(tiles(u), v1 - real_base(u)); }
+  __device__ __forceinline__ int owner(int u, int tile) const { return (real_base(u) + tile) / vtpc; }
+  __device__ __forceinline__ int unit_of(int v) const {
+    int b = 0;
+    if (!pref) {
+      b = v / (per_seq * span0);
+    } else {
+      int hi = batch - 1;
+      while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (pref[mid] <= v) b = mid;
+        else hi = mid - 1;
+      }
+    }
+    return b * per_seq + (v - seq_base(b)) / span(b);
+  }
+  // Lays the sequences out in `table` (shared, batch + 1 ints) and cuts the list anew over their tiles.
+  template <int NTHREADS, int KEYS>
+  __device__ __forceinline__ void lay_out(const int32_t* seq_lens, int t_ctx, int n_q, int least, int* wtot, int* table) {
+    auto tiles_of = [&](int b) { return per_seq * ((paged_context(seq_lens, b, t_ctx, nullptr) + n_q + KEYS - 1) / KEYS + a); };
+    lay_out_spans<NTHREADS>(batch, tiles_of, wtot, table);
+    pref = table;
+    vtpc = max((table[batch] + (int)gridDim.x - 1) / (int)gridDim.x, least);
+  }
+};
+
+// A verify block on the tcgen05 kernel.
+struct PagedTcParams : VerifyParams {
+  PageTable pages;
+  int box_shift;       // log2 of a box's rows
+  int batch;
+};
+// Its instance for q_tiles M tiles of query rows per unit, and for boxes of 16 rows and both halves of a row (head_dim 128) or
+// of a half; it takes 16 + head_dim ints of shared memory beside the sequences' table.
+const void* paged_tc_fn(int head_dim, int q_tiles, bool box16);
+
+// Rows [r0, r1) of a V tile in shared memory are hidden from some of the block's queries, to whom 0 times a NaN would be
+// NaN: elements that are no finite number become zero, and from[column] the first row of the block that has one there (the
+// queries that see it have NaN written at the end).  first: row r0's index in the block; the tile's rows lie in pieces of 2^ps
+// rows, each [half][row][128 B].
+template <int D>
+__device__ __noinline__ void scrub_rows(uint32_t tile, int ps, int r0, int r1, int first, int* from, int lane) {
+  constexpr int CH = D / 8;
+  bool any = false;
+  for (int i = lane; i < (r1 - r0) * CH; i += 32) {
+    const int r = r0 + i / CH, col = i % CH * 8;
+    const uint32_t at = tile + ((uint32_t)(r >> ps) * (2 * D) << ps) + sw128_offset(r & ((1 << ps) - 1), col, 128u << ps);
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((w[e] & 0x7f80u) == 0x7f80u) atomicMin(from + col + 2 * e, first + r - r0), w[e] &= 0xffff0000u, odd = true;
+      if ((w[e] & 0x7f800000u) == 0x7f800000u) atomicMin(from + col + 2 * e + 1, first + r - r0), w[e] &= 0xffffu, odd = true;
+    }
+    if (odd) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    any |= odd;
+  }
+  if (__any_sync(0xffffffffu, any)) fence_proxy_async_smem();      // (before the next copy into this stage)
+  __syncwarp();
+}
 
 }  // namespace bd

@@ -24,7 +24,8 @@ constexpr int kPvKeys = 64;           // keys of a tile
 constexpr int kPvWarps = 4;           // consumer warps
 constexpr int kPvThreads = 160;       // + one producer warp
 constexpr int kPvStages = 5;
-constexpr int kPvMaxRows = 24;        // query rows of a unit
+constexpr int kPvMaxRows = 24;        // query rows of a unit; more go to the tcgen05 kernel,
+constexpr int kPvTcMaxRows = 256;     // which takes this many: two M tiles
 
 struct PagedVerifyParams {
   const __nv_bfloat16* q;             // [kv units][rows_total][D]
@@ -42,45 +43,6 @@ struct PagedVerifyParams {
   float scale_log2;
 };
 
-// The virtual tile list: unit u's `a` virtual tiles, then its real ones; a sequence's units (KV heads x chunks) are
-// alike.  pref (per-sequence lengths): where each sequence's units begin.
-struct PagedMap {
-  const int* pref;
-  int span0, a, per_seq, batch, vtpc;
-  __device__ __forceinline__ int seq_base(int b) const { return pref ? pref[b] : b * per_seq * span0; }
-  __device__ __forceinline__ int span(int b) const { return pref ? (pref[b + 1] - pref[b]) / per_seq : span0; }
-  __device__ __forceinline__ int unit_of(int v) const {
-    int b;
-    if (!pref) {
-      b = v / (per_seq * span0);
-    } else {
-      int lo = 0, hi = batch - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (pref[mid] <= v) lo = mid;
-        else hi = mid - 1;
-      }
-      b = lo;
-    }
-    return b * per_seq + (v - seq_base(b)) / span(b);
-  }
-};
-// A unit's place in the list, and its tiles [tb, te) of a CTA's range [v0, v1).
-struct PagedUnit {
-  int seq, rem, base, tiles, tb, te;
-  __device__ __forceinline__ PagedUnit(const PagedMap& m, int u, int v0, int v1) {
-    seq = u / m.per_seq;
-    rem = u - seq * m.per_seq;
-    const int span = m.span(seq);
-    base = m.seq_base(seq) + rem * span + m.a;
-    tiles = span - m.a;
-    tb = max(0, v0 - base);
-    te = min(tiles, v1 - base);
-  }
-  __device__ __forceinline__ int first_owner(const PagedMap& m) const { return base / m.vtpc; }
-  __device__ __forceinline__ int last_owner(const PagedMap& m) const { return (base + tiles - 1) / m.vtpc; }
-};
-
 template <int D, int NT>
 struct PagedSmem {
   static constexpr int NQC = 8 * NT;
@@ -90,31 +52,6 @@ struct PagedSmem {
   // alignment, barriers and the poison table, stages, merge scratch; then the sequences' table
   static constexpr size_t kTotal = 1024 + 1024 + (size_t)kPvStages * STAGE + kMerge;
 };
-
-// Rows [r0, r1) of a V sub-tile in shared memory are hidden from some of the block's queries, to whom 0 times a NaN would be
-// NaN: elements that are no finite number become zero, and from[column] the first row of the block that has one there (the
-// queries that see it have NaN written at the end).  first: row r0's index in the block.
-template <int D>
-__device__ __noinline__ void scrub_rows(uint32_t tile, uint32_t half_bytes, int r0, int r1, int first, int* from, int lane) {
-  constexpr int CH = D / 8;
-  bool any = false;
-  for (int i = lane; i < (r1 - r0) * CH; i += 32) {
-    const int r = r0 + i / CH, col = i % CH * 8;
-    const uint32_t at = tile + sw128_offset(r, col, half_bytes);
-    uint32_t w[4];
-    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
-    bool odd = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if ((w[e] & 0x7f80u) == 0x7f80u) atomicMin(from + col + 2 * e, first + r - r0), w[e] &= 0xffff0000u, odd = true;
-      if ((w[e] & 0x7f800000u) == 0x7f800000u) atomicMin(from + col + 2 * e + 1, first + r - r0), w[e] &= 0xffffu, odd = true;
-    }
-    if (odd) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-    any |= odd;
-  }
-  if (__any_sync(0xffffffffu, any)) fence_proxy_async_smem();      // (before the next copy into this stage)
-  __syncwarp();
-}
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_constant__ PagedVerifyParams p,
@@ -152,13 +89,7 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
   allow_dependent_launch();
   PagedMap map{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
   if (p.seq_lens) {
-    auto span = [&](int b) {
-      const int t = paged_context(p.seq_lens, b, p.t_ctx, nullptr);
-      return map.per_seq * ((t + p.n_q + kPvKeys - 1) / kPvKeys + p.seg_cost);
-    };
-    lay_out_spans<kPvThreads>(p.batch, span, reinterpret_cast<int*>(smem + 256), pref);
-    map.pref = pref;
-    map.vtpc = max((pref[p.batch] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
+    map.lay_out<kPvThreads, kPvKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 256), pref);
   } else {
     __syncthreads();
   }
@@ -170,60 +101,52 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
   if (warp == kPvWarps) {
     // ------------------------------------------------------------------ producer
     fence_proxy_async_global();
-    const int n_box = kPvKeys >> p.box_shift;              // pieces of a tile
-    const int piece = lane & (n_box - 1), which = lane / n_box;
-    const int piece_key = piece << p.box_shift;
+    // A tile is n_box pieces (a page's rows, or 64 of them) of K and of V; lane (tensor, piece) fetches one.  The entries of 32
+    // pieces are looked up at once, the next 32 while these are used: one tile's at a time, a CTA's first tiles came a
+    // round trip to memory apart.
+    const int n_box = kPvKeys >> p.box_shift, piece = lane & (n_box - 1), which = lane / n_box;
     const uint32_t piece_bytes = (uint32_t)D * 2 << p.box_shift;
-    struct At {
-      int unit, tile, te, seq, head, end;                  // end: rows of the sequence, its block's among them
-    };
-    auto settle = [&](int unit) {                          // the first tile from `unit` on (unit > u_last: none)
-      At a{unit, 0, 0, 0, 0, 0};
-      for (; a.unit <= u_last; ++a.unit) {
-        const PagedUnit u(map, a.unit, v0, v1);
-        if (u.tb >= u.te) continue;
-        a.tile = u.tb;
-        a.te = u.te;
-        a.seq = u.seq;
-        a.head = u.rem / p.row_chunks;
-        a.end = paged_context(p.seq_lens, u.seq, p.t_ctx, nullptr) + p.n_q;
-        break;
-      }
-      return a;
-    };
-    auto look_up = [&](const At& a) {
-      const int key = a.tile * kPvKeys + piece_key;
-      return a.unit <= u_last && which < 2 && key < a.end ? p.pages.entry(a.seq, key) : -1;
-    };
-    At at = settle(u_first);
-    int entry = look_up(at), issued = 0;
+    const int page_mask = (1 << p.pages.shift) - 1;
+    int issued = 0;
     bool ok = true;
-    while (at.unit <= u_last) {
-      At next = at;
-      if (++next.tile >= at.te) next = settle(at.unit + 1);
-      const int next_entry = look_up(next);
-      const int s = issued % STAGES;
-      if (issued >= STAGES) ok = mbar_wait_warp(&empty_bar[s], ((issued / STAGES) & 1) ^ 1, p.status, abort_flag);
-      if (!ok) break;
-      const bool there = p.pages.there(entry);
-      if (entry >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
-      const uint32_t pieces = __ballot_sync(0xffffffffu, there) & ((1u << n_box) - 1);
-      if (lane == 0) {
-        int hide = 0;
+    for (int unit = u_first; unit <= u_last && ok; ++unit) {
+      const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
+      if (n <= 0) continue;
+      const int seq = map.seq_of(unit), head = unit / p.row_chunks - seq * p.h_kv;
+      const int end = paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + p.n_q;   // rows of the sequence, its block's among them
+      auto look_up = [&](int first) {                      // entry of the segment's piece first + lane
+        const int at = first + lane, key = tb * kPvKeys + (at << p.box_shift);
+        return at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
+      };
+      int now = look_up(0), then = look_up(32);
+      for (int i = 0; i < n; ++i) {
+        const int at = i * n_box;
+        if (i > 0 && (at & 31) == 0) {
+          now = then;
+          then = look_up(at + 32);
+        }
+        const int entry = __shfl_sync(0xffffffffu, now, (at & 31) + piece);
+        const int s = issued % STAGES;
+        if (issued >= STAGES) ok = mbar_wait_warp(&empty_bar[s], ((issued / STAGES) & 1) ^ 1, p.status, abort_flag);
+        if (!ok) break;
+        const bool there = p.pages.there(entry);
+        if (entry >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
+        const uint32_t pieces = __ballot_sync(0xffffffffu, there) & ((1u << n_box) - 1);
+        if (lane == 0) {
+          int hide = 0;
 #pragma unroll
-        for (int sub = 0; sub < kPvWarps; ++sub) hide |= (int)(~pieces >> (16 * sub >> p.box_shift) & 1) << sub;
-        hide_s[s] = hide;
-        if (pieces) mbar_arrive_expect_tx(&full_bar[s], 2 * __popc(pieces) * piece_bytes);
-        else mbar_arrive(&full_bar[s]);
+          for (int sub = 0; sub < kPvWarps; ++sub) hide |= (int)(~pieces >> (16 * sub >> p.box_shift) & 1) << sub;
+          hide_s[s] = hide;
+          if (pieces) mbar_arrive_expect_tx(&full_bar[s], 2 * __popc(pieces) * piece_bytes);
+          else mbar_arrive(&full_bar[s]);
+        }
+        __syncwarp();
+        if (there && which < 2)
+          tma_load_page(stage_base + s * L::STAGE + which * L::TILE + piece * piece_bytes, which ? &vmap : &kmap, &full_bar[s],
+                        ((tb + i) * kPvKeys + (piece << p.box_shift)) & page_mask, 0, head, entry);
+        __syncwarp();
+        ++issued;
       }
-      __syncwarp();
-      if (there)
-        tma_load_page(stage_base + s * L::STAGE + which * L::TILE + piece * piece_bytes, which ? &vmap : &kmap, &full_bar[s],
-                      (at.tile * kPvKeys + piece_key) & ((1 << p.pages.shift) - 1), 0, at.head, entry);
-      __syncwarp();
-      ++issued;
-      at = next;
-      entry = next_entry;
     }
     if (*abort_flag && lane == 0) {      // never leave a copy in flight behind an aborted CTA
       for (int t = max(0, issued - STAGES); t < issued; ++t)
@@ -254,10 +177,7 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
     }
   };
   auto next_unit = [&](int u) {
-    for (; u <= u_last; ++u) {
-      const PagedUnit x(map, u, v0, v1);
-      if (x.tb < x.te) break;
-    }
+    while (u <= u_last && map.first_tile(u, v0) >= map.end_tile(u, v1)) ++u;
     return u;
   };
   int lim[NT][2];                                          // last visible key of each of this thread's columns
@@ -266,10 +186,10 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
   int unit = next_unit(u_first);
   if (unit <= u_last) load_q(unit);
   while (unit <= u_last) {
-    const PagedUnit u(map, unit, v0, v1);
+    const int tb = map.first_tile(unit, v0), te = map.end_tile(unit, v1);
     const int kv_unit = unit / p.row_chunks, row_base = (unit - kv_unit * p.row_chunks) * p.nq_rows;
     const int rows = min(p.nq_rows, p.rows_total - row_base);
-    const int t_unit = paged_context(p.seq_lens, u.seq, p.t_ctx, tid == 0 ? p.status : nullptr);
+    const int t_unit = paged_context(p.seq_lens, map.seq_of(unit), p.t_ctx, tid == 0 ? p.status : nullptr);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -279,7 +199,7 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
       }
     WarpAttn<D, NT> wa;
     wa.init();
-    for (int tile = u.tb; tile < u.te; ++tile, ++t) {
+    for (int tile = tb; tile < te; ++tile, ++t) {
       const int s = t % STAGES;
       if (!mbar_wait(&full_bar[s], (t / STAGES) & 1, p.status, abort_flag)) {
         alive = false;
@@ -290,7 +210,7 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
         const uint32_t kbase = smem_u32(stage_base + s * L::STAGE) + sub_off, vbase = kbase + L::TILE;
         // rows of the block behind its first one, which its first query does not see
         const int block0 = max(0, t_unit + 1 - key_base);
-        if (block0 <= min(last, 15)) scrub_rows<D>(vbase, half_bytes, block0, min(last, 15) + 1, key_base + block0 - t_unit, nan_from, lane);
+        if (block0 <= min(last, 15)) scrub_rows<D>(vbase, p.box_shift, block0, min(last, 15) + 1, key_base + block0 - t_unit, nan_from, lane);
         wa.step(kbase, vbase, half_bytes, 0, bq, p.scale_log2, lane, [&](int ko, int nt, int e) { return key_base + ko <= lim[nt][e]; },
                 last);
       }
@@ -305,7 +225,7 @@ __global__ void __launch_bounds__(kPvThreads) paged_verify_kernel(const __grid_c
     // ---------------------------------------------------------------- end of a segment
     wa.store(m_s, l_s, o_s, warp, NQC, 0, lane);
     named_bar(1, NCT);
-    const int c_first = u.first_owner(map), n_seg = u.last_owner(map) - c_first + 1;
+    const int c_first = map.owner(unit, 0), n_seg = map.owner(unit, map.tiles(unit) - 1) - c_first + 1;
     const bool whole = n_seg == 1;
     if (p.max_seg > 1 && (int)blockIdx.x == c_first && tid == 0) p.nseg[unit] = n_seg;
     const size_t slot = ((size_t)unit * p.max_seg + ((int)blockIdx.x - c_first)) * p.nq_rows;
@@ -371,22 +291,32 @@ PvInfo pv_kernel(int d, int nt) {
 // CTAs an SM holds, by shared memory (228 KB, a CTA taking 1 KB more than it asks for).
 int pv_per_sm(size_t smem) { return std::max(1, (int)(228 * 1024 / (smem + 1024))); }
 
-void pv_rows(int rows, PagedVerifyPlan* plan) {
-  plan->chunks = (rows + kPvMaxRows - 1) / kPvMaxRows;
+// Which kernel takes this many query rows of a KV head, and in which chunks.
+void pv_rows(int rows, bool tc, PagedVerifyPlan* plan) {
+  const int most = tc ? kPvTcMaxRows : kPvMaxRows;
+  plan->chunks = (rows + most - 1) / most;
   plan->nq_rows = (rows + plan->chunks - 1) / plan->chunks;
-  plan->nt = plan->nq_rows <= 8 ? 1 : 3;
+  plan->q_tiles = tc ? (plan->nq_rows > 128 ? 2 : 1) : 0;
+  plan->nt = tc ? 0 : plan->nq_rows <= 8 ? 1 : 3;
+}
+size_t pv_smem(const bd_shape& s, const PagedVerifyPlan& plan) {
+  return plan.q_tiles ? verify_tc_smem(s.head_dim, plan.q_tiles) + (16 + s.head_dim) * 4 : pv_kernel(s.head_dim, plan.nt).smem;
+}
+long pv_ctas(const PagedVerifyPlan& plan, size_t smem) {
+  return (long)std::max(1, current_sm_count()) * (plan.q_tiles ? 1 : pv_per_sm(smem));
 }
 
 }  // namespace
 
 bool paged_verify_plan(const bd_shape& s, int rows, int n_q, PagedVerifyPlan* plan) {
-  pv_rows(rows, plan);
-  plan->smem = pv_kernel(s.head_dim, plan->nt).smem;
-  const long units = (long)s.batch * s.h_kv * plan->chunks;
-  const long ctas = (long)std::max(1, current_sm_count()) * pv_per_sm(plan->smem);
-  const long tpu = ((long)s.t_ctx + n_q + kPvKeys - 1) / kPvKeys;
+  const bool tc = rows > kPvMaxRows;
+  pv_rows(rows, tc, plan);
+  plan->smem = pv_smem(s, *plan);
+  const int keys = tc ? kVTcKeys : kPvKeys;
+  const long units = (long)s.batch * s.h_kv * plan->chunks, ctas = pv_ctas(*plan, plan->smem);
+  const long tpu = ((long)s.t_ctx + n_q + keys - 1) / keys;
   // A segment's end and the next one's start cost about 5 us of streaming (as in verify_plan), charged as virtual tiles.
-  const double tile_us = (double)kPvKeys * s.head_dim * 4 / (6.5e6 / std::max(1, current_sm_count()));
+  const double tile_us = (double)keys * s.head_dim * 4 / (6.5e6 / std::max(1, current_sm_count()));
   const long a = (long)std::min(16.0, std::max(0.0, 5.0 / tile_us + 0.5));
   const long vtotal = units * (tpu + a);
   if (vtotal >= 1L << 30) return false;
@@ -417,9 +347,8 @@ size_t paged_verify_bytes(const bd_shape& s, const PagedVerifyPlan& plan) {
 size_t paged_verify_room(const bd_shape& s, int rows) {
   // A unit's tpu tiles lie in at most ceil((tpu - 1) / vtpc) + 1 ranges of vtpc >= units (tpu + a) / ctas.
   PagedVerifyPlan plan = {};
-  pv_rows(rows, &plan);
-  const long units = (long)s.batch * s.h_kv * plan.chunks;
-  const long ctas = (long)std::max(1, current_sm_count()) * pv_per_sm(pv_kernel(s.head_dim, plan.nt).smem);
+  pv_rows(rows, rows > kPvMaxRows, &plan);
+  const long units = (long)s.batch * s.h_kv * plan.chunks, ctas = pv_ctas(plan, pv_smem(s, plan));
   plan.max_seg = s.seq_lens ? kVMaxSeg : (int)std::min<long>(kVMaxSeg, (ctas + units - 1) / units + 1);
   return paged_verify_bytes(s, plan);
 }
@@ -427,44 +356,70 @@ size_t paged_verify_room(const bd_shape& s, int rows) {
 cudaError_t launch_paged_verify(const bd_shape& s, const PagedVerifyPlan& plan, int rows, int n_q, const void* q,
                                 const bd_paged_cache& c, const int32_t* table, int table_pages, void* o_out, float* lse_out,
                                 void* ws_region, int* status, cudaStream_t stream) {
-  PagedVerifyParams p;
-  const int box = std::min(c.page_size, kPvKeys);
+  const bool tc = plan.q_tiles != 0;
+  // (tcgen05: a K tile's operand is halves of 128 rows, so a box is one half of a piece's rows.  Boxes of 16 rows so are too
+  // many: 64 units of 16K, 32 rows, d 128 112.9 us in pages of 16, 93.4 in larger ones.  Those take both halves.)
+  const bool box16 = tc && c.page_size == 16 && s.head_dim == 128;
+  const int box = std::min<int>(c.page_size, tc ? kVTcKeys : kPvKeys), halves = tc && !box16 ? 1 : s.head_dim / 64;
   CUtensorMap kmap, vmap;
-  cudaError_t err = make_paged_map(&kmap, c.k, c.k_strides, s.head_dim, s.h_kv, c.page_size, c.n_pages, box, s.head_dim / 64);
-  if (err == cudaSuccess) err = make_paged_map(&vmap, c.v, c.v_strides, s.head_dim, s.h_kv, c.page_size, c.n_pages, box, s.head_dim / 64);
+  cudaError_t err = make_paged_map(&kmap, c.k, c.k_strides, s.head_dim, s.h_kv, c.page_size, c.n_pages, box, halves);
+  if (err == cudaSuccess) err = make_paged_map(&vmap, c.v, c.v_strides, s.head_dim, s.h_kv, c.page_size, c.n_pages, box, halves);
   if (err != cudaSuccess) return err;
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.o = static_cast<__nv_bfloat16*>(o_out);
-  p.lse = lse_out;
-  const size_t units = (size_t)s.batch * s.h_kv * plan.chunks, part_rows = units * plan.max_seg * plan.nq_rows;
-  p.o_part = static_cast<float*>(ws_region);
-  p.lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws_region) + align_up(part_rows * s.head_dim * 4, 256));
-  p.nseg = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(p.lse_part) + align_up(part_rows * 4, 256));
-  p.status = status;
-  p.seq_lens = s.seq_lens;
-  p.pages = {table, table_pages, c.n_pages, page_shift(c)};
-  p.box_shift = 0;
-  while (1 << p.box_shift < box) ++p.box_shift;
-  p.batch = s.batch;
-  p.h_kv = s.h_kv;
-  p.n_q = n_q;
-  p.nq_rows = plan.nq_rows;
-  p.rows_total = rows;
-  p.row_chunks = plan.chunks;
-  p.t_ctx = s.t_ctx;
-  p.max_seg = plan.max_seg;
-  p.seg_cost = plan.seg_cost;
-  p.tiles_per_unit = plan.tiles_per_unit;
-  p.vtiles_per_cta = plan.tiles_per_cta;
-  p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
+  const PageTable pages = {table, table_pages, c.n_pages, page_shift(c)};
+  int box_shift = 0;
+  while (1 << box_shift < box) ++box_shift;
+  const int units = s.batch * s.h_kv * plan.chunks;
+  const size_t part_rows = (size_t)units * plan.max_seg * plan.nq_rows;
+  // what the two kernels' parameters have in common
+  auto fill = [&](auto& p) {
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.o = static_cast<__nv_bfloat16*>(o_out);
+    p.lse = lse_out;
+    p.o_part = static_cast<float*>(ws_region);
+    p.lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws_region) + align_up(part_rows * s.head_dim * 4, 256));
+    p.nseg = reinterpret_cast<int*>(reinterpret_cast<uint8_t*>(p.lse_part) + align_up(part_rows * 4, 256));
+    p.status = status;
+    p.seq_lens = s.seq_lens;
+    p.pages = pages;
+    p.box_shift = box_shift;
+    p.batch = s.batch;
+    p.h_kv = s.h_kv;
+    p.n_q = n_q;
+    p.nq_rows = plan.nq_rows;
+    p.rows_total = rows;
+    p.row_chunks = plan.chunks;
+    p.t_ctx = s.t_ctx;
+    p.max_seg = plan.max_seg;
+    p.seg_cost = plan.seg_cost;
+    p.tiles_per_unit = plan.tiles_per_unit;
+    p.vtiles_per_cta = plan.tiles_per_cta;
+    p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
+  };
+  if (tc) {
+    PagedTcParams p;
+    fill(p);
+    p.counters = nullptr;
+    p.units = units;
+    p.tile_rows = plan.q_tiles == 2 ? (plan.nq_rows + 1) / 2 : plan.nq_rows;
+    CUtensorMap qmap;
+    err = make_rows_map(&qmap, q, (long long)s.batch * s.h_kv * rows, s.head_dim, 128);
+    const void* fn = paged_tc_fn(s.head_dim, plan.q_tiles, box16);
+    if (err == cudaSuccess) err = allow_shared_memory(fn);
+    if (err != cudaSuccess) return err;
+    void* args[] = {&p, &kmap, &vmap, &qmap};
+    err = launch_kernel(fn, dim3(plan.grid), dim3(kVTcThreads), plan.smem, stream, args, 0);
+    if (err != cudaSuccess || plan.max_seg <= 1) return err;
+    return launch_verify_tc_merge(s.head_dim, units, p, stream, true);
+  }
+  PagedVerifyParams p;
+  fill(p);
   const PvInfo k = pv_kernel(s.head_dim, plan.nt);
   err = allow_shared_memory(k.fn);
   if (err != cudaSuccess) return err;
   void* args[] = {&p, &kmap, &vmap};
   err = launch_kernel(k.fn, dim3(plan.grid), dim3(kPvThreads), plan.smem, stream, args, 0);
   if (err != cudaSuccess || plan.max_seg <= 1) return err;
-  return launch_row_merge(s.head_dim, {p.o_part, p.lse_part, p.nseg, plan.max_seg, plan.nq_rows, rows, plan.chunks, (int)units, o_out, lse_out},
-                          stream);
+  return launch_row_merge(s.head_dim, {p.o_part, p.lse_part, p.nseg, plan.max_seg, plan.nq_rows, rows, plan.chunks, units, o_out, lse_out}, stream);
 }
 
 }  // namespace bd

@@ -110,6 +110,6 @@ __device__ __forceinline__ void lay_out_units(const VerifyParams& p, int n_units
 // shared memory without the units' table of per-sequence lengths.
 size_t verify_tc_smem(int head_dim, int q_tiles);
 const void* verify_tc_fn(int head_dim, int q_tiles, bool ragged);
-cudaError_t launch_verify_tc_merge(int head_dim, int units, const VerifyParams& p, cudaStream_t stream);
+cudaError_t launch_verify_tc_merge(int head_dim, int units, const VerifyParams& p, cudaStream_t stream, bool keep_nan = false);
 
 }  // namespace bd

@@ -24,8 +24,12 @@
 // Every segment of a unit that spans CTAs is written as a partial, four columns of all rows at a
 // time ([D/4][rows] float4: a warp of row threads writes 512 contiguous bytes; row-major partials
 // took 3 us to write), and verify_tc_merge_kernel merges.
+#include <climits>
+#include <type_traits>
+
 #include "bd_common.cuh"
 #include "bd_internal.h"
+#include "bd_paged.cuh"
 #include "bd_verify.cuh"
 
 namespace bd {
@@ -46,25 +50,38 @@ struct VerifyTcSmem {
 // Rows [r0, 128) of a V tile in shared memory become zero, by one warp, before that warp's MMAs read them.
 // With per-sequence lengths the last tile of a sequence shorter than the longest one reaches cache rows
 // past its own block, which nobody has promised to be finite, and a weight of 0 times NaN is NaN.
-template <int D>
+template <int D, bool BOX16>
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int r0, int lane) {
   if (r0 >= kVTcKeys) return;
   constexpr int CH = D / 8, PER = 32 / CH;          // 16-byte chunks of a row; rows at a time
   const int c = lane % CH;
-  uint8_t* at = tile + c / 8 * kTHalf + c % 8 * 16;
+  uint8_t* at = tile + c / 8 * (BOX16 ? 2048 : kTHalf) + c % 8 * 16;
 #pragma unroll 1
-  for (int r = r0 + lane / CH; r < kVTcKeys; r += PER) *reinterpret_cast<uint4*>(at + r * 128) = make_uint4(0u, 0u, 0u, 0u);
+  for (int r = r0 + lane / CH; r < kVTcKeys; r += PER)
+    *reinterpret_cast<uint4*>(at + r * 128 + (BOX16 ? (r >> 4) * 2048 : 0)) = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
   __syncwarp();
 }
 
+enum { CONTIGUOUS = 0, PAGED_HALVES = 1, PAGED_BOX16 = 2 };
+template <int MODE>
+using VerifyTcParams = std::conditional_t<MODE != CONTIGUOUS, PagedTcParams, VerifyParams>;
+
 // UNIFORM: one shared context length; the other instance lays out per-sequence lengths.
-template <int D, int NQT, bool UNIFORM>
-__global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyParams p,
+// PAGED (not UNIFORM): keys lie in pages; the boxes of kmap and vmap are pieces of a tile.  A piece whose page is not there
+// reads as zeros, and its 16-key groups are hidden; rows of the block that are hidden from some queries have no part in
+// those even if they are NaN, and a NaN that is seen is passed on to the lse.
+//   PAGED_HALVES  a box is 64 columns of a piece, and a tile lies as in the contiguous kernel;
+//   PAGED_BOX16   a box is 16 whole rows (D 128), two atoms of 8 rows in each half.  The atoms' distance is even between
+//                 pieces (4096 bytes), not along the tile, so S takes the pieces' first atoms as its columns 0 .. 63 and the
+//                 second ones as 64 .. 127, and P V the V atoms of two pieces as 16 keys, in the same order.
+template <int D, int NQT, bool UNIFORM, int MODE>
+__global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyTcParams<MODE> p,
                                                                  const __grid_constant__ CUtensorMap kmap,
                                                                  const __grid_constant__ CUtensorMap vmap,
                                                                  const __grid_constant__ CUtensorMap qmap) {
   using L = VerifyTcSmem<D, NQT>;
+  constexpr bool PAGED = MODE != CONTIGUOUS, BOX16 = MODE == PAGED_BOX16;
   constexpr int SLOTS = L::SLOTS;
   constexpr uint32_t TILE = L::TILE;
   extern __shared__ uint8_t smem_raw[];
@@ -86,40 +103,66 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
   uint8_t* ring = qbuf + NQT * TILE;                        // SLOTS x TILE
   int* pref = reinterpret_cast<int*>(ring + SLOTS * TILE);  // per-sequence lengths: [units + 1]
 
+  int* hide_s = pref;                                       // PAGED: [16] by tile, 16-key groups that are not there
+  int* nan_from = hide_s + 16;                              // PAGED: [D] first row of the block (from 1 on) whose V is no number there
+  if (PAGED) pref = nan_from + D;
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
-  VerifyMap map{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
-  if (!UNIFORM) {
+  auto start = [&] {                                // barriers, tensor memory
+    if (tid == 0) {
+      for (int s = 0; s < SLOTS; ++s) {
+        mbar_init(&full_bar[s], 1);
+        mbar_init(&empty_bar[s], 1);
+      }
+      for (int b = 0; b < 2; ++b) {
+        // (PAGED: beside the commit an arrival of the issuer's own, which passes on what it has seen of hide_s and nan_from)
+        mbar_init(&s_full[b], PAGED ? 2 : 1);
+        mbar_init(&p_ready[b], 4);
+        mbar_init(&pv_done[b], PAGED ? 2 : 1);
+      }
+      mbar_init(q_full, 1);
+      mbar_init(q_empty, 1);
+      mbar_init(o_free, 8);
+      mbar_init(drain_bar, 1);
+      *abort_flag = 0;
+      mbar_fence_init();
+    }
+    if (warp == 1) {
+      tmem_alloc(tmem_slot, 512);
+      tmem_relinquish();
+    }
+  };
+  std::conditional_t<PAGED, PagedMap, VerifyMap> map;
+  if constexpr (PAGED) {
+    map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
+    if (tid < D) nan_from[tid] = INT_MAX;
+    start();                                        // (nothing of it depends on what other kernels wrote)
+    grid_dependency_wait();
+    if (p.seq_lens) map.template lay_out<kVTcThreads, kVTcKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 512), pref);
+  } else {
+    map = VerifyMap{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
+  }
+  if constexpr (!UNIFORM && !PAGED) {
     grid_dependency_wait();
     lay_out_units<kVTcThreads, kVTcKeys>(p, p.units, reinterpret_cast<int*>(smem + 512), pref);
     map.pref = pref;
     map.vtpc = max((pref[p.units] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
   }
-  const int v_total = map.vbase(p.units);
+  int v_total;
+  if constexpr (PAGED) v_total = map.seq_base(p.batch);
+  else v_total = map.vbase(p.units);
   const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
-  if (v0 >= v1) return;                           // whole CTA idle
+  if (v0 >= v1) {                                 // whole CTA idle
+    if constexpr (PAGED) {
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+      if (warp == 1) tmem_dealloc(*tmem_slot, 512);
+    }
+    return;
+  }
   const int u_first = map.unit_of(v0), u_last = map.unit_of(v1 - 1);
 
-  if (tid == 0) {
-    for (int s = 0; s < SLOTS; ++s) {
-      mbar_init(&full_bar[s], 1);
-      mbar_init(&empty_bar[s], 1);
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(&s_full[b], 1);
-      mbar_init(&p_ready[b], 4);
-      mbar_init(&pv_done[b], 1);
-    }
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
-    mbar_init(o_free, 8);
-    mbar_init(drain_bar, 1);
-    *abort_flag = 0;
-    mbar_fence_init();
-  }
-  if (warp == 1) {
-    tmem_alloc(tmem_slot, 512);
-    tmem_relinquish();
-  }
+  if constexpr (!PAGED) start();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -149,7 +192,84 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
   if (warp == 0) {
     // ---------------------------------------------------------------- producer
     allow_dependent_launch();
-    if (lane == 0) {
+    if constexpr (PAGED) {
+      // A tile is n_box pieces (a page's rows, or 128 of them); lane (half, piece) fetches 64 columns of one.  The entries of
+      // 32 pieces are looked up at once, the next 32 while these are used; V's entries are K's of a tile earlier.
+      fence_proxy_async_global();
+      if (lane == 0) {
+        tma_prefetch_map(&kmap);
+        tma_prefetch_map(&vmap);
+        tma_prefetch_map(&qmap);
+      }
+      const int n_box = kVTcKeys >> p.box_shift, piece = lane & (n_box - 1), half = lane / n_box;
+      const int page_mask = (1 << p.pages.shift) - 1;
+      bool ok = true;
+      int issued = 0, seg = 0, tiles_done = 0;
+      for (int unit = u_first; unit <= u_last && ok; ++unit) {
+        const int tb = map.first_tile(unit, v0), te = map.end_tile(unit, v1), n = te - tb;
+        if (n <= 0) continue;
+        const int kv_unit = unit / p.row_chunks, seq = kv_unit / p.h_kv, head = kv_unit - seq * p.h_kv;
+        const int end = paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + p.n_q;   // rows of the sequence
+        auto look_up = [&](int first) {                    // entry of the segment's piece first + lane
+          const int at = first + lane, key = tb * kVTcKeys + (at << p.box_shift);
+          return at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
+        };
+        int now = look_up(0), then = look_up(32), e_k = -1, e_before = -1;
+        auto issue = [&](int i) {
+          const int s = issued % SLOTS;
+          const bool k = i == 0 || ((i & 1) && i != 2 * n - 1);
+          const int tile = i == 0 ? 0 : i == 2 * n - 1 ? n - 1 : (i & 1) ? (i + 1) >> 1 : (i >> 1) - 1;
+          if (k) {
+            const int at = tile * n_box;
+            if (tile > 0 && (at & 31) == 0) {
+              now = then;
+              then = look_up(at + 32);
+            }
+            e_before = e_k;
+            e_k = __shfl_sync(0xffffffffu, now, (at & 31) + piece);
+            if (e_k >= p.pages.n_pages && half == 0) record_error(p.status, BD_ERR_INVALID_ARG);
+          }
+          if (issued >= SLOTS) ok = mbar_wait_warp(&empty_bar[s], ((issued / SLOTS) & 1) ^ 1, p.status, abort_flag);
+          if (!ok) return;
+          const int e = k || i == 2 * n - 1 ? e_k : e_before;
+          const bool there = p.pages.there(e);
+          const int key0 = (tb + tile) * kVTcKeys;
+          const uint32_t here = __ballot_sync(0xffffffffu, there);
+          if (lane == 0) {
+            if (k) {
+              int hide = 0;
+#pragma unroll
+              for (int g = 0; g < kVTcKeys / 16; ++g) hide |= (int)(~here >> (16 * g >> p.box_shift) & 1) << g;
+              hide_s[(tiles_done + tile) & 15] = hide;
+            }
+            if (i == 2 * n - 1) live_s[s] = end - key0;
+            mbar_arrive_expect_tx(&full_bar[s], TILE);
+          }
+          __syncwarp();
+          if (half < (BOX16 ? 1 : D / 64))                 // (a page that the pool has not: zeros)
+            tma_load_page(ring + s * TILE + (BOX16 ? piece * 4096u : half * kTHalf + (piece << p.box_shift) * 128), k ? &kmap : &vmap, &full_bar[s],
+                          (key0 + (piece << p.box_shift)) & page_mask, half, head, there ? e : p.pages.n_pages);
+          __syncwarp();
+          ++issued;
+        };
+        const int pre = seg == 0 ? 0 : min(2 * n, SLOTS - 1);
+        for (int i = 0; i < pre && ok; ++i) issue(i);
+        if (ok && seg > 0) {
+          ok = mbar_wait_warp(q_empty, (seg - 1) & 1, p.status, abort_flag);
+          if (ok && lane == 0) load_q(unit);
+          __syncwarp();
+        }
+        if (!ok) break;
+        ++seg;
+        for (int i = pre; i < 2 * n && ok; ++i) issue(i);
+        tiles_done += n;
+      }
+      if (*abort_flag && lane == 0) {   // no copy may land in shared memory after the CTA exits
+        for (int t = max(0, issued - SLOTS); t < issued; ++t)
+          mbar_wait(&full_bar[t % SLOTS], (t / SLOTS) & 1, p.status, nullptr);
+        if (seg > 0) mbar_wait(q_full, (seg - 1) & 1, p.status, nullptr);
+      }
+    } else if (lane == 0) {
       tma_prefetch_map(&kmap);
       tma_prefetch_map(&vmap);
       tma_prefetch_map(&qmap);
@@ -209,6 +329,8 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
       const int tb = map.first_tile(unit, v0), te = map.end_tile(unit, v1), n = te - tb;
       if (n <= 0) continue;
       const int nj = n * NQT;
+      int t_seg = 0;
+      if constexpr (PAGED) t_seg = paged_context(p.seq_lens, map.seq_of(unit), p.t_ctx, nullptr);
       if (!mbar_wait_warp(q_full, seg & 1, p.status, abort_flag)) break;
       for (int j = 0; j <= nj; ++j) {
         if (j < nj) {                               // S of job j
@@ -224,9 +346,19 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             const uint32_t off = ((ks >> 2) * kTHalf + (ks & 3) * 32) / 16;
-            tc_mma_ss(lead, tmem_base + 128 * b, a_lo + off, b_lo + off, idesc_s, ks > 0 ? 1u : 0u);
+            if constexpr (BOX16) {
+              const uint32_t b_off = ((ks >> 2) * 2048 + (ks & 3) * 32) / 16;
+#pragma unroll
+              for (int atom = 0; atom < 2; ++atom)
+                tc_mma_ss(lead, tmem_base + 128 * b + 64 * atom, a_lo + off, b_lo + b_off + atom * (1024 / 16),
+                          umma_idesc_bf16(128, kVTcKeys / 2), ks > 0 ? 1u : 0u, desc_hi(4096));
+            } else {
+              tc_mma_ss(lead, tmem_base + 128 * b, a_lo + off, b_lo + off, idesc_s, ks > 0 ? 1u : 0u);
+            }
           }
           tc_commit(lead, &s_full[b]);
+          if (PAGED && lane == 0) mbar_arrive(&s_full[b]);
+          if (PAGED) __syncwarp();
           if (qt == NQT - 1) tc_commit(lead, &empty_bar[s]);
           if (j == nj - 1) tc_commit(lead, q_empty);
         }
@@ -234,21 +366,33 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
           const int jj = jg + j - 1, b = jj & 1, i = (j - 1) / NQT, qt = (j - 1) % NQT;
           const int r = base + v_pos(i, n), s = r % SLOTS;
           if (j == 1 && seg > 0) ok = mbar_wait_warp(o_free, (seg - 1) & 1, p.status, abort_flag);
+          if constexpr (PAGED) {                    // (every softmax warp is done with the last segment's)
+            if (j == 1 && seg > 0)
+              for (int c = lane; c < D; c += 32) nan_from[c] = INT_MAX;
+            __syncwarp();
+          }
           if (ok && qt == 0) ok = mbar_wait_warp(&full_bar[s], (r / SLOTS) & 1, p.status, abort_flag);
-          if (!UNIFORM && ok && i == n - 1 && qt == 0) clear_rows<D>(ring + s * TILE, live_s[s], lane);
+          if (!UNIFORM && ok && i == n - 1 && qt == 0) clear_rows<D, BOX16>(ring + s * TILE, live_s[s], lane);
+          if constexpr (PAGED) {                    // rows of the block behind its first one, which its first query does not see
+            const int key0 = (tb + i) * kVTcKeys, r0 = max(0, t_seg + 1 - key0), r1 = min(kVTcKeys, t_seg + p.n_q - key0);
+            if (ok && qt == 0 && r0 < r1) scrub_rows<D>(smem_u32(ring + s * TILE), BOX16 ? 4 : 7, r0, r1, key0 + r0 - t_seg, nan_from, lane);
+          }
           if (ok) ok = mbar_wait_warp(&p_ready[b], (jj >> 1) & 1, p.status, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t v_lo = desc_mn(smem_u32(ring + s * TILE), kTHalf);
+          const uint32_t v_lo = desc_mn(smem_u32(ring + s * TILE), BOX16 ? 2048 : kTHalf);
           const uint32_t d_tmem = tmem_base + 256 + D * b, a_tmem = tmem_base + 128 * b;
           const uint32_t first = j - 1 < 2 ? 0u : 1u;   // O[b]'s first job of the segment
 #pragma unroll 1
           for (int t = 0; t < 2; ++t)                // P_hi, then P_lo
 #pragma unroll
             for (int ks = 0; ks < kVTcKeys / 16; ++ks)
-              tc_mma_ts(lead, d_tmem, a_tmem + 32 * (ks >> 1) + 8 * (ks & 1) + 16 * t, v_lo + ks * (16 * 128 / 16), idesc_o,
-                        t + ks > 0 ? 1u : first);
+              tc_mma_ts(lead, d_tmem, a_tmem + 32 * (ks >> 1) + 8 * (ks & 1) + 16 * t,
+                        v_lo + (BOX16 ? ((ks & 3) * 8192 + (ks >> 2) * 1024) / 16 : ks * (16 * 128 / 16)), idesc_o,
+                        t + ks > 0 ? 1u : first, BOX16 ? desc_hi(4096) : kDescHi);
           tc_commit(lead, &pv_done[b]);
+          if (PAGED && lane == 0) mbar_arrive(&pv_done[b]);
+          if (PAGED) __syncwarp();
           if (qt == NQT - 1) tc_commit(lead, &empty_bar[s]);
         }
       }
@@ -284,8 +428,9 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
       const int kv_unit = unit / p.row_chunks;
       const int row_base = (unit - kv_unit * p.row_chunks) * p.nq_rows;   // first row of this chunk
       const int rows = min(p.nq_rows, p.rows_total - row_base);
-      const int t_unit =
-          UNIFORM ? p.t_ctx : unit_context(p.seq_lens, kv_unit, p.h_kv, p.t_ctx, tid == 64 ? p.status : nullptr);
+      int t_unit;
+      if constexpr (PAGED) t_unit = paged_context(p.seq_lens, map.seq_of(unit), p.t_ctx, tid == 64 ? p.status : nullptr);
+      else t_unit = UNIFORM ? p.t_ctx : unit_context(p.seq_lens, kv_unit, p.h_kv, p.t_ctx, tid == 64 ? p.status : nullptr);
       const int m0 = NQT == 2 ? grp * p.tile_rows : 0;                    // the M tile's first row of the chunk
       const int m_rows = NQT == 2 && grp == 0 ? min(rows, p.tile_rows) : rows - m0;
       const int lim = row < m_rows ? t_unit + (row_base + m0 + row) % p.n_q : -1;   // last visible key
@@ -301,7 +446,8 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
           // two passes over halves of 64 keys: the second half's maximum, the first half's (its
           // scores stay in registers), the weights of the first, the second again
           const int key0 = (tb + j / NQT) * kVTcKeys;
-          const bool masked = key0 + kVTcKeys - 1 > t_unit;   // some key is hidden from some row
+          const int hide = PAGED ? hide_s[(jg + j) / NQT & 15] : 0;
+          const bool masked = key0 + kVTcKeys - 1 > t_unit || (PAGED && hide);   // some key is hidden from some row
           float v[64];
           auto load_half = [&](int h) {
             tc_ld_32cols(t_s + 64 * h, *reinterpret_cast<float(*)[32]>(&v[0]));
@@ -309,7 +455,10 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
             tc_wait_ld();
             if (masked) {
 #pragma unroll
-              for (int c = 0; c < 64; ++c) v[c] = key0 + 64 * h + c <= lim ? v[c] : -INFINITY;
+              for (int c = 0; c < 64; ++c) {
+                const int key = BOX16 ? c / 8 * 16 + 8 * h + c % 8 : 64 * h + c;
+                v[c] = key0 + key <= lim && !(PAGED && (hide >> (BOX16 ? c / 8 : 4 * h + c / 16) & 1)) ? v[c] : -INFINITY;
+              }
             }
           };
           auto half_max = [&]() {
@@ -403,7 +552,9 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
         f_oth = o.x == -INFINITY ? 0.f : fast_exp2(o.x - M);
         S = f_own * l + f_oth * o.y;
       }
-      const float inv = S > 0.f ? 1.f / S : 0.f;
+      const bool seen = PAGED ? S != 0.f : S > 0.f;   // (PAGED: a NaN stays one)
+      const float inv = seen ? 1.f / S : 0.f;
+      const int qi = PAGED ? (row_base + m0 + row) % p.n_q : 0;
       f_own *= inv;
       f_oth *= inv;
       const int c = blockIdx.x, c_first = map.owner(unit, 0), c_last = map.owner(unit, map.tiles(unit) - 1);
@@ -413,7 +564,7 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
       const size_t orow = (size_t)kv_unit * p.rows_total + row_base + m0 + row;                 // output row
       if (alive && warp_live) {
         if (row < m_rows && (NQT == 2 || grp == 0)) {
-          const float lse = S > 0.f ? (M + log2f(S)) * kLn2 : -INFINITY;
+          const float lse = seen ? ((PAGED && M == -INFINITY ? 0.f : M) + log2f(S)) * kLn2 : -INFINITY;
           if (!whole) p.lse_part[pslot * p.nq_rows + m0 + row] = lse;
           else if (p.lse) p.lse[orow] = lse;
         }
@@ -430,6 +581,7 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
           for (int e = 0; e < 16; ++e) {
             const float a = has_own ? o[e] * f_own : 0.f;
             o[e] = has_oth ? fmaf(x[e], f_oth, a) : a;
+            if (PAGED && qi >= nan_from[col0 + cb + e]) o[e] = NAN;
           }
           if (row < m_rows) {
             if (whole) {
@@ -468,7 +620,8 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyP
 // 4 us longer.)
 constexpr int kTMergeRows = 8;
 constexpr int kTMergePer = 9;       // parts in flight per thread
-template <int D, int NG>
+// KEEP_NAN: a part that is NaN counts however little it weighs, and reaches the lse.
+template <int D, int NG, bool KEEP_NAN>
 __global__ void __launch_bounds__(kTMergeRows* D / 4 * NG)
     verify_tc_merge_kernel(const float* o_part, const float* lse_part, const int* nseg, int max_seg, int nq,
                            int rows_total, int row_chunks, __nv_bfloat16* o, float* lse) {
@@ -498,22 +651,22 @@ __global__ void __launch_bounds__(kTMergeRows* D / 4 * NG)
     float mx = fmaxf(l0, l1);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-    const float e0 = mx == -INFINITY ? 0.f : fast_exp2((l0 - mx) * kLog2e);
-    const float e1 = mx == -INFINITY ? 0.f : fast_exp2((l1 - mx) * kLog2e);
+    const float e0 = (KEEP_NAN ? l0 : mx) == -INFINITY ? 0.f : fast_exp2((l0 - mx) * kLog2e);
+    const float e1 = (KEEP_NAN ? l1 : mx) == -INFINITY ? 0.f : fast_exp2((l1 - mx) * kLog2e);
     float tot = e0 + e1;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, off);
-    const float inv = tot > 0.f ? 1.f / tot : 0.f;
+    const float inv = (KEEP_NAN ? tot != 0.f : tot > 0.f) ? 1.f / tot : 0.f;
     if (lane < n) w[i][lane] = e0 * inv;
     if (lane + 32 < n) w[i][lane + 32] = e1 * inv;
-    if (lane == 0 && lse) lse[orow0 + rr] = mx == -INFINITY ? -INFINITY : mx + logf(tot);
+    if (lane == 0 && lse) lse[orow0 + rr] = (KEEP_NAN ? tot == 0.f : mx == -INFINITY) ? -INFINITY : mx + logf(tot);
   }
   __syncthreads();
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const float wk = g + NG * k < n && r < rows ? w[item % R][g + NG * k] : 0.f;
-    if (wk != 0.f) {                              // an empty part never enters the sum
+    if (KEEP_NAN || wk != 0.f) {                  // an empty part never enters the sum (KEEP_NAN: it holds zeros)
       acc.x += wk * v[k].x;
       acc.y += wk * v[k].y;
       acc.z += wk * v[k].z;
@@ -541,7 +694,7 @@ __global__ void __launch_bounds__(kTMergeRows* D / 4 * NG)
 
 // ============================================================================ host side
 
-cudaError_t launch_verify_tc_merge(int head_dim, int units, const VerifyParams& p, cudaStream_t stream) {
+cudaError_t launch_verify_tc_merge(int head_dim, int units, const VerifyParams& p, cudaStream_t stream, bool keep_nan) {
   const float* op = p.o_part;
   const float* lp = p.lse_part;
   const int* ns = p.nseg;
@@ -551,8 +704,9 @@ cudaError_t launch_verify_tc_merge(int head_dim, int units, const VerifyParams& 
   void* args[] = {&op, &lp, &ns, &max_seg, &nq, &rows_total, &chunks, &o, &l};
   const int ng = max_seg <= kTMergePer ? 1 : max_seg <= 2 * kTMergePer ? 2 : 4;
   const void* fn = nullptr;
-#define BD_TM(D, N) \
-  if (head_dim == D && ng == N) fn = reinterpret_cast<const void*>(&verify_tc_merge_kernel<D, N>);
+#define BD_TM(D, N)             \
+  if (head_dim == D && ng == N) \
+    fn = keep_nan ? reinterpret_cast<const void*>(&verify_tc_merge_kernel<D, N, true>) : reinterpret_cast<const void*>(&verify_tc_merge_kernel<D, N, false>);
   BD_TM(64, 1) BD_TM(64, 2) BD_TM(64, 4) BD_TM(128, 1) BD_TM(128, 2) BD_TM(128, 4)
 #undef BD_TM
   return launch_kernel(fn, dim3(units, (nq + kTMergeRows - 1) / kTMergeRows), dim3(kTMergeRows * head_dim / 4 * ng), 0,
@@ -567,9 +721,18 @@ size_t verify_tc_smem(int head_dim, int q_tiles) {
 const void* verify_tc_fn(int head_dim, int q_tiles, bool ragged) {
 #define BD_VT(D, N) \
   if (head_dim == D && q_tiles == N)            \
-    return ragged ? reinterpret_cast<const void*>(&verify_tc_kernel<D, N, false>) : reinterpret_cast<const void*>(&verify_tc_kernel<D, N, true>);
+    return ragged ? reinterpret_cast<const void*>(&verify_tc_kernel<D, N, false, CONTIGUOUS>) : reinterpret_cast<const void*>(&verify_tc_kernel<D, N, true, CONTIGUOUS>);
   BD_VT(64, 1) BD_VT(64, 2) BD_VT(128, 1) BD_VT(128, 2)
 #undef BD_VT
+  return nullptr;
+}
+
+const void* paged_tc_fn(int head_dim, int q_tiles, bool box16) {
+#define BD_PT(D, N, M) \
+  if (head_dim == D && q_tiles == N && box16 == (M == PAGED_BOX16)) return reinterpret_cast<const void*>(&verify_tc_kernel<D, N, false, M>);
+  BD_PT(64, 1, PAGED_HALVES) BD_PT(64, 2, PAGED_HALVES) BD_PT(128, 1, PAGED_HALVES) BD_PT(128, 2, PAGED_HALVES)
+  BD_PT(128, 1, PAGED_BOX16) BD_PT(128, 2, PAGED_BOX16)
+#undef BD_PT
   return nullptr;
 }
 
