@@ -204,6 +204,7 @@ int quant_rows(const bd_shape& s, const void* rows, const int64_t* strides, int 
 // ---- paged caches
 
 constexpr int kPagedMaxRows = 768;        // query rows of a KV head in one block
+constexpr int kPagedMaxRagged = 2048;     // sequences of a block with per-sequence lengths (their table lies in shared memory)
 
 int check_paged_shape(const bd_shape* s) {
   if (!s) return BD_ERR_INVALID_ARG;
@@ -266,7 +267,7 @@ size_t paged_workspace(const bd_shape* shape, int op, int budget, int n_q) {
     if (budget < 1 || units > 65535 || !draft_plan(s, budget, n_q, SIZE_MAX, &dp)) return 0;
     return ws_region_offset((int)units) + draft_region_bytes(s);
   }
-  if (g * n_q > kPagedMaxRows) return 0;
+  if (g * n_q > kPagedMaxRows || (s.seq_lens && s.batch > kPagedMaxRagged)) return 0;
   size_t bytes = 0;
   for (int n = 1; n <= n_q; ++n) {           // (a shorter block may need more partials than a longer one)
     PagedVerifyPlan pp;
@@ -669,7 +670,7 @@ int bd_paged_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd
   const long long rows = (long long)(s.h_q / s.h_kv) * n_q;
   const int units = s.batch * s.h_kv;
   PagedVerifyPlan pp;
-  if (rows > kPagedMaxRows || !paged_verify_plan(s, (int)rows, n_q, &pp)) return BD_ERR_UNSUPPORTED;
+  if (rows > kPagedMaxRows || (s.seq_lens && s.batch > kPagedMaxRagged) || !paged_verify_plan(s, (int)rows, n_q, &pp)) return BD_ERR_UNSUPPORTED;
   if (!ws) return BD_ERR_WORKSPACE;
   if (!aligned(ws, 256)) return BD_ERR_MISALIGNED;
   if (ws_bytes < ws_region_offset(units) + paged_verify_bytes(s, pp)) return BD_ERR_WORKSPACE;

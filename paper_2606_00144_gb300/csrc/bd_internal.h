@@ -258,6 +258,8 @@ cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const v
 struct PagedVerifyPlan {
   int q_tiles;          // M tiles of a unit's query rows on the tcgen05 kernel, 0: the mma.sync kernel
   int nt;               // mma.sync: n8 tiles of a unit's query rows
+  int cluster;          // mma.sync: CTAs of a unit, as a cluster; 0: ranges of the tile list
+  int stages;           // a cluster's CTA: tiles in flight
   int chunks, nq_rows;  // chunks of a KV head's query rows, rows of one: units = batch * h_kv * chunks
   int tiles_per_unit, tiles_per_cta, seg_cost, grid, max_seg;   // as in VerifyPlan
   size_t smem;

@@ -33,12 +33,15 @@ __device__ __forceinline__ int paged_context(const int32_t* seq_lens, int seq, i
   return t;
 }
 
-// Boxes of the pool's tensor map (make_paged_map): 64 columns x rows x halves x head x page.
-__device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, int row, int half, int head, int page) {
+// Boxes of the pool's tensor map (make_paged_map): 64 columns x rows x halves x head x page.  Issued by the lane with lead
+// != 0 of a whole warp whose operands are alike (see tc_mma_ss).
+__device__ __forceinline__ void tma_load_page(uint32_t lead, uint32_t dst, const CUtensorMap* map, uint64_t* bar, int row, int half, int head, int page) {
   asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %0, 0;\n\t"
+      "@q cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%1], [%2, {%3, %4, %5, %6, %7}], [%8];\n\t}" ::"r"(lead),
+      "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(half), "r"(head), "r"(page), "r"(smem_u32(bar))
       : "memory");
 }
 // What other kernels wrote is read through the async proxy from here on (after the dependency wait).

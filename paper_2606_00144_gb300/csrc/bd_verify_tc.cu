@@ -193,16 +193,17 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
     // ---------------------------------------------------------------- producer
     allow_dependent_launch();
     if constexpr (PAGED) {
-      // A tile is n_box pieces (a page's rows, or 128 of them); lane (half, piece) fetches 64 columns of one.  The entries of
-      // 32 pieces are looked up at once, the next 32 while these are used; V's entries are K's of a tile earlier.
+      // A tile is n_box pieces (a page's rows, or 128 of them).  The entries of 32 pieces are looked up at once, the next 32
+      // while these are used; V's are K's of a tile earlier.  The copies are issued by an elected lane of the converged warp.
       fence_proxy_async_global();
+      const uint32_t lead = elect_leader();
       if (lane == 0) {
         tma_prefetch_map(&kmap);
         tma_prefetch_map(&vmap);
         tma_prefetch_map(&qmap);
       }
-      const int n_box = kVTcKeys >> p.box_shift, piece = lane & (n_box - 1), half = lane / n_box;
-      const int page_mask = (1 << p.pages.shift) - 1;
+      __syncwarp();
+      const int n_box = kVTcKeys >> p.box_shift, page_mask = (1 << p.pages.shift) - 1;
       bool ok = true;
       int issued = 0, seg = 0, tiles_done = 0;
       for (int unit = u_first; unit <= u_last && ok; ++unit) {
@@ -210,46 +211,53 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
         if (n <= 0) continue;
         const int kv_unit = unit / p.row_chunks, seq = kv_unit / p.h_kv, head = kv_unit - seq * p.h_kv;
         const int end = paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + p.n_q;   // rows of the sequence
-        auto look_up = [&](int first) {                    // entry of the segment's piece first + lane
+        auto look_up = [&](int first) {                    // entry of the segment's piece first + lane; n_pages: not there
           const int at = first + lane, key = tb * kVTcKeys + (at << p.box_shift);
-          return at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
+          const int e = at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
+          if (e >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
+          return p.pages.there(e) ? e : p.pages.n_pages;
         };
-        int now = look_up(0), then = look_up(32), e_k = -1, e_before = -1;
+        // (three registers: V of the last tile of a batch comes after K of the next one's first)
+        int before = 0, now = look_up(0), then = look_up(32);
         auto issue = [&](int i) {
           const int s = issued % SLOTS;
           const bool k = i == 0 || ((i & 1) && i != 2 * n - 1);
           const int tile = i == 0 ? 0 : i == 2 * n - 1 ? n - 1 : (i & 1) ? (i + 1) >> 1 : (i >> 1) - 1;
-          if (k) {
-            const int at = tile * n_box;
-            if (tile > 0 && (at & 31) == 0) {
-              now = then;
-              then = look_up(at + 32);
-            }
-            e_before = e_k;
-            e_k = __shfl_sync(0xffffffffu, now, (at & 31) + piece);
-            if (e_k >= p.pages.n_pages && half == 0) record_error(p.status, BD_ERR_INVALID_ARG);
+          const int at = tile * n_box & 31, key0 = (tb + tile) * kVTcKeys;
+          if (k && tile > 0 && at == 0) {
+            before = now;
+            now = then;
+            then = look_up(tile * n_box + 32);
           }
+          // a V tile whose successor began a batch
+          const int entries = !k && i != 2 * n - 1 && ((tile + 1) * n_box & 31) == 0 ? before : now;
           if (issued >= SLOTS) ok = mbar_wait_warp(&empty_bar[s], ((issued / SLOTS) & 1) ^ 1, p.status, abort_flag);
           if (!ok) return;
-          const int e = k || i == 2 * n - 1 ? e_k : e_before;
-          const bool there = p.pages.there(e);
-          const int key0 = (tb + tile) * kVTcKeys;
-          const uint32_t here = __ballot_sync(0xffffffffu, there);
+          const uint32_t gone = __ballot_sync(0xffffffffu, entries == p.pages.n_pages) >> at;
           if (lane == 0) {
             if (k) {
               int hide = 0;
 #pragma unroll
-              for (int g = 0; g < kVTcKeys / 16; ++g) hide |= (int)(~here >> (16 * g >> p.box_shift) & 1) << g;
+              for (int g = 0; g < kVTcKeys / 16; ++g) hide |= (int)(gone >> (16 * g >> p.box_shift) & 1) << g;
               hide_s[(tiles_done + tile) & 15] = hide;
             }
             if (i == 2 * n - 1) live_s[s] = end - key0;
             mbar_arrive_expect_tx(&full_bar[s], TILE);
           }
           __syncwarp();
-          if (half < (BOX16 ? 1 : D / 64))                 // (a page that the pool has not: zeros)
-            tma_load_page(ring + s * TILE + (BOX16 ? piece * 4096u : half * kTHalf + (piece << p.box_shift) * 128), k ? &kmap : &vmap, &full_bar[s],
-                          (key0 + (piece << p.box_shift)) & page_mask, half, head, there ? e : p.pages.n_pages);
-          __syncwarp();
+          const uint32_t dst = smem_u32(ring + s * TILE);
+          const CUtensorMap* m = k ? &kmap : &vmap;
+#pragma unroll 2
+          for (int j = 0; j < n_box; ++j) {                // (a page that the pool has not: zeros)
+            const int e = __shfl_sync(0xffffffffu, entries, at + j), row = (key0 + (j << p.box_shift)) & page_mask;
+            if constexpr (BOX16) {
+              tma_load_page(lead, dst + j * 4096, m, &full_bar[s], row, 0, head, e);
+            } else {
+#pragma unroll
+              for (int h = 0; h < D / 64; ++h)
+                tma_load_page(lead, dst + h * kTHalf + (j << p.box_shift) * 128, m, &full_bar[s], row, h, head, e);
+            }
+          }
           ++issued;
         };
         const int pre = seg == 0 ? 0 : min(2 * n, SLOTS - 1);
@@ -446,14 +454,16 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
           // two passes over halves of 64 keys: the second half's maximum, the first half's (its
           // scores stay in registers), the weights of the first, the second again
           const int key0 = (tb + j / NQT) * kVTcKeys;
-          const int hide = PAGED ? hide_s[(jg + j) / NQT & 15] : 0;
-          const bool masked = key0 + kVTcKeys - 1 > t_unit || (PAGED && hide);   // some key is hidden from some row
+          // some key is hidden from some row (which groups is read again where it counts: held over the tile, in a register
+          // that is not there, 64 units of 16K, 32 rows, d 64 took 74.5 us for 65)
+          const bool masked = key0 + kVTcKeys - 1 > t_unit || (PAGED && hide_s[(jg + j) / NQT & 15]);
           float v[64];
           auto load_half = [&](int h) {
             tc_ld_32cols(t_s + 64 * h, *reinterpret_cast<float(*)[32]>(&v[0]));
             tc_ld_32cols(t_s + 64 * h + 32, *reinterpret_cast<float(*)[32]>(&v[32]));
             tc_wait_ld();
             if (masked) {
+              const int hide = PAGED ? hide_s[(jg + j) / NQT & 15] : 0;
 #pragma unroll
               for (int c = 0; c < 64; ++c) {
                 const int key = BOX16 ? c / 8 * 16 + 8 * h + c % 8 : 64 * h + c;
