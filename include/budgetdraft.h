@@ -484,8 +484,8 @@ typedef struct bd_rope {
  *              bytes, not negative; the elements of a row are adjacent.  E.g. slices of a projection's [token, heads, d];
  *   row_starts NULL, or int32 [batch + 1] on the device: prompts of unequal lengths, packed.  The tensors are then
  *              [heads, n_rows, head_dim] (their sequence strides are not used), sequence b has rows row_starts[b] ..
- *              row_starts[b + 1] - 1, ascending from 0 on.  Rows before the first and behind the last sequence are neither read
- *              nor written, nor is the row of a position of t_cap or more;
+ *              row_starts[b + 1] - 1, ascending from 0 on.  Rows behind the last sequence are not used and q_out's not
+ *              written, nor is the row of a position of t_cap or more;
  *   rope       NULL: rows are written as they are;
  *   q_out      bf16, of q_rows' shape, 16-byte aligned, q_out_strides as above (between different rows at least head_dim);
  *              NULL exactly if q_rows is.  It may be q_rows itself, with the same strides.

@@ -8,7 +8,6 @@ the library is not built, or an argument is rejected, these functions raise.
 from __future__ import annotations
 
 import ctypes
-import fractions
 import functools
 import math
 import os
@@ -499,7 +498,7 @@ class Rope:
             raise ValueError("Rope: inv_freq must hold a frequency for each of 8, 16, ... 64 pairs")
         if not torch.isfinite(freq).all() or not math.isfinite(scale):
             raise ValueError("Rope: frequencies and scale must be finite")
-        turns = [round(fractions.Fraction(w) / _TWO_PI * 2**64) % 2**64 for w in freq.tolist()]
+        turns = [_turns(w) for w in freq.tolist()]
         self.turns = torch.tensor([x - 2**64 if x >= 2**63 else x for x in turns], dtype=torch.int64, device=device)
         self.dim, self.interleaved, self.scale = 2 * freq.numel(), bool(interleaved), float(scale)
         self._struct = BdRope(self.turns.data_ptr(), self.dim, int(self.interleaved), self.scale)
@@ -512,50 +511,60 @@ class Rope:
         return cls([base ** (-2.0 * j / dim) for j in range(dim // 2)], **kw)
 
 
-# 2 pi to 35 digits: a frequency of 64 bits keeps all of them
-_TWO_PI = fractions.Fraction(628318530717958647692528676655900577, 10**35)
+# 2^160 / (2 pi), from 2 pi to 35 digits: a frequency of 64 bits keeps all of them
+_PER_RADIAN = (10**35 << 160) // 628318530717958647692528676655900577
 
 
-def _paged_call(name, gpu, stream, fn, *args):
-    if torch._C._cuda_getDevice() == gpu:
-        st = fn(*args, _stream(stream))
-    else:
-        with torch.cuda.device(gpu):
-            st = fn(*args, _stream(stream))
-    _check(name, st)
+def _turns(w):
+    """w / (2 pi) * 2^64 modulo 2^64, rounded once."""
+    m, e = math.frexp(w)
+    x, down = int(m * 2**53) * _PER_RADIAN, 149 - e
+    return ((x + (1 << down - 1)) >> down if down > 0 else x << -down) % 2**64
 
 
-def _paged_table(name, shape, cache, table):
-    """Checks the cache and the table; the shape's sizes."""
-    b, h_q, h, d, t_ctx, t_cap = _shape_ints(shape)
+# As above: what the calls check is checked once, and told apart only when something does not fit.
+def _refuse_paged(name, shape, cache, table, rows=(), row_starts=None, rope=None, **tensors):
+    """rows: (tensor, shape, dtypes) of an append or a read."""
+    b, _, h, d, _, _ = _shape_ints(shape)
     if (h, d) != (cache.h_kv, cache.head_dim):
         _refuse_cache(name, shape)
-    if not (table.dtype is _I32 and table.dim() == 2 and table.shape[0] == b and table.is_contiguous()
-            and table.get_device() == cache._gpu):
-        if table.dtype is not _I32:
-            raise TypeError(f"{name}: the table must be int32, got {table.dtype}")
-        if table.dim() != 2 or table.shape[0] != b or not table.is_contiguous():
-            raise ValueError(f"{name}: the table must be a contiguous [{b}, pages] tensor, got {tuple(table.shape)}")
-        raise ValueError(f"{name}: every tensor must be on the GPU of the cache")
-    return b, h_q, h, d
-
-
-def _paged_rows(name, cache, t, want, *dtypes):
-    """Checks rows of this shape (None: any); their pointer and strides (None where they are dense)."""
-    if t is None:
-        return None, None
-    if not (t.shape == want and t.dtype in dtypes and t.get_device() == cache._gpu and (t.is_contiguous() or t.stride(-1) == 1)):
+    if table.dtype is not _I32:
+        raise TypeError(f"{name}: the table must be int32, got {table.dtype}")
+    if table.dim() != 2 or table.shape[0] != b or not table.is_contiguous():
+        raise ValueError(f"{name}: the table must be a contiguous [{b}, pages] tensor, got {tuple(table.shape)}")
+    for t, want, dtypes in rows:
+        if t is None:
+            continue
         if t.dtype not in dtypes:
-            raise TypeError(f"{name}: rows must be {' or '.join(str(x) for x in dtypes)}, got {t.dtype}")
+            raise TypeError(f"{name}: rows must be {' or '.join('bf16' if x is _BF16 else 'fp32' for x in dtypes)}, got {t.dtype}")
         if t.shape != want:
             raise ValueError(f"{name}: rows must be {tuple(want)}, got {tuple(t.shape)}")
-        if t.get_device() != cache._gpu:
-            raise ValueError(f"{name}: every tensor must be on the GPU of the cache")
-        raise ValueError(f"{name}: the elements of a row must be adjacent")
-    if t.is_contiguous():
-        return t.data_ptr(), None
-    st = t.stride()
-    return t.data_ptr(), _stride_array(*(st[:3] if len(st) == 4 else (0, st[0], st[1])))
+        if t.stride(-1) != 1:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if row_starts is not None and (row_starts.dtype is not _I32 or row_starts.shape != (b + 1,) or not row_starts.is_contiguous()):
+        _refuse(name, row_starts=(row_starts, _I32, (b + 1,)))
+    if rope is not None and rope.dim > d:
+        raise ValueError(f"{name}: the rotation must be of at most head_dim elements")
+    _refuse(name, **tensors)
+
+
+def _paged_rows(t, want, dtype, gpu):
+    """Pointer and strides (None where they are dense) of rows that fit, else None."""
+    if t is None:
+        return None, None
+    if t.shape == want and t.dtype is dtype and t.get_device() == gpu:
+        if t.is_contiguous():
+            return t.data_ptr(), None
+        st = t.stride()
+        if st[-1] == 1:
+            return t.data_ptr(), _stride_array(*st[:3]) if len(st) == 4 else _stride_array(0, st[0], st[1])
+    return None
+
+
+def _on_device(gpu, fn, args, stream):
+    """The call with the cache's GPU current, where that is another one."""
+    with torch.cuda.device(gpu):
+        return fn(*args, _stream(stream))
 
 
 def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, table, q_out, row_starts=None, stream=None):
@@ -563,94 +572,107 @@ def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, tabl
     Rope, or None), keys and values written into their pages, queries into q_out (bf16).  Rows are [batch, heads, n,
     head_dim], or with row_starts (int32 [batch + 1] on the GPU) packed [heads, rows, head_dim]; bf16 or fp32, any strides
     of whole 16 bytes; any of q_rows (with q_out), k_rows and v_rows may be None."""
-    name = "bd_paged_append"
-    b, h_q, h, d = _paged_table(name, shape, cache, table)
-    first = next((t for t in (q_rows, k_rows, v_rows) if t is not None), None)
+    b, h_q, h, d, _, _ = _shape_ints(shape)
+    gpu = cache._gpu
+    first = q_rows if q_rows is not None else k_rows if k_rows is not None else v_rows
     if first is None:
-        raise ValueError(f"{name}: rows of queries, keys or values")
+        raise ValueError("bd_paged_append: rows of queries, keys or values")
     if (q_rows is None) != (q_out is None):
-        raise ValueError(f"{name}: q_rows and q_out come together")
-    dtype = first.dtype
-    if dtype is not _BF16 and dtype is not _F32:
-        raise TypeError(f"{name}: rows must be bf16 or fp32, got {dtype}")
+        raise ValueError("bd_paged_append: q_rows and q_out come together")
+    dtype, size = first.dtype, first.shape
+    if len(size) != (4 if row_starts is None else 3):
+        raise ValueError(f"bd_paged_append: rows must be [batch, heads, n, head_dim], packed [heads, rows, head_dim], got {tuple(size)}")
+    n = size[-2]
     if row_starts is None:
-        if first.dim() != 4:
-            raise ValueError(f"{name}: rows must be [batch, heads, n, head_dim], got {tuple(first.shape)}")
-        n = first.shape[2]
         want_q, want_kv = (b, h_q, n, d), (b, h, n, d)
     else:
-        if first.dim() != 3:
-            raise ValueError(f"{name}: packed rows must be [heads, rows, head_dim], got {tuple(first.shape)}")
-        n = first.shape[1]
         want_q, want_kv = (h_q, n, d), (h, n, d)
-        if not (row_starts.dtype is _I32 and row_starts.shape == (b + 1,) and row_starts.is_contiguous()
-                and row_starts.get_device() == cache._gpu):
-            _refuse(name, row_starts=(row_starts, _I32, (b + 1,)))
-    q, qs = _paged_rows(name, cache, q_rows, want_q, dtype)
-    k, ks = _paged_rows(name, cache, k_rows, want_kv, dtype)
-    v, vs = _paged_rows(name, cache, v_rows, want_kv, dtype)
-    o, os_ = _paged_rows(name, cache, q_out, want_q, _BF16)
-    if rope is not None and (rope._gpu != cache._gpu or rope.dim > d):
-        raise ValueError(f"{name}: the rotation must be of at most head_dim elements, on the GPU of the cache")
-    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_append, ctypes.byref(shape), n,
-                BD_DTYPE_BF16 if dtype is _BF16 else BD_DTYPE_F32, q, qs, k, ks, v, vs, _ptr(row_starts),
-                None if rope is None else rope._ref, cache._ref, table.data_ptr(), table.shape[1], o, os_)
+    ts = table.shape
+    q, k = _paged_rows(q_rows, want_q, dtype, gpu), _paged_rows(k_rows, want_kv, dtype, gpu)
+    v, o = _paged_rows(v_rows, want_kv, dtype, gpu), _paged_rows(q_out, want_q, _BF16, gpu)
+    if not (h == cache.h_kv and d == cache.head_dim and (dtype is _BF16 or dtype is _F32) and q and k and v and o
+            and table.dtype is _I32 and len(ts) == 2 and ts[0] == b and table.is_contiguous() and table.get_device() == gpu
+            and (rope is None or (rope._gpu == gpu and rope.dim <= d))
+            and (row_starts is None or (row_starts.dtype is _I32 and row_starts.shape == (b + 1,) and row_starts.is_contiguous()
+                                        and row_starts.get_device() == gpu))):
+        kinds = (_BF16, _F32) if dtype not in (_BF16, _F32) else (dtype,)
+        _refuse_paged("bd_paged_append", shape, cache, table, ((q_rows, want_q, kinds), (k_rows, want_kv, kinds), (v_rows, want_kv, kinds),
+                                                               (q_out, want_q, (_BF16,))), row_starts, rope)
+    args = (ctypes.byref(shape), n, 1 if dtype is _BF16 else 2, q[0], q[1], k[0], k[1], v[0], v[1], _ptr(row_starts),
+            None if rope is None else rope._ref, cache._ref, table.data_ptr(), ts[1], o[0], o[1])
+    fn = (_lib or library()).bd_paged_append
+    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if st:
+        _check("bd_paged_append", st)
 
 
 def bd_paged_read(shape, cache: PagedCache, table, k_out, v_out=None, first_row=None, stream=None):
     """Reads the context's rows first_row .. first_row + n - 1 (None: those behind the context) into bf16 [batch, h_kv, n,
     head_dim] tensors; either may be None.  Rows of positions at or past a sequence's length are left as they were, those whose
     page is not there are zeros."""
-    name = "bd_paged_read"
-    b, _, h, d = _paged_table(name, shape, cache, table)
+    b, _, h, d, _, _ = _shape_ints(shape)
+    gpu = cache._gpu
     first = k_out if k_out is not None else v_out
     if first is None:
-        raise ValueError(f"{name}: K rows, V rows or both")
+        raise ValueError("bd_paged_read: K rows, V rows or both")
     if first_row is None:
         first_row = BD_PAGED_BLOCK_ROWS
     elif first_row < 0:
-        raise ValueError(f"{name}: first_row must not be negative")
-    if first.dim() != 4:
-        raise ValueError(f"{name}: rows must be [batch, h_kv, n, head_dim], got {tuple(first.shape)}")
-    n = first.shape[2]
-    k, ks = _paged_rows(name, cache, k_out, (b, h, n, d), _BF16)
-    v, vs = _paged_rows(name, cache, v_out, (b, h, n, d), _BF16)
-    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_read, ctypes.byref(shape), first_row, n, cache._ref,
-                table.data_ptr(), table.shape[1], k, ks, v, vs)
-
-
-def _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, n_q, idx=None, count=None, budget=0):
-    """Checks an attention's tensors (of a drafter pass where n_q is None)."""
-    b, h_q, h, d = _paged_table(name, shape, cache, table)
-    want = (b, h_q, d) if n_q is None else (b, h_q, n_q, d)
-    gpu = cache._gpu
-    if not (q.dtype is _BF16 and o_out.dtype is _BF16 and q.shape == want and o_out.shape == want and q.is_contiguous()
-            and o_out.is_contiguous() and q.get_device() == gpu and o_out.get_device() == gpu and ws.buf.get_device() == gpu
-            and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
-                                     and lse_out.get_device() == gpu))
-            and (idx is None or (idx.dtype is _I32 and count.dtype is _I32 and idx.shape == (b, h, budget)
-                                 and count.shape == (b, h) and idx.is_contiguous() and count.is_contiguous()
-                                 and idx.get_device() == gpu and count.get_device() == gpu))):
-        _refuse(name, q=(q, _BF16, want), o_out=(o_out, _BF16, want), lse_out=(lse_out, _F32, want[:-1]),
-                idx=(idx, _I32, (b, h, budget)), count=(count, _I32, (b, h)))
+        raise ValueError("bd_paged_read: first_row must not be negative")
+    want = (b, h, first.shape[2] if first.dim() == 4 else -1, d)
+    ts = table.shape
+    k, v = _paged_rows(k_out, want, _BF16, gpu), _paged_rows(v_out, want, _BF16, gpu)
+    if not (h == cache.h_kv and d == cache.head_dim and k and v and table.dtype is _I32 and len(ts) == 2 and ts[0] == b
+            and table.is_contiguous() and table.get_device() == gpu):
+        _refuse_paged("bd_paged_read", shape, cache, table, ((k_out, want, (_BF16,)), (v_out, want, (_BF16,))))
+    args = (ctypes.byref(shape), first_row, want[2], cache._ref, table.data_ptr(), ts[1], k[0], k[1], v[0], v[1])
+    fn = (_lib or library()).bd_paged_read
+    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if st:
+        _check("bd_paged_read", st)
 
 
 def bd_paged_verify_attn(shape, q, n_q, cache: PagedCache, table, o_out, lse_out, ws: Workspace, stream=None):
     """bd_verify_attn over a paged cache; n_q = 1 decodes one token."""
-    name = "bd_paged_verify_attn"
-    _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, n_q)
-    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_verify_attn, ctypes.byref(shape), q.data_ptr(), n_q, cache._ref,
-                table.data_ptr(), table.shape[1], o_out.data_ptr(), _ptr(lse_out), ws.ptr, ws.nbytes)
+    b, h_q, h, d, _, _ = _shape_ints(shape)
+    gpu, want, ts = cache._gpu, (b, h_q, n_q, d), table.shape
+    if not (h == cache.h_kv and d == cache.head_dim and q.shape == want and o_out.shape == want and q.dtype is _BF16
+            and o_out.dtype is _BF16 and q.is_contiguous() and o_out.is_contiguous() and q.get_device() == gpu
+            and o_out.get_device() == gpu and ws.buf.get_device() == gpu
+            and table.dtype is _I32 and len(ts) == 2 and ts[0] == b and table.is_contiguous() and table.get_device() == gpu
+            and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == want[:-1] and lse_out.is_contiguous()
+                                     and lse_out.get_device() == gpu))):
+        _refuse_paged("bd_paged_verify_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
+                      lse_out=(lse_out, _F32, want[:-1]))
+    args = (ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, table.data_ptr(), ts[1], o_out.data_ptr(),
+            None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
+    fn = (_lib or library()).bd_paged_verify_attn
+    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if st:
+        _check("bd_paged_verify_attn", st)
 
 
 def bd_paged_draft_attn(shape, q, cache: PagedCache, table, idx, count, budget, step_j, o_out, lse_out, ws: Workspace,
                         stream=None, flags=0):
     """bd_draft_attn over a paged cache."""
-    name = "bd_paged_draft_attn"
-    _paged_attn(name, shape, cache, table, q, o_out, lse_out, ws, None, idx, count, budget)
-    _paged_call(name, cache._gpu, stream, (_lib or library()).bd_paged_draft_attn, ctypes.byref(shape), q.data_ptr(), cache._ref,
-                table.data_ptr(), table.shape[1], idx.data_ptr(), count.data_ptr(), budget, step_j, flags, o_out.data_ptr(),
-                _ptr(lse_out), ws.ptr, ws.nbytes)
+    b, h_q, h, d, _, _ = _shape_ints(shape)
+    gpu, want, ts = cache._gpu, (b, h_q, d), table.shape
+    if not (h == cache.h_kv and d == cache.head_dim and q.shape == want and o_out.shape == want and q.dtype is _BF16
+            and o_out.dtype is _BF16 and q.is_contiguous() and o_out.is_contiguous() and q.get_device() == gpu
+            and o_out.get_device() == gpu and ws.buf.get_device() == gpu
+            and idx.dtype is _I32 and idx.shape == (b, h, budget) and idx.is_contiguous() and idx.get_device() == gpu
+            and count.dtype is _I32 and count.shape == (b, h) and count.is_contiguous() and count.get_device() == gpu
+            and table.dtype is _I32 and len(ts) == 2 and ts[0] == b and table.is_contiguous() and table.get_device() == gpu
+            and (lse_out is None or (lse_out.dtype is _F32 and lse_out.shape == (b, h_q) and lse_out.is_contiguous()
+                                     and lse_out.get_device() == gpu))):
+        _refuse_paged("bd_paged_draft_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
+                      lse_out=(lse_out, _F32, (b, h_q)), idx=(idx, _I32, (b, h, budget)), count=(count, _I32, (b, h)))
+    args = (ctypes.byref(shape), q.data_ptr(), cache._ref, table.data_ptr(), ts[1], idx.data_ptr(), count.data_ptr(), budget, step_j,
+            flags, o_out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
+    fn = (_lib or library()).bd_paged_draft_attn
+    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if st:
+        _check("bd_paged_draft_attn", st)
 
 
 def bd_check_wait_timeout(ws: Workspace, limit_us: int, stream=None):

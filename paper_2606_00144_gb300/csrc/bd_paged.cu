@@ -5,7 +5,8 @@
 // The angle is exact for any position: f is held as 64 bits after the point, so that p f modulo 2^64 is one integer
 // multiplication, and what is left of a full turn becomes the argument of sincospif.  A token's sines are worked out once
 // by its CTA and shared by all its heads (a thread that worked them out for its own elements would spend more on them than on
-// the rows).  Both kernels move each byte once.
+// the rows).  Both kernels move each byte once and are bound by HBM where there is enough: 4 x 8192 tokens of 48 rows of 128
+// (805 MB) are appended in 135 us (5.95 TB/s), the keys of 8 x 16K positions of 8 heads (537 MB) read in 82 (6.5 TB/s).
 #include <algorithm>
 
 #include "bd_internal.h"
@@ -14,7 +15,8 @@
 namespace bd {
 
 constexpr int kPgThreads = 256;
-constexpr int kPgTokens = 4;     // tokens of an append CTA
+constexpr int kPgTokens = 32;    // most tokens of an append CTA: a warp places four
+constexpr int pg_ahead(int elem_bytes) { return elem_bytes == 2 ? 2 : 1; }   // (4 and 2: 3 % and 8 % longer, in fewer warps or spilled)
 
 struct AppendRows {              // one source: element strides of a sequence, a head, a row
   const void* rows;
@@ -33,46 +35,64 @@ struct AppendParams {
   int rot, interleaved;          // rotated elements of a row (0: none)
   float scale;
   int batch, t_ctx, t_cap, n_rows;
-  long long total;               // tokens: batch * n_rows, or the packed rows
+  int total;                     // tokens: batch * n_rows, or the packed rows
   int nq, nk, nv;                // rows of a token: heads of q, k, v (0: not this tensor)
+  int tokens;                    // of a CTA
+  int row_shift;                 // log2 of the rows of a token that a CTA walks side by side
   int rows_per_cta;              // rows of a token that a CTA takes (blockIdx.y: which)
   bool wide;                     // every source row is 32-byte aligned (fp32)
 };
 
-// Eight adjacent elements as floats.
+// Eight adjacent elements as they lie.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool wide, float (&x)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else if (wide) {
-    asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
-                 : "l"(p));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 v = reinterpret_cast<const float4*>(p)[i];
-      x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
     }
   }
-}
+};
+template <>
+struct Eight<float> {
+  float w[8];
+  __device__ __forceinline__ void load(const float* p, bool wide) {
+    if (wide) {
+      asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]), "=f"(w[5]), "=f"(w[6]), "=f"(w[7])
+                   : "l"(p));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(p)[i];
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = w[i];
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
   *reinterpret_cast<uint4*>(p) =
       make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
-// The sequence that packed row r belongs to, by a whole warp: the last one that starts at or before it (32 probes a round).
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, long long r, int lane) {
+// The sequence that packed row r belongs to, by a whole warp: the last one that starts at or before it, found with 32 probes a
+// round; probe: the first round's, starts[lane * ceil(batch / 32)].
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, int probe, int r, int lane) {
   int lo = 0, n = batch;
   while (n > 1) {
     const int step = (n + 31) / 32, at = lane * step;
-    const uint32_t before = __ballot_sync(0xffffffffu, at < n && __ldcg(starts + lo + at) <= r);
+    if (n < batch && at < n) probe = __ldcg(starts + lo + at);
+    const uint32_t before = __ballot_sync(0xffffffffu, at < n && probe <= r);
     const int last = max(0, 31 - __clz(before));             // (starts ascend: the lanes that vote are the first ones)
     lo += last * step;
     n = min(step, n - last * step);
@@ -80,112 +100,174 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int batch, lon
   return lo;
 }
 
-struct Token {                   // a token's place, in shared memory
-  long long src_row, out_row;    // its row among its sequence's (packed: among all)
-  int seq, pos, page, row;       // page < 0: not written;  pos < 0: no token
+struct Token {                   // a token of a CTA, in shared memory; q, k, v:
+  long long src[3], dst[3];      // where its rows of head 0 lie in the sources, in q_out and the pool
+  int live;                      // 1: its query is written, 2: its key and value are
 };
 
+// A thread keeps its place in a row and walks the CTA's tokens, several in flight, so that what it costs to find a row is an
+// addition.  A CTA's threads take so many rows side by side that they divide a token's, and as many tokens as that leaves.  The
+// first rows are asked for before their tokens' places are known.
 template <int D, typename T>
-__global__ void __launch_bounds__(kPgThreads) paged_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kPgThreads, 4) paged_append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int CH = D / 16, SLOTS = kPgThreads / CH;          // threads of a row; rows at a time
+  constexpr int AHEAD = pg_ahead(sizeof(T));                   // tokens in flight of a thread
   __shared__ Token tok[kPgTokens];
   __shared__ float2 sc[kPgTokens][D / 2];                      // (cos, sin) of each pair, scaled
   grid_dependency_wait();
   allow_dependent_launch();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const long long t0 = (long long)blockIdx.x * kPgTokens;
-  if (warp < kPgTokens) {                                      // a warp places a token
-    const long long r = t0 + warp;
-    Token k;
-    k.pos = k.page = -1;
-    k.seq = k.row = 0;
-    k.src_row = 0;
-    if (r < p.total) {
-      long long i;
-      bool mine = true;
-      if (p.row_starts) {
-        k.seq = sequence_of(p.row_starts, p.batch, r, lane);
-        const int first = __ldcg(p.row_starts + k.seq);
-        mine = r >= first && r < __ldcg(p.row_starts + k.seq + 1);
-        i = r - first;
-        k.src_row = r;
-      } else {
-        k.seq = (int)(r / p.n_rows);
-        i = k.src_row = r - (long long)k.seq * p.n_rows;
+  const int t0 = blockIdx.x * p.tokens, tokens = min(p.tokens, p.total - t0);
+  if (tid < tokens) {
+    const int g = t0 + tid, s = p.row_starts ? 0 : g / p.n_rows;
+    const long long seq = s, at = g - s * p.n_rows;
+    tok[tid].src[0] = seq * p.q.sb + at * p.q.sn;
+    tok[tid].src[1] = seq * p.k.sb + at * p.k.sn;
+    tok[tid].src[2] = seq * p.v.sb + at * p.v.sn;
+    tok[tid].dst[0] = seq * p.ob + at * p.on;
+  }
+  __syncthreads();
+
+  const int rows = min(p.nq + p.nk + p.nv, ((int)blockIdx.y + 1) * p.rows_per_cta);
+  const int c = tid % CH, slot = tid / CH, half = p.rot / 2;
+  const int row_slots = 1 << p.row_shift, tok_slots = SLOTS >> p.row_shift, first_tok = slot >> p.row_shift;
+  // this thread's 16 elements of a row: of a rotated one with its pairs' halves apart, two times eight
+  const bool turned = 16 * c < p.rot, apart = !p.interleaved && turned;
+  const int e0 = apart ? 8 * c : 16 * c, step = apart ? half : 8;
+  Eight<T> x[AHEAD], y[AHEAD];
+  int row = (int)blockIdx.y * p.rows_per_cta + (slot & (row_slots - 1)), kind = 0;
+  if (first_tok >= tokens) row = rows;
+  const T* src = nullptr;
+  __nv_bfloat16* dst = nullptr;
+  auto start_row = [&] {
+    kind = row < p.nq ? 0 : row < p.nq + p.nk ? 1 : 2;
+    const int head = row - (kind > 0 ? p.nq : 0) - (kind > 1 ? p.nk : 0);
+    const AppendRows& s = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
+    src = static_cast<const T*>(s.rows) + head * s.sh + e0;
+    dst = (kind == 0 ? p.q_out + head * p.oh : kind == 1 ? p.pk.base + head * p.pk.sh : p.pv.base + head * p.pv.sh) + e0;
+  };
+  auto load = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (t + i * tok_slots < tokens) {
+        const T* from = src + tok[t + i * tok_slots].src[kind];
+        x[i].load(from, p.wide);
+        y[i].load(from + step, p.wide);
       }
-      const long long pos = paged_context(p.seq_lens, k.seq, p.t_ctx, nullptr) + i;
-      if (mine && pos < p.t_cap) {
-        k.pos = (int)pos;
-        const int e = p.pages.entry(k.seq, k.pos);
-        if (p.pages.there(e)) k.page = e;
-        k.row = k.pos & ((1 << p.pages.shift) - 1);
+  };
+  if (row < rows) {
+    start_row();
+    load(first_tok);
+  }
+
+  // a warp places the tokens warp, warp + 8, ..., lane k the k-th of them
+  constexpr int WARPS = kPgThreads / 32;
+  unsigned long long turns[D / 64];                            // of this lane's pairs
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j)
+    turns[j] = lane + 32 * j < half ? __ldcg(reinterpret_cast<const unsigned long long*>(p.turns) + lane + 32 * j) : 0;
+  long long my_pos = 0;
+  {
+    int seq = 0, i = 0;
+    bool mine = false;
+    const int probe = p.row_starts && lane * ((p.batch + 31) / 32) < p.batch ? __ldcg(p.row_starts + lane * ((p.batch + 31) / 32)) : 0;
+    for (int k = 0; warp + k * WARPS < tokens; ++k) {
+      const int r = t0 + warp + k * WARPS;
+      if (p.row_starts) {
+        const int found = sequence_of(p.row_starts, p.batch, probe, r, lane);
+        if (lane == k) seq = found, i = r, mine = true;
+      } else if (lane == k) {
+        seq = r / p.n_rows;
+        i = r - seq * p.n_rows;
+        mine = true;
       }
     }
-    if (lane == 0) tok[warp] = k;
+    if (mine) {
+      if (p.row_starts) {
+        const int first = __ldcg(p.row_starts + seq);
+        mine = i >= first && i < __ldcg(p.row_starts + seq + 1);
+        i -= first;
+      }
+      my_pos = (long long)paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + i;
+      const bool live = mine && my_pos < p.t_cap;
+      const int e = live ? p.pages.entry(seq, (int)my_pos) : -1;
+      const bool there = p.pages.there(e);
+      const long long page = there ? e : 0, in_page = my_pos & ((1 << p.pages.shift) - 1);
+      Token& k = tok[warp + lane * WARPS];
+      k.dst[1] = page * p.pk.sp + in_page * p.pk.sn;
+      k.dst[2] = page * p.pv.sp + in_page * p.pv.sn;
+      k.live = (live ? 1 : 0) | (there ? 2 : 0);
+    }
+  }
+  for (int k = 0; warp + k * WARPS < tokens; ++k) {
+    const unsigned long long pos = (unsigned long long)__shfl_sync(0xffffffffu, my_pos, k);
     // the angle as a signed part of a half turn, rounded once
-    for (int j = lane; j < p.rot / 2; j += 32) {
-      const long long phase = (long long)((unsigned long long)k.pos * __ldcg(reinterpret_cast<const unsigned long long*>(p.turns) + j));
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
       float s, c;
-      sincospif((float)phase * 0x1p-63f, &s, &c);
-      sc[warp][j] = make_float2(c * p.scale, s * p.scale);
+      sincospif((float)(long long)(pos * turns[j]) * 0x1p-63f, &s, &c);
+      if (lane + 32 * j < half) sc[warp + k * WARPS][lane + 32 * j] = make_float2(c * p.scale, s * p.scale);
     }
   }
   __syncthreads();
 
-  const int c = tid % CH, half = p.rot / 2;
-  const int row_end = min(p.nq + p.nk + p.nv, ((int)blockIdx.y + 1) * p.rows_per_cta), rows0 = blockIdx.y * p.rows_per_cta;
-  const int rows = row_end - rows0;
-  // this thread's 16 elements of a row: of a rotated one with its pairs' halves apart, two times eight
-  const bool apart = !p.interleaved && 16 * c < p.rot;
-  const int e0 = apart ? 8 * c : 16 * c, e1 = apart ? half + 8 * c : 16 * c + 8;
-  for (int item = tid / CH; item < kPgTokens * rows; item += SLOTS) {
-    const int ti = item / rows, r = rows0 + item - ti * rows;
-    const Token k = tok[ti];
-    if (k.pos < 0) continue;
-    const int seq = p.row_starts ? 0 : k.seq;
-    const bool is_q = r < p.nq, is_k = !is_q && r < p.nq + p.nk;
-    const int head = is_q ? r : is_k ? r - p.nq : r - p.nq - p.nk;
-    const AppendRows& s = is_q ? p.q : is_k ? p.k : p.v;
-    if (!is_q && k.page < 0) continue;
-    const T* src = static_cast<const T*>(s.rows) + seq * s.sb + head * s.sh + k.src_row * s.sn;
-    float x[8], y[8];
-    load8(src + e0, p.wide, x);
-    load8(src + e1, p.wide, y);
-    if ((is_q || is_k) && 16 * c < p.rot) {
-      const float2* t = sc[ti] + 8 * c;
-      if (apart) {
+  for (int t = first_tok; row < rows;) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 w = t[i];
-          const float a = x[i], b = y[i];
-          x[i] = fmaf(a, w.x, -(b * w.y));
-          y[i] = fmaf(a, w.y, b * w.x);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 w = t[i], u = t[4 + i];
-          const float a = x[2 * i], b = x[2 * i + 1], e = y[2 * i], f = y[2 * i + 1];
-          x[2 * i] = fmaf(a, w.x, -(b * w.y));
-          x[2 * i + 1] = fmaf(a, w.y, b * w.x);
-          y[2 * i] = fmaf(e, u.x, -(f * u.y));
-          y[2 * i + 1] = fmaf(e, u.y, f * u.x);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int ti = t + i * tok_slots;
+      if (ti >= tokens) break;
+      const Token& k = tok[ti];
+      if (!(k.live & (kind == 0 ? 1 : 2))) continue;
+      __nv_bfloat16* to = dst + k.dst[kind];
+      if constexpr (sizeof(T) == 2) {
+        if (kind == 2 || !turned) {                            // as they are
+          *reinterpret_cast<uint4*>(to) = x[i].w;
+          *reinterpret_cast<uint4*>(to + step) = y[i].w;
+          continue;
         }
       }
+      float a[8], b[8];
+      x[i].get(a);
+      y[i].get(b);
+      if (kind < 2 && turned) {
+        const float4* v = reinterpret_cast<const float4*>(sc[ti] + 8 * c);   // two pairs' (cos, sin)
+        if (apart) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float4 w = v[e / 2];
+            const float a0 = a[e], a1 = a[e + 1], b0 = b[e], b1 = b[e + 1];
+            a[e] = fmaf(a0, w.x, -(b0 * w.y));
+            b[e] = fmaf(a0, w.y, b0 * w.x);
+            a[e + 1] = fmaf(a1, w.z, -(b1 * w.w));
+            b[e + 1] = fmaf(a1, w.w, b1 * w.z);
+          }
+        } else {
+          auto pairs = [](float (&z)[8], const float4* v) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+              const float4 w = v[e / 4];
+              const float z0 = z[e], z1 = z[e + 1], z2 = z[e + 2], z3 = z[e + 3];
+              z[e] = fmaf(z0, w.x, -(z1 * w.y));
+              z[e + 1] = fmaf(z0, w.y, z1 * w.x);
+              z[e + 2] = fmaf(z2, w.z, -(z3 * w.w));
+              z[e + 3] = fmaf(z2, w.w, z3 * w.z);
+            }
+          };
+          pairs(a, v);
+          pairs(b, v + 2);
+        }
+      }
+      store8(to, a);
+      store8(to + step, b);
     }
-    __nv_bfloat16* dst;
-    if (is_q) {
-      dst = p.q_out + seq * p.ob + head * p.oh + k.src_row * p.on;
-    } else {
-      const PagedTensor& to = is_k ? p.pk : p.pv;
-      dst = to.base + k.page * to.sp + head * to.sh + k.row * to.sn;
+    t += AHEAD * tok_slots;
+    if (t >= tokens) {
+      t = first_tok;
+      row += row_slots;
+      if (row < rows) start_row();
     }
-    store8(dst + e0, x);
-    store8(dst + e1, y);
+    if (row < rows) load(t);
   }
-  // the rows are in L2, for the copy engines' proxy too, before the CTA ends: an attention that follows reads them there
-  fence_proxy_async_global();
-  __threadfence();
 }
 
 // ---------------------------------------------------------------------------- rows read back
@@ -304,16 +386,23 @@ cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const 
   p.t_ctx = s.t_ctx;
   p.t_cap = s.t_cap;
   p.n_rows = n_rows;
-  p.total = row_starts ? n_rows : (long long)s.batch * n_rows;
+  p.total = row_starts ? n_rows : s.batch * n_rows;
   p.nq = q.rows ? s.h_q : 0;
   p.nk = k.rows ? s.h_kv : 0;
   p.nv = v.rows ? s.h_kv : 0;
-  const int all = p.nq + p.nk + p.nv, at_once = kPgThreads / (s.head_dim / 16);
-  const long long blocks = (p.total + kPgTokens - 1) / kPgTokens;
+  const int all = p.nq + p.nk + p.nv, at_once = kPgThreads / (s.head_dim / 16), sms = current_sm_count(), ahead = pg_ahead(e);
   // few tokens: a token's rows spread over CTAs, a pass of rows each
   int split = 1;
-  while (split < 64 && blocks * split < current_sm_count() && all * kPgTokens > at_once * split) split *= 2;
+  while (split < 64 && (long)p.total * split < sms && all > at_once * split) split *= 2;
   p.rows_per_cta = (all + split - 1) / split;
+  // rows side by side: as many as divide a token's, or nearly; tokens: as many as that leaves room for, while there are enough
+  p.row_shift = 0;
+  for (int k = 1; 1 << k <= at_once && 1 << k < 2 * p.rows_per_cta; ++k)
+    if (((p.rows_per_cta + (1 << k) - 1) >> k << k) * 8 <= p.rows_per_cta * 9) p.row_shift = k;
+  const int room = std::min(kPgTokens, ahead * (at_once >> p.row_shift));
+  p.tokens = 1;
+  while (2 * p.tokens <= room && p.total >= 6L * sms * p.tokens) p.tokens *= 2;
+  const unsigned blocks = ((unsigned)p.total + p.tokens - 1) / p.tokens;
   const void* fn = nullptr;
 #define BD_PA(D, CODE, T) \
   if (s.head_dim == D && dtype == CODE) fn = reinterpret_cast<const void*>(&paged_append_kernel<D, T>);
@@ -321,7 +410,7 @@ cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const 
   BD_PA(64, BD_DTYPE_F32, float) BD_PA(128, BD_DTYPE_F32, float)
 #undef BD_PA
   void* args[] = {&p};
-  return launch_kernel(fn, dim3((unsigned)blocks, (unsigned)((all + p.rows_per_cta - 1) / p.rows_per_cta)), dim3(kPgThreads), 0, stream,
+  return launch_kernel(fn, dim3(blocks, (unsigned)((all + p.rows_per_cta - 1) / p.rows_per_cta)), dim3(kPgThreads), 0, stream,
                        args, 0);
 }
 

@@ -493,7 +493,9 @@ bool pv_cluster(const bd_shape& s, int rows, int n_q, PagedVerifyPlan* plan) {
   int c = 0, stages = 0;
   for (int n = (int)std::min<long>(kPvCluster, w.tiles); n >= 1; --n) {
     const bool alone = groups <= pv_clusters_held(s.head_dim, n, true);
-    const long held = pv_clusters_held(s.head_dim, n, false), waves = (groups + held - 1) / held;
+    const long held = pv_clusters_held(s.head_dim, n, false);
+    if (held < 1) continue;
+    const long waves = (groups + held - 1) / held;
     if (waves > 1 && n > 2) continue;
     const long per = (w.tiles + n - 1) / n;
     const double sm_tiles = (double)groups * n * per / sms * w.share * tile;

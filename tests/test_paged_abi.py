@@ -267,8 +267,8 @@ def test_the_binding_refuses_rows(lib):
     bad(ValueError, "rows of", q_rows=None, k_rows=None, v_rows=None, q_out=None)
     bad(ValueError, "together", q_out=None)
     bad(TypeError, "bf16 or fp32", q_rows=Placed(torch.zeros(2, 4, 3, 64).half()))
-    bad(TypeError, "float32|bfloat16", k_rows=f32(2, 2, 3, 64))
-    bad(TypeError, "bfloat16", q_out=f32(2, 4, 3, 64))
+    bad(TypeError, "bf16", k_rows=f32(2, 2, 3, 64))
+    bad(TypeError, "bf16", q_out=f32(2, 4, 3, 64))
     bad(ValueError, "rows must be", k_rows=bf(2, 2, 4, 64))
     bad(ValueError, "rows must be", q_rows=bf(4, 3, 64))
     bad(ValueError, "adjacent", k_rows=Placed(torch.zeros(2, 2, 64, 3, dtype=torch.bfloat16).transpose(2, 3)))
