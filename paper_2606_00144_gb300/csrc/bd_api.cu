@@ -623,6 +623,7 @@ int bd_paged_append(const bd_shape* shape, int n_rows, int dtype, const void* q_
   if (!packed && (long long)s.t_ctx + n_rows > s.t_cap) return BD_ERR_INVALID_ARG;
   if (!packed && (long long)s.batch * n_rows >= 1LL << 31) return BD_ERR_UNSUPPORTED;
   if (dtype != BD_DTYPE_BF16 && dtype != BD_DTYPE_F32) return BD_ERR_INVALID_ARG;
+  if (n_rows == 0) return BD_OK;             // (what has no elements may be anywhere)
   if ((q_rows == nullptr) != (q_out == nullptr)) return BD_ERR_INVALID_ARG;
   if (packed && !aligned(row_starts, 4)) return BD_ERR_MISALIGNED;
   if (rope) {
@@ -637,7 +638,6 @@ int bd_paged_append(const bd_shape* shape, int n_rows, int dtype, const void* q_
   BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, bytes, packed, false, &k));
   BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, bytes, packed, false, &v));
   BD_TRY(paged_rows(s, s.h_q, q_out, q_out_strides, n_rows, 2, packed, true, &o));
-  if (n_rows == 0) return BD_OK;
   return map_cuda(launch_paged_append(s, n_rows, dtype, q, k, v, row_starts, rope, *cache, table, table_pages, o,
                                       static_cast<cudaStream_t>(stream)));
 }
@@ -649,12 +649,12 @@ int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_pag
   const bd_shape& s = *shape;
   const long long first = first_row == BD_PAGED_BLOCK_ROWS ? s.t_ctx : first_row;
   if (first < 0 || n_rows < 0 || first + n_rows > s.t_cap || (n_rows > 0 && !k_rows && !v_rows)) return BD_ERR_INVALID_ARG;
+  if (n_rows == 0) return BD_OK;
   BD_TRY(check_paged_cache(s, cache, table, table_pages, k_rows != nullptr, v_rows != nullptr));
   RowTensor k, v;
   BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, 2, false, true, &k));
   BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, 2, false, true, &v));
   if ((n_rows / 128 + 1LL) * s.batch * s.h_kv * 2 >= 1LL << 31) return BD_ERR_UNSUPPORTED;   // (CTAs)
-  if (n_rows == 0) return BD_OK;
   return map_cuda(launch_paged_read(s, first_row, n_rows, *cache, table, table_pages, k, v, static_cast<cudaStream_t>(stream)));
 }
 

@@ -156,6 +156,10 @@ __global__ void __launch_bounds__(DraftSmem<D, G, LONG>::THREADS) draft_kernel(c
   const bool early = (p.flags & BD_DRAFT_VIEW_READY) != 0;
   // the pass's queries (read after the wait below) on their way into L2 meanwhile
   prefetch_lines_l2(p.q + (size_t)blockIdx.y * p.g * D, (size_t)p.g * D * 2, threadIdx.x, kThreads);
+  if constexpr (PAGED) {   // and the sequence's pages, which the indices lead to
+    const int seq = (int)blockIdx.y / p.h_kv, pages = min(p.pages.pages, ((p.t_ctx + p.step_j) >> p.pages.shift) + 1);
+    prefetch_lines_l2(p.pages.table + (size_t)seq * p.pages.pages, min(pages, 8192) * sizeof(int32_t), threadIdx.x, kThreads);
+  }
   if (!early) {
     grid_dependency_wait();
     allow_dependent_launch();

@@ -89,7 +89,8 @@ struct PagedMap {
   }
 };
 
-// A verify block on the tcgen05 kernel.
+// A verify block on the tcgen05 kernel, which has a second producer warp then.
+constexpr int kPagedTcThreads = kVTcThreads + 32;
 struct PagedTcParams : VerifyParams {
   PageTable pages;
   int box_shift;       // log2 of a box's rows

@@ -113,6 +113,11 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     tma_prefetch_map(&vmap);
   }
   if (tid < D) nan_from[tid] = INT_MAX;
+  if (CLUSTER) {   // the sequence's entries and the queries on their way into L2 meanwhile
+    const int seq = (int)blockIdx.y / (p.h_kv * p.row_chunks), pages = min(p.pages.pages, ((p.t_ctx + p.n_q - 1) >> p.pages.shift) + 1);
+    prefetch_lines_l2(p.pages.table + (size_t)seq * p.pages.pages, min(pages, 2048) * sizeof(int32_t), tid, L::THREADS);
+    prefetch_lines_l2(p.q + (size_t)(blockIdx.y / p.row_chunks) * p.rows_total * D, (size_t)p.rows_total * D * 2, tid, L::THREADS);
+  }
   grid_dependency_wait();
   allow_dependent_launch();
   using Map = std::conditional_t<CLUSTER, ClusterMap, PagedMap>;
@@ -621,7 +626,7 @@ cudaError_t launch_paged_verify(const bd_shape& s, const PagedVerifyPlan& plan, 
     if (err == cudaSuccess) err = allow_shared_memory(fn);
     if (err != cudaSuccess) return err;
     void* args[] = {&p, &kmap, &vmap, &qmap};
-    err = launch_kernel(fn, dim3(plan.grid), dim3(kVTcThreads), plan.smem, stream, args, 0);
+    err = launch_kernel(fn, dim3(plan.grid), dim3(kPagedTcThreads), plan.smem, stream, args, 0);
     if (err != cudaSuccess || plan.max_seg <= 1) return err;
     return launch_verify_tc_merge(s.head_dim, units, p, stream, true);
   }

@@ -76,7 +76,7 @@ using VerifyTcParams = std::conditional_t<MODE != CONTIGUOUS, PagedTcParams, Ver
 //                 pieces (4096 bytes), not along the tile, so S takes the pieces' first atoms as its columns 0 .. 63 and the
 //                 second ones as 64 .. 127, and P V the V atoms of two pieces as 16 keys, in the same order.
 template <int D, int NQT, bool UNIFORM, int MODE>
-__global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyTcParams<MODE> p,
+__global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThreads, 1) verify_tc_kernel(const VerifyTcParams<MODE> p,
                                                                  const __grid_constant__ CUtensorMap kmap,
                                                                  const __grid_constant__ CUtensorMap vmap,
                                                                  const __grid_constant__ CUtensorMap qmap) {
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
     if (tid < D) nan_from[tid] = INT_MAX;
     start();                                        // (nothing of it depends on what other kernels wrote)
     grid_dependency_wait();
-    if (p.seq_lens) map.template lay_out<kVTcThreads, kVTcKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 512), pref);
+    if (p.seq_lens) map.template lay_out<kPagedTcThreads, kVTcKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 512), pref);
   } else {
     map = VerifyMap{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
   }
@@ -189,23 +189,27 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
         tma_load_2d(qbuf + qt * TILE + h * kTHalf, &qmap, q_full, 64 * h, row0 + qt * p.tile_rows);
   };
 
-  if (warp == 0) {
+  if (warp == 0 || (PAGED && warp == kVTcThreads / 32)) {
     // ---------------------------------------------------------------- producer
     allow_dependent_launch();
     if constexpr (PAGED) {
-      // A tile is n_box pieces (a page's rows, or 128 of them).  The entries of 32 pieces are looked up at once, the next 32
-      // while these are used; V's are K's of a tile earlier.  The copies are issued by an elected lane of the converged warp.
+      // Two producers, of K (warp 0) and of V (the last warp), each walking its own entries of the ring.  A tile is n_box pieces (a
+      // page's rows, or 128 of them), each some 130 cycles of a warp (both in one warp: 64 units of 16K, 32 rows, d 64, pages of
+      // 16 took 81.8 us).  The entries of 32 pieces are looked up at once, the next 32 while these are used.  The copies are issued by an elected
+      // lane of the converged warp.
       fence_proxy_async_global();
       const uint32_t lead = elect_leader();
+      const bool k = warp == 0;
+      const CUtensorMap* my_map = k ? &kmap : &vmap;
       if (lane == 0) {
-        tma_prefetch_map(&kmap);
-        tma_prefetch_map(&vmap);
-        tma_prefetch_map(&qmap);
+        tma_prefetch_map(my_map);
+        if (k) tma_prefetch_map(&qmap);
       }
       __syncwarp();
       const int n_box = kVTcKeys >> p.box_shift, page_mask = (1 << p.pages.shift) - 1;
       bool ok = true;
-      int issued = 0, seg = 0, tiles_done = 0;
+      int base = 0, seg = 0, tiles_done = 0;
+      uint32_t armed = 0, phases = 0;               // stages this warp has filled, and the parities of the last time
       for (int unit = u_first; unit <= u_last && ok; ++unit) {
         const int tb = map.first_tile(unit, v0), te = map.end_tile(unit, v1), n = te - tb;
         if (n <= 0) continue;
@@ -214,68 +218,69 @@ __global__ void __launch_bounds__(kVTcThreads, 1) verify_tc_kernel(const VerifyT
         auto look_up = [&](int first) {                    // entry of the segment's piece first + lane; n_pages: not there
           const int at = first + lane, key = tb * kVTcKeys + (at << p.box_shift);
           const int e = at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
-          if (e >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
+          if (k && e >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
           return p.pages.there(e) ? e : p.pages.n_pages;
         };
-        // (three registers: V of the last tile of a batch comes after K of the next one's first)
-        int before = 0, now = look_up(0), then = look_up(32);
-        auto issue = [&](int i) {
-          const int s = issued % SLOTS;
-          const bool k = i == 0 || ((i & 1) && i != 2 * n - 1);
-          const int tile = i == 0 ? 0 : i == 2 * n - 1 ? n - 1 : (i & 1) ? (i + 1) >> 1 : (i >> 1) - 1;
-          const int at = tile * n_box & 31, key0 = (tb + tile) * kVTcKeys;
-          if (k && tile > 0 && at == 0) {
-            before = now;
-            now = then;
-            then = look_up(tile * n_box + 32);
+        int now = look_up(0), then = look_up(32);
+        // the queries behind the first keys: a later segment's stream while its predecessor's last scores still read them
+        const int early = k && seg > 0 ? min(n, (SLOTS + 1) / 2) : 0;
+        for (int i = 0; i < n; ++i) {
+          if (i == early && k && seg > 0) {
+            ok = mbar_wait_warp(q_empty, (seg - 1) & 1, p.status, abort_flag);
+            if (!ok) break;
+            if (lane == 0) load_q(unit);
+            __syncwarp();
           }
-          // a V tile whose successor began a batch
-          const int entries = !k && i != 2 * n - 1 && ((tile + 1) * n_box & 31) == 0 ? before : now;
-          if (issued >= SLOTS) ok = mbar_wait_warp(&empty_bar[s], ((issued / SLOTS) & 1) ^ 1, p.status, abort_flag);
-          if (!ok) return;
-          const uint32_t gone = __ballot_sync(0xffffffffu, entries == p.pages.n_pages) >> at;
+          const int at = i * n_box & 31, key0 = (tb + i) * kVTcKeys;
+          if (i > 0 && at == 0) {
+            now = then;
+            then = look_up(i * n_box + 32);
+          }
+          const int r = base + (k ? k_pos(i) : v_pos(i, n)), s = r % SLOTS;
+          if (r >= SLOTS) ok = mbar_wait_warp(&empty_bar[s], ((r / SLOTS) & 1) ^ 1, p.status, abort_flag);
+          if (!ok) break;
+          const uint32_t gone = __ballot_sync(0xffffffffu, now == p.pages.n_pages) >> at;
           if (lane == 0) {
             if (k) {
               int hide = 0;
 #pragma unroll
               for (int g = 0; g < kVTcKeys / 16; ++g) hide |= (int)(gone >> (16 * g >> p.box_shift) & 1) << g;
-              hide_s[(tiles_done + tile) & 15] = hide;
+              hide_s[(tiles_done + i) & 15] = hide;
+            } else if (i == n - 1) {
+              live_s[s] = end - key0;
             }
-            if (i == 2 * n - 1) live_s[s] = end - key0;
             mbar_arrive_expect_tx(&full_bar[s], TILE);
           }
+          armed |= 1u << s;
+          phases = (phases & ~(1u << s)) | (uint32_t)((r / SLOTS) & 1) << s;
           __syncwarp();
           const uint32_t dst = smem_u32(ring + s * TILE);
-          const CUtensorMap* m = k ? &kmap : &vmap;
 #pragma unroll 2
           for (int j = 0; j < n_box; ++j) {                // (a page that the pool has not: zeros)
-            const int e = __shfl_sync(0xffffffffu, entries, at + j), row = (key0 + (j << p.box_shift)) & page_mask;
+            const int e = __shfl_sync(0xffffffffu, now, at + j), row = (key0 + (j << p.box_shift)) & page_mask;
             if constexpr (BOX16) {
-              tma_load_page(lead, dst + j * 4096, m, &full_bar[s], row, 0, head, e);
+              tma_load_page(lead, dst + j * 4096, my_map, &full_bar[s], row, 0, head, e);
             } else {
 #pragma unroll
               for (int h = 0; h < D / 64; ++h)
-                tma_load_page(lead, dst + h * kTHalf + (j << p.box_shift) * 128, m, &full_bar[s], row, h, head, e);
+                tma_load_page(lead, dst + h * kTHalf + (j << p.box_shift) * 128, my_map, &full_bar[s], row, h, head, e);
             }
           }
-          ++issued;
-        };
-        const int pre = seg == 0 ? 0 : min(2 * n, SLOTS - 1);
-        for (int i = 0; i < pre && ok; ++i) issue(i);
-        if (ok && seg > 0) {
+        }
+        if (ok && early == n && k && seg > 0) {            // (all its keys were early)
           ok = mbar_wait_warp(q_empty, (seg - 1) & 1, p.status, abort_flag);
           if (ok && lane == 0) load_q(unit);
           __syncwarp();
         }
         if (!ok) break;
         ++seg;
-        for (int i = pre; i < 2 * n && ok; ++i) issue(i);
+        base += 2 * n;
         tiles_done += n;
       }
       if (*abort_flag && lane == 0) {   // no copy may land in shared memory after the CTA exits
-        for (int t = max(0, issued - SLOTS); t < issued; ++t)
-          mbar_wait(&full_bar[t % SLOTS], (t / SLOTS) & 1, p.status, nullptr);
-        if (seg > 0) mbar_wait(q_full, (seg - 1) & 1, p.status, nullptr);
+        for (int s = 0; s < SLOTS; ++s)
+          if (armed >> s & 1) mbar_wait_for(&full_bar[s], phases >> s & 1, p.status, nullptr, 20000000);
+        if (k && seg > 0) mbar_wait_for(q_full, (seg - 1) & 1, p.status, nullptr, 20000000);
       }
     } else if (lane == 0) {
       tma_prefetch_map(&kmap);
