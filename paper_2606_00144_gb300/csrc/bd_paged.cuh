@@ -89,6 +89,38 @@ struct PagedMap {
   }
 };
 
+// A producer warp's walk over its CTA's segments (a segment: the tiles of a unit in the CTA's range), and the pages of a
+// segment's pieces (a piece: a page's rows of a tile, or the whole tile), 32 looked up at once, a lane each.
+template <int KEYS, typename Map, typename Params>
+struct PageWalk {
+  const Map& map;
+  const Params& p;
+  int u_last, v0, v1;
+  struct Segment {
+    int unit, tb, n, seq, head, end;   // n tiles from tb; end: rows of the sequence, its block's among them (unit > u_last: none)
+  };
+  __device__ __forceinline__ Segment from(int unit) const {
+    Segment s{unit, 0, 0, 0, 0, 0};
+    for (; s.unit <= u_last; ++s.unit) {
+      s.tb = map.first_tile(s.unit, v0);
+      s.n = map.end_tile(s.unit, v1) - s.tb;
+      if (s.n <= 0) continue;
+      s.seq = map.seq_of(s.unit);
+      s.head = s.unit / p.row_chunks - s.seq * p.h_kv;
+      s.end = paged_context(p.seq_lens, s.seq, p.t_ctx, nullptr) + p.n_q;
+      return s;
+    }
+    s.n = 0;
+    return s;
+  }
+  // The entry of the segment's piece first + lane (nothing looks at it here, so that the load is on its way while others are
+  // used); negative past the segment and the sequence's rows.
+  __device__ __forceinline__ int entry(const Segment& s, int first, int lane) const {
+    const int at = first + lane, key = s.tb * KEYS + (at << p.box_shift);
+    return at < s.n * (KEYS >> p.box_shift) && key < s.end ? p.pages.entry(s.seq, key) : -1;
+  }
+};
+
 // A verify block on the tcgen05 kernel, which has a second producer warp then.
 constexpr int kPagedTcThreads = kVTcThreads + 32;
 struct PagedTcParams : VerifyParams {

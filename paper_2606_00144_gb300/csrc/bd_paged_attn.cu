@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     tma_prefetch_map(&vmap);
   }
   if (tid < D) nan_from[tid] = INT_MAX;
-  if (CLUSTER) {   // the sequence's entries and the queries on their way into L2 meanwhile
+  if (CLUSTER) {   // the sequence's entries and the queries on their way into L2 while the kernel before ends
     const int seq = (int)blockIdx.y / (p.h_kv * p.row_chunks), pages = min(p.pages.pages, ((p.t_ctx + p.n_q - 1) >> p.pages.shift) + 1);
     prefetch_lines_l2(p.pages.table + (size_t)seq * p.pages.pages, min(pages, 2048) * sizeof(int32_t), tid, L::THREADS);
     prefetch_lines_l2(p.q + (size_t)(blockIdx.y / p.row_chunks) * p.rows_total * D, (size_t)p.rows_total * D * 2, tid, L::THREADS);
@@ -130,11 +130,9 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     const int tiles = (t + p.n_q + kPvKeys - 1) / kPvKeys, per = (tiles + (int)gridDim.x - 1) / (int)gridDim.x;
     v0 = min(tiles, (int)blockIdx.x * per);
     v1 = min(tiles, v0 + per);
-    __syncthreads();
   } else {
     map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
     if (p.seq_lens) map.template lay_out<L::THREADS, kPvKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 256), pref);
-    else __syncthreads();
     const int v_total = map.seq_base(p.batch);
     v0 = min(v_total, (int)blockIdx.x * map.vtpc);
     v1 = min(v_total, v0 + map.vtpc);
@@ -143,13 +141,23 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     u_last = map.unit_of(v1 - 1);
   }
 
+  // the producers' first look-ups, whose round trip is the longest thing before the first tile
+  const PageWalk<kPvKeys, Map, PagedVerifyParams> walk{map, p, u_last, v0, v1};
+  typename PageWalk<kPvKeys, Map, PagedVerifyParams>::Segment seg{};
+  int now = -1, then = -1;
+  if (warp >= WARPS) {
+    seg = walk.from(u_first);
+    now = walk.entry(seg, 0, lane);
+    then = walk.entry(seg, 32, lane);
+  }
+  if (CLUSTER || !p.seq_lens) __syncthreads();             // (else the layout was one)
+
   if (warp >= WARPS) {
     // ------------------------------------------------------------------ producers: K, V
     fence_proxy_async_global();
-    // A tile is n_box pieces (a page's rows, or 64 of them); a lane fetches one, which takes a warp some 130 cycles a piece,
-    // so K and V have one each (both in one warp: 0.55 us a tile in pages of 16, whatever the consumers do).  The
-    // entries of 32 pieces are looked up at once, the next 32 while these are used: one tile's at a time, a CTA's first tiles
-    // came a round trip to memory apart.
+    // A tile is n_box pieces of K and of V; a lane fetches one, which takes a warp some 130 cycles a piece, so K and V have a warp
+    // each (both in one: 0.55 us a tile in pages of 16, whatever the consumers do).  Entries are looked up 32 pieces, and the
+    // next segment's, ahead: a tile at a time, a CTA's first tiles came a round trip to memory apart.
     const int which = warp - WARPS, n_box = kPvKeys >> p.box_shift, piece = lane & (n_box - 1);
     const uint32_t piece_bytes = (uint32_t)D * 2 << p.box_shift;
     const int page_mask = (1 << p.pages.shift) - 1;
@@ -157,26 +165,18 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     int issued = 0, s = 0;
     uint32_t phase = 1;                                    // of the stage's last use (its first waits for none)
     bool ok = true;
-    for (int unit = u_first; unit <= u_last && ok; ++unit) {
-      const int tb = map.first_tile(unit, v0), n = map.end_tile(unit, v1) - tb;
-      if (n <= 0) continue;
-      const int seq = map.seq_of(unit), head = unit / p.row_chunks - seq * p.h_kv;
-      const int end = paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + p.n_q;   // rows of the sequence, its block's among them
-      auto look_up = [&](int first) {                      // entry of the segment's piece first + lane; -1: not there
-        const int at = first + lane, key = tb * kPvKeys + (at << p.box_shift);
-        const int e = at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
-        if (e >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
-        return p.pages.there(e) ? e : -1;
-      };
-      int now = look_up(0), then = look_up(32);
-      for (int i = 0; i < n; ++i) {
+    while (seg.unit <= u_last && ok) {
+      auto next = seg;
+      int next_now = -1, next_then = -1;
+      for (int i = 0; i < seg.n; ++i) {
         const int at = i * n_box & 31;
         if (i > 0 && at == 0) {
           now = then;
-          then = look_up(i * n_box + 32);
+          then = walk.entry(seg, i * n_box + 32, lane);
         }
         const int entry = __shfl_sync(0xffffffffu, now, at + piece);
-        const uint32_t pieces = __ballot_sync(0xffffffffu, now >= 0) >> at & ((1u << n_box) - 1);
+        const uint32_t pieces = __ballot_sync(0xffffffffu, p.pages.there(now)) >> at & ((1u << n_box) - 1);
+        if (entry >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
         if (issued >= stages) ok = mbar_wait_warp(&empty_bar[s], phase, p.status, abort_flag);
         if (!ok) break;
         if (lane == 0) {
@@ -190,13 +190,25 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
           else mbar_arrive(&full_bar[s]);
         }
         __syncwarp();
-        if (entry >= 0 && lane < n_box)
+        if (p.pages.there(entry) && lane < n_box)
           tma_load_page(1, smem_u32(stage_base + s * L::STAGE + which * L::TILE) + piece * piece_bytes, my_map, &full_bar[s],
-                        ((tb + i) * kPvKeys + (piece << p.box_shift)) & page_mask, 0, head, entry);
+                        ((seg.tb + i) * kPvKeys + (piece << p.box_shift)) & page_mask, 0, seg.head, entry);
         __syncwarp();
         ++issued;
         if (++s == stages) s = 0, phase ^= 1;
+        if (i == 0) {
+          if (CLUSTER) {
+            next.unit = u_last + 1;
+          } else {
+            next = walk.from(seg.unit + 1);
+            next_now = walk.entry(next, 0, lane);
+            next_then = walk.entry(next, 32, lane);
+          }
+        }
       }
+      seg = next;
+      now = next_now;
+      then = next_then;
     }
     if (*abort_flag && lane == 0) {      // never leave a copy in flight behind an aborted CTA
       for (int t = max(0, issued - stages); t < issued; ++t)

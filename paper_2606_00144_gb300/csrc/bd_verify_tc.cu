@@ -163,6 +163,18 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
   const int u_first = map.unit_of(v0), u_last = map.unit_of(v1 - 1);
 
   if constexpr (!PAGED) start();
+  // PAGED: the producers' first look-ups, whose round trip is the longest thing before the first tile
+  using Walk = PageWalk<kVTcKeys, decltype(map), VerifyTcParams<MODE>>;
+  [[maybe_unused]] std::conditional_t<PAGED, typename Walk::Segment, int> first_seg{};
+  [[maybe_unused]] int now = -1, then = -1;
+  if constexpr (PAGED) {
+    if (warp == 0 || warp == kVTcThreads / 32) {
+      const Walk walk{map, p, u_last, v0, v1};
+      first_seg = walk.from(u_first);
+      now = walk.entry(first_seg, 0, lane);
+      then = walk.entry(first_seg, 32, lane);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -195,8 +207,8 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
     if constexpr (PAGED) {
       // Two producers, of K (warp 0) and of V (the last warp), each walking its own entries of the ring.  A tile is n_box pieces (a
       // page's rows, or 128 of them), each some 130 cycles of a warp (both in one warp: 64 units of 16K, 32 rows, d 64, pages of
-      // 16 took 81.8 us).  The entries of 32 pieces are looked up at once, the next 32 while these are used.  The copies are issued by an elected
-      // lane of the converged warp.
+      // 16 took 81.8 us).  Entries are looked up 32 pieces, and the next segment's, ahead.  The copies are issued by an elected lane of the
+      // converged warp.
       fence_proxy_async_global();
       const uint32_t lead = elect_leader();
       const bool k = warp == 0;
@@ -210,18 +222,12 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
       bool ok = true;
       int base = 0, seg = 0, tiles_done = 0;
       uint32_t armed = 0, phases = 0;               // stages this warp has filled, and the parities of the last time
-      for (int unit = u_first; unit <= u_last && ok; ++unit) {
-        const int tb = map.first_tile(unit, v0), te = map.end_tile(unit, v1), n = te - tb;
-        if (n <= 0) continue;
-        const int kv_unit = unit / p.row_chunks, seq = kv_unit / p.h_kv, head = kv_unit - seq * p.h_kv;
-        const int end = paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + p.n_q;   // rows of the sequence
-        auto look_up = [&](int first) {                    // entry of the segment's piece first + lane; n_pages: not there
-          const int at = first + lane, key = tb * kVTcKeys + (at << p.box_shift);
-          const int e = at < n * n_box && key < end ? p.pages.entry(seq, key) : -1;
-          if (k && e >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
-          return p.pages.there(e) ? e : p.pages.n_pages;
-        };
-        int now = look_up(0), then = look_up(32);
+      const Walk walk{map, p, u_last, v0, v1};
+      auto at_seg = first_seg;
+      while (at_seg.unit <= u_last && ok) {
+        const int unit = at_seg.unit, tb = at_seg.tb, n = at_seg.n;
+        auto next = at_seg;
+        int next_now = -1, next_then = -1;
         // the queries behind the first keys: a later segment's stream while its predecessor's last scores still read them
         const int early = k && seg > 0 ? min(n, (SLOTS + 1) / 2) : 0;
         for (int i = 0; i < n; ++i) {
@@ -234,12 +240,13 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           const int at = i * n_box & 31, key0 = (tb + i) * kVTcKeys;
           if (i > 0 && at == 0) {
             now = then;
-            then = look_up(i * n_box + 32);
+            then = walk.entry(at_seg, i * n_box + 32, lane);
           }
           const int r = base + (k ? k_pos(i) : v_pos(i, n)), s = r % SLOTS;
           if (r >= SLOTS) ok = mbar_wait_warp(&empty_bar[s], ((r / SLOTS) & 1) ^ 1, p.status, abort_flag);
           if (!ok) break;
-          const uint32_t gone = __ballot_sync(0xffffffffu, now == p.pages.n_pages) >> at;
+          const uint32_t gone = ~__ballot_sync(0xffffffffu, p.pages.there(now)) >> at;
+          if (k && now >= p.pages.n_pages && lane >= at && lane < at + n_box) record_error(p.status, BD_ERR_INVALID_ARG);
           if (lane == 0) {
             if (k) {
               int hide = 0;
@@ -247,7 +254,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
               for (int g = 0; g < kVTcKeys / 16; ++g) hide |= (int)(gone >> (16 * g >> p.box_shift) & 1) << g;
               hide_s[(tiles_done + i) & 15] = hide;
             } else if (i == n - 1) {
-              live_s[s] = end - key0;
+              live_s[s] = at_seg.end - key0;
             }
             mbar_arrive_expect_tx(&full_bar[s], TILE);
           }
@@ -257,7 +264,8 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           const uint32_t dst = smem_u32(ring + s * TILE);
 #pragma unroll 2
           for (int j = 0; j < n_box; ++j) {                // (a page that the pool has not: zeros)
-            const int e = __shfl_sync(0xffffffffu, now, at + j), row = (key0 + (j << p.box_shift)) & page_mask;
+            const int found = __shfl_sync(0xffffffffu, now, at + j), row = (key0 + (j << p.box_shift)) & page_mask, head = at_seg.head;
+            const int e = p.pages.there(found) ? found : p.pages.n_pages;
             if constexpr (BOX16) {
               tma_load_page(lead, dst + j * 4096, my_map, &full_bar[s], row, 0, head, e);
             } else {
@@ -265,6 +273,11 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
               for (int h = 0; h < D / 64; ++h)
                 tma_load_page(lead, dst + h * kTHalf + (j << p.box_shift) * 128, my_map, &full_bar[s], row, h, head, e);
             }
+          }
+          if (i == 0) {
+            next = walk.from(unit + 1);
+            next_now = walk.entry(next, 0, lane);
+            next_then = walk.entry(next, 32, lane);
           }
         }
         if (ok && early == n && k && seg > 0) {            // (all its keys were early)
@@ -276,6 +289,9 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
         ++seg;
         base += 2 * n;
         tiles_done += n;
+        at_seg = next;
+        now = next_now;
+        then = next_then;
       }
       if (*abort_flag && lane == 0) {   // no copy may land in shared memory after the CTA exits
         for (int s = 0; s < SLOTS; ++s)
