@@ -3,14 +3,21 @@
 //
 //   o_i = sum_k 2^(s_ik - M) v_k / sum_k 2^(s_ik - M),  s = q k log2(e) / sqrt(d)
 //
-// One pass over K and V with a running maximum and sum.  The (unit, 64-key tile) pairs of all (sequence, KV head)
-// units form one list, cut into contiguous ranges of equal cost, one per CTA; each piece of a unit ("segment") ends in
-// a normalised partial, and row-merge joins the segments of units that span CTAs.
-//   warp 4      producer: a tile is 64 / (rows of a box) pages' pieces of K and of V, each one TMA box (rows x both
-//               64-column halves), one lane each, which looked its page up a tile ahead.  Pieces whose page is not there, or that
-//               lie past the sequence's block, are not read.
-//   warps 0..3  16 keys of a tile each on mma.sync (bd_attn_warp.cuh), the query rows on the N side.
-// The pieces of a tile lie one behind the other, so a warp's 16 keys are in one piece (pages hold at least 16 rows).
+// One pass over K and V with a running maximum and sum, in 64-key tiles.  Two producer warps fetch a tile's pieces of K and of
+// V (a page's rows of the tile, each one TMA box of whole rows); the consumer warps take 16 keys of it each on mma.sync
+// (bd_attn_warp.cuh), the query rows on the N side.  The pieces of a tile lie one behind the other, so a warp's 16 keys are in
+// one piece (pages hold at least 16 rows).  Pieces whose page is not there, or that lie past the sequence's block, are not
+// fetched, and their keys are passed over.
+//   cluster  a unit's tiles (a unit: a sequence's KV head, and up to 8 of its query rows) are split over the CTAs of a
+//            cluster, or go to one CTA.  For short units, and for many, which the hardware deals out.
+//   stream   the (unit, tile) pairs of all units form one list, cut into contiguous ranges of equal cost, one per CTA; each
+//            piece of a unit ("segment") ends in a partial, and a second kernel joins those of units that span CTAs.  For
+//            few long units.
+// More query rows than that are the tcgen05 kernel's (bd_verify_tc.cu, PAGED).
+//
+// Bound by HBM where there is enough to read: 256 units of 1.6K to 8K (630 MB) take 94 us (6.7 TB/s), 256 of 4K 82 (6.5), 8
+// of 128K 87 to 89 (6.1: a start of some 6 us, of which the page's look-up and the first tile, both from DRAM, are 5, and an
+// end of 5), in pages of 16 as in larger ones.  Short calls are a chain of latencies: 8 units of 1K 5.3 us, 2 of 1K (d 64) 4.0.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -27,7 +34,7 @@ namespace cg = cooperative_groups;
 namespace bd {
 
 constexpr int kPvKeys = 64;           // keys of a tile
-constexpr int kPvSubs = kPvKeys / 16; // sub-tiles of a warp's
+constexpr int kPvSubs = kPvKeys / 16; // a warp's sub-tiles
 constexpr int kPvStages = 5;          // tiles in flight of a stream
 constexpr int kPvMaxStages = 12;      // and at most
 constexpr int kPvCluster = 8;         // most CTAs of a cluster (the portable size)
@@ -76,13 +83,12 @@ struct PagedSmem {
   static size_t slots(int C) { return (size_t)C * slot_rows(C) * (D + 1) * 4; }
 };
 
-// CLUSTER: a unit's tiles are split over the CTAs of a cluster, which meet in shared memory: no partials, no second launch.
-// For blocks that the device holds all at once this way, where a chain of latencies counts; there six warps take the
-// sub-tiles in turn.
+// CLUSTER: a unit's tiles are split over the CTAs of a cluster, which meet in shared memory: no partials, no second launch; six
+// warps take the sub-tiles in turn.
 template <int D, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER || D == 64 ? 2 : 1) paged_verify_kernel(const __grid_constant__ PagedVerifyParams p,
-                                                                  const __grid_constant__ CUtensorMap kmap,
-                                                                  const __grid_constant__ CUtensorMap vmap) {
+__global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER || D == 64 ? 2 : 1)
+    paged_verify_kernel(const __grid_constant__ PagedVerifyParams p, const __grid_constant__ CUtensorMap kmap,
+                        const __grid_constant__ CUtensorMap vmap) {
   using L = PagedSmem<D, NT, CLUSTER>;
   constexpr int NQC = L::NQC, WARPS = L::WARPS, NCT = 32 * WARPS;
   const int stages = CLUSTER ? p.stages : kPvStages;

@@ -298,3 +298,58 @@ def test_rows_behind_two_gigabytes_of_elements():
         want = ref.attend(qs, k[0, h].double(), v[0, h].double(), torch.ones(2, n, dtype=torch.bool))
         ref.check(o[0, 2 * h:2 * h + 2, 0], lse[0, 2 * h:2 * h + 2, 0], *want)
         ref.check(o2[0, 2 * h:2 * h + 2], lse2[0, 2 * h:2 * h + 2], *want)
+
+
+def test_no_rows_is_nothing():
+    cache = bd.PagedCache.empty(2, 2, 16, 64)
+    table = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    shape = cache.shape(1, 4, 0, 32)
+    none = [torch.empty(1, h, 0, 64, dtype=BF, device="cuda") for h in (4, 2, 2, 4)]
+    bd.bd_paged_append(shape, *none[:3], None, cache, table, none[3])
+    some = torch.zeros(1, 4, 3, 64, dtype=BF, device="cuda")
+    bd.bd_paged_append(shape, some[:, :, :0], some[:, :2, :0], some[:, 2:, :0], None, cache, table, none[3])
+    starts = torch.zeros(2, dtype=torch.int32, device="cuda")
+    packed = [torch.empty(h, 0, 64, dtype=BF, device="cuda") for h in (4, 2, 2, 4)]
+    bd.bd_paged_append(shape, *packed[:3], None, cache, table, packed[3], row_starts=starts)
+    bd.bd_paged_read(shape, cache, table, none[1], none[2], first_row=0)
+    bd.bd_paged_read(shape, cache, table, none[1], first_row=32)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("h_q,h_kv,d", [(1, 1, 64), (3, 1, 128), (71, 1, 64), (12, 12, 128), (5, 5, 64), (64, 8, 128)])
+@pytest.mark.parametrize("total", [1, 7, 3000])
+def test_append_head_counts(h_q, h_kv, d, total):
+    """Rows of a token that divide a CTA's slots in many ways, few tokens and many."""
+    pool = ref.Pool([total], h_kv, 64, d, seed=1)
+    freq = frequencies(d, 10000.0)
+    got = run_append(pool, [0], [total], h_q, d, BF, bd.Rope(freq), by_token=True, h_kv=h_kv, uniform=True, t=0)
+    src, q_out, K, V = got
+    want = ref.rotate(src["q"][0], torch.arange(total), freq, False)
+    assert ((q_out[0].double() - want).abs() <= ref.rotate_tolerance(src["q"][0], want, freq, False)).all()
+    pos = torch.arange(total)
+    at = pool.table[0][pos // 64].long()
+    want = ref.rotate(src["k"][0], pos, freq, False)
+    for h in range(h_kv):
+        assert ((K[at, h, pos % 64].double() - want[h]).abs() <= ref.rotate_tolerance(src["k"][0, h], want[h], freq, False)).all()
+        assert torch.equal(V[at, h, pos % 64], src["v"][0, h])
+
+
+@pytest.mark.parametrize("batch", [33, 1025, 1100])
+def test_packed_prompts_of_many_sequences(batch):
+    """More sequences than one round of probes, and two, tell apart; many of them empty."""
+    d, h = 64, 1
+    g = torch.Generator().manual_seed(batch)
+    counts = [int(x) for x in torch.randint(0, 4, (batch,), generator=g)]
+    counts[:3], counts[-2:] = [0, 0, 2], [3, 0]
+    pool = ref.Pool([max(c, 1) for c in counts], h, 16, d, seed=3, cap=16)
+    K, V, table = pool.cuda()
+    cache = bd.PagedCache(K, V)
+    n = sum(counts)
+    rows = torch.randn(h, n, d, generator=g).to(BF)
+    starts = torch.tensor([0] + torch.tensor(counts).cumsum(0).tolist(), dtype=torch.int32)
+    bd.bd_paged_append(cache.shape(batch, h, 0, 16), None, rows.cuda(), rows.cuda(), None, cache, table, None, row_starts=starts.cuda())
+    K, V = K.cpu(), V.cpu()
+    for i in range(batch):
+        e = int(pool.table[i, 0])
+        assert torch.equal(K[e, 0, :counts[i]], rows[0, int(starts[i]):int(starts[i + 1])])
+        assert torch.equal(V[e, 0, :counts[i]], rows[0, int(starts[i]):int(starts[i + 1])])

@@ -208,3 +208,56 @@ def test_a_chain_of_calls_on_another_stream():
         visible = (torch.arange(t + 4)[None, :] <= (t + torch.arange(4).repeat(G))[:, None]) & there
         want = ref.attend(out[-4][i, 12:16].cpu().reshape(-1, d), kk, vv, visible)
         ref.check(out[-3][i, 12:16].reshape(-1, d), out[-2][i, 12:16].reshape(-1), *want)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Graphs of blocks that take different routes (partials of different sizes), one workspace, replayed in turn; and both at
+    once with workspaces of their own."""
+    d, page = 128, 16
+    g = torch.Generator("cuda").manual_seed(2)
+
+    def make(b, h_kv, G, t, n):
+        per = -(-(t + n) // page)
+        k, v = (torch.randn(b * per, h_kv, page, d, generator=g, device="cuda").to(BF) for _ in "kv")
+        table = torch.randperm(b * per, generator=g, device="cuda").view(b, per).int()
+        q = torch.randn(b, h_kv * G, n, d, generator=g, device="cuda").to(BF)
+        cache = bd.PagedCache(k, v)
+        shape = cache.shape(b, h_kv * G, t, t + n)
+        return shape, q, n, cache, table
+
+    calls = [make(1, 2, 4, 30000, 1), make(4, 8, 8, 1500, 21), make(2, 8, 4, 500, 1)]
+    sizes = [bd.bd_workspace_size(c[0], bd.BD_OP_PAGED_VERIFY, 0, c[2]) for c in calls]
+    shared = bd.Workspace(max(sizes))
+    want = []
+    for c, size in zip(calls, sizes):
+        o, lse = torch.empty_like(c[1]), torch.empty(c[1].shape[:3], device="cuda")
+        bd.bd_paged_verify_attn(*c, o, lse, bd.Workspace(size))
+        want.append((o, lse))
+    graphs, outs = [], []
+    for c in calls:
+        o, lse = torch.empty_like(c[1]), torch.empty(c[1].shape[:3], device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            bd.bd_paged_verify_attn(*c, o, lse, shared)
+        graphs.append(graph)
+        outs.append((o, lse))
+    for order in ([0, 1, 2], [2, 1, 0], [1, 1, 0, 2]):
+        for o, lse in outs:
+            o.fill_(7)
+            lse.fill_(7)
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for (o, lse), (wo, wl) in zip(outs, want):
+            assert torch.equal(o, wo) and torch.equal(lse, wl)
+    assert shared.status() == 0
+    # at once, on streams of their own
+    streams = [torch.cuda.Stream() for _ in calls]
+    spaces = [bd.Workspace(size) for size in sizes]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, s, w, (o, lse) in zip(calls, streams, spaces, outs):
+            bd.bd_paged_verify_attn(*c, o, lse, w, stream=s)
+    torch.cuda.synchronize()
+    for w, (o, lse), (wo, wl) in zip(spaces, outs, want):
+        assert w.status() == 0 and torch.equal(o, wo) and torch.equal(lse, wl)
