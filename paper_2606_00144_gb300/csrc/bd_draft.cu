@@ -23,6 +23,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <type_traits>
 
@@ -548,11 +549,11 @@ bool draft_plan(const bd_shape& s, int budget, int n_steps, size_t room, DraftPl
                                    draft_pos_slots(*plan)) <= kMaxSmem;
 }
 
-// p: what the caller's cache needs is set; the rest is set here.  (A short instance takes the first part of DraftLongParams.)
+// p: what the caller's cache needs is set; the rest is set here.  allowed: the instance's own, or null.  (A short instance takes the first part of DraftLongParams.)
 static cudaError_t launch_instance(const bd_shape& s, const DraftPlan& plan, const void* q, const int32_t* idx,
                                    const int32_t* count, int budget, int step_j, unsigned flags, void* o_out, float* lse_out,
                                    void* ws_region, int* counters, int* status, cudaStream_t stream, DraftFn fn,
-                                   DraftLongParams& p) {
+                                   std::atomic<uint64_t>* allowed, DraftLongParams& p) {
   const int units = s.batch * s.h_kv;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.idx = idx;
@@ -579,7 +580,8 @@ static cudaError_t launch_instance(const bd_shape& s, const DraftPlan& plan, con
   const int g_kernel = draft_group_instance(g);
   p.g = g;
   const size_t smem = smem_bytes(s.head_dim, g_kernel, plan.longs, p.n_stage, plan.n_split, p.pos_slots);
-  cudaError_t err = allow_shared_memory(fn, plan.longs ? kDLongStatic : 0);
+  const size_t fixed = plan.longs ? kDLongStatic : 0;
+  const cudaError_t err = allowed ? allow_shared_memory_once(fn, fixed, allowed) : allow_shared_memory(fn, fixed);
   if (err != cudaSuccess) return err;
 
   void* args[] = {&p};
@@ -596,20 +598,22 @@ cudaError_t launch_draft(const bd_shape& s, const DraftPlan& plan, const void* q
   p.k = static_cast<const __nv_bfloat16*>(k_cache);
   p.v = static_cast<const __nv_bfloat16*>(v_cache);
   return launch_instance(s, plan, q, idx, count, budget, step_j, flags, o_out, lse_out, ws_region, counters, status, stream,
-                         pick(s.head_dim, draft_group_instance(s.h_q / s.h_kv), plan.longs), p);
+                         pick(s.head_dim, draft_group_instance(s.h_q / s.h_kv), plan.longs), nullptr, p);
 }
 
 cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const bd_paged_cache& c,
                                const int32_t* table, int table_pages, const int32_t* idx, const int32_t* count, int budget,
                                int step_j, unsigned flags, void* o_out, float* lse_out, void* ws_region, int* counters,
                                int* status, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed[2][17][2];
+  const int g = draft_group_instance(s.h_q / s.h_kv);
   DraftPagedParams p;
   p.k = p.v = nullptr;
   p.pk = {static_cast<__nv_bfloat16*>(c.k), c.k_strides[0], c.k_strides[1], c.k_strides[2]};
   p.pv = {static_cast<__nv_bfloat16*>(c.v), c.v_strides[0], c.v_strides[1], c.v_strides[2]};
   p.pages = {table, table_pages, c.n_pages, page_shift(c)};
   return launch_instance(s, plan, q, idx, count, budget, step_j, flags, o_out, lse_out, ws_region, counters, status, stream,
-                         pick<true>(s.head_dim, draft_group_instance(s.h_q / s.h_kv), plan.longs), p);
+                         pick<true>(s.head_dim, g, plan.longs), &allowed[s.head_dim == 128][g][plan.longs], p);
 }
 
 // ============================================================================ allocation-free variant

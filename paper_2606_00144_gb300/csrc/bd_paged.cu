@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kPgThreads, 4) paged_append_kernel(const __gri
     if (mine) {
       if (p.row_starts) {
         const int first = __ldcg(p.row_starts + seq);
-        mine = i >= first && i < __ldcg(p.row_starts + seq + 1);
+        mine = first >= 0 && i >= first && i < __ldcg(p.row_starts + seq + 1);
         i -= first;
       }
       my_pos = (long long)paged_context(p.seq_lens, seq, p.t_ctx, nullptr) + i;

@@ -208,7 +208,8 @@ def test_broken_row_starts_stay_in_bounds():
     K, V, table = pool.cuda()
     cache = bd.PagedCache(K, V)
     rows = torch.ones(2, n, d, dtype=BF, device="cuda")
-    for starts in ([0, 8, 2, 10], [5, 5, 5, 5], [-3, 0, 4, 1000], [1000, 0, -7, 3], [9, 8, 7, 6]):
+    for starts in ([0, 8, 2, 10], [5, 5, 5, 5], [-3, 0, 4, 1000], [1000, 0, -7, 3], [9, 8, 7, 6],
+                   [-2**31, -2**31, -2**31, 10], [-2**31, 2**31 - 1, 0, 10]):
         q_out = torch.full((2, n, d), 7.0, dtype=BF, device="cuda")
         bd.bd_paged_append(cache.shape(b, 2, 0, 32), rows, rows, rows, None, cache, table, q_out,
                            row_starts=torch.tensor(starts, dtype=torch.int32, device="cuda"))
