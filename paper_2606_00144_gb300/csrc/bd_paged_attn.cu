@@ -124,39 +124,45 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     prefetch_lines_l2(p.pages.table + (size_t)seq * p.pages.pages, min(pages, 2048) * sizeof(int32_t), tid, L::THREADS);
     prefetch_lines_l2(p.q + (size_t)(blockIdx.y / p.row_chunks) * p.rows_total * D, (size_t)p.rows_total * D * 2, tid, L::THREADS);
   }
+  using Map = std::conditional_t<CLUSTER, ClusterMap, PagedMap>;
+  using Walk = PageWalk<kPvKeys, Map, PagedVerifyParams>;
+  Map map;
+  int v0, v1, u_first, u_last;                             // this CTA's range of tiles, its units
+  typename Walk::Segment seg{};                            // the producers' first
+  auto plan = [&] {
+    if constexpr (CLUSTER) {
+      u_first = u_last = blockIdx.y;
+      map.per_seq = p.h_kv * p.row_chunks;
+      const int t = paged_context(p.seq_lens, map.seq_of(u_first), p.t_ctx, nullptr);
+      const int tiles = (t + p.n_q + kPvKeys - 1) / kPvKeys, per = (tiles + (int)gridDim.x - 1) / (int)gridDim.x;
+      v0 = min(tiles, (int)blockIdx.x * per);
+      v1 = min(tiles, v0 + per);
+    } else {
+      map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
+      if (p.seq_lens) map.template lay_out<L::THREADS, kPvKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 256), pref);
+      const int v_total = map.seq_base(p.batch);
+      v0 = min(v_total, (int)blockIdx.x * map.vtpc);
+      v1 = min(v_total, v0 + map.vtpc);
+      if (v0 < v1) {
+        u_first = map.unit_of(v0);
+        u_last = map.unit_of(v1 - 1);
+      }
+    }
+    if ((CLUSTER || v0 < v1) && warp >= WARPS) seg = Walk{map, p, u_last, v0, v1}.from(u_first);
+  };
+  if (!p.seq_lens) plan();                                 // (as much as can be before the wait)
+  __syncthreads();
   grid_dependency_wait();
   allow_dependent_launch();
-  using Map = std::conditional_t<CLUSTER, ClusterMap, PagedMap>;
-  Map map;
-  int v0, v1, u_first, u_last;
-  if constexpr (CLUSTER) {
-    u_first = u_last = blockIdx.y;
-    map.per_seq = p.h_kv * p.row_chunks;
-    const int t = paged_context(p.seq_lens, map.seq_of(u_first), p.t_ctx, nullptr);
-    const int tiles = (t + p.n_q + kPvKeys - 1) / kPvKeys, per = (tiles + (int)gridDim.x - 1) / (int)gridDim.x;
-    v0 = min(tiles, (int)blockIdx.x * per);
-    v1 = min(tiles, v0 + per);
-  } else {
-    map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
-    if (p.seq_lens) map.template lay_out<L::THREADS, kPvKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 256), pref);
-    const int v_total = map.seq_base(p.batch);
-    v0 = min(v_total, (int)blockIdx.x * map.vtpc);
-    v1 = min(v_total, v0 + map.vtpc);
-    if (v0 >= v1) return;
-    u_first = map.unit_of(v0);
-    u_last = map.unit_of(v1 - 1);
-  }
-
+  if (p.seq_lens) plan();
+  if (!CLUSTER && v0 >= v1) return;
   // the producers' first look-ups, whose round trip is the longest thing before the first tile
-  const PageWalk<kPvKeys, Map, PagedVerifyParams> walk{map, p, u_last, v0, v1};
-  typename PageWalk<kPvKeys, Map, PagedVerifyParams>::Segment seg{};
+  const Walk walk{map, p, u_last, v0, v1};
   int now = -1, then = -1;
   if (warp >= WARPS) {
-    seg = walk.from(u_first);
     now = walk.entry(seg, 0, lane);
     then = walk.entry(seg, 32, lane);
   }
-  if (CLUSTER || !p.seq_lens) __syncthreads();             // (else the layout was one)
 
   if (warp >= WARPS) {
     // ------------------------------------------------------------------ producers: K, V

@@ -132,12 +132,50 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
     }
   };
   std::conditional_t<PAGED, PagedMap, VerifyMap> map;
+  int v0 = 0, v1 = 0, u_first = 0, u_last = -1;     // this CTA's range of the list, its units
+  auto cut = [&](int v_total) {
+    v0 = min(v_total, (int)blockIdx.x * map.vtpc);
+    v1 = min(v_total, v0 + map.vtpc);
+    if (v0 >= v1) return;
+    u_first = map.unit_of(v0);
+    u_last = map.unit_of(v1 - 1);
+  };
+  using Walk = PageWalk<kVTcKeys, decltype(map), VerifyTcParams<MODE>>;
+  [[maybe_unused]] std::conditional_t<PAGED, typename Walk::Segment, int> first_seg{};
+  [[maybe_unused]] int now = -1, then = -1;         // entries of the first pieces
+  [[maybe_unused]] const bool producer = warp == 0 || warp == kVTcThreads / 32;
   if constexpr (PAGED) {
     map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
     if (tid < D) nan_from[tid] = INT_MAX;
+    if (tid == 32 * 2) {
+      tma_prefetch_map(&kmap);
+      tma_prefetch_map(&vmap);
+      tma_prefetch_map(&qmap);
+    }
     start();                                        // (nothing of it depends on what other kernels wrote)
+    auto first = [&] {
+      cut(map.seq_base(p.batch));
+      if (v0 < v1 && producer) first_seg = Walk{map, p, u_last, v0, v1}.from(u_first);
+    };
+    if (!p.seq_lens) first();                       // (as much as can be before the wait)
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
     grid_dependency_wait();
-    if (p.seq_lens) map.template lay_out<kPagedTcThreads, kVTcKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 512), pref);
+    if (p.seq_lens) {
+      map.template lay_out<kPagedTcThreads, kVTcKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 512), pref);
+      first();
+    }
+    if (v0 >= v1) {                                 // whole CTA idle
+      if (warp == 1) tmem_dealloc(*tmem_slot, 512);
+      return;
+    }
+    // the producers' first look-ups, whose round trip is the longest thing before the first tile
+    if (producer) {
+      const Walk walk{map, p, u_last, v0, v1};
+      now = walk.entry(first_seg, 0, lane);
+      then = walk.entry(first_seg, 32, lane);
+    }
   } else {
     map = VerifyMap{nullptr, p.tiles_per_unit, p.seg_cost, p.units, p.vtiles_per_cta};
   }
@@ -147,37 +185,14 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
     map.pref = pref;
     map.vtpc = max((pref[p.units] + (int)gridDim.x - 1) / (int)gridDim.x, p.vtiles_per_cta);
   }
-  int v_total;
-  if constexpr (PAGED) v_total = map.seq_base(p.batch);
-  else v_total = map.vbase(p.units);
-  const int v0 = min(v_total, (int)blockIdx.x * map.vtpc), v1 = min(v_total, v0 + map.vtpc);
-  if (v0 >= v1) {                                 // whole CTA idle
-    if constexpr (PAGED) {
-      tc_fence_before();
-      __syncthreads();
-      tc_fence_after();
-      if (warp == 1) tmem_dealloc(*tmem_slot, 512);
-    }
-    return;
+  if constexpr (!PAGED) {
+    cut(map.vbase(p.units));
+    if (v0 >= v1) return;                           // whole CTA idle
+    start();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
   }
-  const int u_first = map.unit_of(v0), u_last = map.unit_of(v1 - 1);
-
-  if constexpr (!PAGED) start();
-  // PAGED: the producers' first look-ups, whose round trip is the longest thing before the first tile
-  using Walk = PageWalk<kVTcKeys, decltype(map), VerifyTcParams<MODE>>;
-  [[maybe_unused]] std::conditional_t<PAGED, typename Walk::Segment, int> first_seg{};
-  [[maybe_unused]] int now = -1, then = -1;
-  if constexpr (PAGED) {
-    if (warp == 0 || warp == kVTcThreads / 32) {
-      const Walk walk{map, p, u_last, v0, v1};
-      first_seg = walk.from(u_first);
-      now = walk.entry(first_seg, 0, lane);
-      then = walk.entry(first_seg, 32, lane);
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   // S/P buffer b: columns 128 b; O[b]: columns 256 + D b
 
@@ -213,11 +228,6 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
       const uint32_t lead = elect_leader();
       const bool k = warp == 0;
       const CUtensorMap* my_map = k ? &kmap : &vmap;
-      if (lane == 0) {
-        tma_prefetch_map(my_map);
-        if (k) tma_prefetch_map(&qmap);
-      }
-      __syncwarp();
       const int n_box = kVTcKeys >> p.box_shift, page_mask = (1 << p.pages.shift) - 1;
       bool ok = true;
       int base = 0, seg = 0, tiles_done = 0;
