@@ -6,7 +6,7 @@
 // multiplication, and what is left of a full turn becomes the argument of sincospif.  A token's sines are worked out once
 // by its CTA and shared by all its heads (a thread that worked them out for its own elements would spend more on them than on
 // the rows).  Both kernels move each byte once and are bound by HBM where there is enough: 4 x 8192 tokens of 48 rows of 128
-// (805 MB) are appended in 135 us (5.95 TB/s), the keys of 8 x 16K positions of 8 heads (537 MB) read in 82 (6.5 TB/s).
+// (805 MB) are appended in 129 us (6.2 TB/s), the keys of 8 x 16K positions of 8 heads (537 MB) read in 82 (6.5 TB/s).
 #include <algorithm>
 
 #include "bd_internal.h"
@@ -390,16 +390,18 @@ cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const 
   p.nq = q.rows ? s.h_q : 0;
   p.nk = k.rows ? s.h_kv : 0;
   p.nv = v.rows ? s.h_kv : 0;
-  const int all = p.nq + p.nk + p.nv, at_once = kPgThreads / (s.head_dim / 16), sms = current_sm_count(), ahead = pg_ahead(e);
+  const int all = p.nq + p.nk + p.nv, at_once = kPgThreads / (s.head_dim / 16), sms = current_sm_count();
   // few tokens: a token's rows spread over CTAs, a pass of rows each
   int split = 1;
   while (split < 64 && (long)p.total * split < sms && all > at_once * split) split *= 2;
   p.rows_per_cta = (all + split - 1) / split;
-  // rows side by side: as many as divide a token's, or nearly; tokens: as many as that leaves room for, while there are enough
+  // rows side by side: as many as divide a token's, or nearly; tokens: up to four of a thread and row, while there are enough.  (A
+  // start, the look-ups and sines, costs a CTA some 2 us.  Two of a thread / four / eight, bf16, and one / four, fp32: 4 x 8192 tokens of 48
+  // rows 133 / 129 / 138 us, 188 / 178; of 40 rows 111 / 115 / 118; 2 x 2048 tokens of 48 rows 22.6 / 20.8 / 20.8, 28.9 / 26.5.)
   p.row_shift = 0;
   for (int k = 1; 1 << k <= at_once && 1 << k < 2 * p.rows_per_cta; ++k)
     if (((p.rows_per_cta + (1 << k) - 1) >> k << k) * 8 <= p.rows_per_cta * 9) p.row_shift = k;
-  const int room = std::min(kPgTokens, ahead * (at_once >> p.row_shift));
+  const int room = std::min(kPgTokens, 4 * (at_once >> p.row_shift));
   p.tokens = 1;
   while (2 * p.tokens <= room && p.total >= 6L * sms * p.tokens) p.tokens *= 2;
   const unsigned blocks = ((unsigned)p.total + p.tokens - 1) / p.tokens;
