@@ -432,10 +432,10 @@ static long clusters_held(int d, int g_kernel, bool longs, int c, size_t smem) {
   static thread_local int cache[2][2][17][kDMaxCluster + 1][5];
   int dev = 0;
   const int per_sm = ctas_per_sm(smem);
-  const long guess = (long)per_sm * current_sm_count() / c;
+  auto guess = [&] { return (long)per_sm * current_sm_count() / c; };
   if (cudaGetDevice(&dev) != cudaSuccess) {
     (void)cudaGetLastError();
-    return guess;
+    return guess();
   }
   if (dev != cache_dev) {
     std::fill_n(&cache[0][0][0][0][0], sizeof(cache) / sizeof(int), -1);
@@ -458,7 +458,7 @@ static long clusters_held(int d, int g_kernel, bool longs, int c, size_t smem) {
     if (allow_shared_memory(fn, longs ? kDLongStatic : 0) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) {
       (void)cudaGetLastError();
-      n = (int)guess;
+      n = (int)guess();
     }
     held = n;
   }

@@ -425,42 +425,53 @@ PvInfo pv_kernel(int d, int nt, bool cluster) {
 int pv_half(int d) { return d == 128 ? 3 : 6; }
 
 // Clusters of c CTAs that the device holds at once, one or two CTAs to an SM (a GPC's SMs are shared out by whole clusters).
-// Asked once per instance and c.
-long pv_clusters_held(int d, int c, bool alone) {
-  static thread_local int cache_dev = -1;
-  static thread_local int cache[2][2][kPvCluster + 1];
-  int dev = 0;
-  const long guess = (alone ? 1L : 2L) * current_sm_count() / c;
-  if (cudaGetDevice(&dev) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return guess;
-  }
-  if (dev != cache_dev) {
-    std::fill_n(&cache[0][0][0], sizeof(cache) / sizeof(int), -1);
-    cache_dev = dev;
-  }
-  int& held = cache[d == 128][alone][c];
-  if (held < 0) {
-    const PvInfo k = pv_kernel(d, 1, true);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(c);
-    cfg.blockDim = dim3(k.threads);
-    cfg.dynamicSmemBytes = k.bytes(pv_half(d) * (alone ? 2 : 1)) + k.slots(c);
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)c;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (allow_shared_memory_once(k.fn, 0, k.allowed) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k.fn, &cfg) != cudaSuccess) {
+// Asked once per instance and c; the device, once a plan (asked 24 times a plan, it was 0.7 of a call of 7 us).
+class PvClusters {
+ public:
+  PvClusters(int d, int sms) : d_(d), sms_(sms) {
+    static thread_local int cache_dev = -1;
+    static thread_local int cache[2][2][kPvCluster + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
       (void)cudaGetLastError();
-      n = (int)guess;
+      return;
     }
-    held = n;
+    if (dev != cache_dev) {
+      std::fill_n(&cache[0][0][0], sizeof(cache) / sizeof(int), -1);
+      cache_dev = dev;
+    }
+    held_ = cache[d == 128];
   }
-  return held;
-}
+  long operator()(int c, bool alone) const {
+    const long guess = (alone ? 1L : 2L) * sms_ / c;
+    if (!held_) return guess;
+    int& held = held_[alone][c];
+    if (held < 0) {
+      const PvInfo k = pv_kernel(d_, 1, true);
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(c);
+      cfg.blockDim = dim3(k.threads);
+      cfg.dynamicSmemBytes = k.bytes(pv_half(d_) * (alone ? 2 : 1)) + k.slots(c);
+      cudaLaunchAttribute at;
+      at.id = cudaLaunchAttributeClusterDimension;
+      at.val.clusterDim.x = (unsigned)c;
+      at.val.clusterDim.y = at.val.clusterDim.z = 1;
+      cfg.attrs = &at;
+      cfg.numAttrs = 1;
+      int n = 0;
+      if (allow_shared_memory_once(k.fn, 0, k.allowed) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k.fn, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = (int)guess;
+      }
+      held = n;
+    }
+    return held;
+  }
+
+ private:
+  int d_, sms_;
+  int (*held_)[kPvCluster + 1] = nullptr;
+};
 
 // CTAs an SM holds, by shared memory (228 KB, a CTA taking 1 KB more than it asks for).
 int pv_per_sm(size_t smem) { return std::max(1, (int)(228 * 1024 / (smem + 1024))); }
@@ -518,11 +529,12 @@ bool pv_cluster(const bd_shape& s, int rows, int n_q, PagedVerifyPlan* plan) {
   const long chunks = (rows + 7) / 8, groups = w.units * chunks, sms = std::max(1, current_sm_count());
   if (groups > 65535) return false;
   const double tile = s.head_dim == 128 ? 0.48 : 0.44;
+  const PvClusters clusters_held(s.head_dim, (int)sms);
   double best = pv_stream_us(s, rows, w);
   int c = 0, stages = 0;
   for (int n = (int)std::min<long>(kPvCluster, w.tiles); n >= 1; --n) {
-    const bool alone = groups <= pv_clusters_held(s.head_dim, n, true);
-    const long held = pv_clusters_held(s.head_dim, n, false);
+    const bool alone = groups <= clusters_held(n, true);
+    const long held = clusters_held(n, false);
     if (held < 1) continue;
     const long waves = (groups + held - 1) / held;
     if (waves > 1 && n > 2) continue;
