@@ -469,7 +469,6 @@ class PagedCache:
         self.k, self.v = k, v
         self._struct = BdPagedCache(k.data_ptr(), v.data_ptr(), (ctypes.c_int64 * 3)(*k.stride()[:3]),
                                     (ctypes.c_int64 * 3)(*v.stride()[:3]), self.n_pages, self.page_size)
-        self._ref = ctypes.byref(self._struct)
         self.is_cuda = k.is_cuda
         self._gpu = k.get_device() if self.is_cuda else None
 
@@ -503,7 +502,6 @@ class Rope:
         self.turns = torch.tensor([x - 2**64 if x >= 2**63 else x for x in turns], dtype=torch.int64, device=device)
         self.dim, self.interleaved, self.scale = 2 * freq.numel(), bool(interleaved), float(scale)
         self._struct = BdRope(self.turns.data_ptr(), self.dim, int(self.interleaved), self.scale)
-        self._ref = ctypes.byref(self._struct)
         self._gpu = self.turns.get_device() if self.turns.is_cuda else None
 
     @classmethod
@@ -602,8 +600,8 @@ def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, tabl
         kinds = (_BF16, _F32) if dtype not in (_BF16, _F32) else (dtype,)
         _refuse_paged("bd_paged_append", shape, cache, table, ((q_rows, want_q, kinds), (k_rows, want_kv, kinds), (v_rows, want_kv, kinds),
                                                                (q_out, want_q, (_BF16,))), row_starts, rope)
-    args = (ctypes.byref(shape), n, 1 if dtype is _BF16 else 2, q[0], q[1], k[0], k[1], v[0], v[1], _ptr(row_starts),
-            None if rope is None else rope._ref, cache._ref, table.data_ptr(), ts[1], o[0], o[1])
+    args = (shape, n, 1 if dtype is _BF16 else 2, q[0], q[1], k[0], k[1], v[0], v[1], _ptr(row_starts),
+            None if rope is None else rope._struct, cache._struct, table.data_ptr(), ts[1], o[0], o[1])
     fn = (_lib or library()).bd_paged_append
     st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
     if st:
@@ -629,7 +627,7 @@ def bd_paged_read(shape, cache: PagedCache, table, k_out, v_out=None, first_row=
     if not (h == cache.h_kv and d == cache.head_dim and k and v and table.dtype is _I32 and len(ts) == 2 and ts[0] == b
             and table.is_contiguous() and table.get_device() == gpu):
         _refuse_paged("bd_paged_read", shape, cache, table, ((k_out, want, (_BF16,)), (v_out, want, (_BF16,))))
-    args = (ctypes.byref(shape), first_row, want[2], cache._ref, table.data_ptr(), ts[1], k[0], k[1], v[0], v[1])
+    args = (shape, first_row, want[2], cache._struct, table.data_ptr(), ts[1], k[0], k[1], v[0], v[1])
     fn = (_lib or library()).bd_paged_read
     st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
     if st:
@@ -648,7 +646,7 @@ def bd_paged_verify_attn(shape, q, n_q, cache: PagedCache, table, o_out, lse_out
                                      and lse_out.get_device() == gpu))):
         _refuse_paged("bd_paged_verify_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
                       lse_out=(lse_out, _F32, want[:-1]))
-    args = (ctypes.byref(shape), q.data_ptr(), n_q, cache._ref, table.data_ptr(), ts[1], o_out.data_ptr(),
+    args = (shape, q.data_ptr(), n_q, cache._struct, table.data_ptr(), ts[1], o_out.data_ptr(),
             None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
     fn = (_lib or library()).bd_paged_verify_attn
     st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
@@ -671,7 +669,7 @@ def bd_paged_draft_attn(shape, q, cache: PagedCache, table, idx, count, budget, 
                                      and lse_out.get_device() == gpu))):
         _refuse_paged("bd_paged_draft_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
                       lse_out=(lse_out, _F32, (b, h_q)), idx=(idx, _I32, (b, h, budget)), count=(count, _I32, (b, h)))
-    args = (ctypes.byref(shape), q.data_ptr(), cache._ref, table.data_ptr(), ts[1], idx.data_ptr(), count.data_ptr(), budget, step_j,
+    args = (shape, q.data_ptr(), cache._struct, table.data_ptr(), ts[1], idx.data_ptr(), count.data_ptr(), budget, step_j,
             flags, o_out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
     fn = (_lib or library()).bd_paged_draft_attn
     st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)

@@ -427,16 +427,13 @@ static int ctas_per_sm(size_t smem) { return (int)std::min<size_t>(4, 228 * 1024
 
 // Clusters of c CTAs of smem bytes that the device holds at once.  (A GPC's SMs are shared out by whole clusters,
 // so it is fewer than the SMs' CTAs divided by c.)  Kept per instance, c and CTAs an SM.
-static long clusters_held(int d, int g_kernel, bool longs, int c, size_t smem) {
+// dev: the current device, or -1 if it is not known.
+static long clusters_held(int dev, int d, int g_kernel, bool longs, int c, size_t smem) {
   static thread_local int cache_dev = -1;
   static thread_local int cache[2][2][17][kDMaxCluster + 1][5];
-  int dev = 0;
   const int per_sm = ctas_per_sm(smem);
   auto guess = [&] { return (long)per_sm * current_sm_count() / c; };
-  if (cudaGetDevice(&dev) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return guess();
-  }
+  if (dev < 0) return guess();
   if (dev != cache_dev) {
     std::fill_n(&cache[0][0][0][0][0], sizeof(cache) / sizeof(int), -1);
     cache_dev = dev;
@@ -492,6 +489,11 @@ bool draft_plan(const bd_shape& s, int budget, int n_steps, size_t room, DraftPl
   // one CTA to an SM), 9.4 in smaller ones; groups of 16 27.9 / 13.1, 48 units of 512 rows 14.3 / 10.3.
   const long units = (long)s.batch * s.h_kv;
   const long sms = current_sm_count();
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    (void)cudaGetLastError();
+    dev = -1;
+  }
   const int most = (int)std::min<long>((entries + kDRows - 1) / kDRows, kDMaxCluster);
   auto dbuf_of = [&](int n) {
     const long rps = (entries + n - 1) / n;
@@ -506,7 +508,7 @@ bool draft_plan(const bd_shape& s, int budget, int n_steps, size_t room, DraftPl
     const bool dbuf = dbuf_of(n_split);
     const size_t smem = smem_of(n_split);
     if (smem <= kMaxSmem && units * n_split <= std::min(dbuf ? 2 : 3, ctas_per_sm(smem)) * sms &&
-        (!dbuf || units <= clusters_held(s.head_dim, g_kernel, false, n_split, smem)))
+        (!dbuf || units <= clusters_held(dev, s.head_dim, g_kernel, false, n_split, smem)))
       break;
   }
   n_split = std::max(n_split, 1);
@@ -528,7 +530,7 @@ bool draft_plan(const bd_shape& s, int budget, int n_steps, size_t room, DraftPl
   // of two CTAs gained nothing.
   double best_us = 3.1 + 1.0 * ((rows_per_split + kDRows - 1) / kDRows);
   for (int c = kDMaxCluster; c >= 3; --c) {
-    const long cap = clusters_held(s.head_dim, g_kernel, true, c, 200 * 1024);   // (one CTA an SM)
+    const long cap = clusters_held(dev, s.head_dim, g_kernel, true, c, 200 * 1024);   // (one CTA an SM)
     for (int k = 1; k <= kDMaxParts && units * k <= cap; ++k) {
       const long rps = (entries + c * k - 1) / (c * k);
       const double us = 3.0 + 1.33 * ((rps + kDLongRows - 1) / kDLongRows) + (k > 1 ? 2.05 : 0.0);
