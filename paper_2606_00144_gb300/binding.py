@@ -547,7 +547,7 @@ def _refuse_paged(name, shape, cache, table, rows=(), row_starts=None, rope=None
     _refuse(name, **tensors)
 
 
-_pack_strides = struct.Struct("3q").pack
+_pack_strides = struct.Struct("4q").pack          # (the last one, of a row's elements, goes unread)
 
 
 def _paged_rows(t, want, dtype, gpu):
@@ -559,14 +559,11 @@ def _paged_rows(t, want, dtype, gpu):
             return t.data_ptr(), None
         st = t.stride()
         if st[-1] == 1:
-            return t.data_ptr(), _pack_strides(*st[:3]) if len(st) == 4 else _pack_strides(0, st[0], st[1])
+            return t.data_ptr(), _pack_strides(*st) if len(st) == 4 else _pack_strides(0, *st)
     return None
 
 
-def _on_device(gpu, fn, args, stream):
-    """The call with the cache's GPU current, where that is another one."""
-    with torch.cuda.device(gpu):
-        return fn(*args, _stream(stream))
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, table, q_out, row_starts=None, stream=None):
@@ -600,10 +597,14 @@ def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, tabl
         kinds = (_BF16, _F32) if dtype not in (_BF16, _F32) else (dtype,)
         _refuse_paged("bd_paged_append", shape, cache, table, ((q_rows, want_q, kinds), (k_rows, want_kv, kinds), (v_rows, want_kv, kinds),
                                                                (q_out, want_q, (_BF16,))), row_starts, rope)
-    args = (shape, n, 1 if dtype is _BF16 else 2, q[0], q[1], k[0], k[1], v[0], v[1], _ptr(row_starts),
-            None if rope is None else rope._struct, cache._struct, table.data_ptr(), ts[1], o[0], o[1])
-    fn = (_lib or library()).bd_paged_append
-    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if _device() != gpu:                       # (the call with the cache's GPU current)
+        with torch.cuda.device(gpu):
+            return bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache, table, q_out, row_starts, stream)
+    st = (_lib or library()).bd_paged_append(
+        shape, n, 1 if dtype is _BF16 else 2, q[0], q[1], k[0], k[1], v[0], v[1],
+        None if row_starts is None else row_starts.data_ptr(),
+        None if rope is None else rope._struct, cache._struct, table.data_ptr(), ts[1], o[0], o[1],
+        _raw_stream(gpu) if stream is None else _stream(stream))
     if st:
         _check("bd_paged_append", st)
 
@@ -627,9 +628,12 @@ def bd_paged_read(shape, cache: PagedCache, table, k_out, v_out=None, first_row=
     if not (h == cache.h_kv and d == cache.head_dim and k and v and table.dtype is _I32 and len(ts) == 2 and ts[0] == b
             and table.is_contiguous() and table.get_device() == gpu):
         _refuse_paged("bd_paged_read", shape, cache, table, ((k_out, want, (_BF16,)), (v_out, want, (_BF16,))))
-    args = (shape, first_row, want[2], cache._struct, table.data_ptr(), ts[1], k[0], k[1], v[0], v[1])
-    fn = (_lib or library()).bd_paged_read
-    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if _device() != gpu:                       # (the call with the cache's GPU current)
+        with torch.cuda.device(gpu):
+            return bd_paged_read(shape, cache, table, k_out, v_out, None if first_row == BD_PAGED_BLOCK_ROWS else first_row, stream)
+    st = (_lib or library()).bd_paged_read(
+        shape, first_row, want[2], cache._struct, table.data_ptr(), ts[1], k[0], k[1], v[0], v[1],
+        _raw_stream(gpu) if stream is None else _stream(stream))
     if st:
         _check("bd_paged_read", st)
 
@@ -646,10 +650,13 @@ def bd_paged_verify_attn(shape, q, n_q, cache: PagedCache, table, o_out, lse_out
                                      and lse_out.get_device() == gpu))):
         _refuse_paged("bd_paged_verify_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
                       lse_out=(lse_out, _F32, want[:-1]))
-    args = (shape, q.data_ptr(), n_q, cache._struct, table.data_ptr(), ts[1], o_out.data_ptr(),
-            None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
-    fn = (_lib or library()).bd_paged_verify_attn
-    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if _device() != gpu:                       # (the call with the cache's GPU current)
+        with torch.cuda.device(gpu):
+            return bd_paged_verify_attn(shape, q, n_q, cache, table, o_out, lse_out, ws, stream)
+    st = (_lib or library()).bd_paged_verify_attn(
+        shape, q.data_ptr(), n_q, cache._struct, table.data_ptr(), ts[1], o_out.data_ptr(),
+        None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+        _raw_stream(gpu) if stream is None else _stream(stream))
     if st:
         _check("bd_paged_verify_attn", st)
 
@@ -669,10 +676,13 @@ def bd_paged_draft_attn(shape, q, cache: PagedCache, table, idx, count, budget, 
                                      and lse_out.get_device() == gpu))):
         _refuse_paged("bd_paged_draft_attn", shape, cache, table, q=(q, _BF16, want), o_out=(o_out, _BF16, want),
                       lse_out=(lse_out, _F32, (b, h_q)), idx=(idx, _I32, (b, h, budget)), count=(count, _I32, (b, h)))
-    args = (shape, q.data_ptr(), cache._struct, table.data_ptr(), ts[1], idx.data_ptr(), count.data_ptr(), budget, step_j,
-            flags, o_out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
-    fn = (_lib or library()).bd_paged_draft_attn
-    st = fn(*args, _stream(stream)) if torch._C._cuda_getDevice() == gpu else _on_device(gpu, fn, args, stream)
+    if _device() != gpu:                       # (the call with the cache's GPU current)
+        with torch.cuda.device(gpu):
+            return bd_paged_draft_attn(shape, q, cache, table, idx, count, budget, step_j, o_out, lse_out, ws, stream, flags)
+    st = (_lib or library()).bd_paged_draft_attn(
+        shape, q.data_ptr(), cache._struct, table.data_ptr(), ts[1], idx.data_ptr(), count.data_ptr(), budget, step_j,
+        flags, o_out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+        _raw_stream(gpu) if stream is None else _stream(stream))
     if st:
         _check("bd_paged_draft_attn", st)
 

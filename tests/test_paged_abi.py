@@ -251,7 +251,7 @@ def setting():
 def test_the_binding_refuses_rows(lib):
     c, s, table = setting()
     q, k, o = bf(2, 4, 3, 64), bf(2, 2, 3, 64), bf(2, 4, 3, 64)
-    r = types.SimpleNamespace(_gpu=0, dim=64, _ref=None)
+    r = types.SimpleNamespace(_gpu=0, dim=64, _struct=None)
 
     def bad(err, match, **kw):
         a = dict(shape=s, q_rows=q, k_rows=k, v_rows=k, rope=r, cache=c, table=table, q_out=o)
@@ -304,3 +304,42 @@ def test_the_binding_refuses_attention_tensors(lib):
     for a in [(bf(2, 4, 1, 64), idx, cnt), (q, i32(2, 2, 7), cnt), (q, idx, i32(4)), (q, i32(2, 2, 8, index=1), cnt)]:
         with pytest.raises(ValueError):
             bd.bd_paged_draft_attn(s, a[0], c, table, a[1], a[2], 8, 0, o, lse, ws)
+
+
+def test_a_call_runs_with_the_caches_gpu_current(monkeypatch):
+    """Tensors on GPU 1 while GPU 0 is current: every call reaches the library on GPU 1, with that GPU's stream, once."""
+    current, calls = [0], []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append((name, current[0], a)) or 0
+
+    monkeypatch.setattr(binding, "_lib", Library())
+    monkeypatch.setattr(binding, "_device", lambda: current[0])
+    monkeypatch.setattr(binding, "_raw_stream", lambda gpu: 100 + gpu)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+
+    def at(make, *shape):
+        return make(*shape, index=1)
+
+    c = bd.PagedCache(at(bf, 4, 2, 16, 64), at(bf, 4, 2, 16, 64))
+    s, table, ws = c.shape(2, 4, 10, 20), at(i32, 2, 2), types.SimpleNamespace(ptr=A, nbytes=BIG, buf=at(bf, 1))
+    q, kv = at(bf, 2, 4, 3, 64), at(bf, 2, 2, 3, 64)
+    bd.bd_paged_append(s, q, kv, kv, None, c, table, q)
+    bd.bd_paged_read(s, c, table, kv)
+    bd.bd_paged_read(s, c, table, kv, first_row=2)
+    bd.bd_paged_verify_attn(s, q, 3, c, table, q, None, ws)
+    bd.bd_paged_draft_attn(s, at(bf, 2, 4, 64), c, table, at(i32, 2, 2, 8), at(i32, 2, 2), 8, 1, at(bf, 2, 4, 64), None, ws)
+    assert [(name, gpu, a[-1]) for name, gpu, a in calls] == [(x, 1, 101) for x in (
+        "bd_paged_append", "bd_paged_read", "bd_paged_read", "bd_paged_verify_attn", "bd_paged_draft_attn")]
+    assert [a[1] for _, _, a in calls[1:3]] == [binding.BD_PAGED_BLOCK_ROWS, 2] and current[0] == 0
