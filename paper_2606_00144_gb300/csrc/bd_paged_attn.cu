@@ -15,9 +15,9 @@
 //            few long units.
 // More query rows than that are the tcgen05 kernel's (bd_verify_tc.cu, PAGED).
 //
-// Bound by HBM where there is enough to read: 256 units of 1.6K to 8K (630 MB) take 94 us (6.7 TB/s), 256 of 4K 82 (6.5), 8
-// of 128K 87 to 89 (6.1: a start of some 6 us, of which the page's look-up and the first tile, both from DRAM, are 5, and an
-// end of 5), in pages of 16 as in larger ones.  Short calls are a chain of latencies: 8 units of 1K 5.3 us, 2 of 1K (d 64) 4.0.
+// Bound by HBM where there is enough to read: 256 units of 1.6K to 8K (630 MB) take 92 us (6.8 TB/s), 256 of 4K 78 (6.9), 8
+// of 128K 83.5 (6.4: a start of some 5 us, of which the page's look-up and the first tile are 4, and an end of 5), in pages of
+// 16 as in larger ones.  Short calls are a chain of latencies: 8 units of 1K 5.3 us, 2 of 1K (d 64) 3.9.
 #include <cooperative_groups.h>
 
 #include <algorithm>
