@@ -54,6 +54,7 @@ __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence
 struct PagedMap {
   const int* pref;
   int span0, a, per_seq, batch, vtpc;
+  __device__ __forceinline__ static constexpr int stride() { return 1; }   // from a segment's tile to its next one
   __device__ __forceinline__ int seq_of(int u) const { return u / per_seq; }
   __device__ __forceinline__ int seq_base(int b) const { return pref ? pref[b] : b * per_seq * span0; }
   __device__ __forceinline__ int span(int b) const { return pref ? (pref[b + 1] - pref[b]) / per_seq : span0; }
@@ -97,13 +98,13 @@ struct PageWalk {
   const Params& p;
   int u_last, v0, v1;
   struct Segment {
-    int unit, tb, n, seq, head, end;   // n tiles from tb; end: rows of the sequence, its block's among them (unit > u_last: none)
+    int unit, tb, n, seq, head, end;   // n tiles, the first tb; end: rows of the sequence, its block's among them (unit > u_last: none)
   };
   __device__ __forceinline__ Segment from(int unit) const {
     Segment s{unit, 0, 0, 0, 0, 0};
     for (; s.unit <= u_last; ++s.unit) {
       s.tb = map.first_tile(s.unit, v0);
-      s.n = map.end_tile(s.unit, v1) - s.tb;
+      s.n = (map.end_tile(s.unit, v1) - s.tb + map.stride() - 1) / map.stride();
       if (s.n <= 0) continue;
       s.seq = map.seq_of(s.unit);
       s.head = s.unit / p.row_chunks - s.seq * p.h_kv;
@@ -116,8 +117,9 @@ struct PageWalk {
   // The entry of the segment's piece first + lane (nothing looks at it here, so that the load is on its way while others are
   // used); negative past the segment and the sequence's rows.
   __device__ __forceinline__ int entry(const Segment& s, int first, int lane) const {
-    const int at = first + lane, key = s.tb * KEYS + (at << p.box_shift);
-    return at < s.n * (KEYS >> p.box_shift) && key < s.end ? p.pages.entry(s.seq, key) : -1;
+    const int at = first + lane, n_box = KEYS >> p.box_shift, i = at << p.box_shift & ~(KEYS - 1);   // (the tiles before, in keys)
+    const int key = s.tb * KEYS + i * map.stride() + ((at << p.box_shift) - i);
+    return at < s.n * n_box && key < s.end ? p.pages.entry(s.seq, key) : -1;
   }
 };
 

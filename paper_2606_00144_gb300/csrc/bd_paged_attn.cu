@@ -8,12 +8,12 @@
 // (bd_attn_warp.cuh), the query rows on the N side.  The pieces of a tile lie one behind the other, so a warp's 16 keys are in
 // one piece (pages hold at least 16 rows).  Pieces whose page is not there, or that lie past the sequence's block, are not
 // fetched, and their keys are passed over.
-//   cluster  a unit's tiles (a unit: a sequence's KV head, and up to 8 of its query rows) are split over the CTAs of a
-//            cluster, or go to one CTA.  For short units, and for many, which the hardware deals out.
+//   cluster  a unit's tiles (a unit: a sequence's KV head, and up to 8 of its query rows) are taken in turn by the CTAs
+//            of a cluster, or go to one CTA.  For short units, and for many, which the hardware deals out.
 //   stream   the (unit, tile) pairs of all units form one list, cut into contiguous ranges of equal cost, one per CTA; each
 //            piece of a unit ("segment") ends in a partial, and a second kernel joins those of units that span CTAs.  For
 //            few long units.
-// More query rows than that are the tcgen05 kernel's (bd_verify_tc.cu, PAGED).
+// More than 8 query rows of long units (24 at d 64) are the tcgen05 kernel's (bd_verify_tc.cu, PAGED).
 //
 // Bound by HBM where there is enough to read: 256 units of 1.6K to 8K (630 MB) take 92 us (6.8 TB/s), 256 of 4K 78 (6.9), 8
 // of 128K 83.5 (6.4: a start of some 5 us, of which the page's look-up and the first tile are 4, and an end of 5), in pages of
@@ -57,9 +57,10 @@ struct PagedVerifyParams {
   float scale_log2;
 };
 
-// A cluster's unit: its CTAs' tile ranges are [v0, v1) themselves.
+// A cluster's unit: its CTAs take its tiles in turn, so that what is left of a context behind a window is spread over all of them.
 struct ClusterMap {
   int per_seq;
+  __device__ __forceinline__ int stride() const { return gridDim.x; }
   __device__ __forceinline__ int seq_of(int u) const { return u / per_seq; }
   __device__ __forceinline__ int first_tile(int, int v0) const { return v0; }
   __device__ __forceinline__ int end_tile(int, int v1) const { return v1; }
@@ -91,6 +92,7 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
                         const __grid_constant__ CUtensorMap vmap) {
   using L = PagedSmem<D, NT, CLUSTER>;
   constexpr int NQC = L::NQC, WARPS = L::WARPS, NCT = 32 * WARPS;
+  constexpr bool kSkips = CLUSTER || NT > 1;               // tiles that are not there are passed over
   const int stages = CLUSTER ? p.stages : kPvStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -98,7 +100,7 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
   uint64_t* empty_bar = full_bar + kPvMaxStages;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(empty_bar + kPvMaxStages);
   int* stop_flag = const_cast<int*>(abort_flag) + 1;
-  int* hide_s = stop_flag + 1;                             // [stages] 16-key sub-tiles that are not there
+  int* hide_s = stop_flag + 1;                             // [stages] 16-key sub-tiles that are not there; the tiles passed over before
   int* nan_from = reinterpret_cast<int*>(smem + 512);      // [D] first row of the block (from 1 on) whose V is no number there
   uint8_t* stage_base = smem + 1024;
   float* m_s = reinterpret_cast<float*>(stage_base + (CLUSTER ? 0 : stages * L::STAGE));
@@ -134,9 +136,8 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
       u_first = u_last = blockIdx.y;
       map.per_seq = p.h_kv * p.row_chunks;
       const int t = paged_context(p.seq_lens, map.seq_of(u_first), p.t_ctx, nullptr);
-      const int tiles = (t + p.n_q + kPvKeys - 1) / kPvKeys, per = (tiles + (int)gridDim.x - 1) / (int)gridDim.x;
-      v0 = min(tiles, (int)blockIdx.x * per);
-      v1 = min(tiles, v0 + per);
+      v0 = blockIdx.x;
+      v1 = (t + p.n_q + kPvKeys - 1) / kPvKeys;
     } else {
       map = PagedMap{nullptr, p.tiles_per_unit + p.seg_cost, p.seg_cost, p.h_kv * p.row_chunks, p.batch, p.vtiles_per_cta};
       if (p.seq_lens) map.template lay_out<L::THREADS, kPvKeys>(p.seq_lens, p.t_ctx, p.n_q, p.vtiles_per_cta, reinterpret_cast<int*>(smem + 256), pref);
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
     bool ok = true;
     while (seg.unit <= u_last && ok) {
       auto next = seg;
-      int next_now = -1, next_then = -1;
+      int next_now = -1, next_then = -1, skipped = 0;
       for (int i = 0; i < seg.n; ++i) {
         const int at = i * n_box & 31;
         if (i > 0 && at == 0) {
@@ -189,6 +190,13 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
         const int entry = __shfl_sync(0xffffffffu, now, at + piece);
         const uint32_t pieces = __ballot_sync(0xffffffffu, p.pages.there(now)) >> at & ((1u << n_box) - 1);
         if (entry >= p.pages.n_pages) record_error(p.status, BD_ERR_INVALID_ARG);
+        // Nothing of it is there (a segment's last tile stands for its end).  256 units of 8K behind a window of 1K, one row: 39.3 us,
+        // 57 without; 64 of 16K, d 64, 16 rows, a window of 500: 20.4 / 27.9.  Not in a stream of few rows, whose ranges hold as many
+        // tiles with a window as without: 8 units of 64K, a window of 4K 34.1 / 33.6, and the check costs 4 % at d 64.
+        if (kSkips && pieces == 0 && i + 1 < seg.n) {
+          ++skipped;
+          continue;
+        }
         if (issued >= stages) ok = mbar_wait_warp(&empty_bar[s], phase, p.status, abort_flag);
         if (!ok) break;
         if (lane == 0) {
@@ -196,7 +204,7 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
             int hide = 0;
 #pragma unroll
             for (int sub = 0; sub < kPvSubs; ++sub) hide |= (int)(~pieces >> (16 * sub >> p.box_shift) & 1) << sub;
-            hide_s[s] = hide;
+            hide_s[s] = skipped << kPvSubs | hide;
           }
           if (pieces) mbar_arrive_expect_tx(&full_bar[s], __popc(pieces) * piece_bytes);
           else mbar_arrive(&full_bar[s]);
@@ -204,11 +212,12 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
         __syncwarp();
         if (p.pages.there(entry) && lane < n_box)
           tma_load_page(1, smem_u32(stage_base + s * L::STAGE + which * L::TILE) + piece * piece_bytes, my_map, &full_bar[s],
-                        ((seg.tb + i) * kPvKeys + (piece << p.box_shift)) & page_mask, 0, seg.head, entry);
+                        ((seg.tb + i * map.stride()) * kPvKeys + (piece << p.box_shift)) & page_mask, 0, seg.head, entry);
         __syncwarp();
+        skipped = 0;
         ++issued;
         if (++s == stages) s = 0, phase ^= 1;
-        if (i == 0) {
+        if (next.unit == seg.unit) {                       // (behind the first tile)
           if (CLUSTER) {
             next.unit = u_last + 1;
           } else {
@@ -281,15 +290,16 @@ __global__ void __launch_bounds__(PagedSmem<D, NT, CLUSTER>::THREADS, CLUSTER ||
       }
     WarpAttn<D, NT> wa;
     wa.init();
-    for (int tile = tb; tile < te; ++tile) {
+    for (int tile = tb, nth = 0; tile < te; ++nth, tile += map.stride()) {
       if (!mbar_wait(&full_bar[s], phase, p.status, abort_flag)) {
         alive = false;
         break;
       }
       // CLUSTER: sub-tiles go round the warps, at most one of a tile to each; some warps have none
-      const int sub = CLUSTER ? (warp - (kPvSubs * (tile - tb)) % WARPS + WARPS) % WARPS : warp;
+      const int sub = CLUSTER ? (warp - kPvSubs * nth % WARPS + WARPS) % WARPS : warp, hide = hide_s[s];
+      if (kSkips) tile += (hide >> kPvSubs) * map.stride();
       const int key_base = tile * kPvKeys + 16 * sub, last = t_unit + p.n_q - 1 - key_base;   // last: the sub-tile's last row of the block
-      if ((!CLUSTER || sub < kPvSubs) && !(hide_s[s] >> sub & 1) && last >= 0) {
+      if ((!CLUSTER || sub < kPvSubs) && !(hide >> sub & 1) && last >= 0) {
         const uint32_t kbase = smem_u32(stage_base + s * L::STAGE) + (CLUSTER ? offset_of(sub) : own_off), vbase = kbase + L::TILE;
         // rows of the block behind its first one, which its first query does not see
         const int block0 = max(0, t_unit + 1 - key_base);

@@ -92,3 +92,30 @@ def test_no_number_in_a_block_row_on_every_route(d, G, n, b):
     if b > 2:
         assert torch.isfinite(o[1:-1, :, :n - 1]).all() and torch.isfinite(o[2:-1]).all()
         check_some(pool, q, [t] * b, n, o, lse, (2, 100, b - 2))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n", [(4, 1), (8, 1), (4, 2), (4, 4), (4, 6)])
+@pytest.mark.parametrize("b,t,page", [(2, 6000, 16), (24, 3000, 64), (40, 1500, 128)])
+def test_what_is_left_behind_a_window(d, G, n, b, t, page):
+    """Many tiles in a row that are not there: behind the first page, in the middle, at the end, all but one, all."""
+    h_kv = 8
+    pool = ref.Pool([t + n] * b, h_kv, page, d, seed=t + n)
+    per = pool.table.shape[1]
+    for i in range(b):
+        kind = i % 6
+        if kind == 0:
+            pool.table[i, 1:per - 2] = -1
+        elif kind == 1:
+            pool.table[i, per // 3:per // 2] = -1
+        elif kind == 2:
+            pool.table[i, per // 2:] = -1
+        elif kind == 3:
+            pool.table[i, torch.arange(per) != per // 2] = -1
+        elif kind == 4:
+            pool.table[i, ::2] = -1
+        else:
+            pool.table[i] = -1
+    q = queries(b, h_kv * G, n, d, 3)
+    o, lse = run_verify(pool, q, t, n)
+    check_some(pool, q, [t] * b, n, o, lse, range(min(6, b)), (0, 5))
