@@ -563,7 +563,7 @@ def _paged_rows(t, want, dtype, gpu):
     return None
 
 
-_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_device, _raw_stream = (getattr(torch._C, x, None) for x in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, table, q_out, row_starts=None, stream=None):
