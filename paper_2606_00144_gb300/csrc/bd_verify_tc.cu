@@ -194,6 +194,10 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
     tc_fence_after();
   }
   const uint32_t tmem_base = *tmem_slot;
+  // PAGED: a tile of which nothing is there (but a segment's first ones, which fill the accumulators) is neither copied nor
+  // multiplied nor weighed; it only goes through the barriers.  (64 units of 16K behind a window of 1K, 24 rows: 53 us, 113 without; it
+  // costs other blocks 1 %, those of two M tiles 2 %.)
+  constexpr int kNothing = (1 << kVTcKeys / 16) - 1;
   // S/P buffer b: columns 128 b; O[b]: columns 256 + D b
 
   // Ring position of a segment's tiles, n of them, relative to its first: the order the MMAs
@@ -257,6 +261,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           if (!ok) break;
           const uint32_t gone = ~__ballot_sync(0xffffffffu, p.pages.there(now)) >> at;
           if (k && now >= p.pages.n_pages && lane >= at && lane < at + n_box) record_error(p.status, BD_ERR_INVALID_ARG);
+          const bool copy = i * NQT < 2 || ~gone << (32 - n_box);   // (see kNothing)
           if (lane == 0) {
             if (k) {
               int hide = 0;
@@ -266,14 +271,15 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
             } else if (i == n - 1) {
               live_s[s] = at_seg.end - key0;
             }
-            mbar_arrive_expect_tx(&full_bar[s], TILE);
+            if (copy) mbar_arrive_expect_tx(&full_bar[s], TILE);
+            else mbar_arrive(&full_bar[s]);
           }
           armed |= 1u << s;
           phases = (phases & ~(1u << s)) | (uint32_t)((r / SLOTS) & 1) << s;
           __syncwarp();
           const uint32_t dst = smem_u32(ring + s * TILE);
 #pragma unroll 2
-          for (int j = 0; j < n_box; ++j) {                // (a page that the pool has not: zeros)
+          for (int j = 0; j < (copy ? n_box : 0); ++j) {   // (a page that the pool has not: zeros)
             const int found = __shfl_sync(0xffffffffu, now, at + j), row = (key0 + (j << p.box_shift)) & page_mask, head = at_seg.head;
             const int e = p.pages.there(found) ? found : p.pages.n_pages;
             if constexpr (BOX16) {
@@ -371,7 +377,9 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
       int t_seg = 0;
       if constexpr (PAGED) t_seg = paged_context(p.seq_lens, map.seq_of(unit), p.t_ctx, nullptr);
       if (!mbar_wait_warp(q_full, seg & 1, p.status, abort_flag)) break;
+      bool gone = false;                            // job j's tile (kNothing)
       for (int j = 0; j <= nj; ++j) {
+        [[maybe_unused]] const bool was_gone = gone;   // job j - 1's
         if (j < nj) {                               // S of job j
           const int b = (jg + j) & 1, i = j / NQT, qt = j % NQT;
           const int r = base + k_pos(i), s = r % SLOTS;
@@ -382,17 +390,20 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           tc_fence_after();
           const uint32_t a_lo = desc_k(smem_u32(qbuf + qt * TILE));
           const uint32_t b_lo = desc_k(smem_u32(ring + s * TILE));
+          if (PAGED && qt == 0) gone = j >= 2 && hide_s[(jg + j) / NQT & 15] == kNothing;
+          if (!gone) {
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t off = ((ks >> 2) * kTHalf + (ks & 3) * 32) / 16;
-            if constexpr (BOX16) {
-              const uint32_t b_off = ((ks >> 2) * 2048 + (ks & 3) * 32) / 16;
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t off = ((ks >> 2) * kTHalf + (ks & 3) * 32) / 16;
+              if constexpr (BOX16) {
+                const uint32_t b_off = ((ks >> 2) * 2048 + (ks & 3) * 32) / 16;
 #pragma unroll
-              for (int atom = 0; atom < 2; ++atom)
-                tc_mma_ss(lead, tmem_base + 128 * b + 64 * atom, a_lo + off, b_lo + b_off + atom * (1024 / 16),
-                          umma_idesc_bf16(128, kVTcKeys / 2), ks > 0 ? 1u : 0u, desc_hi(4096));
-            } else {
-              tc_mma_ss(lead, tmem_base + 128 * b, a_lo + off, b_lo + off, idesc_s, ks > 0 ? 1u : 0u);
+                for (int atom = 0; atom < 2; ++atom)
+                  tc_mma_ss(lead, tmem_base + 128 * b + 64 * atom, a_lo + off, b_lo + b_off + atom * (1024 / 16),
+                            umma_idesc_bf16(128, kVTcKeys / 2), ks > 0 ? 1u : 0u, desc_hi(4096));
+              } else {
+                tc_mma_ss(lead, tmem_base + 128 * b, a_lo + off, b_lo + off, idesc_s, ks > 0 ? 1u : 0u);
+              }
             }
           }
           tc_commit(lead, &s_full[b]);
@@ -414,7 +425,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           if (!UNIFORM && ok && i == n - 1 && qt == 0) clear_rows<D, BOX16>(ring + s * TILE, live_s[s], lane);
           if constexpr (PAGED) {                    // rows of the block behind its first one, which its first query does not see
             const int key0 = (tb + i) * kVTcKeys, r0 = max(0, t_seg + 1 - key0), r1 = min(kVTcKeys, t_seg + p.n_q - key0);
-            if (ok && qt == 0 && r0 < r1) scrub_rows<D>(smem_u32(ring + s * TILE), BOX16 ? 4 : 7, r0, r1, key0 + r0 - t_seg, nan_from, lane);
+            if (ok && qt == 0 && r0 < r1 && !was_gone) scrub_rows<D>(smem_u32(ring + s * TILE), BOX16 ? 4 : 7, r0, r1, key0 + r0 - t_seg, nan_from, lane);
           }
           if (ok) ok = mbar_wait_warp(&p_ready[b], (jj >> 1) & 1, p.status, abort_flag);
           if (!ok) break;
@@ -423,7 +434,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           const uint32_t d_tmem = tmem_base + 256 + D * b, a_tmem = tmem_base + 128 * b;
           const uint32_t first = j - 1 < 2 ? 0u : 1u;   // O[b]'s first job of the segment
 #pragma unroll 1
-          for (int t = 0; t < 2; ++t)                // P_hi, then P_lo
+          for (int t = 0; t < (was_gone ? 0 : 2); ++t)   // P_hi, then P_lo
 #pragma unroll
             for (int ks = 0; ks < kVTcKeys / 16; ++ks)
               tc_mma_ts(lead, d_tmem, a_tmem + 32 * (ks >> 1) + 8 * (ks & 1) + 16 * t,
@@ -481,13 +492,14 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
         alive = __all_sync(0xffffffffu, alive && mbar_wait(&s_full[grp], use & 1, p.status, abort_flag));
         if (!alive) continue;
         tc_fence_after();
-        if (warp_live) {
+        const int gone = PAGED ? hide_s[(jg + j) / NQT & 15] : 0;   // 16-key groups that are not there
+        if (warp_live && !(PAGED && j >= 2 && gone == kNothing)) {
           // two passes over halves of 64 keys: the second half's maximum, the first half's (its
           // scores stay in registers), the weights of the first, the second again
           const int key0 = (tb + j / NQT) * kVTcKeys;
           // some key is hidden from some row (which groups is read again where it counts: held over the tile, in a register
           // that is not there, 64 units of 16K, 32 rows, d 64 took 74.5 us for 65)
-          const bool masked = key0 + kVTcKeys - 1 > t_unit || (PAGED && hide_s[(jg + j) / NQT & 15]);
+          const bool masked = key0 + kVTcKeys - 1 > t_unit || gone;
           float v[64];
           auto load_half = [&](int h) {
             tc_ld_32cols(t_s + 64 * h, *reinterpret_cast<float(*)[32]>(&v[0]));

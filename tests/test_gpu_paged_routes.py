@@ -119,3 +119,24 @@ def test_what_is_left_behind_a_window(d, G, n, b, t, page):
     q = queries(b, h_kv * G, n, d, 3)
     o, lse = run_verify(pool, q, t, n)
     check_some(pool, q, [t] * b, n, o, lse, range(min(6, b)), (0, 5))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n", [(4, 6), (8, 4), (8, 21)])
+@pytest.mark.parametrize("page", [16, 32, 256])
+def test_stale_tiles_behind_a_window(d, G, n, page):
+    """Long units whose middle, end or block is not there, after units that are whole and hold NaN in rows that are hidden: what
+    lay in shared memory before has no part in them.  A block's rows among what is there, and not."""
+    b, h_kv, t = 6, 4, 9000
+    pool = ref.Pool([t + n] * b, h_kv, page, d, seed=n)
+    per = pool.table.shape[1]
+    for i, (lo, hi) in enumerate([(0, 0), (1, per - 1), (0, 0), (3, per), (per // 4, per - per // 8), (0, per)]):
+        pool.table[i, lo:hi] = -1
+    for i in (0, 2):                       # the block's last V row: hidden from its first queries, seen by the last
+        pool.v[int(pool.table[i, (t + n - 1) // page]), :, (t + n - 1) % page] = math.nan
+    q = queries(b, h_kv * G, n, d, n)
+    o, lse = run_verify(pool, q, t, n)
+    assert not torch.isnan(o[[1, 3, 4, 5]].float()).any() and (o[5] == 0).all() and (lse[5] == -math.inf).all()
+    for i in (0, 2):
+        assert torch.isnan(o[i, :, -1].float()).all() and not torch.isnan(o[i, :, :-1].float()).any()
+    check_some(pool, q, [t] * b, n, o, lse, (1, 3, 4), (0, 3))
