@@ -446,7 +446,7 @@ int bd_quant_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd
  * bd_shape means what it means elsewhere (t_cap: the most positions of a sequence, up to 2^30); t_ctx, and a
  * sequence's own length, may also be 0, and batch * h_kv may be anything below 2^20, per-sequence lengths or not.  What a
  * call reads may have been written by the kernel just before it on the stream: no call here starts reading early, but for
- * BD_DRAFT_VIEW_READY.
+ * BD_DRAFT_VIEW_READY.  Tables and lengths must not change while a call that reads them runs.
  */
 typedef struct bd_paged_cache {
   void* k;
