@@ -488,7 +488,8 @@ typedef struct bd_rope {
  *              written, nor is the row of a position of t_cap or more;
  *   rope       NULL: rows are written as they are;
  *   q_out      bf16, of q_rows' shape, 16-byte aligned, q_out_strides as above (between different rows at least head_dim);
- *              NULL exactly if q_rows is.  It may be q_rows itself, with the same strides.
+ *              NULL exactly if q_rows is.  It may be q_rows itself if those are bf16, with the same strides (else q_out == q_rows is
+ *              BD_ERR_INVALID_ARG), and lies over no other rows that the call reads.
  * A T_b outside [0, t_ctx] is clamped.  Constraints: n_rows >= 0 (0 is a no-op); t_ctx + n_rows <= t_cap without
  * row_starts; batch * n_rows < 2^31 (n_rows with row_starts).  Two tokens must not share a row of the pool.  No workspace.
  */

@@ -570,7 +570,7 @@ def bd_paged_append(shape, q_rows, k_rows, v_rows, rope, cache: PagedCache, tabl
     """New tokens join a paged cache behind each sequence's context: queries and keys are rotated to their positions (rope: a
     Rope, or None), keys and values written into their pages, queries into q_out (bf16).  Rows are [batch, heads, n,
     head_dim], or with row_starts (int32 [batch + 1] on the GPU) packed [heads, rows, head_dim]; bf16 or fp32, any strides
-    of whole 16 bytes; any of q_rows (with q_out), k_rows and v_rows may be None."""
+    of whole 16 bytes; any of q_rows (with q_out), k_rows and v_rows may be None.  q_out may be a bf16 q_rows itself."""
     b, h_q, h, d, _, _ = _shape_ints(shape)
     gpu = cache._gpu
     first = q_rows if q_rows is not None else k_rows if k_rows is not None else v_rows

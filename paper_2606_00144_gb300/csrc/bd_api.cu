@@ -635,9 +635,11 @@ int bd_paged_append(const bd_shape* shape, int n_rows, int dtype, const void* q_
   const int bytes = dtype == BD_DTYPE_F32 ? 4 : 2;
   RowTensor q, k, v, o;
   BD_TRY(paged_rows(s, s.h_q, q_rows, q_strides, n_rows, bytes, packed, false, &q));
+  BD_TRY(paged_rows(s, s.h_q, q_out, q_out_strides, n_rows, 2, packed, true, &o));
+  // (in place a thread writes the bytes that it has read; with rows of other bytes it would write those of others)
+  if (q_rows && q_rows == q_out && (bytes != 2 || q.sb != o.sb || q.sh != o.sh || q.sn != o.sn)) return BD_ERR_INVALID_ARG;
   BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, bytes, packed, false, &k));
   BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, bytes, packed, false, &v));
-  BD_TRY(paged_rows(s, s.h_q, q_out, q_out_strides, n_rows, 2, packed, true, &o));
   return map_cuda(launch_paged_append(s, n_rows, dtype, q, k, v, row_starts, rope, *cache, table, table_pages, o,
                                       static_cast<cudaStream_t>(stream)));
 }
