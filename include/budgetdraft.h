@@ -154,7 +154,8 @@ enum {
  *               chunk == s > 1: the top floor((budget - n_sink - n_recent)/s) chunks,
  *                 chunk c = positions [c s, c s + s) within the middle, scored by the
  *                 sum of its members;
- *          ties go to the lower position (chunk); a score that is NaN counts as 0.
+ *          ties go to the lower position (chunk); a score that is NaN counts as 0, and its key has no part in
+ *          the normalisers if they are computed here.
  *          If budget >= t_ctx, keep = [0, t_ctx).
  *
  *   k_cache     bf16 [batch, h_kv, t_cap, d]; rows [0, t_ctx) are read.

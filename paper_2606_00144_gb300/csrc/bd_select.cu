@@ -406,6 +406,7 @@ struct LseParams {
   const int32_t* seq_lens;   // per-sequence context lengths [batch] (RAGGED instance) or null
   int len_offset;            // added to every length (a verify block ends n_q past its context)
   int h_kv, units;
+  int hide_nan;              // a key whose score is NaN has no part in a row (a selection's rows), or makes the row one (a verify block's)
 };
 // Segments of one unit with per-sequence lengths (bounds the partials): 33 while the units are not many
 // times the SMs, since all but a few sequences may be short.  (One sequence of 64K, 8 units of 24 or 32 rows:
@@ -708,15 +709,24 @@ __global__ void __launch_bounds__(kLThreads, 1) window_lse_kernel(const LseParam
           }
           const float2 cc = make_float2(p.scale_log2, p.scale_log2);
           const float2 nm = make_float2(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m);
-          float2 a0 = make_float2(0.f, 0.f), a1 = a0;
+          auto weights = [&] {
+            float2 a0 = make_float2(0.f, 0.f), a1 = a0;
 #pragma unroll
-          for (int j = 0; j < COLS; j += 4) {
-            const float2 x0 = ffma2(make_float2(v[j], v[j + 1]), cc, nm);
-            const float2 x1 = ffma2(make_float2(v[j + 2], v[j + 3]), cc, nm);
-            a0 = fadd2(a0, make_float2(fast_exp2(x0.x), fast_exp2(x0.y)));
-            a1 = fadd2(a1, make_float2(fast_exp2(x1.x), fast_exp2(x1.y)));
+            for (int j = 0; j < COLS; j += 4) {
+              const float2 x0 = ffma2(make_float2(v[j], v[j + 1]), cc, nm);
+              const float2 x1 = ffma2(make_float2(v[j + 2], v[j + 3]), cc, nm);
+              a0 = fadd2(a0, make_float2(fast_exp2(x0.x), fast_exp2(x0.y)));
+              a1 = fadd2(a1, make_float2(fast_exp2(x1.x), fast_exp2(x1.y)));
+            }
+            return (a0.x + a0.y) + (a1.x + a1.y);
+          };
+          float sum = weights();
+          if (sum != sum && p.hide_nan) {           // (the maxima above pass over a NaN by themselves)
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) v[j] = fmaxf(v[j], -INFINITY);
+            sum = weights();
           }
-          l += (a0.x + a0.y) + (a1.x + a1.y);
+          l += sum;
         }
         tc_fence_before();
         __syncwarp();
@@ -1594,6 +1604,7 @@ cudaError_t launch_lse(const bd_shape& s, const LsePlan& plan, const void* k_cac
   p.len_offset = len_offset;
   p.h_kv = s.h_kv;
   p.units = units;
+  p.hide_nan = len_offset == 0;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
   void* fn = nullptr;
 #define BD_LSE(DD, R, C) \
