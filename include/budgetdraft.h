@@ -23,9 +23,9 @@
  * and a 4-bit form of the caches in four more:
  *   bd_quant_write / bd_quant_read  quantise rows into a 4-bit cache and read them back;
  *   bd_quant_draft_attn / bd_quant_verify_attn  the two attentions over it.
- * and a paged form of the caches in four more:
+ * and a paged form of the caches in five more:
  *   bd_paged_append   rotates new rows to their positions and writes them into their pages;
- *   bd_paged_read     reads rows back as a dense tensor;
+ *   bd_paged_read     reads rows back as a dense tensor, bd_paged_keys the keys as bd_select_budget takes them;
  *   bd_paged_verify_attn / bd_paged_draft_attn  the two attentions over it.
  * Around them: bd_workspace_size / bd_workspace_status (scratch and device-side
  * errors), bd_draft_attn_static / bd_draft_static_status (bd_draft_attn without a
@@ -512,6 +512,16 @@ enum { BD_PAGED_BLOCK_ROWS = -1 };
 int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_paged_cache* cache, const int32_t* table,
                   int table_pages, void* k_rows, const int64_t* k_strides, void* v_rows, const int64_t* v_strides,
                   void* stream);
+
+/*
+ * The keys of positions 0 .. n_rows - 1 for a selection: as bd_paged_read's with first_row 0, but a row whose page is not
+ * there holds NaN, which bd_select_budget counts as score 0 and leaves out of the normalisers that it computes: no such
+ * position is kept before one that is there, but for sinks and recent ones.  (Normalisers that are carried are over the keys
+ * that are there too, as bd_paged_verify_attn leaves them.)
+ * Constraints: 0 <= n_rows <= t_cap (0 is a no-op); k_rows as of bd_paged_read.  The cache's v is not looked at.
+ */
+int bd_paged_keys(const bd_shape* shape, int n_rows, const bd_paged_cache* cache, const int32_t* table, int table_pages,
+                  void* k_rows, const int64_t* k_strides, void* stream);
 
 /*
  * bd_verify_attn over a paged cache (n_q = 1: decoding one token): query i of head h attends to the keys of [0, t_ctx + i]

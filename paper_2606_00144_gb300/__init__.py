@@ -35,6 +35,7 @@ from .binding import (  # noqa: F401
     bd_draft_static_status,
     bd_paged_append,
     bd_paged_draft_attn,
+    bd_paged_keys,
     bd_paged_read,
     bd_paged_verify_attn,
     bd_quant_draft_attn,

@@ -95,6 +95,7 @@ _SIGNATURES = {
                                        _ROPE, _PCACHE, _P, ctypes.c_int, _P, _P, _P]),
     "bd_paged_read": (ctypes.c_int, [_SHAPE, ctypes.c_int, ctypes.c_int, _PCACHE, _P, ctypes.c_int, _P, _P, _P,
                                      _P, _P]),
+    "bd_paged_keys": (ctypes.c_int, [_SHAPE, ctypes.c_int, _PCACHE, _P, ctypes.c_int, _P, _P, _P]),
     "bd_paged_verify_attn": (ctypes.c_int, [_SHAPE, _P, ctypes.c_int, _PCACHE, _P, ctypes.c_int, _P, _P, _P,
                                             ctypes.c_size_t, _P]),
     "bd_paged_draft_attn": (ctypes.c_int, [_SHAPE, _P, _PCACHE, _P, ctypes.c_int, _P, _P, ctypes.c_int, ctypes.c_int,
@@ -636,6 +637,26 @@ def bd_paged_read(shape, cache: PagedCache, table, k_out, v_out=None, first_row=
         _raw_stream(gpu) if stream is None else _stream(stream))
     if st:
         _check("bd_paged_read", st)
+
+
+def bd_paged_keys(shape, cache: PagedCache, table, k_out, stream=None):
+    """Reads the keys of positions 0 .. n - 1 into a bf16 [batch, h_kv, n, head_dim] tensor as bd_select_budget takes them: those
+    whose page is not there are NaN, which counts as score 0.  Rows of positions at or past a sequence's length are left as
+    they were."""
+    b, _, h, d, _, _ = _shape_ints(shape)
+    gpu = cache._gpu
+    want, ts = (b, h, k_out.shape[2] if k_out.dim() == 4 else -1, d), table.shape
+    k = _paged_rows(k_out, want, _BF16, gpu)
+    if not (h == cache.h_kv and d == cache.head_dim and k and table.dtype is _I32 and len(ts) == 2 and ts[0] == b
+            and table.is_contiguous() and table.get_device() == gpu):
+        _refuse_paged("bd_paged_keys", shape, cache, table, ((k_out, want, (_BF16,)),))
+    if _device() != gpu:                       # (the call with the cache's GPU current)
+        with torch.cuda.device(gpu):
+            return bd_paged_keys(shape, cache, table, k_out, stream)
+    st = (_lib or library()).bd_paged_keys(
+        shape, want[2], cache._struct, table.data_ptr(), ts[1], k[0], k[1], _raw_stream(gpu) if stream is None else _stream(stream))
+    if st:
+        _check("bd_paged_keys", st)
 
 
 def bd_paged_verify_attn(shape, q, n_q, cache: PagedCache, table, o_out, lse_out, ws: Workspace, stream=None):

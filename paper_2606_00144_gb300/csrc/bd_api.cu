@@ -657,7 +657,20 @@ int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_pag
   BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, 2, false, true, &k));
   BD_TRY(paged_rows(s, s.h_kv, v_rows, v_strides, n_rows, 2, false, true, &v));
   if ((n_rows / 128 + 1LL) * s.batch * s.h_kv * 2 >= 1LL << 31) return BD_ERR_UNSUPPORTED;   // (CTAs)
-  return map_cuda(launch_paged_read(s, first_row, n_rows, *cache, table, table_pages, k, v, static_cast<cudaStream_t>(stream)));
+  return map_cuda(launch_paged_read(s, first_row, n_rows, *cache, table, table_pages, k, v, false, static_cast<cudaStream_t>(stream)));
+}
+
+int bd_paged_keys(const bd_shape* shape, int n_rows, const bd_paged_cache* cache, const int32_t* table, int table_pages,
+                  void* k_rows, const int64_t* k_strides, void* stream) {
+  BD_TRY(check_paged_shape(shape));
+  const bd_shape& s = *shape;
+  if (n_rows < 0 || n_rows > s.t_cap || (n_rows > 0 && !k_rows)) return BD_ERR_INVALID_ARG;
+  if (n_rows == 0) return BD_OK;
+  BD_TRY(check_paged_cache(s, cache, table, table_pages, true, false));
+  RowTensor k;
+  BD_TRY(paged_rows(s, s.h_kv, k_rows, k_strides, n_rows, 2, false, true, &k));
+  if ((n_rows / 128 + 1LL) * s.batch * s.h_kv >= 1LL << 31) return BD_ERR_UNSUPPORTED;   // (CTAs)
+  return map_cuda(launch_paged_read(s, 0, n_rows, *cache, table, table_pages, k, {}, true, static_cast<cudaStream_t>(stream)));
 }
 
 int bd_paged_verify_attn(const bd_shape* shape, const void* q, int n_q, const bd_paged_cache* cache, const int32_t* table,

@@ -247,7 +247,7 @@ cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const 
                                 const int32_t* row_starts, const bd_rope* rope, const bd_paged_cache& c, const int32_t* table,
                                 int table_pages, const RowTensor& q_out, cudaStream_t stream);
 cudaError_t launch_paged_read(const bd_shape& s, int first_row, int n_rows, const bd_paged_cache& c, const int32_t* table,
-                              int table_pages, const RowTensor& k, const RowTensor& v, cudaStream_t stream);
+                              int table_pages, const RowTensor& k, const RowTensor& v, bool nan_absent, cudaStream_t stream);
 
 cudaError_t launch_paged_draft(const bd_shape& s, const DraftPlan& plan, const void* q, const bd_paged_cache& c,
                                const int32_t* table, int table_pages, const int32_t* idx, const int32_t* count, int budget,

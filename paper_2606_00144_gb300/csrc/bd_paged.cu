@@ -1,4 +1,4 @@
-// Rows that join a paged cache with their position rotation (bd_paged_append), and rows read back (bd_paged_read).
+// Rows that join a paged cache with their position rotation (bd_paged_append), and rows read back (bd_paged_read, bd_paged_keys).
 //
 //   (x, y) -> s (x cos a - y sin a, x sin a + y cos a),  a = 2 pi frac(p f) for pair j's turns f a position
 //
@@ -283,12 +283,17 @@ struct ReadParams {
   const int32_t* seq_lens;
   int t_ctx, first, n_rows, h_kv, units;   // first < 0: the rows behind each sequence's length
   int blocks;                              // CTAs of a unit's rows
+  uint32_t absent;                         // two elements of a row whose page is not there
   bool wide;                               // 32-byte aligned everywhere
 };
 constexpr int kPgPasses = 4;               // rows of a thread
 
 struct Half16 {                            // 16 elements as they lie
   uint32_t w[8];
+  __device__ __forceinline__ void fill(uint32_t two) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = two;
+  }
   __device__ __forceinline__ void load(const void* p, bool wide) {
     if (wide) {
       asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
@@ -335,9 +340,10 @@ __global__ void __launch_bounds__(kPgThreads) paged_read_kernel(const __grid_con
     e[i] = r < n ? p.pages.entry(seq, first + r) : -1;
   }
   const __nv_bfloat16* pool = t.pool.base + head * t.pool.sh + 16 * c;
-  Half16 x[kPgPasses] = {};
+  Half16 x[kPgPasses];
 #pragma unroll
   for (int i = 0; i < kPgPasses; ++i) {
+    x[i].fill(p.absent);
     const int in_page = (first + row0 + i * STEP) & ((1 << p.pages.shift) - 1);
     if (p.pages.there(e[i])) x[i].load(pool + e[i] * t.pool.sp + in_page * t.pool.sn, p.wide);
   }
@@ -417,7 +423,7 @@ cudaError_t launch_paged_append(const bd_shape& s, int n_rows, int dtype, const 
 }
 
 cudaError_t launch_paged_read(const bd_shape& s, int first_row, int n_rows, const bd_paged_cache& c, const int32_t* table,
-                              int table_pages, const RowTensor& k, const RowTensor& v, cudaStream_t stream) {
+                              int table_pages, const RowTensor& k, const RowTensor& v, bool nan_absent, cudaStream_t stream) {
   ReadParams p;
   int n = 0;
   p.wide = true;
@@ -435,6 +441,7 @@ cudaError_t launch_paged_read(const bd_shape& s, int first_row, int n_rows, cons
   p.t_ctx = s.t_ctx;
   p.first = first_row;
   p.n_rows = n_rows;
+  p.absent = nan_absent ? 0x7fc07fc0u : 0u;
   p.h_kv = s.h_kv;
   p.units = s.batch * s.h_kv;
   const int rows = kPgThreads / (s.head_dim / 16) * kPgPasses;

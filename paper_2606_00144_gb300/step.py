@@ -186,17 +186,21 @@ class QuantSpecStep(_ReadBackStep):
 
 class PagedSpecStep(_ReadBackStep):
     """A step over a paged cache (PagedCache) of one layer: bd_paged_append for new tokens, bd_paged_draft_attn and
-    bd_paged_verify_attn in place of the bf16 attentions; bd_paged_read gives the selection its keys.  Every call takes the
-    batch's table of pages, int32 [batch, pages].  The selection does not know of pages that are not there: a position on one
-    reads as a key of zeros, and is skipped by the passes if it is kept."""
+    bd_paged_verify_attn in place of the bf16 attentions; bd_paged_keys gives the selection its keys.  Every call takes the
+    batch's table of pages, int32 [batch, pages].  A position whose page is not there is hidden from the window's normalisers
+    as it is from the attentions, and scores 0 in the selection; it is kept among the sinks and the recent positions, or
+    where nothing else is left, and then skipped by the passes."""
 
     def _workspace(self, device):
+        # of the window's normalisers, for every context (a window that is too wide: 0 here, and its status when called)
+        self._lse_bytes = B.bd_workspace_size(self.shape, B.BD_OP_PAGED_VERIFY, 0, self.window)
         return self._workspace_for(device, B.BD_OP_PAGED_DRAFT, B.BD_OP_PAGED_VERIFY)
 
     def keys(self, cache, table, stream=None):
-        """The context's keys as bf16, in the step's own buffer (rows past a sequence's length are not read)."""
+        """The context's keys as bf16, in the step's own buffer (rows past a sequence's length are not read; NaN where the page
+        is not there)."""
         return self._read_keys(cache.k.device,
-                               lambda rows: B.bd_paged_read(self.shape, cache, table, rows, first_row=0, stream=stream), stream)
+                               lambda rows: B.bd_paged_keys(self.shape, cache, table, rows, stream=stream), stream)
 
     def append(self, q_rows, k_rows, v_rows, rope, cache, table, q_out, stream=None):
         """New tokens behind the context: rows [batch, heads, n, head_dim] rotated by rope to their positions, keys and values
@@ -220,4 +224,20 @@ class PagedSpecStep(_ReadBackStep):
         self.verify(q_verify, cache, table, stream)
 
     def window_lse(self, cache, table, q_win, out=None, stream=None):
-        return super().window_lse(self.keys(cache, table, stream), q_win, out, stream)
+        """LSE of the window queries over the keys of their prefixes that are there, by bd_paged_verify_attn: a block that
+        starts W positions before the context's end (of each sequence, which is at least W long)."""
+        return super().window_lse((cache, table), q_win, out, stream)
+
+    def _window_lse(self, where, q_win, out, stream):
+        cache, table = where
+        s, W = self.shape, self.window
+        lens = None if self.seq_lens is None else torch.sub(self.seq_lens, W)
+        sh = cache.shape(s.batch, s.h_q, s.t_ctx - W, s.t_cap, lens)
+        device = cache.k.device
+        if out is None:
+            out = torch.empty(s.batch, s.h_q, W, dtype=torch.float32, device=device)
+        o = torch.empty(s.batch, s.h_q, W, s.head_dim, dtype=torch.bfloat16, device=device)
+        ws = B.Workspace(self._lse_bytes, device, units=s.batch * s.h_kv)   # of this call's own, as in the base class
+        # K is V too: what the weights sum up is not looked at, and the same rows are read from memory once
+        B.bd_paged_verify_attn(sh, q_win, W, B.PagedCache(cache.k, cache.k), table, o, out, ws, stream)
+        return out
