@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "bd_common.cuh"
+#include "bd_copies.h"
 #include "bd_internal.h"
 #include "bd_paged.cuh"
 #include "bd_verify.cuh"
@@ -236,6 +237,12 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
       bool ok = true;
       int base = 0, seg = 0, tiles_done = 0;
       uint32_t armed = 0, phases = 0;               // stages this warp has filled, and the parities of the last time
+      CopyCount queries{first_seg.unit <= u_last ? 1 : 0};   // (the first segment's are warp 2's)
+      auto next_q = [&](int unit) {
+        if (lane == 0) load_q(unit);
+        queries.add();
+        __syncwarp();
+      };
       const Walk walk{map, p, u_last, v0, v1};
       auto at_seg = first_seg;
       while (at_seg.unit <= u_last && ok) {
@@ -248,8 +255,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
           if (i == early && k && seg > 0) {
             ok = mbar_wait_warp(q_empty, (seg - 1) & 1, p.status, abort_flag);
             if (!ok) break;
-            if (lane == 0) load_q(unit);
-            __syncwarp();
+            next_q(unit);
           }
           const int at = i * n_box & 31, key0 = (tb + i) * kVTcKeys;
           if (i > 0 && at == 0) {
@@ -298,8 +304,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
         }
         if (ok && early == n && k && seg > 0) {            // (all its keys were early)
           ok = mbar_wait_warp(q_empty, (seg - 1) & 1, p.status, abort_flag);
-          if (ok && lane == 0) load_q(unit);
-          __syncwarp();
+          if (ok) next_q(unit);
         }
         if (!ok) break;
         ++seg;
@@ -312,7 +317,7 @@ __global__ void __launch_bounds__(MODE == CONTIGUOUS ? kVTcThreads : kPagedTcThr
       if (*abort_flag && lane == 0) {   // no copy may land in shared memory after the CTA exits
         for (int s = 0; s < SLOTS; ++s)
           if (armed >> s & 1) mbar_wait_for(&full_bar[s], phases >> s & 1, p.status, nullptr, 20000000);
-        if (k && seg > 0) mbar_wait_for(q_full, (seg - 1) & 1, p.status, nullptr, 20000000);
+        if (k && queries.any()) mbar_wait_for(q_full, queries.last_parity(), p.status, nullptr, 20000000);
       }
     } else if (lane == 0) {
       tma_prefetch_map(&kmap);
