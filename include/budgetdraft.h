@@ -136,7 +136,10 @@ enum {
    * before the kernel that immediately precedes this call on `stream` (not by it:
    * bd_advance, for one, rewrites all three in place): the call may read them while
    * that kernel finishes. */
-  BD_SELECT_WINDOW_READY = 1
+  BD_SELECT_WINDOW_READY = 1,
+  /* Rows of the cache may hold NaN in the place of keys that are not there (bd_paged_keys): they have no part in the
+   * normalisers that the call computes.  (Without it such a normaliser is -inf.  2 is not a flag.) */
+  BD_SELECT_NAN_HIDDEN = 4
 };
 
 /*
@@ -154,8 +157,7 @@ enum {
  *               chunk == s > 1: the top floor((budget - n_sink - n_recent)/s) chunks,
  *                 chunk c = positions [c s, c s + s) within the middle, scored by the
  *                 sum of its members;
- *          ties go to the lower position (chunk); a score that is NaN counts as 0, and its key has no part in
- *          the normalisers if they are computed here.
+ *          ties go to the lower position (chunk); a score that is NaN counts as 0.
  *          If budget >= t_ctx, keep = [0, t_ctx).
  *
  *   k_cache     bf16 [batch, h_kv, t_cap, d]; rows [0, t_ctx) are read.
@@ -163,7 +165,7 @@ enum {
  *   window_lse  fp32 [batch, h_q, window]: each window row's softmax normaliser over
  *               keys [0, p_w] (carried from the step that verified that token), or
  *               NULL to have it computed here (reads K a second time).
- *   flags       0 or BD_SELECT_WINDOW_READY.
+ *   flags       0, BD_SELECT_WINDOW_READY, BD_SELECT_NAN_HIDDEN or both.
  *   idx_out     int32 [batch, h_kv, budget]: kept positions ascending, then -1 padding.
  *   count_out   int32 [batch, h_kv]: number of kept positions.
  * Constraints: 1 <= window <= t_ctx, (h_q/h_kv)*window <= 256 (<= 128 with window_lse
@@ -515,9 +517,9 @@ int bd_paged_read(const bd_shape* shape, int first_row, int n_rows, const bd_pag
 
 /*
  * The keys of positions 0 .. n_rows - 1 for a selection: as bd_paged_read's with first_row 0, but a row whose page is not
- * there holds NaN, which bd_select_budget counts as score 0 and leaves out of the normalisers that it computes: no such
- * position is kept before one that is there, but for sinks and recent ones.  (Normalisers that are carried are over the keys
- * that are there too, as bd_paged_verify_attn leaves them.)
+ * there holds NaN, which bd_select_budget counts as score 0, and with BD_SELECT_NAN_HIDDEN leaves out of the normalisers that
+ * it computes: no such position is kept before one that is there, but for sinks and recent ones.  (Normalisers that are carried are over the keys
+ * that were there when bd_paged_verify_attn left them.)
  * Constraints: 0 <= n_rows <= t_cap (0 is a no-op); k_rows as of bd_paged_read.  The cache's v is not looked at.
  */
 int bd_paged_keys(const bd_shape* shape, int n_rows, const bd_paged_cache* cache, const int32_t* table, int table_pages,

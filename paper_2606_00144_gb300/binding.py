@@ -25,7 +25,7 @@ BD_PAGED_BLOCK_ROWS = -1
 BD_QUANT_BLOCK_ROWS = -1
 BD_QUANT_GROUP = 32
 BD_DRAFT_VIEW_READY = 1
-BD_SELECT_WINDOW_READY = 1
+BD_SELECT_WINDOW_READY, BD_SELECT_NAN_HIDDEN = 1, 4
 BD_DTYPE_BF16, BD_DTYPE_F32 = 1, 2
 
 

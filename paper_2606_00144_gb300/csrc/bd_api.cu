@@ -345,7 +345,7 @@ int bd_select_budget(const bd_shape* shape, const void* k_cache, const void* q_w
   if (window < 1 || window > s.t_ctx || budget < 1 || n_sink < 0 || n_recent < 0 || chunk < 1)
     return BD_ERR_INVALID_ARG;
   if (budget < s.t_ctx && (long long)n_sink + n_recent > budget) return BD_ERR_INVALID_ARG;
-  if (flags & ~BD_SELECT_WINDOW_READY) return BD_ERR_INVALID_ARG;
+  if (flags & ~(BD_SELECT_WINDOW_READY | BD_SELECT_NAN_HIDDEN)) return BD_ERR_INVALID_ARG;
   if ((s.h_q / s.h_kv) * window > 256) return BD_ERR_UNSUPPORTED;
   SelectPlan sp;
   if (!select_plan(s, window, budget, n_sink, n_recent, chunk, &sp)) return BD_ERR_UNSUPPORTED;
@@ -436,7 +436,7 @@ int bd_verify_attn(const bd_shape* shape, const void* q, int n_q, const void* k_
     return BD_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!with_v)
-    return map_cuda(launch_lse(block_context(s, n_q), lp, k_cache, q, n_q, n_q, false, lse_out, region(ws, units),
+    return map_cuda(launch_lse(block_context(s, n_q), lp, k_cache, q, n_q, n_q, false, false, lse_out, region(ws, units),
                                counters(ws), status_word(ws), st));
   return map_cuda(launch_verify(s, vp, n_q, q, k_cache, v_cache, o_out, lse_out, region(ws, units), counters(ws),
                                 status_word(ws), st));

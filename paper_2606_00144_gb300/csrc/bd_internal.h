@@ -117,8 +117,8 @@ inline bd_shape block_context(const bd_shape& s, int n_q) {
 size_t lse_region_bytes(const bd_shape& s, int n_q);
 // len_offset is added to every sequence's length (seq_lens); part: plan.part_bytes of scratch.
 cudaError_t launch_lse(const bd_shape& s, const LsePlan& plan, const void* k_cache, const void* q, int window,
-                       int len_offset, bool window_ready, float* lse_out, void* part, int* counters, int* status,
-                       cudaStream_t stream);
+                       int len_offset, bool window_ready, bool hide_nan, float* lse_out, void* part, int* counters,
+                       int* status, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------- select
 struct SelectPlan {

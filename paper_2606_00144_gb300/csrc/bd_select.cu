@@ -406,7 +406,6 @@ struct LseParams {
   const int32_t* seq_lens;   // per-sequence context lengths [batch] (RAGGED instance) or null
   int len_offset;            // added to every length (a verify block ends n_q past its context)
   int h_kv, units;
-  int hide_nan;              // a key whose score is NaN has no part in a row (a selection's rows), or makes the row one (a verify block's)
 };
 // Segments of one unit with per-sequence lengths (bounds the partials): 33 while the units are not many
 // times the SMs, since all but a few sequences may be short.  (One sequence of 64K, 8 units of 24 or 32 rows:
@@ -432,7 +431,8 @@ __device__ __forceinline__ float row_lse(float m, float l) {
 
 // COPIES: how often the unit's rows (at most 128 / COPIES) lie in the A operand, each copy taking its share
 // of a tile's columns: a quarter of the lanes holding all the rows would have all the exponentials.
-template <int D, bool RAGGED, int COPIES>
+// HIDE_NAN: BD_SELECT_NAN_HIDDEN, a key whose score is NaN has no part in a row (else the row is -inf).
+template <int D, bool RAGGED, int COPIES, bool HIDE_NAN>
 __global__ void __launch_bounds__(kLThreads, 1) window_lse_kernel(const LseParams p,
                                                                   const __grid_constant__ CUtensorMap kmap,
                                                                   const __grid_constant__ CUtensorMap qmap) {
@@ -682,17 +682,20 @@ __global__ void __launch_bounds__(kLThreads, 1) window_lse_kernel(const LseParam
         {
           const int c0 = 64 * half + COLS * copy;
           float v[COLS];
-          if constexpr (COLS == 16) {
-            tc_ld_16cols(taddr + c0, v);
-          } else {
+          auto load = [&] {
+            if constexpr (COLS == 16) {
+              tc_ld_16cols(taddr + c0, v);
+            } else {
 #pragma unroll
-            for (int j = 0; j < COLS; j += 32) tc_ld_32cols(taddr + c0 + j, *reinterpret_cast<float(*)[32]>(&v[j]));
-          }
-          tc_wait_ld();
-          if (masked) {
+              for (int j = 0; j < COLS; j += 32) tc_ld_32cols(taddr + c0 + j, *reinterpret_cast<float(*)[32]>(&v[j]));
+            }
+            tc_wait_ld();
+            if (masked) {
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) v[j] = key0 + c0 + j <= pw ? v[j] : -INFINITY;
-          }
+              for (int j = 0; j < COLS; ++j) v[j] = key0 + c0 + j <= pw ? v[j] : -INFINITY;
+            }
+          };
+          load();
           float mx0 = fmaxf(v[0], v[1]), mx1 = fmaxf(v[2], v[3]);
 #pragma unroll
           for (int j = 4; j < COLS; j += 4) {
@@ -721,10 +724,15 @@ __global__ void __launch_bounds__(kLThreads, 1) window_lse_kernel(const LseParam
             return (a0.x + a0.y) + (a1.x + a1.y);
           };
           float sum = weights();
-          if (sum != sum && p.hide_nan) {           // (the maxima above pass over a NaN by themselves)
+          // (the maxima above pass over a NaN by themselves.  Loaded again: held until here the scores take 138 registers for 94.
+          // An instance of its own: a selection over 64 ragged units of 16K takes 105.4 us, 107.3 with a parameter for it.)
+          if constexpr (HIDE_NAN) {
+            if (__any_sync(0xffffffffu, sum != sum)) {
+              load();
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) v[j] = fmaxf(v[j], -INFINITY);
-            sum = weights();
+              for (int j = 0; j < COLS; ++j) v[j] = fmaxf(v[j], -INFINITY);
+              sum = weights();
+            }
           }
           l += sum;
         }
@@ -1576,8 +1584,8 @@ size_t lse_region_bytes(const bd_shape& s, int n_q) {
 static int lse_copies(int nq_rows) { return nq_rows <= 32 ? 4 : nq_rows <= 64 ? 2 : 1; }
 
 cudaError_t launch_lse(const bd_shape& s, const LsePlan& plan, const void* k_cache, const void* q, int window,
-                       int len_offset, bool window_ready, float* lse_out, void* part, int* counters, int* status,
-                       cudaStream_t stream) {
+                       int len_offset, bool window_ready, bool hide_nan, float* lse_out, void* part, int* counters,
+                       int* status, cudaStream_t stream) {
   const int units = s.batch * s.h_kv;
   CUtensorMap kmap, qmap;
   cudaError_t err = make_cache_map(&kmap, k_cache, units, s.t_cap, s.t_ctx, s.head_dim, kSKeys);
@@ -1604,11 +1612,12 @@ cudaError_t launch_lse(const bd_shape& s, const LsePlan& plan, const void* k_cac
   p.len_offset = len_offset;
   p.h_kv = s.h_kv;
   p.units = units;
-  p.hide_nan = len_offset == 0;
   p.scale_log2 = kLog2e / sqrtf((float)s.head_dim);
   void* fn = nullptr;
-#define BD_LSE(DD, R, C) \
-  if (s.head_dim == DD && (s.seq_lens != nullptr) == R && copies == C) fn = reinterpret_cast<void*>(&window_lse_kernel<DD, R, C>);
+#define BD_LSE(DD, R, C)                                                                        \
+  if (s.head_dim == DD && (s.seq_lens != nullptr) == R && copies == C)                         \
+    fn = hide_nan ? reinterpret_cast<void*>(&window_lse_kernel<DD, R, C, true>)                \
+                  : reinterpret_cast<void*>(&window_lse_kernel<DD, R, C, false>);
   BD_LSE(64, false, 1) BD_LSE(64, false, 2) BD_LSE(64, false, 4) BD_LSE(64, true, 1) BD_LSE(64, true, 2) BD_LSE(64, true, 4)
   BD_LSE(128, false, 1) BD_LSE(128, false, 2) BD_LSE(128, false, 4) BD_LSE(128, true, 1) BD_LSE(128, true, 2)
   BD_LSE(128, true, 4)
@@ -1672,8 +1681,9 @@ cudaError_t launch_select(const bd_shape& s, const SelectPlan& plan, const void*
     const float* lse = window_lse;
     if (lse == nullptr) {   // self mode: window LSE over [0, p_w]
       float* lse_buf = reinterpret_cast<float*>(region + plan.score_bytes);
-      err = launch_lse(s, plan.lse, k_cache, q_window, window, 0, (flags & BD_SELECT_WINDOW_READY) != 0, lse_buf,
-                       region + plan.score_bytes + plan.lse_bytes, counters, status, stream);
+      err = launch_lse(s, plan.lse, k_cache, q_window, window, 0, (flags & BD_SELECT_WINDOW_READY) != 0,
+                       (flags & BD_SELECT_NAN_HIDDEN) != 0, lse_buf, region + plan.score_bytes + plan.lse_bytes, counters,
+                       status, stream);
       if (err != cudaSuccess) return err;
       lse = lse_buf;
     }

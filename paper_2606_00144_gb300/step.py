@@ -14,6 +14,8 @@ class SpecStep:
     The same object may serve many layers of one shape (the workspace is reused; calls
     on one stream are ordered)."""
 
+    _select_flags = 0
+
     def __init__(self, batch, h_q, h_kv, head_dim, t_ctx, t_cap, budget, n_sink, n_recent,
                  window=32, gamma=5, chunk=1, device="cuda", seq_lens=None):
         """seq_lens: optional int32 device tensor [batch] of per-sequence context lengths
@@ -54,7 +56,7 @@ class SpecStep:
         while it finishes."""
         B.bd_select_budget(self.shape, k_cache, q_win, window_lse, self.window, self.budget, self.n_sink,
                            self.n_recent, self.chunk, self.idx, self.count, self.ws, stream,
-                           flags=B.BD_SELECT_WINDOW_READY if window_ready else 0)
+                           flags=self._select_flags | (B.BD_SELECT_WINDOW_READY if window_ready else 0))
 
     def draft(self, j, q_j, k_cache, v_cache, stream=None, view_ready=False):
         """Draft pass j.  view_ready: the selection was not written by the kernel launched
@@ -190,6 +192,8 @@ class PagedSpecStep(_ReadBackStep):
     batch's table of pages, int32 [batch, pages].  A position whose page is not there is hidden from the window's normalisers
     as it is from the attentions, and scores 0 in the selection; it is kept among the sinks and the recent positions, or
     where nothing else is left, and then skipped by the passes."""
+
+    _select_flags = B.BD_SELECT_NAN_HIDDEN
 
     def _workspace(self, device):
         # of the window's normalisers, for every context (a window that is too wide: 0 here, and its status when called)

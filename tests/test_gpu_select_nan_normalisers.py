@@ -1,5 +1,6 @@
-"""A selection that computes its window's normalisers itself (window_lse NULL): keys that hold NaN have no part in them, so the
-other keys' scores, and what is kept, are as without those keys; against 64 bits.  A verify block's rows stay as they were."""
+"""A selection that computes its window's normalisers itself (window_lse NULL), with BD_SELECT_NAN_HIDDEN: keys that hold NaN
+have no part in them, so the other keys' scores, and what is kept, are as without those keys; against 64 bits.  A verify block's
+rows, and a selection's without the flag, stay as they were."""
 
 import math
 
@@ -32,7 +33,8 @@ def test_nan_keys_have_no_part(d, G, W, lens, bad):
     k[gone] = math.nan
     seq = torch.tensor(lens, dtype=torch.int32, device="cuda") if b > 1 else None
     step = bd.SpecStep(b, h_kv * G, h_kv, d, max(lens), t_cap, budget, sink, recent, W, 1, seq_lens=seq)
-    step.select(k.cuda(), q.cuda())
+    bd.bd_select_budget(step.shape, k.cuda(), q.cuda(), None, W, budget, sink, recent, 1, step.idx, step.count, step.ws,
+                        flags=bd.BD_SELECT_NAN_HIDDEN)
     assert step.ws.status() == 0
     for i, t in enumerate(lens):
         for h in range(h_kv):
@@ -57,3 +59,18 @@ def test_a_verify_blocks_normalisers_keep_their_nan(d):
     shape = bd.make_shape(1, 2, 2, d, t, t + n)
     bd.bd_verify_attn(shape, q, n, k, None, None, lse, bd.Workspace(bd.bd_workspace_size(shape, bd.BD_OP_VERIFY, 1, n)))
     assert (lse[0, 0] == -math.inf).all() and torch.isfinite(lse[0, 1]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("W", [8, 32])
+def test_the_flag_changes_nothing_where_there_is_no_nan(d, W):
+    b, h_kv, G, t, budget = 3, 2, 4, 4097, 300
+    k, q = (torch.randn(b, h, n, d, device="cuda").to(BF) for h, n in ((h_kv, t), (h_kv * G, W)))
+    step = bd.SpecStep(b, h_kv * G, h_kv, d, t, t, budget, 4, 64, W, 0)
+    step.select(k, q)
+    plain = step.idx.clone()
+    for flags in (bd.BD_SELECT_NAN_HIDDEN, bd.BD_SELECT_NAN_HIDDEN | bd.BD_SELECT_WINDOW_READY):
+        step.idx.fill_(-7)
+        torch.cuda.synchronize()
+        bd.bd_select_budget(step.shape, k, q, None, W, budget, 4, 64, 1, step.idx, step.count, step.ws, flags=flags)
+        assert torch.equal(step.idx, plain) and step.ws.status() == 0

@@ -33,6 +33,15 @@ def test_validation(lib):  # noqa: F811
     assert keys(lib, shape(), c=cache(v=None, v_strides=strides(1, 1, 1)), k=A + 8) == MISALIGNED
 
 
+def test_the_selections_flag(lib):  # noqa: F811
+    def select(flags):           # (the workspace's address keeps a call with good flags from launching)
+        return lib.bd_select_budget(ctypes.byref(shape()), A, A, None, 8, 64, 4, 16, 1, flags, A, A, A + 16, 1 << 30, None)
+
+    ready, hidden = bd.BD_SELECT_WINDOW_READY, bd.BD_SELECT_NAN_HIDDEN
+    assert [select(f) for f in (0, ready, hidden, ready | hidden)] == [MISALIGNED] * 4
+    assert [select(f) for f in (2, 8, 2 | hidden)] == [INVALID] * 3
+
+
 def test_the_binding(lib, monkeypatch):  # noqa: F811
     c, s, table = setting()
     for rows, err in [(bf(2, 4, 3, 64), ValueError), (bf(2, 3, 64), ValueError), (f32(2, 2, 3, 64), TypeError),
