@@ -6,7 +6,7 @@
 // multiplication, and what is left of a full turn becomes the argument of sincospif.  A token's sines are worked out once
 // by its CTA and shared by all its heads (a thread that worked them out for its own elements would spend more on them than on
 // the rows).  Both kernels move each byte once and are bound by HBM where there is enough: 4 x 8192 tokens of 48 rows of 128
-// (805 MB) are appended in 129 us (6.2 TB/s), the keys of 8 x 16K positions of 8 heads (537 MB) read in 82 (6.5 TB/s).
+// (805 MB) are appended in 128 us (6.3 TB/s), the keys of 8 x 16K positions of 8 heads (537 MB) read in 82 (6.5 TB/s).
 #include <algorithm>
 
 #include "bd_internal.h"

@@ -16,7 +16,7 @@
 // More than 8 query rows of long units (24 at d 64) are the tcgen05 kernel's (bd_verify_tc.cu, PAGED).
 //
 // Bound by HBM where there is enough to read: 256 units of 1.6K to 8K (630 MB) take 92 us (6.8 TB/s), 256 of 4K 78 (6.9), 8
-// of 128K 83.5 (6.4: a start of some 5 us, of which the page's look-up and the first tile are 4, and an end of 5), in pages of
+// of 128K 83.1 (6.5: a start of some 5 us, of which the page's look-up and the first tile are 4, and an end of 5), in pages of
 // 16 as in larger ones.  Short calls are a chain of latencies: 8 units of 1K 5.3 us, 2 of 1K (d 64) 3.9.
 #include <cooperative_groups.h>
 
@@ -523,6 +523,8 @@ PvWork pv_work(const bd_shape& s, int n_q) {
   w.units = (long)s.batch * s.h_kv;
   w.tiles = ((long)s.t_ctx + n_q + kPvKeys - 1) / kPvKeys;
   w.mb = (double)w.units * w.tiles * kPvKeys * s.head_dim * 4e-6;
+  // (the host does not know the lengths.  Where they are all alike half is wrong, and the lay-out waits for them: 256 units of 4K 82.7 us,
+  // 80.7 without lengths; 8 of 8K 15.4 / 11.8; 32 of 8K 28.2 / 24.2.)
   w.share = s.seq_lens ? 0.5 : 1.0;
   return w;
 }
@@ -586,7 +588,9 @@ bool paged_verify_plan(const bd_shape& s, int rows, int n_q, PagedVerifyPlan* pl
   const long a = (long)std::min(16.0, std::max(0.0, 5.0 / tile_us + 0.5));
   const long vtotal = units * (tpu + a);
   if (vtotal >= 1L << 30) return false;
-  const long least = (tpu + a + kVMaxSeg - 2) / (kVMaxSeg - 1);     // <= kVMaxSeg segments
+  // <= kVMaxSeg segments, as many as the merges hold the weights of: few long units do not fill the GPU (one of 128K, d 128, has
+  // 32 CTAs: 38.4 us, 4 times what its bytes take; two 39.8, four 48.2, eight 83.1), and pv_stream_us does not know it.
+  const long least = (tpu + a + kVMaxSeg - 2) / (kVMaxSeg - 1);
   const long vtpc = std::max((vtotal + ctas - 1) / ctas, least);
   plan->tiles_per_unit = (int)tpu;
   plan->seg_cost = (int)a;
